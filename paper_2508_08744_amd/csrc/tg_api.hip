@@ -3,6 +3,7 @@
 #include "../../include/tagore_knn.h"
 #include "tg_kernels.h"
 #include "tg_device.h"
+#include "tg_error.h"
 #include "tg_exact.h"
 
 #include <cmath>
@@ -16,7 +17,7 @@
 
 static thread_local char g_err[256] = "";
 
-static int fail(int code, const char* fmt, ...)
+int tg_fail(int code, const char* fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -24,6 +25,7 @@ static int fail(int code, const char* fmt, ...)
     va_end(ap);
     return code;
 }
+#define fail tg_fail
 extern "C" const char* tg_last_error(void) { return g_err; }
 
 #define HIP_TRY(expr)                                                                         \

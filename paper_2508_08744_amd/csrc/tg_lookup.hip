@@ -1,0 +1,437 @@
+// Rows of a table by id, and the gradient that goes back to them.
+//
+// The lookup is a copy: bound by its bytes.  The gradient is a sum over the tokens of an id.  Adding them to the table with atomics
+// would make the result depend on the order of arrival and, where few ids take most tokens, wait for the same words; so the
+// tokens are sorted by id (ties by position) and the sorted list is cut into tiles of equal length, whatever the ids: a run of one id that lies inside a
+// tile is written at once, one that crosses tiles leaves its parts in fp32 and is added up by a second kernel in the tiles' order.
+#include "tg_embed.h"
+#include "tg_device.h"
+
+#define LOOKUP_GRID 65536          // workgroups of a launch at most: the rest is walked
+
+// ---- lookup: G lanes (a power of two) a row
+template <class E>
+__global__ __launch_bounds__(256) void lookup_kernel(const E* __restrict__ table, int64_t ld, int64_t n_rows, int d, const void* __restrict__ ids,
+                                                     int ids64, int64_t n, float scale, int gshift, E* __restrict__ out)
+{
+    typedef TgPiece<E> P;
+    const int lane = threadIdx.x & ((1 << gshift) - 1);
+    const int64_t step = (int64_t)gridDim.x * (256 >> gshift);
+    for (int64_t t = (int64_t)blockIdx.x * (256 >> gshift) + (threadIdx.x >> gshift); t < n; t += step) {
+        const int64_t v = tg_row_of(ids, ids64, t, n_rows);
+        for (int at = lane * P::E; at < d; at += P::E << gshift) {
+            P p;
+            p.load(table + (v < 0 ? 0 : v) * ld + at, v < 0 ? 0 : d - at);
+#pragma unroll
+            for (int i = 0; i < P::E; ++i) p.v[i] *= scale;
+            p.store(out + t * d + at, d - at);
+        }
+    }
+}
+
+static int lanes_shift(int pieces)
+{
+    int s = 0;
+    while (s < 6 && (1 << s) < pieces) ++s;
+    return s;
+}
+
+void tg_launch_lookup(const void* table, int64_t ld, int dtype, int64_t n_rows, int d, const void* ids, int ids64, int64_t n, float scale,
+                      void* out, hipStream_t s)
+{
+    if (n == 0) return;
+    TG_WITH_TYPE(dtype, E, {
+        const int gs = lanes_shift((d + TgPiece<E>::E - 1) / TgPiece<E>::E);
+        const int64_t wgs = (n + (256 >> gs) - 1) / (256 >> gs);
+        hipLaunchKernelGGL(lookup_kernel<E>, dim3((unsigned)(wgs < LOOKUP_GRID ? wgs : LOOKUP_GRID)), dim3(256), 0, s, (const E*)table, ld, n_rows,
+                           d, ids, ids64, n, scale, gs, (E*)out);
+    });
+}
+
+// ---- zeros: `halves` values of 16 bits, the first `head` of them in front of a 16-byte boundary
+__global__ __launch_bounds__(256) void zero_kernel(uint16_t* __restrict__ p, size_t halves, size_t head)
+{
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, step = (size_t)gridDim.x * 256;
+    uint4* q = reinterpret_cast<uint4*>(p + head);
+    const size_t pieces = (halves - head) / 8;
+    for (size_t j = i; j < pieces; j += step) q[j] = make_uint4(0, 0, 0, 0);
+    if (i < head) p[i] = 0;
+    if (i < (halves - head) % 8) p[head + pieces * 8 + i] = 0;
+}
+void tg_launch_zero(void* p, size_t bytes, hipStream_t s)
+{
+    const size_t halves = bytes / 2;
+    if (halves == 0) return;
+    size_t head = ((16 - ((uintptr_t)p & 15)) & 15) / 2;
+    if (head > halves) head = halves;
+    const size_t wgs = (halves / 8 + 255) / 256 + 1;
+    hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(256), 0, s, (uint16_t*)p, halves, head);
+}
+
+// ---- the tokens sorted by id.  A token without a row gets the key n_rows and ends up behind the others.
+__device__ inline u32 token_key(const void* ids, int ids64, int64_t t, int64_t n_rows)
+{
+    const int64_t v = tg_row_of(ids, ids64, t, n_rows);
+    return (u32)(v < 0 ? n_rows : v);
+}
+
+// Few tokens: the place of a token is the number of those in front of it, counted.  16 lanes count for one token, over all keys in LDS.
+// One launch instead of the six of the digits' sort (8192 tokens: RANK_MAX squared comparisons are 6 us; twice as many would be 24).
+#define RANK_MAX 8192
+__global__ __launch_bounds__(256) void rank_sort_kernel(const void* __restrict__ ids, int ids64, int n, int64_t n_rows, u32* __restrict__ skey,
+                                                        u32* __restrict__ spos)
+{
+    extern __shared__ __align__(16) u32 s_rank_keys[];      // n rounded up to 64, the rest larger than any key
+    const int full = (n + 63) & ~63;
+    for (int i = threadIdx.x; i < full; i += 256) s_rank_keys[i] = i < n ? token_key(ids, ids64, i, n_rows) : 0xFFFFFFFFu;
+    __syncthreads();
+    const int part = threadIdx.x & 15;
+    const int t = blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (t >= n) return;                                     // (16 lanes together: their sums stay among themselves)
+    const u32 key = s_rank_keys[t];
+    int before = 0;
+    for (int i = part * 4; i < full; i += 64) {
+        const uint4 k = *reinterpret_cast<const uint4*>(s_rank_keys + i);
+        before += (k.x < key || (k.x == key && i < t)) + (k.y < key || (k.y == key && i + 1 < t)) +
+                  (k.z < key || (k.z == key && i + 2 < t)) + (k.w < key || (k.w == key && i + 3 < t));
+    }
+#pragma unroll
+    for (int m = 1; m < 16; m <<= 1) before += __shfl_xor(before, m);
+    if (part == 0) {
+        skey[before] = key;
+        spos[before] = (u32)t;
+    }
+}
+
+// Many tokens: by digits of up to 11 bits, the lowest first, every pass keeping the order of equal digits.  A workgroup takes a
+// chunk of the tokens, each of its four waves a quarter of it in one piece.
+#define DIGIT_MAX 11
+#define SORT_WGS 256
+struct SortShape {
+    int passes, bits;        // digits, and bits of one
+    int64_t wgs, chunk;      // workgroups, and tokens of one (a multiple of 256)
+};
+static SortShape sort_shape(int64_t n, int64_t n_rows)
+{
+    SortShape f;
+    int b = 1;
+    while (b < 31 && (n_rows >> b) != 0) ++b;               // bits of the largest key, n_rows
+    f.passes = (b + DIGIT_MAX - 1) / DIGIT_MAX;
+    f.bits = (b + f.passes - 1) / f.passes;
+    int64_t chunk = (n + SORT_WGS - 1) / SORT_WGS;
+    chunk = (chunk + 1023) & ~(int64_t)1023;
+    f.chunk = chunk;
+    f.wgs = (n + chunk - 1) / chunk;
+    return f;
+}
+// how many of the wave's tokens have which digit: s_count[wave][digit]
+__device__ inline u32 digit_of(u32 key, int shift, int bits) { return (key >> shift) & ((1u << bits) - 1u); }
+__device__ inline void count_digits(const void* ids, int ids64, const u32* key_in, int64_t n, int64_t n_rows, int64_t from, int64_t to, int shift,
+                                    int bits, u32* count)
+{
+    for (int64_t t = from + tg_lane(); t < to; t += 64) {
+        const u32 key = key_in ? key_in[t] : token_key(ids, ids64, t, n_rows);
+        atomicAdd(count + digit_of(key, shift, bits), 1u);
+    }
+}
+// per workgroup and digit: how many.  table: digit-major, wgs a digit
+__global__ __launch_bounds__(256) void digit_count_kernel(const void* __restrict__ ids, int ids64, const u32* __restrict__ key_in, int64_t n,
+                                                          int64_t n_rows, int64_t chunk, int shift, int bits, u32* __restrict__ table)
+{
+    __shared__ u32 s_count[1 << DIGIT_MAX];
+    for (int i = threadIdx.x; i < 1 << bits; i += 256) s_count[i] = 0;
+    __syncthreads();
+    const int64_t from = (int64_t)blockIdx.x * chunk + (threadIdx.x >> 6) * (chunk / 4);
+    int64_t to = from + chunk / 4;
+    if (to > n) to = n;
+    count_digits(ids, ids64, key_in, n, n_rows, from, to, shift, bits, s_count);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 1 << bits; i += 256) table[(int64_t)i * gridDim.x + blockIdx.x] = s_count[i];
+}
+// a wave a digit: its counts become the number of tokens in workgroups before, their sum goes to total[digit]
+__global__ __launch_bounds__(256) void digit_scan_kernel(u32* __restrict__ table, int wgs, int digits, u32* __restrict__ total)
+{
+    const int digit = blockIdx.x * 4 + (threadIdx.x >> 6), lane = tg_lane();
+    if (digit >= digits) return;
+    u32 base = 0;
+    for (int i0 = 0; i0 < wgs; i0 += 64) {
+        const int i = i0 + lane;
+        const u32 c = i < wgs ? table[(int64_t)digit * wgs + i] : 0u;
+        u32 x = c;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const u32 y = (u32)__shfl_up((int)x, m);
+            if (lane >= m) x += y;
+        }
+        if (i < wgs) table[(int64_t)digit * wgs + i] = base + x - c;
+        base += (u32)__shfl((int)x, 63);
+    }
+    if (lane == 0) total[digit] = base;
+}
+// every token to its place: the smaller digits' tokens, those of its digit in workgroups before, in waves before, and in its wave before
+__global__ __launch_bounds__(256) void digit_place_kernel(const void* __restrict__ ids, int ids64, const u32* __restrict__ key_in,
+                                                          const u32* __restrict__ pos_in, int64_t n, int64_t n_rows, int64_t chunk, int shift,
+                                                          int bits, const u32* __restrict__ table, const u32* __restrict__ total,
+                                                          u32* __restrict__ key_out, u32* __restrict__ pos_out)
+{
+    __shared__ u32 s_next[4][1 << DIGIT_MAX];
+    __shared__ u32 s_wave[4];
+    const int wave = threadIdx.x >> 6, lane = tg_lane(), digits = 1 << bits;
+    for (int i = threadIdx.x; i < digits; i += 256) s_next[0][i] = s_next[1][i] = s_next[2][i] = s_next[3][i] = 0;
+    __syncthreads();
+    const int64_t from = (int64_t)blockIdx.x * chunk + wave * (chunk / 4);
+    int64_t to = from + chunk / 4;
+    if (to > n) to = n;
+    count_digits(ids, ids64, key_in, n, n_rows, from, to, shift, bits, s_next[wave]);
+    __syncthreads();
+    // sum of the totals before a digit: 256 threads a stretch, in order
+    u32 base = 0;
+    for (int i0 = 0; i0 < digits; i0 += 256) {
+        const int i = i0 + threadIdx.x;
+        const u32 c = i < digits ? total[i] : 0u;
+        u32 x = c;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const u32 y = (u32)__shfl_up((int)x, m);
+            if (lane >= m) x += y;
+        }
+        if (lane == 63) s_wave[wave] = x;
+        __syncthreads();
+        u32 before = base;
+        for (int j = 0; j < wave; ++j) before += s_wave[j];
+        base += s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
+        if (i < digits) {
+            u32 at = before + x - c + table[(int64_t)i * gridDim.x + blockIdx.x];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const u32 k = s_next[j][i];
+                s_next[j][i] = at;
+                at += k;
+            }
+        }
+        __syncthreads();
+    }
+    // (the wave's own words from here on; a row of tokens is placed before the next one reads them)
+    for (int64_t t0 = from; t0 < to; t0 += 64) {
+        const int64_t t = t0 + lane;
+        const bool real = t < to;
+        const u32 key = !real ? 0u : key_in ? key_in[t] : token_key(ids, ids64, t, n_rows);
+        const u32 digit = digit_of(key, shift, bits);
+        u64 same = __ballot(real);
+        for (int b = 0; b < bits; ++b) {
+            const bool one = (digit >> b) & 1u;
+            const u64 ones = __ballot(one);
+            same &= one ? ones : ~ones;
+        }
+        u32 at = 0;
+        if (real) at = s_next[wave][digit];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const int before = __popcll(same & tg_lanemask_lt());
+        if (real) {
+            key_out[at + before] = key;
+            pos_out[at + before] = pos_in ? pos_in[t] : (u32)t;
+            if (before == 0) s_next[wave][digit] = at + (u32)__popcll(same);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// ---- sums over the runs of the sorted list
+#define RUN_TILE 32
+template <class E, class O>
+__device__ inline void write_row(const float* v, int left, O* p, float scale, bool add)
+{
+    // in pieces of the output's type
+    constexpr int EO = TgPiece<O>::E < TgPiece<E>::E ? TgPiece<O>::E : TgPiece<E>::E;
+#pragma unroll
+    for (int j = 0; j < TgPiece<E>::E; j += EO) {
+        typedef O vec __attribute__((ext_vector_type(EO), aligned(sizeof(O))));
+        if (left >= j + EO) {
+            vec x;
+            if (add) {
+                x = *reinterpret_cast<const vec*>(p + j);
+#pragma unroll
+                for (int i = 0; i < EO; ++i) x[i] = (O)((float)x[i] + v[j + i] * scale);
+            } else {
+#pragma unroll
+                for (int i = 0; i < EO; ++i) x[i] = (O)(v[j + i] * scale);
+            }
+            *reinterpret_cast<vec*>(p + j) = x;
+        } else {
+#pragma unroll
+            for (int i = 0; i < EO; ++i)
+                if (j + i < left) p[j + i] = (O)((add ? (float)p[j + i] : 0.0f) + v[j + i] * scale);
+        }
+    }
+}
+
+// G lanes a tile, a piece of the row a lane, as many columns of tiles as the row has G pieces.  parts: two rows of d per tile: of a run
+// that came from the tile before, and of one that goes on in the next but began here.
+template <class E, class O>
+__global__ __launch_bounds__(256) void run_sum_kernel(const E* __restrict__ grad, int64_t ld, const u32* __restrict__ skey,
+                                                      const u32* __restrict__ spos, int64_t n, int64_t n_rows, int d, float scale, int add,
+                                                      int gshift, int columns, O* __restrict__ out, float* __restrict__ parts)
+{
+    typedef TgPiece<E> P;
+    const int lane = threadIdx.x & ((1 << gshift) - 1);
+    const int64_t unit = (int64_t)blockIdx.x * (256 >> gshift) + (threadIdx.x >> gshift);
+    const int64_t tile = unit / columns;
+    const int at = (int)(((unit - tile * columns) << gshift) + lane) * P::E;
+    const int64_t i0 = tile * RUN_TILE;
+    if (i0 >= n || at >= d) return;
+    const int count = (int)(n - i0 < RUN_TILE ? n - i0 : RUN_TILE);
+    const u32 none = (u32)n_rows;
+    u32 cur = skey[i0];
+    if (cur == none) return;                                // (from here on there are only tokens without a row)
+    bool carried = i0 > 0 && skey[i0 - 1] == cur;
+    float acc[P::E];
+#pragma unroll
+    for (int i = 0; i < P::E; ++i) acc[i] = 0.0f;
+    constexpr int AHEAD = 8;
+    for (int j0 = 0; j0 < count; j0 += AHEAD) {
+        u32 key[AHEAD];
+        P g[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const bool real = j0 + j < count;
+            key[j] = real ? skey[i0 + j0 + j] : none;
+            const u32 pos = real ? spos[i0 + j0 + j] : 0u;
+            g[j].load(grad + (int64_t)pos * ld + at, key[j] == none ? 0 : d - at);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (key[j] != cur) {
+                if (cur != none) {
+                    if (carried) {
+                        for (int i = 0; i < P::E; ++i)
+                            if (at + i < d) parts[2 * tile * d + at + i] = acc[i];
+                    } else write_row<E, O>(acc, d - at, out + (int64_t)cur * d + at, scale, add != 0);
+                }
+                carried = false;
+                cur = key[j];
+#pragma unroll
+                for (int i = 0; i < P::E; ++i) acc[i] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < P::E; ++i) acc[i] += g[j].v[i];
+        }
+    }
+    if (cur == none) return;
+    const bool goes_on = i0 + count < n && skey[i0 + count] == cur;
+    if (!carried && !goes_on) { write_row<E, O>(acc, d - at, out + (int64_t)cur * d + at, scale, add != 0); return; }
+    float* p = parts + (2 * tile + (carried ? 0 : 1)) * (int64_t)d + at;
+#pragma unroll
+    for (int i = 0; i < P::E; ++i)
+        if (at + i < d) p[i] = acc[i];
+}
+
+// A workgroup a tile: where a run begins in the tile and goes on, its parts are added: the waves take an equal stretch of the tiles each,
+// and are added in their order.
+template <class O>
+__global__ __launch_bounds__(256) void run_join_kernel(const u32* __restrict__ skey, int64_t n, int64_t n_rows, int d, float scale, int add,
+                                                       const float* __restrict__ parts, O* __restrict__ out)
+{
+    __shared__ float s[4][64];
+    for (int64_t tile = blockIdx.x; (tile + 1) * RUN_TILE < n; tile += gridDim.x) {
+        const int64_t last = (tile + 1) * RUN_TILE - 1;
+        const u32 key = skey[last];
+        if (key == (u32)n_rows || skey[last + 1] != key) continue;              // does not go on
+        if (tile > 0 && skey[tile * RUN_TILE - 1] == key) continue;             // began before
+        // the run's end: the first place behind `last` with another key
+        int64_t lo = last + 1, hi = n;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) >> 1;
+            if (skey[mid] == key) lo = mid + 1; else hi = mid;
+        }
+        const int64_t end = (lo - 1) / RUN_TILE;                                // its last tile
+        const int wave = threadIdx.x >> 6, lane = tg_lane();
+        const int64_t each = (end - tile + 3) / 4, from = tile + 1 + wave * each;
+        const int64_t to = from + each < end + 1 ? from + each : end + 1;
+        for (int c0 = blockIdx.y * 64; c0 < d; c0 += gridDim.y * 64) {
+            const int c = c0 + lane;
+            float sum = 0.0f;
+            if (c < d) {
+                if (wave == 0) sum = parts[(2 * tile + 1) * d + c];
+#pragma unroll 8
+                for (int64_t t = from; t < to; ++t) sum += parts[2 * t * d + c];
+            }
+            s[wave][lane] = sum;
+            __syncthreads();
+            if (wave == 0 && c < d) {
+                const float v = ((s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane])) * scale;
+                O* p = out + (int64_t)key * d + c;
+                *p = (O)((add ? (float)*p : 0.0f) + v);
+            }
+            __syncthreads();
+        }
+    }
+}
+
+struct GradSpace {
+    u32 *key[2], *pos[2], *table, *total;
+    float* parts;
+};
+static size_t carve_grad(GradSpace* g, void* base, int64_t n, int64_t n_rows, int d)
+{
+    TgCarve c{(char*)base, 0};
+    const bool few = n <= RANK_MAX;
+    const SortShape f = sort_shape(n, n_rows);
+    g->key[0] = c.take<u32>(n);
+    g->pos[0] = c.take<u32>(n);
+    g->key[1] = few ? nullptr : c.take<u32>(n);
+    g->pos[1] = few ? nullptr : c.take<u32>(n);
+    g->table = few ? nullptr : c.take<u32>((size_t)f.wgs << f.bits);
+    g->total = few ? nullptr : c.take<u32>((size_t)1 << f.bits);
+    g->parts = c.take<float>((size_t)((n + RUN_TILE - 1) / RUN_TILE) * 2 * d);
+    return c.used;
+}
+size_t tg_lookup_grad_space(int64_t n, int64_t n_rows, int d)
+{
+    GradSpace g;
+    return n == 0 ? 0 : carve_grad(&g, nullptr, n, n_rows, d);
+}
+
+void tg_launch_lookup_grad(const void* grad, int64_t ld, int dtype, const void* ids, int ids64, int64_t n, int64_t n_rows, int d, float scale,
+                           int accumulate, void* out, int out_dtype, void* space, hipStream_t s)
+{
+    if (!accumulate) tg_launch_zero(out, (size_t)n_rows * d * tg_type_bytes(out_dtype), s);
+    if (n == 0) return;
+    GradSpace g;
+    carve_grad(&g, space, n, n_rows, d);
+    int at = 0;
+    if (n <= RANK_MAX) {
+        const int full = ((int)n + 63) & ~63;
+        hipLaunchKernelGGL(rank_sort_kernel, dim3((unsigned)((n + 15) / 16)), dim3(256), full * 4, s, ids, ids64, (int)n, n_rows, g.key[0], g.pos[0]);
+    } else {
+        const SortShape f = sort_shape(n, n_rows);
+        for (int p = 0; p < f.passes; ++p) {
+            const u32* ki = p ? g.key[at] : nullptr;
+            const u32* pi = p ? g.pos[at] : nullptr;
+            const int to = p ? at ^ 1 : 0;
+            hipLaunchKernelGGL(digit_count_kernel, dim3((unsigned)f.wgs), dim3(256), 0, s, ids, ids64, ki, n, n_rows, f.chunk, p * f.bits, f.bits, g.table);
+            hipLaunchKernelGGL(digit_scan_kernel, dim3((unsigned)(((1 << f.bits) + 3) / 4)), dim3(256), 0, s, g.table, (int)f.wgs, 1 << f.bits, g.total);
+            hipLaunchKernelGGL(digit_place_kernel, dim3((unsigned)f.wgs), dim3(256), 0, s, ids, ids64, ki, pi, n, n_rows, f.chunk, p * f.bits, f.bits,
+                               g.table, g.total, g.key[to], g.pos[to]);
+            at = to;
+        }
+    }
+    const int64_t tiles = (n + RUN_TILE - 1) / RUN_TILE;
+    TG_WITH_TYPE(dtype, E, {
+        const int pieces = (d + TgPiece<E>::E - 1) / TgPiece<E>::E;
+        const int gs = lanes_shift(pieces), columns = (pieces + (1 << gs) - 1) >> gs;
+        const int64_t per = 256 >> gs;
+        // (fewer than 2^32 work-items: 64 of them stand for 32 KB of a gradient that fits the card, or for 32 tokens of a short row)
+        const unsigned wgs = (unsigned)((tiles * columns + per - 1) / per);
+        if (out_dtype == 0) hipLaunchKernelGGL((run_sum_kernel<E, float>), dim3(wgs), dim3(256), 0, s, (const E*)grad, ld, g.key[at], g.pos[at], n,
+                                               n_rows, d, scale, accumulate, gs, columns, (float*)out, g.parts);
+        else hipLaunchKernelGGL((run_sum_kernel<E, E>), dim3(wgs), dim3(256), 0, s, (const E*)grad, ld, g.key[at], g.pos[at], n, n_rows, d, scale,
+                                accumulate, gs, columns, (E*)out, g.parts);
+    });
+    if (tiles > 1) {
+        const unsigned cy = d <= 64 ? 1 : d <= 256 ? (d + 63) / 64 : 4;
+        TG_WITH_TYPE(out_dtype, O, hipLaunchKernelGGL(run_join_kernel<O>, dim3((unsigned)(tiles - 1 < LOOKUP_GRID ? tiles - 1 : LOOKUP_GRID), cy), dim3(256), 0, s, g.key[at], n, n_rows, d, scale,
+                                                      accumulate, g.parts, (O*)out));
+    }
+}

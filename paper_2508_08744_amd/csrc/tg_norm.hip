@@ -1,0 +1,383 @@
+// Root-mean-square norm with the residual's addition, its gradient, and rows on an 8-bit grid with a scale each.
+//
+// All of these are bound by the bytes of their rows: a row is read once, stays in the registers of the lanes that share it (a wave where
+// it is short, a workgroup of up to 16 waves where it is long) through its sums, and is written once.
+#include "tg_embed.h"
+#include "tg_device.h"
+
+// T lanes of a workgroup share a row; CH pieces of 16 bytes of it a lane.
+template <int T> struct NormShare { static constexpr int ROWS = T < 256 ? 256 / T : 1, THREADS = T < 256 ? 256 : T; };
+
+template <class V>
+__device__ inline V wave_sum(V x)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+    return x;
+}
+__device__ inline float wave_max(float x)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x = fmaxf(x, __shfl_xor(x, m));
+    return x;
+}
+// sum over the T lanes of a row, the same in all of them; `s`: a word per wave, not used by the sum before
+template <int T, class V>
+__device__ inline V row_sum(V x, V* s)
+{
+    x = wave_sum(x);
+    if (T == 64) return x;
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    V y = s[0];
+#pragma unroll
+    for (int i = 1; i < T / 64; ++i) y += s[i];
+    return y;
+}
+template <int T>
+__device__ inline float row_max(float x, float* s)
+{
+    x = wave_max(x);
+    if (T == 64) return x;
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float y = s[0];
+#pragma unroll
+    for (int i = 1; i < T / 64; ++i) y = fmaxf(y, s[i]);
+    return y;
+}
+
+template <class E, int T, int CH>
+__global__ __launch_bounds__(NormShare<T>::THREADS) void norm_kernel(const E* x, int64_t ld_x, const E* res, int64_t ld_res,
+                                                                     const E* __restrict__ w, int64_t n, int d, float eps, E* __restrict__ y,
+                                                                     E* r, float* __restrict__ rstd_out)
+{
+    typedef TgPiece<E> P;
+    __shared__ float s_sum[16];
+    const int lane = threadIdx.x % T;
+    const int64_t row = (int64_t)blockIdx.x * NormShare<T>::ROWS + threadIdx.x / T;
+    if (row >= n) return;                                   // (whole waves: with T > 64 a workgroup has one row)
+    P p[CH];
+    float sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) p[c].load(x + row * ld_x + (lane + c * T) * P::E, d - (lane + c * T) * P::E);
+    if (res) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int at = (lane + c * T) * P::E;
+            P q;
+            q.load(res + row * ld_res + at, d - at);
+#pragma unroll
+            for (int i = 0; i < P::E; ++i) p[c].v[i] += q.v[i];
+            p[c].round();
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) p[c].store(r + row * d + (lane + c * T) * P::E, d - (lane + c * T) * P::E);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < P::E; ++i) sum = fmaf(p[c].v[i], p[c].v[i], sum);
+    const float rstd = 1.0f / sqrtf(row_sum<T>(sum, s_sum) / (float)d + eps);
+    if (rstd_out && lane == 0) rstd_out[row] = rstd;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int at = (lane + c * T) * P::E;
+        P g;
+        g.load(w + at, d - at);
+#pragma unroll
+        for (int i = 0; i < P::E; ++i) g.v[i] *= p[c].v[i] * rstd;
+        g.store(y + row * d + at, d - at);
+    }
+}
+
+// The norm in 64 bits, the normed row on its grid.  Which whole number a value next to a border becomes must not depend on how its row
+// was summed, so sum, scale and quotient are taken in 64 bits; the bytes of the rows still bound the kernel.
+template <class E, int T, int CH, bool NORM>
+__global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E* x, int64_t ld_x, const E* res, int64_t ld_res,
+                                                                        const E* __restrict__ w, int64_t n, int d, float eps,
+                                                                        int8_t* __restrict__ q_out, float* __restrict__ scale_out, E* r)
+{
+    typedef TgPiece<E> P;
+    typedef char qvec __attribute__((ext_vector_type(P::E), aligned(1)));
+    __shared__ double s_sum[16];
+    __shared__ double s_max[16];
+    const int lane = threadIdx.x % T;
+    const int64_t row = (int64_t)blockIdx.x * NormShare<T>::ROWS + threadIdx.x / T;
+    if (row >= n) return;
+    P p[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) p[c].load(x + row * ld_x + (lane + c * T) * P::E, d - (lane + c * T) * P::E);
+    double rstd = 1.0;
+    if (NORM) {
+        if (res) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int at = (lane + c * T) * P::E;
+                P q;
+                q.load(res + row * ld_res + at, d - at);
+#pragma unroll
+                for (int i = 0; i < P::E; ++i) p[c].v[i] += q.v[i];
+                p[c].round();
+            }
+#pragma unroll
+            for (int c = 0; c < CH; ++c) p[c].store(r + row * d + (lane + c * T) * P::E, d - (lane + c * T) * P::E);
+        }
+        double sum = 0.0;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < P::E; ++i) sum = fma((double)p[c].v[i], (double)p[c].v[i], sum);
+        rstd = 1.0 / sqrt(row_sum<T>(sum, s_sum) / (double)d + (double)eps);
+    }
+    // max |r w|, and whether a value is NaN (a maximum leaves it out)
+    double top = 0.0;
+    bool odd = false;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int at = (lane + c * T) * P::E;
+        P g;
+        if (NORM) g.load(w + at, d - at);
+#pragma unroll
+        for (int i = 0; i < P::E; ++i) {
+            const double t = NORM ? (double)p[c].v[i] * (double)g.v[i] : (double)p[c].v[i];
+            odd |= !(t == t);
+            top = fmax(top, fabs(t));
+        }
+    }
+    if (odd) top = __builtin_inf();
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) top = fmax(top, __shfl_xor(top, m));
+    if (T > 64) {
+        if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < T / 64; ++i) top = fmax(top, s_max[i]);
+    }
+    float scale = (float)(top * rstd / 127.0);
+    // not a number, an infinite row, or one whose norm is: no grid
+    const bool none = !(top <= 1.79e308) || !(rstd <= 1.79e308) || !(scale <= 3.4028234e38f);
+    if (none) scale = __builtin_nanf("");
+    if (lane == 0) scale_out[row] = scale;
+    const double f = none || scale == 0.0f ? 0.0 : rstd / (double)scale;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int at = (lane + c * T) * P::E, left = d - at;
+        P g;
+        if (NORM) g.load(w + at, left);
+        qvec q;
+#pragma unroll
+        for (int i = 0; i < P::E; ++i) {
+            const double t = NORM ? (double)p[c].v[i] * (double)g.v[i] : (double)p[c].v[i];
+            // (a scale below fp32's normal numbers has few bits of its own: the quotient can pass 127)
+            const double u = none ? 0.0 : fmin(fmax(rint(t * f), -127.0), 127.0);
+            q[i] = (char)(int)u;
+        }
+        int8_t* o = q_out + row * d + at;
+        if (left >= P::E) *reinterpret_cast<qvec*>(o) = q;
+        else
+#pragma unroll
+            for (int i = 0; i < P::E; ++i)
+                if (i < left) o[i] = (int8_t)q[i];
+    }
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void dequantize_kernel(const int8_t* __restrict__ q, const float* __restrict__ scale, int64_t n, int d,
+                                                         int pieces, E* __restrict__ out)
+{
+    typedef TgPiece<E> P;
+    typedef char qvec __attribute__((ext_vector_type(P::E), aligned(1)));
+    const int64_t all = n * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / pieces;
+        const int at = (int)(i - row * pieces) * P::E, left = d - at;
+        const float s = scale[row];
+        P p;
+        if (left >= P::E) {
+            const qvec x = *reinterpret_cast<const qvec*>(q + row * d + at);
+#pragma unroll
+            for (int j = 0; j < P::E; ++j) p.v[j] = (float)(int8_t)x[j] * s;
+        } else {
+#pragma unroll
+            for (int j = 0; j < P::E; ++j) p.v[j] = j < left ? (float)q[row * d + at + j] * s : 0.0f;
+        }
+        p.store(out + row * d + at, left);
+    }
+}
+
+// u = dy w, c = mean(u r): dx = dr + rstd (u - r rstd^2 c), dw = sum over rows of dy r rstd.  A workgroup takes every gridDim.x-th
+// group of rows and keeps its part of dw in registers; the parts are added by norm_dw_kernel in the workgroups' order.
+template <class E, int T, int CH>
+__global__ __launch_bounds__(NormShare<T>::THREADS) void norm_grad_kernel(const E* __restrict__ dy, int64_t ld_dy, const E* dr, int64_t ld_dr,
+                                                                          const E* __restrict__ r, int64_t ld_r, const E* __restrict__ w,
+                                                                          const float* __restrict__ rstd_in, int64_t n, int d, E* dx,
+                                                                          float* __restrict__ parts)
+{
+    typedef TgPiece<E> P;
+    constexpr int ROWS = NormShare<T>::ROWS;
+    __shared__ float s_sum[2][16];
+    const int lane = threadIdx.x % T;
+    float dw[CH][P::E];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < P::E; ++i) dw[c][i] = 0.0f;
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T; row < n; row += (int64_t)gridDim.x * ROWS) {
+        P u[CH], z[CH];
+        const float rstd = rstd_in[row];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int at = (lane + c * T) * P::E;
+            u[c].load(dy + row * ld_dy + at, d - at);
+            z[c].load(r + row * ld_r + at, d - at);
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int at = (lane + c * T) * P::E;
+            P g;
+            g.load(w + at, d - at);
+#pragma unroll
+            for (int i = 0; i < P::E; ++i) {
+                z[c].v[i] *= rstd;
+                dw[c][i] = fmaf(u[c].v[i], z[c].v[i], dw[c][i]);
+                u[c].v[i] *= g.v[i];
+                sum = fmaf(u[c].v[i], z[c].v[i], sum);
+            }
+        }
+        // (two sets of words in turn: a wave may be a row ahead of another that still reads its sum)
+        const float mean = row_sum<T>(sum, s_sum[turn]) / (float)d;
+        turn ^= 1;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int at = (lane + c * T) * P::E;
+            P o;
+            if (dr) o.load(dr + row * ld_dr + at, d - at);
+#pragma unroll
+            for (int i = 0; i < P::E; ++i) {
+                const float v = rstd * (u[c].v[i] - z[c].v[i] * mean);
+                o.v[i] = dr ? o.v[i] + v : v;
+            }
+            o.store(dx + row * d + at, d - at);
+        }
+    }
+    // the rows of a workgroup are added where there are several
+    const int64_t part = (int64_t)blockIdx.x * ROWS + threadIdx.x / T;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int at = (lane + c * T) * P::E;
+#pragma unroll
+        for (int i = 0; i < P::E; ++i)
+            if (at + i < d) parts[part * d + at + i] = dw[c][i];
+    }
+}
+// 16 columns a workgroup, 64 lanes a column: lane j of a column adds the parts j, j + 64, ..., then the lanes are added as a tree
+template <class E>
+__global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__ parts, int count, int d, E* __restrict__ dw)
+{
+    __shared__ float s[64][17];
+    const int c = threadIdx.x & 15, j = threadIdx.x >> 4;
+    const int col = blockIdx.x * 16 + c;
+    float sum = 0.0f;
+    if (col < d) {
+#pragma unroll 8
+        for (int p = j; p < count; p += 64) sum += parts[(int64_t)p * d + col];
+    }
+    s[j][c] = sum;
+    __syncthreads();
+#pragma unroll
+    for (int h = 32; h >= 1; h >>= 1) {
+        if (j < h) s[j][c] += s[j + h][c];
+        __syncthreads();
+    }
+    if (j == 0 && col < d) dw[col] = (E)s[0][c];
+}
+
+// The lanes a row of `d` elements gets and the pieces a lane holds: a wave up to four pieces a lane (2048 elements of 16 bits), four
+// waves up to four (8192), sixteen beyond (8192 elements of 32 bits).
+#define NORM_SHAPES(E, d, LAUNCH)                                                    \
+    do {                                                                             \
+        const int pieces_ = ((d) + TgPiece<E>::E - 1) / TgPiece<E>::E;               \
+        if (pieces_ <= 64) { LAUNCH(64, 1); }                                        \
+        else if (pieces_ <= 128) { LAUNCH(64, 2); }                                  \
+        else if (pieces_ <= 256) { LAUNCH(256, 1); }                                 \
+        else if (pieces_ <= 512) { LAUNCH(256, 2); }                                 \
+        else if (pieces_ <= 1024) { LAUNCH(256, 4); }                                \
+        else { LAUNCH(1024, 2); }                                                    \
+    } while (0)
+
+// rows of one launch: below 2^32 work-items
+#define NORM_LAUNCH_ROWS (1ll << 21)
+
+template <class F>
+static void norm_chunks(int64_t n, F launch)
+{
+    for (int64_t r0 = 0; r0 < n; r0 += NORM_LAUNCH_ROWS) launch(r0, n - r0 < NORM_LAUNCH_ROWS ? n - r0 : NORM_LAUNCH_ROWS);
+}
+
+void tg_launch_norm(const void* x, int64_t ld_x, const void* res, int64_t ld_res, const void* w, int dtype, int64_t n, int d, float eps,
+                    void* y, void* r, float* rstd, hipStream_t s)
+{
+    norm_chunks(n, [&](int64_t r0, int64_t nr) {
+#define NORM_FWD(T, CH)                                                                                                                  \
+    hipLaunchKernelGGL((norm_kernel<E, T, CH>), dim3((unsigned)((nr + NormShare<T>::ROWS - 1) / NormShare<T>::ROWS)),                     \
+                       dim3(NormShare<T>::THREADS), 0, s, (const E*)x + r0 * ld_x, ld_x, res ? (const E*)res + r0 * ld_res : nullptr,     \
+                       ld_res, (const E*)w, nr, d, eps, (E*)y + r0 * d, r ? (E*)r + r0 * d : nullptr, rstd ? rstd + r0 : nullptr)
+        TG_WITH_TYPE(dtype, E, NORM_SHAPES(E, d, NORM_FWD));
+    });
+}
+
+void tg_launch_norm_q8(const void* x, int64_t ld_x, const void* res, int64_t ld_res, const void* w, int dtype, int64_t n, int d, float eps,
+                       int8_t* q, float* scale, void* r, hipStream_t s)
+{
+    norm_chunks(n, [&](int64_t r0, int64_t nr) {
+#define NORM_Q8(T, CH)                                                                                                                   \
+    do {                                                                                                                                 \
+        const dim3 g((unsigned)((nr + NormShare<T>::ROWS - 1) / NormShare<T>::ROWS)), b(NormShare<T>::THREADS);                           \
+        const E* xr = (const E*)x + r0 * ld_x;                                                                                           \
+        const E* rr = res ? (const E*)res + r0 * ld_res : nullptr;                                                                       \
+        if (w) hipLaunchKernelGGL((norm_q8_kernel<E, T, CH, true>), g, b, 0, s, xr, ld_x, rr, ld_res, (const E*)w, nr, d, eps, q + r0 * d, \
+                                  scale + r0, r ? (E*)r + r0 * d : nullptr);                                                             \
+        else hipLaunchKernelGGL((norm_q8_kernel<E, T, CH, false>), g, b, 0, s, xr, ld_x, rr, ld_res, (const E*)w, nr, d, eps, q + r0 * d,  \
+                                scale + r0, (E*)nullptr);                                                                                \
+    } while (0)
+        TG_WITH_TYPE(dtype, E, NORM_SHAPES(E, d, NORM_Q8));
+    });
+}
+
+void tg_launch_dequantize(const int8_t* q, const float* scale, int64_t n, int d, int dtype, void* out, hipStream_t s)
+{
+    if (n == 0) return;
+    TG_WITH_TYPE(dtype, E, {
+        const int pieces = (d + TgPiece<E>::E - 1) / TgPiece<E>::E;
+        const int64_t wgs = (n * pieces + 255) / 256;
+        hipLaunchKernelGGL(dequantize_kernel<E>, dim3((unsigned)(wgs < 16384 ? wgs : 16384)), dim3(256), 0, s, q, scale, n, d, pieces, (E*)out);
+    });
+}
+
+// workgroups of the gradient, and the parts of dw they leave (one per row they have in hand at a time)
+#define NORM_GRAD_WGS 1024
+static int64_t norm_grad_parts(int64_t n, int rows)
+{
+    const int64_t wgs = (n + rows - 1) / rows;
+    return (wgs < NORM_GRAD_WGS ? wgs : NORM_GRAD_WGS) * rows;
+}
+size_t tg_norm_grad_space(int64_t n, int d) { return (size_t)norm_grad_parts(n, 4) * d * sizeof(float); }
+
+void tg_launch_norm_grad(const void* dy, int64_t ld_dy, const void* dr, int64_t ld_dr, const void* r, int64_t ld_r, const void* w,
+                         const float* rstd, int dtype, int64_t n, int d, void* dx, void* dw, void* space, hipStream_t s)
+{
+    float* parts = (float*)space;
+    int64_t count = 0;
+#define NORM_BWD(T, CH)                                                                                                                  \
+    do {                                                                                                                                 \
+        count = norm_grad_parts(n, NormShare<T>::ROWS);                                                                                  \
+        if (n > 0)                                                                                                                       \
+            hipLaunchKernelGGL((norm_grad_kernel<E, T, CH>), dim3((unsigned)(count / NormShare<T>::ROWS)), dim3(NormShare<T>::THREADS), 0, \
+                               s, (const E*)dy, ld_dy, (const E*)dr, ld_dr, (const E*)r, ld_r, (const E*)w, rstd, n, d, (E*)dx, parts);   \
+        hipLaunchKernelGGL(norm_dw_kernel<E>, dim3((unsigned)((d + 15) / 16)), dim3(1024), 0, s, parts, (int)count, d, (E*)dw);           \
+    } while (0)
+    TG_WITH_TYPE(dtype, E, NORM_SHAPES(E, d, NORM_BWD));
+}

@@ -1,0 +1,186 @@
+// Products of 8-bit rows with a scale per token and channel: out[i][j] = a_scale[i] b_scale[j] sum_k a[i][k] b[j][k] (+ bias[j]).
+//
+// The sum is a whole number below 2^31 and exact, in whatever order it is taken; the scales and the bias are the epilogue's.  Many
+// tokens: tiles in LDS (tg_tiles.h), bound by the matrix instructions, or by the bytes of the output where rows are short.  A few
+// tokens: every byte of b is needed once and nothing else counts, so a wave reads its rows of b straight into the matrix
+// instructions' registers, with several loads in flight, and the waves of a workgroup share the contraction between them.
+#include "tg_embed.h"
+#include "tg_tiles.h"
+
+// x: channels, y: tokens
+template <class O, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void product_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
+                                                               const float* __restrict__ bs, const float* __restrict__ bias, uint32_t nx,
+                                                               uint32_t ny, uint32_t group, O* __restrict__ out)
+{
+    typedef Tile<int8_t, BM, BN, WM, WN> T;
+    __shared__ __align__(1024) char s0[T::STAGE];
+    __shared__ __align__(1024) char s1[T::STAGE];
+    uint32_t tx, ty;
+    tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
+    const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
+    T t;
+    t.run(X, Y, x0, y0, 0, bytes, s0, s1);
+    float c[T::FM][4], b[T::FM][4];
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t x = x0 + t.x_of(i) + e;
+            c[i][e] = x < X.rows ? bs[x] : 0.0f;
+            b[i][e] = bias && x < X.rows ? bias[x] : 0.0f;
+        }
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+        const int64_t y = y0 + t.y_of(j);
+        if (y >= Y.rows) continue;
+        const float s = as[y];
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+            const int64_t x = x0 + t.x_of(i);
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = (float)t.acc[i][j][e] * s * c[i][e] + b[i][e];
+            tile_put(out + y * X.rows + x, v, X.rows - x);
+        }
+    }
+}
+
+// Up to 16 FN tokens.  A workgroup has 16 channels, a wave every fourth piece of 64 bytes x STEPS of the contraction.
+template <class O, int FN>
+__global__ __launch_bounds__(256) void product_few_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
+                                                          const float* __restrict__ bs, const float* __restrict__ bias, int64_t first,
+                                                          O* __restrict__ out)
+{
+    constexpr int STEPS = 4;
+    __shared__ tg_i32x4 s_part[3][FN][64];
+    const int wave = threadIdx.x >> 6, lane = tg_lane(), row = lane & 15, q = lane >> 4;
+    const int64_t x0 = first + (int64_t)blockIdx.x * 16;
+    const bool xin = x0 + row < X.rows;
+    const char* xp = X.p + (xin ? x0 + row : 0) * X.pitch + q * 16;
+    const char* yp[FN];
+    bool yin[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        yin[j] = j * 16 + row < Y.rows;
+        yp[j] = Y.p + (int64_t)(yin[j] ? j * 16 + row : 0) * Y.pitch + q * 16;
+    }
+    tg_i32x4 acc[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[j] = tg_i32x4{0, 0, 0, 0};
+    const tg_i32x4 none = {0, 0, 0, 0};
+    for (int k = wave * 64 * STEPS; k < bytes; k += 4 * 64 * STEPS) {
+        tg_i32x4 x[STEPS], y[STEPS][FN];
+#pragma unroll
+        for (int h = 0; h < STEPS; ++h) {
+            const bool in = k + h * 64 + q * 16 < bytes;
+            x[h] = in && xin ? *reinterpret_cast<const tg_i32x4*>(xp + k + h * 64) : none;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) y[h][j] = in && yin[j] ? *reinterpret_cast<const tg_i32x4*>(yp[j] + k + h * 64) : none;
+        }
+#pragma unroll
+        for (int h = 0; h < STEPS; ++h)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[j] = TileMul<int8_t>::mul(x[h], y[h][j], acc[j]);
+    }
+    if (wave > 0) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) s_part[wave - 1][j][lane] = acc[j];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    const int64_t x = x0 + q * 4;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int64_t y = j * 16 + row;
+        const tg_i32x4 sum = acc[j] + s_part[0][j][lane] + s_part[1][j][lane] + s_part[2][j][lane];
+        if (y >= Y.rows) continue;
+        const float s = as[y];
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool in = x + e < X.rows;
+            v[e] = (float)sum[e] * s * (in ? bs[x + e] : 0.0f) + (in && bias ? bias[x + e] : 0.0f);
+        }
+        if (x < X.rows) tile_put(out + y * X.rows + x, v, X.rows - x);
+    }
+}
+
+// rows of `bytes` bytes, `from` apart, to rows `to` apart (a multiple of 16), the rest zero
+template <class W>
+__global__ __launch_bounds__(256) void pack_kernel(const W* __restrict__ p, int64_t ld, int64_t rows, int d, int per /* W in a row of out */,
+                                                   W* __restrict__ out)
+{
+    const int64_t all = rows * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / per;
+        const int c = (int)(i - r * per);
+        out[i] = c < d ? p[r * ld + c] : (W)0;
+    }
+}
+void tg_launch_pack(const void* p, int64_t ld, int64_t rows, int d, int e, void* out, hipStream_t s)
+{
+    if (rows == 0) return;
+    const int per = (int)(tile_pitch(d, e) / e);
+    const int64_t wgs = (rows * per + 255) / 256;
+    const dim3 g((unsigned)(wgs < 32768 ? wgs : 32768)), b(256);
+    if (e == 1) hipLaunchKernelGGL(pack_kernel<uint8_t>, g, b, 0, s, (const uint8_t*)p, ld, rows, d, per, (uint8_t*)out);
+    else if (e == 2) hipLaunchKernelGGL(pack_kernel<uint16_t>, g, b, 0, s, (const uint16_t*)p, ld, rows, d, per, (uint16_t*)out);
+    else hipLaunchKernelGGL(pack_kernel<uint32_t>, g, b, 0, s, (const uint32_t*)p, ld, rows, d, per, (uint32_t*)out);
+}
+
+size_t tg_product_space(int64_t m, int64_t n, int k, bool ready)
+{
+    if (m == 0 || (ready && (k & 15) == 0)) return 0;
+    TgCarve c{nullptr, 0};
+    c.take<char>((size_t)m * tile_pitch(k, 1));
+    c.take<char>((size_t)n * tile_pitch(k, 1));
+    return c.used;
+}
+
+template <class O, int BM, int BN, int WM, int WN>
+static void launch_tiles(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
+{
+    const uint32_t nx = (uint32_t)((X.rows + BM - 1) / BM), ny = (uint32_t)((Y.rows + BN - 1) / BN);
+    hipLaunchKernelGGL((product_kernel<O, BM, BN, WM, WN>), dim3(nx * ny), dim3(64 * WM * WN), 0, s, X, Y, bytes, as, bs, bias, nx, ny, 8u, out);
+}
+template <class O>
+static void launch_product(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
+{
+    const auto tiles = [&](int64_t bm, int64_t bn) { return ((X.rows + bm - 1) / bm) * ((Y.rows + bn - 1) / bn); };
+    if (bytes > 512 && tiles(256, 256) >= 200) launch_tiles<O, 256, 256, 2, 4>(X, Y, bytes, as, bs, bias, out, s);
+    else if (tiles(128, 128) >= 200) launch_tiles<O, 128, 128, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
+    else launch_tiles<O, 64, 64, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
+}
+
+#define PRODUCT_FEW 64            // tokens up to which b is read straight into the registers
+
+void tg_launch_product(const int8_t* a, const float* as, const int8_t* b, const float* bs, const float* bias, int64_t m, int64_t n, int k,
+                       void* out, int dtype, void* space, hipStream_t s)
+{
+    TileRows Y{(const char*)a, m, (uint32_t)k, (uint32_t)k}, X{(const char*)b, n, (uint32_t)k, (uint32_t)k};
+    if (!tile_ready(a, k, k, 1) || !tile_ready(b, k, k, 1)) {
+        TgCarve c{(char*)space, 0};
+        Y.pitch = X.pitch = Y.width = X.width = tile_pitch(k, 1);
+        char* pa = c.take<char>((size_t)m * Y.pitch);
+        char* pb = c.take<char>((size_t)n * X.pitch);
+        tg_launch_pack(a, k, m, k, 1, pa, s);
+        tg_launch_pack(b, k, n, k, 1, pb, s);
+        Y.p = pa;
+        X.p = pb;
+    }
+    const int bytes = (int)X.pitch;
+    if (m <= PRODUCT_FEW) {
+        const int64_t most = TILE_LAUNCH_ITEMS / 256 * 16;
+        for (int64_t x0 = 0; x0 < n; x0 += most) {
+            const dim3 g((unsigned)(((n - x0 < most ? n - x0 : most) + 15) / 16)), t(256);
+            TG_WITH_TYPE(dtype, O, {
+                if (m <= 16) hipLaunchKernelGGL((product_few_kernel<O, 1>), g, t, 0, s, X, Y, bytes, as, bs, bias, x0, (O*)out);
+                else if (m <= 32) hipLaunchKernelGGL((product_few_kernel<O, 2>), g, t, 0, s, X, Y, bytes, as, bs, bias, x0, (O*)out);
+                else hipLaunchKernelGGL((product_few_kernel<O, 4>), g, t, 0, s, X, Y, bytes, as, bs, bias, x0, (O*)out);
+            });
+        }
+        return;
+    }
+    TG_WITH_TYPE(dtype, O, launch_product<O>(X, Y, bytes, as, bs, bias, (O*)out, s));
+}

@@ -1,0 +1,465 @@
+// Softmax cross entropy of n rows against all rows of a table, and its gradients, without the logits.
+//
+// Forward: a tile of logits stays in the registers of the workgroup that formed it and leaves a maximum and a sum of exponentials for
+// every token and wave; a second kernel joins them over the table.  2 n n_rows d operations on the matrix instructions bound it, or, for
+// few tokens, the bytes of the table.
+//
+// Gradient: the logits are formed again, a piece of the table at a time, and become P = scale dloss (softmax - [target]) in the
+// inputs' type, which goes to memory once (a piece is small enough to be read again while the last-level cache holds it) and into two products:
+// dh += P w over the piece's rows, dw = P^T h over the tokens.  The products read w, h and, for dw, P across their rows, through LDS
+// reads that turn them; no transposed copy is made.  dh is kept in fp32 over the pieces.
+#include "tg_embed.h"
+#include "tg_tiles.h"
+
+#define XENT_LOG2E 1.4426950408889634f
+
+__device__ inline float xent_exp(float x) { return __builtin_amdgcn_exp2f(x * XENT_LOG2E); }
+
+// (maximum, sum) pairs: one that stands for nothing is (-infinity, 0)
+__device__ inline void xent_join(float& m, float& l, float m2, float l2)
+{
+    const float top = fmaxf(m, m2);
+    l = (m == -__builtin_inff() ? l : l * xent_exp(m - top)) + (m2 == -__builtin_inff() ? l2 : l2 * xent_exp(m2 - top));
+    m = top;
+}
+
+// x: rows of the table, y: tokens.  parts: for every stretch of BM / WM rows of the table, (maximum, sum) of every token.
+template <class E, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
+                                                                 float scale, uint32_t nx, uint32_t ny, uint32_t group, float2* __restrict__ parts,
+                                                                 int64_t parts_pitch, float* __restrict__ at_target)
+{
+    typedef Tile<E, BM, BN, WM, WN> T;
+    __shared__ __align__(1024) char s0[T::STAGE];
+    __shared__ __align__(1024) char s1[T::STAGE];
+    uint32_t tx, ty;
+    tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
+    const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
+    T t;
+    t.run(X, Y, x0, y0, 0, bytes, s0, s1);
+    const bool whole = x0 + BM <= X.rows;
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+        const int64_t y = y0 + t.y_of(j);
+        const int64_t target = y < Y.rows ? tg_row_of(targets, targets64, y, X.rows) : -1;
+        float m = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t x = x0 + t.x_of(i) + e;
+                float z = t.acc[i][j][e] * scale;
+                if (x == target) at_target[y] = z;
+                if (!whole && x >= X.rows) z = -__builtin_inff();
+                t.acc[i][j][e] = z;
+                m = fmaxf(m, z);
+            }
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const float b = (m == -__builtin_inff() ? 0.0f : m) * XENT_LOG2E;
+        float l = 0.0f;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], XENT_LOG2E, -b));
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (tg_lane() < 16 && y < Y.rows) parts[((int64_t)tx * WM + (threadIdx.x >> 6) / WN) * parts_pitch + y] = make_float2(m, l);
+    }
+}
+
+// 16 tokens a workgroup, 64 lanes a token: lane j joins the parts j, j + 64, ..., then the lanes are joined as a tree
+__global__ __launch_bounds__(1024) void xent_join_kernel(const float2* __restrict__ parts, int64_t count, int64_t n, int64_t n_rows,
+                                                         const void* __restrict__ targets, int targets64, const float* __restrict__ at_target,
+                                                         float* __restrict__ loss, float* __restrict__ lse)
+{
+    __shared__ float s_m[64][17], s_l[64][17];
+    const int c = threadIdx.x & 15, j = threadIdx.x >> 4;
+    for (int64_t y0 = (int64_t)blockIdx.x * 16; y0 < n; y0 += (int64_t)gridDim.x * 16) {
+        const int64_t y = y0 + c;
+        float m = -__builtin_inff(), l = 0.0f;
+        if (y < n) {
+            for (int64_t p0 = j; p0 < count; p0 += 4 * 64) {
+                float2 v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = p0 + i * 64 < count ? parts[(p0 + i * 64) * n + y] : make_float2(-__builtin_inff(), 0.0f);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) xent_join(m, l, v[i].x, v[i].y);
+            }
+        }
+        s_m[j][c] = m;
+        s_l[j][c] = l;
+        __syncthreads();
+#pragma unroll
+        for (int h = 32; h >= 1; h >>= 1) {
+            if (j < h) {
+                xent_join(m, l, s_m[j + h][c], s_l[j + h][c]);
+                s_m[j][c] = m;
+                s_l[j][c] = l;
+            }
+            __syncthreads();
+        }
+        if (j == 0 && y < n) {
+            const float v = m + logf(l);
+            lse[y] = v;
+            loss[y] = tg_row_of(targets, targets64, y, n_rows) >= 0 ? v - at_target[y] : 0.0f;
+        }
+    }
+}
+
+// ---- gradient
+
+// h without the rows of tokens that have no target (nothing of theirs, not even a NaN, may reach dw), packed for the tiles; per token
+// what P is multiplied by; and, for fp16, the power of two that P is kept under: P is at most |scale| max |dloss|, so that times
+// c it stays below 2^14, and values down to 2^-28 of the largest keep all their bits (bf16 and fp32 have the range as they are: c = 1).
+template <class E>
+__global__ __launch_bounds__(256) void xent_rows_kernel(const E* __restrict__ h, int64_t ld, int64_t n, int64_t n_rows, int d, int per,
+                                                        const void* __restrict__ targets, int targets64, E* __restrict__ out)
+{
+    const int64_t all = n * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        typedef TgPiece<E> P;
+        const int64_t r = i / per;
+        const int at = (int)(i - r * per) * P::E;
+        P p;
+        p.load(h + r * ld + at, tg_row_of(targets, targets64, r, n_rows) >= 0 ? d - at : 0);
+        p.store(out + r * per * P::E + at, P::E);
+    }
+}
+__global__ __launch_bounds__(1024) void xent_range_kernel(const float* __restrict__ dloss, const void* __restrict__ targets, int targets64, int64_t n,
+                                                          int64_t n_rows, float scale, int narrow, float* __restrict__ c)
+{
+    __shared__ float s[16];
+    float top = 0.0f;
+    if (narrow)
+        for (int64_t t = threadIdx.x; t < n; t += 1024)
+            if (tg_row_of(targets, targets64, t, n_rows) >= 0) top = fmaxf(top, fabsf(dloss[t] * scale));
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    int e = 0;
+    if (narrow && top > 0.0f && top <= 3.4028234e38f) (void)frexpf(top, &e);     // top in [2^(e-1), 2^e)
+    else e = 14;
+    int up = 14 - e;
+    up = up < -100 ? -100 : up > 100 ? 100 : up;
+    c[0] = ldexpf(1.0f, up);
+    c[1] = ldexpf(1.0f, -up);
+}
+
+// P of a piece: x: rows v0.. of the table, y: tokens; p: n rows, `pitch` elements apart, zeros behind the piece's rows
+template <class E, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
+                                                              const float* __restrict__ lse, const float* __restrict__ dloss,
+                                                              const float* __restrict__ c, float scale, int64_t v0, int64_t n_rows, uint32_t nx,
+                                                              uint32_t ny, uint32_t group, E* __restrict__ p, int64_t pitch)
+{
+    typedef Tile<E, BM, BN, WM, WN> T;
+    __shared__ __align__(1024) char s0[T::STAGE];
+    __shared__ __align__(1024) char s1[T::STAGE];
+    uint32_t tx, ty;
+    tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
+    const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
+    T t;
+    t.run(X, Y, x0, y0, 0, bytes, s0, s1);
+    const float up = c[0];
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+        const int64_t y = y0 + t.y_of(j);
+        if (y >= Y.rows) continue;
+        const int64_t target = tg_row_of(targets, targets64, y, n_rows);
+        const float g = target >= 0 ? dloss[y] * scale * up : 0.0f, b = lse[y] * XENT_LOG2E;
+        const int64_t hit = target >= 0 ? target - v0 : -1;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+            const int64_t x = x0 + t.x_of(i);
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float s = __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e] * scale, XENT_LOG2E, -b)) - (x + e == hit ? 1.0f : 0.0f);
+                // (a token without a target has no part in anything, whatever its logits are)
+                v[e] = target >= 0 && x + e < X.rows ? s * g : 0.0f;
+            }
+            if (x < pitch) tile_put(p + y * pitch + x, v, pitch - x);
+        }
+    }
+}
+
+// dh: x: columns of w (turned), y: tokens, over the rows of the piece from part `s` of `splits`.  sums: splits x n x d, added to but for the
+// first piece
+template <class E, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void xent_dh_kernel(TileRows X, TileRows Y, int64_t bytes, int64_t each, int d, uint32_t nx, uint32_t ny,
+                                                               int splits, int first, float* __restrict__ sums)
+{
+    typedef Tile<E, BM, BN, WM, WN, true, false> T;
+    __shared__ __align__(1024) char s0[T::STAGE];
+    __shared__ __align__(1024) char s1[T::STAGE];
+    const uint32_t b = tile_of_block(blockIdx.x, nx * ny * splits);
+    const uint32_t s = b / (nx * ny), in = b - s * (nx * ny);
+    const uint32_t tx = in % nx, ty = in / nx;
+    const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
+    const int64_t k0 = s * each, k1 = k0 + each < bytes ? k0 + each : bytes;
+    T t;
+    t.run(X, Y, x0, y0, k0, k1, s0, s1);
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+        const int64_t y = y0 + t.y_of(j);
+        if (y >= Y.rows) continue;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+            const int x = (int)x0 + t.x_of(i);
+            if (x >= d) continue;
+            float* o = sums + ((int64_t)s * Y.rows + y) * d + x;
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = t.acc[i][j][e] + (!first && x + e < d ? o[e] : 0.0f);
+            tile_put(o, v, d - x);
+        }
+    }
+}
+template <class E>
+__global__ __launch_bounds__(256) void xent_dh_out_kernel(const float* __restrict__ sums, int splits, int64_t n, int64_t n_rows, int d, int pieces,
+                                                          const void* __restrict__ targets, int targets64, const float* __restrict__ c,
+                                                          E* __restrict__ dh)
+{
+    const int64_t all = n * pieces;
+    const float down = c[1];
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t y = i / pieces;
+        const int at = (int)(i - y * pieces) * 4;
+        TgPiece<float> sum;
+        sum.load(sums + y * d + at, d - at);
+        for (int s = 1; s < splits; ++s) {
+            TgPiece<float> q;
+            q.load(sums + (s * n + y) * d + at, d - at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum.v[e] += q.v[e];
+        }
+        const bool there = tg_row_of(targets, targets64, y, n_rows) >= 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum.v[e] = there ? sum.v[e] * down : 0.0f;
+        tile_put(dh + y * d + at, sum.v, d - at);
+    }
+}
+
+// dw: x: columns of h (turned), y: columns of P, rows of the piece (turned), over the tokens
+template <class E, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void xent_dw_kernel(TileRows X, TileRows Y, int64_t rows, int64_t bytes, int d, const float* __restrict__ c,
+                                                               uint32_t nx, uint32_t ny, E* __restrict__ dw)
+{
+    typedef Tile<E, BM, BN, WM, WN, true, true> T;
+    __shared__ __align__(1024) char s0[T::STAGE];
+    __shared__ __align__(1024) char s1[T::STAGE];
+    const uint32_t b = tile_of_block(blockIdx.x, nx * ny);
+    const uint32_t tx = b % nx, ty = b / nx;
+    const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
+    T t;
+    t.run(X, Y, x0, y0, 0, bytes, s0, s1);
+    const float down = c[1];
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+        const int64_t y = y0 + t.y_of(j);
+        if (y >= rows) continue;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+            const int x = (int)x0 + t.x_of(i);
+            if (x >= d) continue;
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = t.acc[i][j][e] * down;
+            tile_put(dw + y * d + x, v, d - x);
+        }
+    }
+}
+
+// ---- workspaces and launches
+struct XentRows {
+    TileRows h, w;
+    void *ph, *pw;            // copies, or null
+};
+static void xent_rows(XentRows* r, TgCarve* c, const void* h, int64_t ld_h, const void* w, int64_t ld_w, int64_t n, int64_t n_rows, int d, int e,
+                      bool ready_h, bool ready_w)
+{
+    const uint32_t pitch = tile_pitch(d, e);
+    r->ph = ready_h ? nullptr : c->take<char>((size_t)n * pitch);
+    r->pw = ready_w ? nullptr : c->take<char>((size_t)n_rows * pitch);
+    r->h = ready_h ? TileRows{(const char*)h, n, (uint32_t)(ld_h * e), pitch} : TileRows{(const char*)r->ph, n, pitch, pitch};
+    r->w = ready_w ? TileRows{(const char*)w, n_rows, (uint32_t)(ld_w * e), pitch} : TileRows{(const char*)r->pw, n_rows, pitch, pitch};
+}
+
+// The tile of the logits: 256 x 256 where that leaves every CU one, smaller ones for fewer tokens.  fp32 keeps twice the bytes a
+// value: 128 x 128 there.
+#define XENT_STRETCH 64         // rows of the table that leave one (maximum, sum) in the smallest tile (BM / WM)
+
+size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready)
+{
+    if (n == 0) return 0;
+    const int e = (int)tg_type_bytes(dtype);
+    TgCarve c{nullptr, 0};
+    XentRows r;
+    const bool rd = ready && (d * e & 15) == 0;
+    xent_rows(&r, &c, nullptr, d, nullptr, d, n, n_rows, d, e, rd, rd);
+    c.take<float2>((size_t)((n_rows + XENT_STRETCH - 1) / XENT_STRETCH + 8) * n);
+    c.take<float>(n);
+    return c.used;
+}
+
+template <class E, int BM, int BN, int WM, int WN>
+static int64_t launch_parts(const TileRows& X, const TileRows& Y, int bytes, const void* targets, int targets64, float scale, float2* parts,
+                            float* at_target, hipStream_t s)
+{
+    const int64_t nx = (X.rows + BM - 1) / BM;
+    // (as many tokens a launch as its work-items allow)
+    const int64_t most = TILE_LAUNCH_ITEMS / (64 * WM * WN) / nx * BN;
+    for (int64_t y0 = 0; y0 < Y.rows; y0 += most) {
+        const int64_t rows = Y.rows - y0 < most ? Y.rows - y0 : most;
+        const uint32_t ny = (uint32_t)((rows + BN - 1) / BN);
+        const TileRows part{Y.p + y0 * Y.pitch, rows, Y.pitch, Y.width};
+        hipLaunchKernelGGL((xent_part_kernel<E, BM, BN, WM, WN>), dim3((unsigned)(nx * ny)), dim3(64 * WM * WN), 0, s, X, part, bytes,
+                           (const char*)targets + y0 * (targets64 ? 8 : 4), targets64, scale, (uint32_t)nx, ny, 8u, parts + y0, Y.rows, at_target + y0);
+    }
+    return nx * WM;
+}
+
+void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const void* targets,
+                    int targets64, float scale, float* loss, float* lse, void* space, hipStream_t s)
+{
+    const int e = (int)tg_type_bytes(dtype);
+    TgCarve c{(char*)space, 0};
+    XentRows r;
+    const bool rh = tile_ready(h, ld_h, d, e), rw = tile_ready(w, ld_w, d, e), both = rh && rw;
+    xent_rows(&r, &c, h, ld_h, w, ld_w, n, n_rows, d, e, both, both);
+    if (!both) {
+        tg_launch_pack(h, ld_h, n, d, e, r.ph, s);
+        tg_launch_pack(w, ld_w, n_rows, d, e, r.pw, s);
+    }
+    float2* parts = c.take<float2>((size_t)((n_rows + XENT_STRETCH - 1) / XENT_STRETCH + 8) * n);
+    float* at = c.take<float>(n);
+    int64_t count = 0;
+    TG_WITH_TYPE(dtype, E, {
+        if (n <= 32) count = launch_parts<E, 128, 32, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+        else if (n <= 64) count = launch_parts<E, 128, 64, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+        else if (sizeof(E) == 4 || ((n_rows + 255) / 256) * ((n + 255) / 256) < 200)
+            count = launch_parts<E, 128, 128, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+        else count = launch_parts<E, 256, 256, 2, 4>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+    });
+    const int64_t wgs = (n + 15) / 16;
+    hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(wgs < 65536 ? wgs : 65536)), dim3(1024), 0, s, parts, count, n, n_rows, targets, targets64, at, loss, lse);
+}
+
+#define XENT_PIECE_BYTES (256ll << 20)     // of P, where the workspace has them
+#define XENT_LEAST_ROWS 256                // of a piece
+
+struct XentGrad {
+    int64_t piece;        // rows of the table at a time, a multiple of 256 unless it is all of them
+    int splits;           // of dh's contraction
+};
+static int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+static int xent_splits(int64_t n, int64_t piece, int d, int e)
+{
+    // tiles of 128 x 128 for at least two a CU, each with eight stages of the contraction or more
+    const int64_t tiles = ((n + 127) / 128) * ((d + 127) / 128), stages = (piece * e + TILE_BYTES - 1) / TILE_BYTES;
+    int64_t s = (512 + tiles - 1) / tiles;
+    if (s > stages / 8) s = stages / 8;
+    return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+}
+static size_t carve_xent_grad(XentRows* r, TgCarve* c, const void* h, int64_t ld_h, const void* w, int64_t ld_w, int64_t n, int64_t n_rows, int d,
+                              int e, bool ready_w, XentGrad g, float** consts, char** p, float** sums)
+{
+    xent_rows(r, c, h, ld_h, w, ld_w, n, n_rows, d, e, false, ready_w);       // (h is always copied: see xent_rows_kernel)
+    *consts = c->take<float>(2);
+    *sums = c->take<float>((size_t)g.splits * n * d);
+    *p = c->take<char>((size_t)n * round_up(g.piece * e, 16));
+    return c->used;
+}
+static XentGrad xent_grad_shape(int64_t n, int64_t n_rows, int d, int e, int64_t p_bytes)
+{
+    XentGrad g;
+    g.piece = p_bytes / ((n > 0 ? n : 1) * e) / 256 * 256;
+    if (g.piece < XENT_LEAST_ROWS) g.piece = XENT_LEAST_ROWS;
+    if (g.piece >= n_rows) g.piece = n_rows;
+    else {
+        // equal pieces
+        const int64_t count = (n_rows + g.piece - 1) / g.piece;
+        g.piece = round_up((n_rows + count - 1) / count, 256);
+    }
+    g.splits = xent_splits(n, g.piece, d, e);
+    return g;
+}
+static size_t xent_grad_bytes(int64_t n, int64_t n_rows, int d, int e, bool ready, int64_t p_bytes)
+{
+    TgCarve c{nullptr, 0};
+    XentRows r;
+    float *k, *sums;
+    char* p;
+    return carve_xent_grad(&r, &c, nullptr, d, nullptr, d, n, n_rows, d, e, ready && (d * e & 15) == 0, xent_grad_shape(n, n_rows, d, e, p_bytes), &k, &p, &sums);
+}
+size_t tg_xent_grad_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready, bool least)
+{
+    if (n == 0) return 0;
+    return xent_grad_bytes(n, n_rows, d, (int)tg_type_bytes(dtype), ready, least ? 0 : XENT_PIECE_BYTES);
+}
+
+template <class E>
+static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h, int64_t ld_h, int64_t n, int64_t n_rows, int d, const void* targets,
+                             int targets64, const float* lse, const float* dloss, float scale, float* consts, char* p, float* sums, E* dh, E* dw,
+                             hipStream_t s)
+{
+    const int e = (int)sizeof(E), per = (int)(r.h.pitch / 16);
+    const int64_t wgs = (n * per + 255) / 256;
+    hipLaunchKernelGGL(xent_range_kernel, dim3(1), dim3(1024), 0, s, dloss, targets, targets64, n, n_rows, scale, __is_same(E, tg_f16) ? 1 : 0, consts);
+    hipLaunchKernelGGL(xent_rows_kernel<E>, dim3((unsigned)(wgs < 16384 ? wgs : 16384)), dim3(256), 0, s, (const E*)h, ld_h, n, n_rows, d, per, targets,
+                       targets64, (E*)r.ph);
+    for (int64_t v0 = 0; v0 < n_rows; v0 += g.piece) {
+        const int64_t rows = n_rows - v0 < g.piece ? n_rows - v0 : g.piece;
+        const TileRows W{r.w.p + v0 * r.w.pitch, rows, r.w.pitch, r.w.width};
+        const uint32_t pitch = (uint32_t)round_up(rows * e, 16);
+        const TileRows P{p, n, pitch, pitch};
+        const auto logits = [&](auto kernel, int bm, int bn, int threads) {
+            const uint32_t nx = (uint32_t)((rows + bm - 1) / bm), ny = (uint32_t)((n + bn - 1) / bn);
+            hipLaunchKernelGGL(kernel, dim3(nx * ny), dim3(threads), 0, s, W, r.h, (int)W.width, targets, targets64, lse, dloss, (const float*)consts, scale,
+                               v0, n_rows, nx, ny, 8u, (E*)p, (int64_t)(pitch / e));
+        };
+        if (n <= 64) logits(xent_p_kernel<E, 128, 64, 2, 2>, 128, 64, 256);
+        else if (sizeof(E) == 4 || ((rows + 255) / 256) * ((n + 255) / 256) < 200) logits(xent_p_kernel<E, 128, 128, 2, 2>, 128, 128, 256);
+        else logits(xent_p_kernel<E, 256, 256, 2, 4>, 256, 256, 512);
+        {
+            const int64_t stages = ((int64_t)pitch + TILE_BYTES - 1) / TILE_BYTES, each = (stages + g.splits - 1) / g.splits * TILE_BYTES;
+            const uint32_t nx = (uint32_t)((d + 127) / 128), ny = (uint32_t)((n + 127) / 128);
+            hipLaunchKernelGGL((xent_dh_kernel<E, 128, 128, 2, 2>), dim3(nx * ny * g.splits), dim3(256), 0, s, W, P, (int64_t)pitch, each, d, nx, ny,
+                               g.splits, v0 == 0 ? 1 : 0, sums);
+        }
+        {
+            const uint32_t nx = (uint32_t)((d + 127) / 128), ny = (uint32_t)((rows + 127) / 128);
+            hipLaunchKernelGGL((xent_dw_kernel<E, 128, 128, 2, 2>), dim3(nx * ny), dim3(256), 0, s, r.h, P, rows, n * e, d, (const float*)consts, nx, ny,
+                               dw + v0 * d);
+        }
+    }
+    const int64_t out_wgs = (n * ((d + 3) / 4) + 255) / 256;
+    hipLaunchKernelGGL(xent_dh_out_kernel<E>, dim3((unsigned)(out_wgs < 16384 ? out_wgs : 16384)), dim3(256), 0, s, sums, g.splits, n, n_rows, d,
+                       (d + 3) / 4, targets, targets64, (const float*)consts, dh);
+}
+
+void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const void* targets,
+                         int targets64, const float* lse, const float* dloss, float scale, void* dh, void* dw, void* space, size_t bytes, hipStream_t s)
+{
+    const int e = (int)tg_type_bytes(dtype);
+    if (n == 0) {
+        tg_launch_zero(dw, (size_t)n_rows * d * e, s);
+        return;
+    }
+    const bool ready = tile_ready(w, ld_w, d, e) && (((uintptr_t)h & 15) == 0 && (ld_h * e & 15) == 0);
+    // the largest piece that the workspace holds
+    int64_t p_bytes = XENT_PIECE_BYTES * 64;
+    while (p_bytes > 0 && xent_grad_bytes(n, n_rows, d, e, ready, p_bytes) > bytes) p_bytes = p_bytes > (1 << 20) ? p_bytes / 2 : 0;
+    const XentGrad g = xent_grad_shape(n, n_rows, d, e, p_bytes);
+    TgCarve c{(char*)space, 0};
+    XentRows r;
+    float *consts, *sums;
+    char* p;
+    carve_xent_grad(&r, &c, h, ld_h, w, ld_w, n, n_rows, d, e, ready, g, &consts, &p, &sums);
+    if (!ready) tg_launch_pack(w, ld_w, n_rows, d, e, r.pw, s);
+    TG_WITH_TYPE(dtype, E, launch_xent_grad<E>(r, g, h, ld_h, n, n_rows, d, targets, targets64, lse, dloss, scale, consts, p, sums, (E*)dh, (E*)dw, s));
+}

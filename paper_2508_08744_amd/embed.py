@@ -1,0 +1,293 @@
+"""Python binding of include/tagore_embed.h: the operators that learn and serve the vectors a graph is built over.
+
+Argument marshalling only, like ``knn``: torch supplies device memory and the current stream, the HIP library does the work, and there
+is no fallback.  Training calls come in pairs, an operator and its gradient; nothing is kept between them but what the caller passes on.
+Matrices may have any row stride (their last dimension must be contiguous); results are new contiguous tensors.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import knn
+from .knn import TagoreError  # noqa: F401  (what a refused call raises)
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+EXPORTS = ["tg_embed_lookup", "tg_embed_lookup_grad_workspace", "tg_embed_lookup_grad", "tg_add_rms_norm", "tg_add_rms_norm_grad_workspace",
+           "tg_add_rms_norm_grad", "tg_add_rms_norm_q8", "tg_quantize_rows", "tg_dequantize_rows", "tg_matmul_q8_workspace", "tg_matmul_q8",
+           "tg_softmax_xent_workspace", "tg_softmax_xent", "tg_softmax_xent_grad_workspace", "tg_softmax_xent_grad"]
+
+_lib = None
+
+
+def lib():
+    """The loaded library with this header's signatures; raises if it has not been built."""
+    global _lib
+    if _lib is None:
+        L = knn.lib()
+        vp, i64, i32, f32, sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
+        L.tg_embed_lookup.argtypes = [vp, i64, i32, i64, i32, vp, i32, i64, f32, vp, vp]
+        L.tg_embed_lookup_grad_workspace.argtypes = [i64, i64, i32]
+        L.tg_embed_lookup_grad.argtypes = [vp, i64, i32, vp, i32, i64, i64, i32, f32, i32, vp, i32, vp, sz, vp]
+        L.tg_add_rms_norm.argtypes = [vp, i64, vp, i64, vp, i32, i64, i32, f32, vp, vp, vp, vp]
+        L.tg_add_rms_norm_grad_workspace.argtypes = [i64, i32]
+        L.tg_add_rms_norm_grad.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, i32, i64, i32, vp, vp, vp, sz, vp]
+        L.tg_add_rms_norm_q8.argtypes = [vp, i64, vp, i64, vp, i32, i64, i32, f32, vp, vp, vp, vp]
+        L.tg_quantize_rows.argtypes = [vp, i64, i32, i64, i32, vp, vp, vp]
+        L.tg_dequantize_rows.argtypes = [vp, vp, i64, i32, i32, vp, vp]
+        L.tg_matmul_q8_workspace.argtypes = [i64, i64, i32, i32]
+        L.tg_matmul_q8.argtypes = [vp, vp, vp, vp, vp, i64, i64, i32, vp, i32, vp, sz, vp]
+        L.tg_softmax_xent_workspace.argtypes = [i64, i64, i32, i32, i32]
+        L.tg_softmax_xent.argtypes = [vp, i64, vp, i64, i32, i64, i64, i32, vp, i32, f32, vp, vp, vp, sz, vp]
+        L.tg_softmax_xent_grad_workspace.argtypes = [i64, i64, i32, i32, i32]
+        L.tg_softmax_xent_grad.argtypes = [vp, i64, vp, i64, i32, i64, i64, i32, vp, i32, vp, vp, f32, vp, vp, vp, sz, vp]
+        for name in EXPORTS:
+            if name.endswith("_workspace"):
+                getattr(L, name).restype = sz
+        _lib = L
+    return _lib
+
+
+def _check(rc):
+    if rc != 0:
+        raise TagoreError("tagore_knn error %d: %s" % (rc, lib().tg_last_error().decode()))
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _on_device(name, t, dtypes, dim):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in dtypes and t.dim() == dim):
+        raise TypeError("%s must be a %d-D CUDA tensor of %s" % (name, dim, " or ".join(str(d) for d in dtypes)))
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is not on the current device" % name)
+    return t
+
+
+def _rows(name, t, like=None, shape=None):
+    """A matrix whose rows are contiguous, and the distance between them."""
+    _on_device(name, t, DTYPES if like is None else (like,), 2)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s" % (name, tuple(shape)))
+    n, d = t.shape
+    if d > 1 and t.stride(1) != 1 or n > 1 and t.stride(0) < d:
+        raise ValueError("%s must have contiguous rows that do not overlap" % name)
+    return t, (t.stride(0) if n > 1 else d)
+
+
+def _vector(name, t, n, dtypes):
+    _on_device(name, t, dtypes, 1)
+    if t.numel() != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError("%s must be contiguous and have %d elements" % (name, n))
+    return t
+
+
+def _ids(name, t, n=None):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in (torch.int32, torch.int64) and t.is_contiguous()):
+        raise TypeError("%s must be a contiguous int32 or int64 CUDA tensor" % name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is not on the current device" % name)
+    if n is not None and t.numel() != n:
+        raise ValueError("%s must have %d elements" % (name, n))
+    return t, int(t.dtype == torch.int64)
+
+
+def _space(nbytes, device):
+    """A workspace and its size; the memory is the current stream's, as the calls are."""
+    if nbytes == 0:
+        return None, None, 0
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), nbytes
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _aligned(*rows):
+    """Whether the matrices start at multiples of 16 bytes and their rows are such a multiple (of at most 1 MiB) apart."""
+    for t, ld in rows:
+        step = ld * t.element_size()
+        if t.data_ptr() % 16 or step % 16 or step > 1 << 20:
+            return 0
+    return 1
+
+
+def lookup(table, ids, scale=1.0):
+    """tg_embed_lookup: scale * table[ids], zeros where an id is no row of the table; the shape of ids and the rows' length."""
+    table, ld = _rows("table", table)
+    ids, wide = _ids("ids", ids)
+    v, d = table.shape
+    out = torch.empty(ids.shape + (d,), dtype=table.dtype, device=table.device)
+    _check(lib().tg_embed_lookup(table.data_ptr(), ld, DTYPES[table.dtype], v, d, ids.data_ptr(), wide, ids.numel(), scale, out.data_ptr(), _stream()))
+    return out
+
+
+def lookup_grad(grad, ids, n_rows, scale=1.0, out=None):
+    """tg_embed_lookup_grad: the gradient of ``lookup`` with respect to its table of ``n_rows`` rows.
+
+    grad has a row for every id (its leading dimensions may be those of ids).  With ``out`` (a contiguous fp32 tensor, or one of
+    grad's type) the sums are added to it and only rows with a token are touched; without, a new tensor of grad's type is returned.
+    """
+    ids, wide = _ids("ids", ids)
+    n = ids.numel()
+    if isinstance(grad, torch.Tensor) and grad.dim() > 2 and grad.shape[:-1] == ids.shape:
+        grad = grad.reshape(-1, grad.shape[-1])
+    grad, ld = _rows("grad", grad)
+    if grad.shape[0] != n:
+        raise ValueError("grad must have a row for every id")
+    d = grad.shape[1]
+    add = out is not None
+    if add:
+        _rows("out", out, shape=(n_rows, d))
+        if out.dtype not in (torch.float32, grad.dtype) or not out.is_contiguous():
+            raise TypeError("out must be contiguous and float32 or of the gradient's type")
+    else:
+        out = torch.empty((n_rows, d), dtype=grad.dtype, device=grad.device)
+    keep, ws, nbytes = _space(lib().tg_embed_lookup_grad_workspace(n, n_rows, d), grad.device)
+    _check(lib().tg_embed_lookup_grad(grad.data_ptr(), ld, DTYPES[grad.dtype], ids.data_ptr(), wide, n, n_rows, d, scale, int(add), out.data_ptr(),
+                                      DTYPES[out.dtype], ws, nbytes, _stream()))
+    return out
+
+
+def add_rms_norm(x, weight, residual=None, eps=1e-6):
+    """tg_add_rms_norm: (y, r, rstd) with r = x + residual (x itself where there is none) and y = r rstd weight."""
+    x, ld = _rows("x", x)
+    n, d = x.shape
+    _vector("weight", weight, d, (x.dtype,))
+    y = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+    r, ld_res = x, 0
+    if residual is not None:
+        residual, ld_res = _rows("residual", residual, x.dtype, x.shape)
+        r = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    _check(lib().tg_add_rms_norm(x.data_ptr(), ld, _ptr(residual), ld_res, weight.data_ptr(), DTYPES[x.dtype], n, d, eps, y.data_ptr(),
+                                 None if residual is None else r.data_ptr(), rstd.data_ptr(), _stream()))
+    return y, r, rstd
+
+
+def add_rms_norm_grad(dy, r, weight, rstd, dr=None):
+    """tg_add_rms_norm_grad: (dx, dweight) from the gradients dy of y and dr of r; dx is the residual's gradient as well."""
+    r, ld_r = _rows("r", r)
+    n, d = r.shape
+    dy, ld_dy = _rows("dy", dy, r.dtype, r.shape)
+    ld_dr = 0
+    if dr is not None:
+        dr, ld_dr = _rows("dr", dr, r.dtype, r.shape)
+    _vector("weight", weight, d, (r.dtype,))
+    _vector("rstd", rstd, n, (torch.float32,))
+    dx = torch.empty((n, d), dtype=r.dtype, device=r.device)
+    dw = torch.empty(d, dtype=r.dtype, device=r.device)
+    keep, ws, nbytes = _space(lib().tg_add_rms_norm_grad_workspace(n, d), r.device)
+    _check(lib().tg_add_rms_norm_grad(dy.data_ptr(), ld_dy, _ptr(dr), ld_dr, r.data_ptr(), ld_r, weight.data_ptr(), rstd.data_ptr(), DTYPES[r.dtype],
+                                      n, d, dx.data_ptr(), dw.data_ptr(), ws, nbytes, _stream()))
+    return dx, dw
+
+
+def add_rms_norm_q8(x, weight, residual=None, eps=1e-6):
+    """tg_add_rms_norm_q8: (q, scale, r), the normed rows as int8 with a scale each, and the residual stream."""
+    x, ld = _rows("x", x)
+    n, d = x.shape
+    _vector("weight", weight, d, (x.dtype,))
+    q = torch.empty((n, d), dtype=torch.int8, device=x.device)
+    scale = torch.empty(n, dtype=torch.float32, device=x.device)
+    r, ld_res = x, 0
+    if residual is not None:
+        residual, ld_res = _rows("residual", residual, x.dtype, x.shape)
+        r = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    _check(lib().tg_add_rms_norm_q8(x.data_ptr(), ld, _ptr(residual), ld_res, weight.data_ptr(), DTYPES[x.dtype], n, d, eps, q.data_ptr(),
+                                    scale.data_ptr(), None if residual is None else r.data_ptr(), _stream()))
+    return q, scale, r
+
+
+def quantize_rows(x):
+    """tg_quantize_rows: (q, scale), the rows as int8 with a scale each."""
+    x, ld = _rows("x", x)
+    n, d = x.shape
+    q = torch.empty((n, d), dtype=torch.int8, device=x.device)
+    scale = torch.empty(n, dtype=torch.float32, device=x.device)
+    _check(lib().tg_quantize_rows(x.data_ptr(), ld, DTYPES[x.dtype], n, d, q.data_ptr(), scale.data_ptr(), _stream()))
+    return q, scale
+
+
+def _codes(name, q, scale):
+    _on_device(name, q, (torch.int8,), 2)
+    if not q.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    _vector(name + "_scale", scale, q.shape[0], (torch.float32,))
+    return q
+
+
+def dequantize_rows(q, scale, dtype=torch.float32):
+    """tg_dequantize_rows: q * scale, rounded to dtype."""
+    _codes("q", q, scale)
+    if dtype not in DTYPES:
+        raise TypeError("dtype must be float32, bfloat16 or float16")
+    n, d = q.shape
+    out = torch.empty((n, d), dtype=dtype, device=q.device)
+    _check(lib().tg_dequantize_rows(q.data_ptr(), scale.data_ptr(), n, d, DTYPES[dtype], out.data_ptr(), _stream()))
+    return out
+
+
+def matmul_q8(a, a_scale, b, b_scale, bias=None, out_dtype=torch.float32):
+    """tg_matmul_q8: (a * a_scale) @ (b * b_scale).T (+ bias) with an exact integer sum; a: m x k tokens, b: n x k channels, int8."""
+    _codes("a", a, a_scale)
+    _codes("b", b, b_scale)
+    m, k = a.shape
+    n = b.shape[0]
+    if b.shape[1] != k:
+        raise ValueError("a and b must have rows of the same length")
+    if bias is not None:
+        _vector("bias", bias, n, (torch.float32,))
+    if out_dtype not in DTYPES:
+        raise TypeError("out_dtype must be float32, bfloat16 or float16")
+    out = torch.empty((m, n), dtype=out_dtype, device=a.device)
+    aligned = int((a.data_ptr() | b.data_ptr()) % 16 == 0)
+    keep, ws, nbytes = _space(lib().tg_matmul_q8_workspace(m, n, k, aligned), a.device)
+    _check(lib().tg_matmul_q8(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(bias), m, n, k, out.data_ptr(),
+                              DTYPES[out_dtype], ws, nbytes, _stream()))
+    return out
+
+
+def softmax_xent(h, w, targets, scale=1.0):
+    """tg_softmax_xent: (loss, lse) of every row of h scored against all rows of w; 0 where a target is no row of w."""
+    h, ld_h = _rows("h", h)
+    n, d = h.shape
+    w, ld_w = _rows("w", w, h.dtype)
+    if w.shape[1] != d:
+        raise ValueError("h and w must have rows of the same length")
+    targets, wide = _ids("targets", targets, n)
+    loss = torch.empty(n, dtype=torch.float32, device=h.device)
+    lse = torch.empty(n, dtype=torch.float32, device=h.device)
+    t = DTYPES[h.dtype]
+    keep, ws, nbytes = _space(lib().tg_softmax_xent_workspace(n, w.shape[0], d, t, _aligned((h, ld_h), (w, ld_w))), h.device)
+    _check(lib().tg_softmax_xent(h.data_ptr(), ld_h, w.data_ptr(), ld_w, t, n, w.shape[0], d, targets.data_ptr(), wide, scale, loss.data_ptr(),
+                                 lse.data_ptr(), ws, nbytes, _stream()))
+    return loss, lse
+
+
+def softmax_xent_grad(h, w, targets, lse, dloss, scale=1.0, workspace=None):
+    """tg_softmax_xent_grad: (dh, dw) from the gradient dloss of every token's loss.  ``workspace``: a uint8 tensor to use instead of
+    a new one; a smaller one makes smaller pieces of the table, down to what the library refuses."""
+    h, ld_h = _rows("h", h)
+    n, d = h.shape
+    w, ld_w = _rows("w", w, h.dtype)
+    if w.shape[1] != d:
+        raise ValueError("h and w must have rows of the same length")
+    targets, wide = _ids("targets", targets, n)
+    _vector("lse", lse, n, (torch.float32,))
+    _vector("dloss", dloss, n, (torch.float32,))
+    dh = torch.empty((n, d), dtype=h.dtype, device=h.device)
+    dw = torch.empty(w.shape, dtype=h.dtype, device=h.device)
+    t = DTYPES[h.dtype]
+    if workspace is None:
+        keep, ws, nbytes = _space(lib().tg_softmax_xent_grad_workspace(n, w.shape[0], d, t, _aligned((h, ld_h), (w, ld_w))), h.device)
+    else:
+        _on_device("workspace", workspace, (torch.uint8,), 1)
+        ws, nbytes = workspace.data_ptr(), workspace.numel()
+    _check(lib().tg_softmax_xent_grad(h.data_ptr(), ld_h, w.data_ptr(), ld_w, t, n, w.shape[0], d, targets.data_ptr(), wide, lse.data_ptr(),
+                                      dloss.data_ptr(), scale, dh.data_ptr(), dw.data_ptr(), ws, nbytes, _stream()))
+    return dh, dw
