@@ -12,6 +12,15 @@ template <class T> struct TgPiece {
     static constexpr int E = 16 / (int)sizeof(T);
     typedef T vec __attribute__((ext_vector_type(E), aligned(sizeof(T))));
     float v[E];
+    // the 16 bytes as they are: held until they are needed they take half the registers of 16-bit values
+    static __device__ inline vec raw(const T* p, int left)
+    {
+        if (left >= E) return *reinterpret_cast<const vec*>(p);
+        vec x;
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = i < left ? p[i] : (T)0.0f;
+        return x;
+    }
     // `left` elements of the row from p on (E or more: a whole piece); what is not there reads as zero
     __device__ inline void load(const T* p, int left)
     {

@@ -48,24 +48,42 @@ void tg_launch_lookup(const void* table, int64_t ld, int dtype, int64_t n_rows, 
     });
 }
 
-// ---- zeros: `halves` values of 16 bits, the first `head` of them in front of a 16-byte boundary
-__global__ __launch_bounds__(256) void zero_kernel(uint16_t* __restrict__ p, size_t halves, size_t head)
+// ---- zeros: `halves` values of 16 bits, the first `head` of them in front of a 16-byte boundary.  The sort has few workgroups and
+// waits for memory most of the time, so the gradient's rows are cleared beside it: every launch of it takes a part of them.
+struct ZeroPart {
+    uint16_t* p;
+    size_t halves, head;
+    uint32_t part, parts;        // which part of the 16-byte pieces this launch clears
+    uint32_t first;              // its workgroups are the ones from here on
+};
+__device__ inline void zero_part(const ZeroPart& z)
 {
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, step = (size_t)gridDim.x * 256;
-    uint4* q = reinterpret_cast<uint4*>(p + head);
-    const size_t pieces = (halves - head) / 8;
-    for (size_t j = i; j < pieces; j += step) q[j] = make_uint4(0, 0, 0, 0);
-    if (i < head) p[i] = 0;
-    if (i < (halves - head) % 8) p[head + pieces * 8 + i] = 0;
+    const size_t i = (size_t)(blockIdx.x - z.first) * blockDim.x + threadIdx.x, step = (size_t)(gridDim.x - z.first) * blockDim.x;
+    uint4* q = reinterpret_cast<uint4*>(z.p + z.head);
+    const size_t pieces = (z.halves - z.head) / 8, from = pieces * z.part / z.parts, to = pieces * (z.part + 1) / z.parts;
+    for (size_t j = from + i; j < to; j += step) q[j] = make_uint4(0, 0, 0, 0);
+    if (z.part) return;
+    if (i < z.head) z.p[i] = 0;
+    if (i < (z.halves - z.head) % 8) z.p[z.head + pieces * 8 + i] = 0;
+}
+__global__ __launch_bounds__(256) void zero_kernel(ZeroPart z) { zero_part(z); }
+static ZeroPart zero_of(void* p, size_t bytes)
+{
+    ZeroPart z{(uint16_t*)p, bytes / 2, ((16 - ((uintptr_t)p & 15)) & 15) / 2, 0, 1, 0};
+    if (z.head > z.halves) z.head = z.halves;
+    return z;
+}
+// workgroups of 256 that clear a part: 16 KB each, up to 2048
+static unsigned zero_wgs(const ZeroPart& z)
+{
+    if (z.halves == 0) return 0;
+    const size_t w = z.halves / 8192 / z.parts + 1;
+    return (unsigned)(w < 2048 ? w : 2048);
 }
 void tg_launch_zero(void* p, size_t bytes, hipStream_t s)
 {
-    const size_t halves = bytes / 2;
-    if (halves == 0) return;
-    size_t head = ((16 - ((uintptr_t)p & 15)) & 15) / 2;
-    if (head > halves) head = halves;
-    const size_t wgs = (halves / 8 + 255) / 256 + 1;
-    hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(256), 0, s, (uint16_t*)p, halves, head);
+    const ZeroPart z = zero_of(p, bytes);
+    if (z.halves) hipLaunchKernelGGL(zero_kernel, dim3(zero_wgs(z)), dim3(256), 0, s, z);
 }
 
 // ---- the tokens sorted by id.  A token without a row gets the key n_rows and ends up behind the others.
@@ -79,8 +97,10 @@ __device__ inline u32 token_key(const void* ids, int ids64, int64_t t, int64_t n
 // One launch instead of the six of the digits' sort (8192 tokens: RANK_MAX squared comparisons are 6 us; twice as many would be 24).
 #define RANK_MAX 8192
 __global__ __launch_bounds__(256) void rank_sort_kernel(const void* __restrict__ ids, int ids64, int n, int64_t n_rows, u32* __restrict__ skey,
-                                                        u32* __restrict__ spos)
+                                                        u32* __restrict__ spos, u32* __restrict__ runs, ZeroPart z)
 {
+    if (blockIdx.x >= z.first) { zero_part(z); return; }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *runs = 0;
     extern __shared__ __align__(16) u32 s_rank_keys[];      // n rounded up to 64, the rest larger than any key
     const int full = (n + 63) & ~63;
     for (int i = threadIdx.x; i < full; i += 256) s_rank_keys[i] = i < n ? token_key(ids, ids64, i, n_rows) : 0xFFFFFFFFu;
@@ -119,7 +139,7 @@ static SortShape sort_shape(int64_t n, int64_t n_rows)
     f.passes = (b + DIGIT_MAX - 1) / DIGIT_MAX;
     f.bits = (b + f.passes - 1) / f.passes;
     int64_t chunk = (n + SORT_WGS - 1) / SORT_WGS;
-    chunk = (chunk + 1023) & ~(int64_t)1023;
+    chunk = (chunk + 255) & ~(int64_t)255;
     f.chunk = chunk;
     f.wgs = (n + chunk - 1) / chunk;
     return f;
@@ -136,8 +156,11 @@ __device__ inline void count_digits(const void* ids, int ids64, const u32* key_i
 }
 // per workgroup and digit: how many.  table: digit-major, wgs a digit
 __global__ __launch_bounds__(256) void digit_count_kernel(const void* __restrict__ ids, int ids64, const u32* __restrict__ key_in, int64_t n,
-                                                          int64_t n_rows, int64_t chunk, int shift, int bits, u32* __restrict__ table)
+                                                          int64_t n_rows, int64_t chunk, int shift, int bits, u32* __restrict__ table,
+                                                          u32* __restrict__ runs, ZeroPart z)
 {
+    if (blockIdx.x >= z.first) { zero_part(z); return; }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *runs = 0;
     __shared__ u32 s_count[1 << DIGIT_MAX];
     for (int i = threadIdx.x; i < 1 << bits; i += 256) s_count[i] = 0;
     __syncthreads();
@@ -146,11 +169,12 @@ __global__ __launch_bounds__(256) void digit_count_kernel(const void* __restrict
     if (to > n) to = n;
     count_digits(ids, ids64, key_in, n, n_rows, from, to, shift, bits, s_count);
     __syncthreads();
-    for (int i = threadIdx.x; i < 1 << bits; i += 256) table[(int64_t)i * gridDim.x + blockIdx.x] = s_count[i];
+    for (int i = threadIdx.x; i < 1 << bits; i += 256) table[(int64_t)i * z.first + blockIdx.x] = s_count[i];
 }
 // a wave a digit: its counts become the number of tokens in workgroups before, their sum goes to total[digit]
-__global__ __launch_bounds__(256) void digit_scan_kernel(u32* __restrict__ table, int wgs, int digits, u32* __restrict__ total)
+__global__ __launch_bounds__(256) void digit_scan_kernel(u32* __restrict__ table, int wgs, int digits, u32* __restrict__ total, ZeroPart z)
 {
+    if (blockIdx.x >= z.first) { zero_part(z); return; }
     const int digit = blockIdx.x * 4 + (threadIdx.x >> 6), lane = tg_lane();
     if (digit >= digits) return;
     u32 base = 0;
@@ -172,8 +196,9 @@ __global__ __launch_bounds__(256) void digit_scan_kernel(u32* __restrict__ table
 __global__ __launch_bounds__(256) void digit_place_kernel(const void* __restrict__ ids, int ids64, const u32* __restrict__ key_in,
                                                           const u32* __restrict__ pos_in, int64_t n, int64_t n_rows, int64_t chunk, int shift,
                                                           int bits, const u32* __restrict__ table, const u32* __restrict__ total,
-                                                          u32* __restrict__ key_out, u32* __restrict__ pos_out)
+                                                          u32* __restrict__ key_out, u32* __restrict__ pos_out, ZeroPart z)
 {
+    if (blockIdx.x >= z.first) { zero_part(z); return; }
     __shared__ u32 s_next[4][1 << DIGIT_MAX];
     __shared__ u32 s_wave[4];
     const int wave = threadIdx.x >> 6, lane = tg_lane(), digits = 1 << bits;
@@ -201,7 +226,7 @@ __global__ __launch_bounds__(256) void digit_place_kernel(const void* __restrict
         for (int j = 0; j < wave; ++j) before += s_wave[j];
         base += s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
         if (i < digits) {
-            u32 at = before + x - c + table[(int64_t)i * gridDim.x + blockIdx.x];
+            u32 at = before + x - c + table[(int64_t)i * z.first + blockIdx.x];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const u32 k = s_next[j][i];
@@ -239,7 +264,7 @@ __global__ __launch_bounds__(256) void digit_place_kernel(const void* __restrict
 }
 
 // ---- sums over the runs of the sorted list
-#define RUN_TILE 32
+#define RUN_TILE 16
 template <class E, class O>
 __device__ inline void write_row(const float* v, int left, O* p, float scale, bool add)
 {
@@ -267,110 +292,118 @@ __device__ inline void write_row(const float* v, int left, O* p, float scale, bo
     }
 }
 
-// G lanes a tile, a piece of the row a lane, as many columns of tiles as the row has G pieces.  parts: two rows of d per tile: of a run
-// that came from the tile before, and of one that goes on in the next but began here.
+// G lanes a tile, a piece of the row a lane, as many columns of tiles as the row has G pieces.  All of a tile's rows are asked for before
+// the first is added.  parts: two rows of d per tile: of a run that came from the tile before, and of one that goes on in the next
+// but began here; such tiles are listed in runs[1..], runs[0] of them, in any order.
 template <class E, class O>
 __global__ __launch_bounds__(256) void run_sum_kernel(const E* __restrict__ grad, int64_t ld, const u32* __restrict__ skey,
                                                       const u32* __restrict__ spos, int64_t n, int64_t n_rows, int d, float scale, int add,
-                                                      int gshift, int columns, O* __restrict__ out, float* __restrict__ parts)
+                                                      int gshift, int columns, O* __restrict__ out, float* __restrict__ parts,
+                                                      u32* __restrict__ runs)
 {
     typedef TgPiece<E> P;
     const int lane = threadIdx.x & ((1 << gshift) - 1);
     const int64_t unit = (int64_t)blockIdx.x * (256 >> gshift) + (threadIdx.x >> gshift);
     const int64_t tile = unit / columns;
-    const int at = (int)(((unit - tile * columns) << gshift) + lane) * P::E;
+    const int column = (int)(unit - tile * columns);
+    const int at = ((column << gshift) + lane) * P::E;
     const int64_t i0 = tile * RUN_TILE;
     if (i0 >= n || at >= d) return;
     const int count = (int)(n - i0 < RUN_TILE ? n - i0 : RUN_TILE);
     const u32 none = (u32)n_rows;
-    u32 cur = skey[i0];
+    u32 key[RUN_TILE];
+    typename P::vec g[RUN_TILE];
+    {
+        // (the arrays hold whole tiles)
+        u32 pos[RUN_TILE];
+#pragma unroll
+        for (int j = 0; j < RUN_TILE; j += 4) {
+            *reinterpret_cast<uint4*>(key + j) = *reinterpret_cast<const uint4*>(skey + i0 + j);
+            *reinterpret_cast<uint4*>(pos + j) = *reinterpret_cast<const uint4*>(spos + i0 + j);
+        }
+#pragma unroll
+        for (int j = 0; j < RUN_TILE; ++j) {
+            if (j >= count) key[j] = none;
+            g[j] = P::raw(grad + (int64_t)(key[j] == none ? 0u : pos[j]) * ld + at, key[j] == none ? 0 : d - at);
+        }
+    }
+    u32 cur = key[0];
     if (cur == none) return;                                // (from here on there are only tokens without a row)
     bool carried = i0 > 0 && skey[i0 - 1] == cur;
+    const bool goes_on = i0 + count < n && skey[i0 + count] == key[RUN_TILE - 1] && key[RUN_TILE - 1] != none;
     float acc[P::E];
 #pragma unroll
     for (int i = 0; i < P::E; ++i) acc[i] = 0.0f;
-    constexpr int AHEAD = 8;
-    for (int j0 = 0; j0 < count; j0 += AHEAD) {
-        u32 key[AHEAD];
-        P g[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const bool real = j0 + j < count;
-            key[j] = real ? skey[i0 + j0 + j] : none;
-            const u32 pos = real ? spos[i0 + j0 + j] : 0u;
-            g[j].load(grad + (int64_t)pos * ld + at, key[j] == none ? 0 : d - at);
+    for (int j = 0; j < RUN_TILE; ++j) {
+        if (key[j] != cur) {
+            if (carried) {
+#pragma unroll
+                for (int i = 0; i < P::E; ++i)
+                    if (at + i < d) parts[2 * tile * d + at + i] = acc[i];
+            } else write_row<E, O>(acc, d - at, out + (int64_t)cur * d + at, scale, add != 0);
+            carried = false;
+            cur = key[j];
+            if (cur == none) return;
+#pragma unroll
+            for (int i = 0; i < P::E; ++i) acc[i] = 0.0f;
         }
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            if (key[j] != cur) {
-                if (cur != none) {
-                    if (carried) {
-                        for (int i = 0; i < P::E; ++i)
-                            if (at + i < d) parts[2 * tile * d + at + i] = acc[i];
-                    } else write_row<E, O>(acc, d - at, out + (int64_t)cur * d + at, scale, add != 0);
-                }
-                carried = false;
-                cur = key[j];
-#pragma unroll
-                for (int i = 0; i < P::E; ++i) acc[i] = 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < P::E; ++i) acc[i] += g[j].v[i];
-        }
+        for (int i = 0; i < P::E; ++i) acc[i] += (float)g[j][i];
     }
-    if (cur == none) return;
-    const bool goes_on = i0 + count < n && skey[i0 + count] == cur;
     if (!carried && !goes_on) { write_row<E, O>(acc, d - at, out + (int64_t)cur * d + at, scale, add != 0); return; }
     float* p = parts + (2 * tile + (carried ? 0 : 1)) * (int64_t)d + at;
 #pragma unroll
     for (int i = 0; i < P::E; ++i)
         if (at + i < d) p[i] = acc[i];
+    if (!carried && column == 0 && lane == 0) runs[1 + atomicAdd(runs, 1u)] = (u32)tile;
 }
 
-// A workgroup a tile: where a run begins in the tile and goes on, its parts are added: the waves take an equal stretch of the tiles each,
-// and are added in their order.
+// 64 columns of a listed run a workgroup: the parts of its tiles are added, an equal stretch of the tiles a wave, then the waves in their order
 template <class O>
-__global__ __launch_bounds__(256) void run_join_kernel(const u32* __restrict__ skey, int64_t n, int64_t n_rows, int d, float scale, int add,
-                                                       const float* __restrict__ parts, O* __restrict__ out)
+__global__ __launch_bounds__(512) void run_join_kernel(const u32* __restrict__ skey, int64_t n, int d, float scale, int add,
+                                                       const float* __restrict__ parts, const u32* __restrict__ runs, O* __restrict__ out)
 {
-    __shared__ float s[4][64];
-    for (int64_t tile = blockIdx.x; (tile + 1) * RUN_TILE < n; tile += gridDim.x) {
-        const int64_t last = (tile + 1) * RUN_TILE - 1;
-        const u32 key = skey[last];
-        if (key == (u32)n_rows || skey[last + 1] != key) continue;              // does not go on
-        if (tile > 0 && skey[tile * RUN_TILE - 1] == key) continue;             // began before
-        // the run's end: the first place behind `last` with another key
-        int64_t lo = last + 1, hi = n;
+    constexpr int WAVES = 8;
+    __shared__ float s[WAVES][64];
+    const int columns = (d + 63) / 64;
+    const int64_t all = (int64_t)runs[0] * columns;
+    for (int64_t item = blockIdx.x; item < all; item += gridDim.x) {
+        const int64_t tile = runs[1 + item / columns];
+        const int wave = threadIdx.x >> 6, lane = tg_lane(), c = (int)(item % columns) * 64 + lane;
+        const u32 key = skey[(tile + 1) * RUN_TILE - 1];
+        // the run's end: the first place behind the tile with another key; most runs end in the next tile
+        int64_t lo = (tile + 1) * RUN_TILE, hi = lo + RUN_TILE;
+        while (hi < n && skey[hi] == key) { lo = hi; hi = hi + (hi - tile * RUN_TILE); }
+        if (hi > n) hi = n;
         while (lo < hi) {
             const int64_t mid = (lo + hi) >> 1;
             if (skey[mid] == key) lo = mid + 1; else hi = mid;
         }
         const int64_t end = (lo - 1) / RUN_TILE;                                // its last tile
-        const int wave = threadIdx.x >> 6, lane = tg_lane();
-        const int64_t each = (end - tile + 3) / 4, from = tile + 1 + wave * each;
+        const int64_t each = (end - tile + WAVES - 1) / WAVES, from = tile + 1 + wave * each;
         const int64_t to = from + each < end + 1 ? from + each : end + 1;
-        for (int c0 = blockIdx.y * 64; c0 < d; c0 += gridDim.y * 64) {
-            const int c = c0 + lane;
-            float sum = 0.0f;
-            if (c < d) {
-                if (wave == 0) sum = parts[(2 * tile + 1) * d + c];
+        float sum = 0.0f;
+        if (c < d) {
+            if (wave == 0) sum = parts[(2 * tile + 1) * d + c];
 #pragma unroll 8
-                for (int64_t t = from; t < to; ++t) sum += parts[2 * t * d + c];
-            }
-            s[wave][lane] = sum;
-            __syncthreads();
-            if (wave == 0 && c < d) {
-                const float v = ((s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane])) * scale;
-                O* p = out + (int64_t)key * d + c;
-                *p = (O)((add ? (float)*p : 0.0f) + v);
-            }
-            __syncthreads();
+            for (int64_t t = from; t < to; ++t) sum += parts[2 * t * d + c];
         }
+        s[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && c < d) {
+            float v = s[0][lane];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) v += s[w][lane];
+            O* p = out + (int64_t)key * d + c;
+            *p = (O)((add ? (float)*p : 0.0f) + v * scale);
+        }
+        __syncthreads();
     }
 }
 
 struct GradSpace {
-    u32 *key[2], *pos[2], *table, *total;
+    u32 *key[2], *pos[2], *table, *total, *runs;
     float* parts;
 };
 static size_t carve_grad(GradSpace* g, void* base, int64_t n, int64_t n_rows, int d)
@@ -378,13 +411,15 @@ static size_t carve_grad(GradSpace* g, void* base, int64_t n, int64_t n_rows, in
     TgCarve c{(char*)base, 0};
     const bool few = n <= RANK_MAX;
     const SortShape f = sort_shape(n, n_rows);
-    g->key[0] = c.take<u32>(n);
-    g->pos[0] = c.take<u32>(n);
-    g->key[1] = few ? nullptr : c.take<u32>(n);
-    g->pos[1] = few ? nullptr : c.take<u32>(n);
+    const size_t tiles = (size_t)((n + RUN_TILE - 1) / RUN_TILE), whole = tiles * RUN_TILE;
+    g->key[0] = c.take<u32>(whole);
+    g->pos[0] = c.take<u32>(whole);
+    g->key[1] = few ? nullptr : c.take<u32>(whole);
+    g->pos[1] = few ? nullptr : c.take<u32>(whole);
     g->table = few ? nullptr : c.take<u32>((size_t)f.wgs << f.bits);
     g->total = few ? nullptr : c.take<u32>((size_t)1 << f.bits);
-    g->parts = c.take<float>((size_t)((n + RUN_TILE - 1) / RUN_TILE) * 2 * d);
+    g->runs = c.take<u32>(tiles + 1);
+    g->parts = c.take<float>(tiles * 2 * d);
     return c.used;
 }
 size_t tg_lookup_grad_space(int64_t n, int64_t n_rows, int d)
@@ -393,45 +428,63 @@ size_t tg_lookup_grad_space(int64_t n, int64_t n_rows, int d)
     return n == 0 ? 0 : carve_grad(&g, nullptr, n, n_rows, d);
 }
 
+template <class E, class O>
+static void launch_sums(const E* grad, int64_t ld, const u32* key, const u32* pos, int64_t n, int64_t n_rows, int d, float scale, int add, O* out,
+                        const GradSpace& g, hipStream_t s)
+{
+    const int64_t tiles = (n + RUN_TILE - 1) / RUN_TILE;
+    const int pieces = (d + TgPiece<E>::E - 1) / TgPiece<E>::E;
+    const int gs = lanes_shift(pieces), columns = (pieces + (1 << gs) - 1) >> gs;
+    const int64_t per = 256 >> gs;
+    // (fewer than 2^32 work-items: 64 of them stand for 16 KB of a gradient that fits the card, or for 16 tokens of a short row)
+    hipLaunchKernelGGL((run_sum_kernel<E, O>), dim3((unsigned)((tiles * columns + per - 1) / per)), dim3(256), 0, s, grad, ld, key, pos, n, n_rows, d,
+                       scale, add, gs, columns, out, g.parts, g.runs);
+    if (tiles > 1) {
+        const int64_t most = (tiles - 1) * ((d + 63) / 64);
+        hipLaunchKernelGGL(run_join_kernel<O>, dim3((unsigned)(most < 2048 ? most : 2048)), dim3(512), 0, s, key, n, d, scale, add, g.parts, g.runs, out);
+    }
+}
+
 void tg_launch_lookup_grad(const void* grad, int64_t ld, int dtype, const void* ids, int ids64, int64_t n, int64_t n_rows, int d, float scale,
                            int accumulate, void* out, int out_dtype, void* space, hipStream_t s)
 {
-    if (!accumulate) tg_launch_zero(out, (size_t)n_rows * d * tg_type_bytes(out_dtype), s);
-    if (n == 0) return;
+    const size_t all = accumulate ? 0 : (size_t)n_rows * d * tg_type_bytes(out_dtype);
+    if (n == 0) {
+        tg_launch_zero(out, all, s);
+        return;
+    }
     GradSpace g;
     carve_grad(&g, space, n, n_rows, d);
+    ZeroPart z = zero_of(out, all);
     int at = 0;
     if (n <= RANK_MAX) {
         const int full = ((int)n + 63) & ~63;
-        hipLaunchKernelGGL(rank_sort_kernel, dim3((unsigned)((n + 15) / 16)), dim3(256), full * 4, s, ids, ids64, (int)n, n_rows, g.key[0], g.pos[0]);
+        z.first = (uint32_t)((n + 15) / 16);
+        hipLaunchKernelGGL(rank_sort_kernel, dim3(z.first + zero_wgs(z)), dim3(256), full * 4, s, ids, ids64, (int)n, n_rows, g.key[0], g.pos[0], g.runs, z);
     } else {
         const SortShape f = sort_shape(n, n_rows);
+        const int digits = 1 << f.bits;
+        z.parts = 3 * f.passes;
         for (int p = 0; p < f.passes; ++p) {
             const u32* ki = p ? g.key[at] : nullptr;
             const u32* pi = p ? g.pos[at] : nullptr;
-            const int to = p ? at ^ 1 : 0;
-            hipLaunchKernelGGL(digit_count_kernel, dim3((unsigned)f.wgs), dim3(256), 0, s, ids, ids64, ki, n, n_rows, f.chunk, p * f.bits, f.bits, g.table);
-            hipLaunchKernelGGL(digit_scan_kernel, dim3((unsigned)(((1 << f.bits) + 3) / 4)), dim3(256), 0, s, g.table, (int)f.wgs, 1 << f.bits, g.total);
-            hipLaunchKernelGGL(digit_place_kernel, dim3((unsigned)f.wgs), dim3(256), 0, s, ids, ids64, ki, pi, n, n_rows, f.chunk, p * f.bits, f.bits,
-                               g.table, g.total, g.key[to], g.pos[to]);
+            const int to = p ? at ^ 1 : 0, shift = p * f.bits;
+            const unsigned zw = zero_wgs(z);
+            z.part = 3 * p;
+            z.first = (uint32_t)f.wgs;
+            hipLaunchKernelGGL(digit_count_kernel, dim3(z.first + zw), dim3(256), 0, s, ids, ids64, ki, n, n_rows, f.chunk, shift, f.bits, g.table, g.runs, z);
+            z.part = 3 * p + 1;
+            z.first = (uint32_t)((digits + 3) / 4);
+            hipLaunchKernelGGL(digit_scan_kernel, dim3(z.first + zw), dim3(256), 0, s, g.table, (int)f.wgs, digits, g.total, z);
+            z.part = 3 * p + 2;
+            z.first = (uint32_t)f.wgs;
+            hipLaunchKernelGGL(digit_place_kernel, dim3(z.first + zw), dim3(256), 0, s, ids, ids64, ki, pi, n, n_rows, f.chunk, shift, f.bits, g.table, g.total,
+                               g.key[to], g.pos[to], z);
             at = to;
         }
     }
-    const int64_t tiles = (n + RUN_TILE - 1) / RUN_TILE;
     TG_WITH_TYPE(dtype, E, {
-        const int pieces = (d + TgPiece<E>::E - 1) / TgPiece<E>::E;
-        const int gs = lanes_shift(pieces), columns = (pieces + (1 << gs) - 1) >> gs;
-        const int64_t per = 256 >> gs;
-        // (fewer than 2^32 work-items: 64 of them stand for 32 KB of a gradient that fits the card, or for 32 tokens of a short row)
-        const unsigned wgs = (unsigned)((tiles * columns + per - 1) / per);
-        if (out_dtype == 0) hipLaunchKernelGGL((run_sum_kernel<E, float>), dim3(wgs), dim3(256), 0, s, (const E*)grad, ld, g.key[at], g.pos[at], n,
-                                               n_rows, d, scale, accumulate, gs, columns, (float*)out, g.parts);
-        else hipLaunchKernelGGL((run_sum_kernel<E, E>), dim3(wgs), dim3(256), 0, s, (const E*)grad, ld, g.key[at], g.pos[at], n, n_rows, d, scale,
-                                accumulate, gs, columns, (E*)out, g.parts);
+        if (out_dtype == 0) launch_sums<E, float>((const E*)grad, ld, g.key[at], g.pos[at], n, n_rows, d, scale, accumulate, (float*)out, g, s);
+        else launch_sums<E, E>((const E*)grad, ld, g.key[at], g.pos[at], n, n_rows, d, scale, accumulate, (E*)out, g, s);
     });
-    if (tiles > 1) {
-        const unsigned cy = d <= 64 ? 1 : d <= 256 ? (d + 63) / 64 : 4;
-        TG_WITH_TYPE(out_dtype, O, hipLaunchKernelGGL(run_join_kernel<O>, dim3((unsigned)(tiles - 1 < LOOKUP_GRID ? tiles - 1 : LOOKUP_GRID), cy), dim3(256), 0, s, g.key[at], n, n_rows, d, scale,
-                                                      accumulate, g.parts, (O*)out));
-    }
 }

@@ -130,8 +130,10 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E*
             for (int i = 0; i < P::E; ++i) sum = fma((double)p[c].v[i], (double)p[c].v[i], sum);
         rstd = 1.0 / sqrt(row_sum<T>(sum, s_sum) / (double)d + (double)eps);
     }
-    // max |r w|, and whether a value is NaN (a maximum leaves it out)
+    // max |r w|, and whether a value is NaN (a maximum leaves it out).  A product of two 16-bit values is exact in 32 bits.
+    constexpr bool SHORT = sizeof(E) == 2;
     double top = 0.0;
+    float top32 = 0.0f;
     bool odd = false;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -140,11 +142,18 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E*
         if (NORM) g.load(w + at, d - at);
 #pragma unroll
         for (int i = 0; i < P::E; ++i) {
-            const double t = NORM ? (double)p[c].v[i] * (double)g.v[i] : (double)p[c].v[i];
-            odd |= !(t == t);
-            top = fmax(top, fabs(t));
+            if (SHORT) {
+                if (NORM) p[c].v[i] *= g.v[i];
+                odd |= !(p[c].v[i] == p[c].v[i]);
+                top32 = fmaxf(top32, fabsf(p[c].v[i]));
+            } else {
+                const double t = NORM ? (double)p[c].v[i] * (double)g.v[i] : (double)p[c].v[i];
+                odd |= !(t == t);
+                top = fmax(top, fabs(t));
+            }
         }
     }
+    if (SHORT) top = (double)top32;
     if (odd) top = __builtin_inf();
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) top = fmax(top, __shfl_xor(top, m));
@@ -160,18 +169,26 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E*
     if (none) scale = __builtin_nanf("");
     if (lane == 0) scale_out[row] = scale;
     const double f = none || scale == 0.0f ? 0.0 : rstd / (double)scale;
+    const float f32 = (float)f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int at = (lane + c * T) * P::E, left = d - at;
         P g;
-        if (NORM) g.load(w + at, left);
+        if (NORM && !SHORT) g.load(w + at, left);
         qvec q;
 #pragma unroll
         for (int i = 0; i < P::E; ++i) {
-            const double t = NORM ? (double)p[c].v[i] * (double)g.v[i] : (double)p[c].v[i];
             // (a scale below fp32's normal numbers has few bits of its own: the quotient can pass 127)
-            const double u = none ? 0.0 : fmin(fmax(rint(t * f), -127.0), 127.0);
-            q[i] = (char)(int)u;
+            if (SHORT) {
+                // the quotient in 32 bits is off by less than 127 x 2^-22: it decides unless it lies that near to a border
+                const float u = p[c].v[i] * f32, whole = rintf(u);
+                q[i] = (char)(int)fminf(fmaxf(whole, -127.0f), 127.0f);
+                if (fabsf(fabsf(u - whole) - 0.5f) < 1e-4f) q[i] = (char)(int)fmin(fmax(rint((double)p[c].v[i] * f), -127.0), 127.0);
+                if (none) q[i] = 0;
+            } else {
+                const double t = NORM ? (double)p[c].v[i] * (double)g.v[i] : (double)p[c].v[i];
+                q[i] = (char)(int)(none ? 0.0 : fmin(fmax(rint(t * f), -127.0), 127.0));
+            }
         }
         int8_t* o = q_out + row * d + at;
         if (left >= P::E) *reinterpret_cast<qvec*>(o) = q;
@@ -263,14 +280,31 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_grad_kernel(const 
             o.store(dx + row * d + at, d - at);
         }
     }
-    // the rows of a workgroup are added where there are several
-    const int64_t part = (int64_t)blockIdx.x * ROWS + threadIdx.x / T;
+    // the rows that a workgroup had in hand at a time are added, the first with the second and so on, and leave one part
+    if (ROWS > 1) {
+        __shared__ float s_dw[ROWS > 1 ? ROWS - 1 : 1][CH * P::E][64];
+        const int wave = threadIdx.x >> 6;
+        if (wave > 0) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < P::E; ++i) s_dw[wave > 0 ? wave - 1 : 0][c * P::E + i][lane] = dw[c][i];
+        }
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int r = 0; r < ROWS - 1; ++r)
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < P::E; ++i) dw[c][i] += s_dw[r][c * P::E + i][lane];
+    }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int at = (lane + c * T) * P::E;
 #pragma unroll
         for (int i = 0; i < P::E; ++i)
-            if (at + i < d) parts[part * d + at + i] = dw[c][i];
+            if (at + i < d) parts[(int64_t)blockIdx.x * d + at + i] = dw[c][i];
     }
 }
 // 16 columns a workgroup, 64 lanes a column: lane j of a column adds the parts j, j + 64, ..., then the lanes are added as a tree
@@ -357,14 +391,14 @@ void tg_launch_dequantize(const int8_t* q, const float* scale, int64_t n, int d,
     });
 }
 
-// workgroups of the gradient, and the parts of dw they leave (one per row they have in hand at a time)
+// workgroups of the gradient: each leaves a part of dw
 #define NORM_GRAD_WGS 1024
-static int64_t norm_grad_parts(int64_t n, int rows)
+static int64_t norm_grad_wgs(int64_t n, int rows)
 {
     const int64_t wgs = (n + rows - 1) / rows;
-    return (wgs < NORM_GRAD_WGS ? wgs : NORM_GRAD_WGS) * rows;
+    return wgs < NORM_GRAD_WGS ? wgs : NORM_GRAD_WGS;
 }
-size_t tg_norm_grad_space(int64_t n, int d) { return (size_t)norm_grad_parts(n, 4) * d * sizeof(float); }
+size_t tg_norm_grad_space(int64_t n, int d) { return (size_t)norm_grad_wgs(n, 1) * d * sizeof(float); }
 
 void tg_launch_norm_grad(const void* dy, int64_t ld_dy, const void* dr, int64_t ld_dr, const void* r, int64_t ld_r, const void* w,
                          const float* rstd, int dtype, int64_t n, int d, void* dx, void* dw, void* space, hipStream_t s)
@@ -373,9 +407,9 @@ void tg_launch_norm_grad(const void* dy, int64_t ld_dy, const void* dr, int64_t 
     int64_t count = 0;
 #define NORM_BWD(T, CH)                                                                                                                  \
     do {                                                                                                                                 \
-        count = norm_grad_parts(n, NormShare<T>::ROWS);                                                                                  \
+        count = norm_grad_wgs(n, NormShare<T>::ROWS);                                                                                  \
         if (n > 0)                                                                                                                       \
-            hipLaunchKernelGGL((norm_grad_kernel<E, T, CH>), dim3((unsigned)(count / NormShare<T>::ROWS)), dim3(NormShare<T>::THREADS), 0, \
+            hipLaunchKernelGGL((norm_grad_kernel<E, T, CH>), dim3((unsigned)count), dim3(NormShare<T>::THREADS), 0, \
                                s, (const E*)dy, ld_dy, (const E*)dr, ld_dr, (const E*)r, ld_r, (const E*)w, rstd, n, d, (E*)dx, parts);   \
         hipLaunchKernelGGL(norm_dw_kernel<E>, dim3((unsigned)((d + 15) / 16)), dim3(1024), 0, s, parts, (int)count, d, (E*)dw);           \
     } while (0)

@@ -68,21 +68,23 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, Til
     }
 }
 
-// 16 tokens a workgroup, 64 lanes a token: lane j joins the parts j, j + 64, ..., then the lanes are joined as a tree
+// TOK tokens a workgroup, 1024 / TOK lanes a token: lane j joins every so manieth part from j on, then the lanes are joined as a tree
+template <int TOK>
 __global__ __launch_bounds__(1024) void xent_join_kernel(const float2* __restrict__ parts, int64_t count, int64_t n, int64_t n_rows,
                                                          const void* __restrict__ targets, int targets64, const float* __restrict__ at_target,
                                                          float* __restrict__ loss, float* __restrict__ lse)
 {
-    __shared__ float s_m[64][17], s_l[64][17];
-    const int c = threadIdx.x & 15, j = threadIdx.x >> 4;
-    for (int64_t y0 = (int64_t)blockIdx.x * 16; y0 < n; y0 += (int64_t)gridDim.x * 16) {
+    constexpr int LANES = 1024 / TOK;
+    __shared__ float s_m[LANES][TOK + 1], s_l[LANES][TOK + 1];
+    const int c = threadIdx.x % TOK, j = threadIdx.x / TOK;
+    for (int64_t y0 = (int64_t)blockIdx.x * TOK; y0 < n; y0 += (int64_t)gridDim.x * TOK) {
         const int64_t y = y0 + c;
         float m = -__builtin_inff(), l = 0.0f;
         if (y < n) {
-            for (int64_t p0 = j; p0 < count; p0 += 4 * 64) {
+            for (int64_t p0 = j; p0 < count; p0 += 4 * LANES) {
                 float2 v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = p0 + i * 64 < count ? parts[(p0 + i * 64) * n + y] : make_float2(-__builtin_inff(), 0.0f);
+                for (int i = 0; i < 4; ++i) v[i] = p0 + i * LANES < count ? parts[(p0 + i * LANES) * n + y] : make_float2(-__builtin_inff(), 0.0f);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) xent_join(m, l, v[i].x, v[i].y);
             }
@@ -91,7 +93,7 @@ __global__ __launch_bounds__(1024) void xent_join_kernel(const float2* __restric
         s_l[j][c] = l;
         __syncthreads();
 #pragma unroll
-        for (int h = 32; h >= 1; h >>= 1) {
+        for (int h = LANES / 2; h >= 1; h >>= 1) {
             if (j < h) {
                 xent_join(m, l, s_m[j + h][c], s_l[j + h][c]);
                 s_m[j][c] = m;
@@ -231,6 +233,7 @@ __global__ __launch_bounds__(256) void xent_dh_out_kernel(const float* __restric
         const int at = (int)(i - y * pieces) * 4;
         TgPiece<float> sum;
         sum.load(sums + y * d + at, d - at);
+#pragma unroll 8
         for (int s = 1; s < splits; ++s) {
             TgPiece<float> q;
             q.load(sums + (s * n + y) * d + at, d - at);
@@ -345,8 +348,12 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
             count = launch_parts<E, 128, 128, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
         else count = launch_parts<E, 256, 256, 2, 4>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
     });
-    const int64_t wgs = (n + 15) / 16;
-    hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(wgs < 65536 ? wgs : 65536)), dim3(1024), 0, s, parts, count, n, n_rows, targets, targets64, at, loss, lse);
+    // few tokens: more lanes each, and more workgroups
+    const int tok = n <= 1024 ? 4 : 16;
+    const int64_t wgs = (n + tok - 1) / tok;
+    const dim3 grid((unsigned)(wgs < 65536 ? wgs : 65536));
+    if (tok == 4) hipLaunchKernelGGL(xent_join_kernel<4>, grid, dim3(1024), 0, s, parts, count, n, n_rows, targets, targets64, at, loss, lse);
+    else hipLaunchKernelGGL(xent_join_kernel<16>, grid, dim3(1024), 0, s, parts, count, n, n_rows, targets, targets64, at, loss, lse);
 }
 
 #define XENT_PIECE_BYTES (256ll << 20)     // of P, where the workspace has them
