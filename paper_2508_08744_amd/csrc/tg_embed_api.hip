@@ -7,6 +7,7 @@
 #define TG_MAX_COUNT (1ll << 30)
 #define TG_MAX_LOOKUP_D 65536
 #define TG_MAX_D 8192
+#define TG_MAX_TOKENS (1ll << 28)  // of a softmax: its gradient runs along them, in bytes of 32 bits
 #define TG_MAX_K 65536
 #define TG_MAX_PITCH (1 << 20)       // bytes between rows that are read where they are
 
@@ -191,6 +192,7 @@ static int check_xent(int64_t n, int64_t n_rows, int32_t d, int32_t dtype)
     CHECK(check_dtype(dtype));
     CHECK(check_count("n", n, 0));
     CHECK(check_count("n_rows", n_rows, 1));
+    if (n >= TG_MAX_TOKENS) return tg_fail(TG_ERR_INVALID_ARG, "n = %lld must be below 2^28", (long long)n);
     return check_length("d", d, TG_MAX_D);
 }
 // the rows begin at multiples of 16 bytes (that their length is one is looked at where it is known, with the sizes)

@@ -7,20 +7,18 @@
 #include "tg_embed.h"
 #include "tg_tiles.h"
 
-// x: channels, y: tokens; ONE: rows of one stage, which do without the memory of a second
-template <class O, int BM, int BN, int WM, int WN, bool ONE>
+// x: channels, y: tokens
+template <class O, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
                                                                const float* __restrict__ bs, const float* __restrict__ bias, uint32_t nx,
                                                                uint32_t ny, uint32_t group, O* __restrict__ out)
 {
     typedef Tile<int8_t, BM, BN, WM, WN> T;
-    __shared__ __align__(1024) char s0[T::STAGE];
-    __shared__ __align__(1024) char s1[ONE ? 16 : T::STAGE];
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
     T t;
-    t.run(X, Y, x0, y0, 0, bytes, s0, ONE ? s0 : s1);
+    t.run(X, Y, x0, y0, 0, bytes);
     float c[T::FM][4], b[T::FM][4];
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
@@ -138,18 +136,17 @@ size_t tg_product_space(int64_t m, int64_t n, int k, bool ready)
     return c.used;
 }
 
-template <class O, int BM, int BN, int WM, int WN, bool ONE = false>
+template <class O, int BM, int BN, int WM, int WN>
 static void launch_tiles(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
 {
     const uint32_t nx = (uint32_t)((X.rows + BM - 1) / BM), ny = (uint32_t)((Y.rows + BN - 1) / BN);
-    hipLaunchKernelGGL((product_kernel<O, BM, BN, WM, WN, ONE>), dim3(nx * ny), dim3(64 * WM * WN), 0, s, X, Y, bytes, as, bs, bias, nx, ny, 8u, out);
+    hipLaunchKernelGGL((product_kernel<O, BM, BN, WM, WN>), dim3(nx * ny), dim3(64 * WM * WN), 0, s, X, Y, bytes, as, bs, bias, nx, ny, 8u, out);
 }
 template <class O>
 static void launch_product(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
 {
     const auto tiles = [&](int64_t bm, int64_t bn) { return ((X.rows + bm - 1) / bm) * ((Y.rows + bn - 1) / bn); };
-    if (bytes <= TILE_BYTES && tiles(128, 128) >= 200) launch_tiles<O, 128, 128, 2, 2, true>(X, Y, bytes, as, bs, bias, out, s);
-    else if (bytes > 512 && tiles(256, 256) >= 200) launch_tiles<O, 256, 256, 2, 4>(X, Y, bytes, as, bs, bias, out, s);
+    if (bytes > 512 && tiles(256, 256) >= 200) launch_tiles<O, 256, 256, 2, 4>(X, Y, bytes, as, bs, bias, out, s);
     else if (tiles(128, 128) >= 200) launch_tiles<O, 128, 128, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
     else launch_tiles<O, 64, 64, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
 }

@@ -1,11 +1,18 @@
 // Products of two row-major matrices whose rows run along the contraction (out[t][u] = sum_k Y[t][k] X[u][k]), in tiles on the matrix
 // instructions, for 8-bit integers, bf16, fp16 and fp32 alike: everything up to the multiplication works on bytes.
 //
-// A workgroup owns BM rows of X and BN rows of Y.  128 bytes of each row are in LDS at a time, in one of two stages: while one is
-// multiplied the other is filled, straight from memory (buffer loads with LDS as their destination; rows and bytes beyond the matrices come as
-// zeros from the buffer's own bounds check).  A stage holds 8 pieces of 16 bytes a row; piece c of row r lies at place c ^ (r & 7), so
-// that the eight rows that a matrix instruction's lanes read at a time lie in different banks.  The loads write LDS in lane order, so
-// the exchange is made by the lanes' addresses in memory.
+// A workgroup owns BM rows of X and BN rows of Y.  They pass through LDS in stages of 128 bytes a row (a line of the caches: shorter
+// stretches halve the rate of the loads), filled straight from memory by buffer loads with LDS as their destination; rows and bytes beyond the
+// matrices come as zeros from the buffer's own bounds check.
+//
+// Each side's stage is two units, its first and second half of the rows, and every wave has as many rows of one as of the other.  The
+// four products of halves are four phases; they go round the halves so that each phase needs one unit more than the phase before, which
+// is read from LDS into registers one phase ahead, and every phase frees one unit, which is filled for two stages on.  So a load has
+// seven phases (of 16 products of 16 x 16 each, at 256 x 256) to land, the matrix instructions find their operands in registers, and a phase
+// costs one barrier, at which all waves have the unit they read next and none still reads the one that is filled next.
+//
+// A unit holds 8 pieces of 16 bytes a row; piece c of row r lies at place c ^ (r & 7), so that the eight rows that a matrix instruction's lanes
+// read at a time lie in different banks.  The loads write LDS in lane order, so the exchange is made by the lanes' addresses in memory.
 //
 // The lane's share of a product of 16 x 16: column t = lane % 16 and rows u = 4 (lane / 16) + 0..3, so that it holds neighbours of an
 // output row (they run along u).
@@ -72,19 +79,22 @@ void tg_launch_pack(const void* p, int64_t ld, int64_t rows, int d, int e, void*
 
 #define TILE_BYTES 128    // of a row, per stage
 
-// One side of a stage: B rows of 128 bytes, or, turned, 128 / sizeof(E) rows of B elements.  Both take B * 128 bytes.
+// One side of a workgroup's tile: B rows, in two units of B / 2.  Turned, a unit is 128 / sizeof(E) rows of the contraction of B / 2 elements.
+// Both take B / 2 * 128 bytes.
 //
 // Turned, the lanes need values of a column: 16-bit values come through the LDS reads that hand every lane of a group of 16 the four values of
 // one column out of four rows, 32-bit values one by one.  Rows that are read at a time have their pieces exchanged in pairs (16 bit) or in
 // fours (32 bit), so that they too lie in different banks.
 template <class E, int B, int WAVES, bool TURNED>
 struct TileSide {
+    static constexpr int UNIT = B / 2;
     static constexpr int DEPTH = TILE_BYTES / (int)sizeof(E);          // of the contraction, per stage
-    static constexpr int ROW = TURNED ? B * (int)sizeof(E) : TILE_BYTES;
+    static constexpr int ROW = TURNED ? UNIT * (int)sizeof(E) : TILE_BYTES;
     static constexpr int PIECES = ROW / 16;                            // of a row
-    static constexpr int LOADS = B / 8 / WAVES;                        // of a wave, 1024 bytes each
-    static_assert((B / 8) % WAVES == 0 && ROW <= 1024, "whole loads");
-    static_assert(!TURNED || (sizeof(E) > 1 && ROW >= 128), "turned bytes are not read");
+    static constexpr int LOADS = (UNIT * TILE_BYTES / 1024 + WAVES - 1) / WAVES;   // of a wave and unit, 1024 bytes each
+    static constexpr int BYTES = LOADS * WAVES * 1024;                 // of a unit, behind its end what surplus loads write
+    static_assert(ROW <= 1024, "a load has whole rows");
+    static_assert(!TURNED || (sizeof(E) > 1 && ROW >= 128 && LOADS * WAVES * 1024 == UNIT * TILE_BYTES), "turned bytes, short or odd rows are not read");
 
     // which piece of row r lies at place 0: place c holds piece c ^ that
     static __device__ inline int exchange(int r)
@@ -96,61 +106,96 @@ struct TileSide {
 
     uint32_t offset[LOADS];
     int in_row;                  // !TURNED: where the lane's piece is in the stage's bytes of a row
-
-#ifdef __HIP_DEVICE_COMPILE__              // (the host's compiler does not know the buffers' types)
-    __amdgpu_buffer_rsrc_t rsrc;
+    // Kept for whole waves, in 32 bits where that will do: the scalar unit compares no more.
+    uint64_t base;               // the first row (column) of the tile, at the contraction's beginning
+    uint32_t pitch;
+    int have;                    // !TURNED: bytes from there to behind the last row, TURNED: of a row, behind that place
+    int depth;                   // TURNED: rows of the contraction
 
     __device__ inline void begin(const TileRows& m, int64_t first, int wave, int lane)
     {
-        const int64_t have = m.rows - first;
+        pitch = m.pitch;
+        if (TURNED) {
+            base = (uint64_t)m.p + first * (int)sizeof(E);
+            have = (int)((int64_t)m.width - first * (int)sizeof(E));
+            depth = (int)m.rows;
+        } else {
+            const int64_t left = m.rows - first;
+            base = (uint64_t)m.p + first * m.pitch;
+            have = (int)(left < B ? left : B) * (int)m.pitch;
+        }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int at = (i * WAVES + wave) * 1024 + lane * 16, r = at / ROW, c = (at % ROW) / 16;
+            // (surplus loads: rows of the other unit, which nobody reads there)
             offset[i] = r * m.pitch + ((c ^ exchange(r)) * 16);
         }
-        in_row = ((lane & 7) ^ ((lane >> 3) & 7)) * 16;
-        // (rows from `first` on: none behind the last; what a row holds behind k1 is never asked for)
-        if (!TURNED)
-            rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(m.p + first * m.pitch), 0, (int)(uint32_t)((have < B ? have : B) * m.pitch), 0x00020000);
+        in_row = ((lane & 7) ^ (lane >> 3)) * 16;
     }
-    // the stage that begins at byte k of the rows (element k / sizeof(E) of the contraction), up to byte k1
-    __device__ inline void fill(const TileRows& m, int64_t first, char* stage, int64_t k, int64_t k1, int wave)
+    // Unit h, the stage that begins at byte k of the contraction, up to byte k1; behind k1 all of it is zeros.  The load is written out, since the
+    // compiler, which knows the built-in one as a store to LDS, waits for all of them in front of every read; it has no result, and
+    // `meet` waits for it.  M0 (which nothing else in these kernels uses) holds where in LDS the wave's 1024 bytes go.
+    __device__ inline void fill(int h, uint32_t unit, int k, int k1, int wave) const
     {
+        uint64_t from;
+        int bytes;
         if (TURNED) {
-            // columns from `first` on: those behind the width belong to the next row (results that nobody stores), or to nobody
-            const int64_t r = k / (int)sizeof(E);
-            const int64_t left = m.rows - r < DEPTH ? m.rows - r : DEPTH;
-            const int64_t bytes = (left - 1) * m.pitch + m.width - first * (int)sizeof(E);
-            rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(m.p + r * m.pitch + first * (int)sizeof(E)), 0, (int)(uint32_t)bytes, 0x00020000);
+            // (columns behind the width belong to the next row, for results that nobody stores, or to nobody)
+            const int r = k / (int)sizeof(E), left = depth - r < DEPTH ? depth - r : DEPTH;
+            from = base + (uint64_t)r * pitch + h * UNIT * (int)sizeof(E);
+            bytes = (left - 1) * (int)pitch + have - h * UNIT * (int)sizeof(E);
+            if (k >= k1 || left < 1) bytes = 0;
+        } else {
+            // (what a row holds behind k1 is never asked for)
+            from = base + (uint64_t)(h * UNIT) * pitch;
+            bytes = have - h * UNIT * (int)pitch;
         }
-        const bool in = TURNED || k + in_row < k1;
+        bytes = bytes < 0 ? 0 : bytes;
+        const tg_i32x4 buffer = {(int)(uint32_t)from, (int)((uint32_t)(from >> 32) & 0xFFFFu), bytes, 0x00020000};
+        const bool in = TURNED || in_row < k1 - k;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (tg_lds_char*)(stage + (i * WAVES + wave) * 1024), 16,
-                                                     !in ? 0x80000000u /* behind every buffer's end */ : TURNED ? offset[i] : offset[i] + (uint32_t)k, 0, 0, 0);
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t at = !in ? 0x80000000u /* behind every buffer's end */ : TURNED ? offset[i] : offset[i] + (uint32_t)k;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(unit + (i * WAVES + wave) * 1024), "v"(at), "s"(buffer) : "memory");
+        }
     }
-    // the lane's 16 bytes of the 16 rows (columns) from b0 on, of the first or second half of the stage
-    static __device__ inline tg_i32x4 read(const char* stage, int b0, int h, int lane)
+#ifdef __HIP_DEVICE_COMPILE__              // (the host's compiler does not know the built-ins)
+    // Where the lane's bytes of the 16 rows (columns) from b0 on are in a unit, for the first and second 64 bytes of the stage; the rows
+    // 16 further on are at a distance that the reads carry, except where the exchange has a part in it.
+    int at[TURNED ? (sizeof(E) == 4 ? 4 : 2) : 2];
+    __device__ inline void begin_reads(int b0, int lane)
     {
         const int row = lane & 15, q = lane >> 4;
-        if (!TURNED) return *reinterpret_cast<const tg_i32x4*>(stage + (b0 + row) * TILE_BYTES + (((q + 4 * h) ^ (row & 7)) * 16));
+        if (!TURNED) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) at[h] = (b0 + row) * TILE_BYTES + (((q + 4 * h) ^ (row & 7)) * 16);
+        } else if (sizeof(E) == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) at[i] = (q * 4 + i) * ROW + (row & 3) * 4;
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) at[s] = (q * 8 + s * 4 + (row >> 2)) * ROW + (row & 3) * 8;
+        }
+    }
+    // i: 16 rows (columns) behind b0 times i
+    __device__ inline tg_i32x4 read(const char* unit, int b0, int i, int h, int lane) const
+    {
+        const int row = lane & 15, q = lane >> 4;
+        if (!TURNED) return *reinterpret_cast<const tg_i32x4*>(unit + at[h] + i * 16 * TILE_BYTES);
+        b0 += i * 16;
         if (sizeof(E) == 4) {
             tg_i32x4 v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = h * 16 + q * 4 + i;
-                v[i] = *reinterpret_cast<const int*>(stage + r * ROW + ((((b0 + row) / 4) ^ exchange(r)) * 16) + (row & 3) * 4);
-            }
+            for (int e = 0; e < 4; ++e)        // (exchange(row of the stage) is that of q alone)
+                v[e] = *reinterpret_cast<const int*>(unit + at[e] + h * 16 * ROW + ((((b0 + row) / 4) ^ exchange(q * 4)) * 16));
             return v;
         }
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
         s16x4 v[2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int r = h * 32 + q * 8 + s * 4 + (row >> 2);
-            v[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tg_lds_char*)(stage + r * ROW + (((b0 / 8) ^ exchange(r)) * 16) + (row & 3) * 8));
-        }
+        for (int s = 0; s < 2; ++s)            // (exchange(row of the stage): bits 0, 1 of row >> 2, bit 3 of q * 8)
+            v[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tg_lds_char*)(unit + at[s] + h * 32 * ROW + (((b0 / 8) ^ exchange(q * 8 + (row >> 2))) * 16)));
         return __builtin_bit_cast(tg_i32x4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 #endif
@@ -161,67 +206,131 @@ template <class E, int BM, int BN, int WM, int WN, bool XT = false, bool YT = fa
 struct Tile {
     static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;       // products of 16 x 16 of a wave
-    static constexpr int STAGE = (BM + BN) * TILE_BYTES;
+    static constexpr int HM = FM / 2, HN = FN / 2;                   // ... of half of its rows
     typedef typename TileMul<E>::acc acc_t;
     typedef TileSide<E, BM, WAVES, XT> SX;
     typedef TileSide<E, BN, WAVES, YT> SY;
+    static constexpr int LX = SX::LOADS, LY = SY::LOADS;
+    static constexpr int LDS = 4 * (SX::BYTES + SY::BYTES);
+    static_assert(FM % 2 == 0 && FN % 2 == 0, "halves");
 
     acc_t acc[FM][FN];
 
-    // rows (columns, where turned) x0.. of X and y0.. of Y, contraction bytes [k0, k1) (multiples of TILE_BYTES, k1 of 16 at its end)
-    __device__ inline void run(const TileRows& X, const TileRows& Y, int64_t x0, int64_t y0, int64_t k0, int64_t k1, char* stage0, char* stage1)
+#ifdef __HIP_DEVICE_COMPILE__
+    struct Run {
+        int k, k1;
+        int wave, lane, wm, wn;
+        char* lds;
+        SX sx;
+        SY sy;
+        tg_i32x4 x[2][2][HM], y[2][2][HN];                           // [half of the rows][half of the stage]
+    };
+    // the memory of unit h of buffer b
+    static __device__ inline char* unit_x(const Run& r, int b, int h) { return r.lds + (b * 2 + h) * SX::BYTES; }
+    static __device__ inline char* unit_y(const Run& r, int b, int h) { return r.lds + 4 * SX::BYTES + (b * 2 + h) * SY::BYTES; }
+    static __device__ inline void fill_x(const Run& r, int b, int h, int k)
+    {
+        r.sx.fill(h, (uint32_t)(uintptr_t)(tg_lds_char*)unit_x(r, b, h), k, r.k1, r.wave);
+    }
+    static __device__ inline void fill_y(const Run& r, int b, int h, int k)
+    {
+        r.sy.fill(h, (uint32_t)(uintptr_t)(tg_lds_char*)unit_y(r, b, h), k, r.k1, r.wave);
+    }
+    // one of the 2 HM (2 HN) reads of a unit
+    static __device__ inline void read_x(Run& r, int b, int h, int n) { r.x[h][n / HM][n % HM] = r.sx.read(unit_x(r, b, h), r.wm * (HM * 16), n % HM, n / HM, r.lane); }
+    static __device__ inline void read_y(Run& r, int b, int h, int n) { r.y[h][n / HN][n % HN] = r.sy.read(unit_y(r, b, h), r.wn * (HN * 16), n % HN, n / HN, r.lane); }
+    // All but the last `LATER` loads of every wave have landed, and no wave has reads under way.
+    template <int LATER>
+    static __device__ inline void meet()
+    {
+        static_assert(LATER < 64, "loads that are counted");
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // The products of halves hx and hy, out of registers; between them the reads of a unit of X (XU) or Y for the next phase, and the loads
+    // of one, so that the matrix instructions wait for neither's turn to be issued.
+    template <bool XU, class Fill>
+    __device__ inline void phase(Run& r, int hx, int hy, int read_buffer, int read_half, Fill fill)
+    {
+        constexpr int PRODUCTS = 2 * HM * HN, READS = XU ? 2 * HM : 2 * HN;
+#pragma unroll
+        for (int m = 0; m < PRODUCTS; ++m) {
+            const int s = m / (HM * HN), i = m / HN % HM, j = m % HN;
+            acc[hx * HM + i][hy * HN + j] = TileMul<E>::mul(r.x[hx][s][i], r.y[hy][s][j], acc[hx * HM + i][hy * HN + j]);
+#pragma unroll
+            for (int n = 0; n < READS; ++n)
+                if (n * PRODUCTS / READS == m) {
+                    if (XU) read_x(r, read_buffer, read_half, n);
+                    else read_y(r, read_buffer, read_half, n);
+                }
+            if (m == PRODUCTS / 2) fill();
+            __builtin_amdgcn_sched_barrier(0);      // (the order as it is written)
+        }
+    }
+    // One stage, out of buffer P; Y's units in the order P, 1 - P.  Of the loads that a phase waits for, those of the six phases
+    // before it may be on their way.
+    template <int P>
+    __device__ inline void stage(Run& r)
+    {
+        meet<4 * LX + 2 * LY>();
+        phase<false>(r, 0, P, P, 1 - P, [&] { fill_y(r, P, P, r.k + 2 * TILE_BYTES); });
+        meet<3 * LX + 3 * LY>();
+        phase<true>(r, 0, 1 - P, P, 1, [&] { fill_y(r, P, 1 - P, r.k + 2 * TILE_BYTES); });
+        meet<2 * LX + 4 * LY>();
+        phase<true>(r, 1, 1 - P, 1 - P, 0, [&] { fill_x(r, P, 1, r.k + 2 * TILE_BYTES); });
+        meet<3 * LX + 3 * LY>();
+        phase<false>(r, 1, P, 1 - P, 1 - P, [&] { fill_x(r, 1 - P, 0, r.k + 3 * TILE_BYTES); });
+        r.k += TILE_BYTES;
+    }
+#endif
+
+    // rows (columns, where turned) x0.. of X and y0.. of Y, contraction bytes [k0, k1) (k0 a multiple of TILE_BYTES, k1 of 16;
+    // below 2^31 - 2^10)
+    __device__ inline void run(const TileRows& X, const TileRows& Y, int64_t x0, int64_t y0, int k0, int k1)
     {
 #ifdef __HIP_DEVICE_COMPILE__
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = tg_lane();
-        const int wm = wave / WN, wn = wave % WN;
+        __shared__ __align__(1024) char lds[LDS];
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        Run r{k0, k1, wave, tg_lane(), wave / WN, wave % WN, lds};
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = acc_t{0, 0, 0, 0};
-        SX sx;
-        SY sy;
-        sx.begin(X, x0, wave, lane);
-        sy.begin(Y, y0, wave, lane);
-        const auto fill = [&](char* stage, int64_t k) {
-            sx.fill(X, x0, stage, k, k1, wave);
-            sy.fill(Y, y0, stage + BM * TILE_BYTES, k, k1, wave);
-        };
-        const auto multiply = [&](const char* stage) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                tg_i32x4 x[FM], y[FN];
-#pragma unroll
-                for (int i = 0; i < FM; ++i) x[i] = SX::read(stage, wm * (BM / WM) + i * 16, h, lane);
-#pragma unroll
-                for (int j = 0; j < FN; ++j) y[j] = SY::read(stage + BM * TILE_BYTES, wn * (BN / WN) + j * 16, h, lane);
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = TileMul<E>::mul(x[i], y[j], acc[i][j]);
-            }
-        };
-        // a stage is there when every wave's loads have landed, and may be filled again when every wave has read it
-        const auto meet = [] {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-        };
         if (k0 >= k1) return;
-        fill(stage0, k0);
-        for (int64_t k = k0; k < k1; k += 2 * TILE_BYTES) {
-            meet();
-            if (k + TILE_BYTES < k1) fill(stage1, k + TILE_BYTES);
-            multiply(stage0);
-            if (k + TILE_BYTES >= k1) break;
-            meet();
-            if (k + 2 * TILE_BYTES < k1) fill(stage0, k + 2 * TILE_BYTES);
-            multiply(stage1);
+        r.sx.begin(X, x0, wave, r.lane);
+        r.sy.begin(Y, y0, wave, r.lane);
+        r.sx.begin_reads(r.wm * (HM * 16), r.lane);
+        r.sy.begin_reads(r.wn * (HN * 16), r.lane);
+        // two stages in the order of the phases that would have filled them, and the reads of the two phases in front of the first
+        fill_x(r, 0, 0, k0);
+        fill_y(r, 0, 0, k0);
+        fill_y(r, 0, 1, k0);
+        fill_x(r, 0, 1, k0);
+        fill_x(r, 1, 0, k0 + TILE_BYTES);
+        fill_y(r, 1, 1, k0 + TILE_BYTES);
+        fill_y(r, 1, 0, k0 + TILE_BYTES);
+        fill_x(r, 1, 1, k0 + TILE_BYTES);
+        meet<2 * LX + 4 * LY>();
+#pragma unroll
+        for (int n = 0; n < 2 * HM; ++n) read_x(r, 0, 0, n);
+        meet<3 * LX + 3 * LY>();
+#pragma unroll
+        for (int n = 0; n < 2 * HN; ++n) read_y(r, 0, 0, n);
+        fill_x(r, 0, 0, k0 + 2 * TILE_BYTES);
+        for (;;) {
+            stage<0>(r);
+            if (r.k >= k1) break;
+            stage<1>(r);
+            if (r.k >= k1) break;
         }
-        __syncthreads();
+        // (loads of zeros behind the end are still on their way into LDS)
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 #endif
     }
     // the rows of X and Y that acc[i][j][0] belongs to; acc[i][j][e] is for x + e
-    __device__ inline int x_of(int i) const { return ((threadIdx.x >> 6) / WN) * (BM / WM) + i * 16 + (tg_lane() >> 4) * 4; }
-    __device__ inline int y_of(int j) const { return ((threadIdx.x >> 6) % WN) * (BN / WN) + j * 16 + (tg_lane() & 15); }
+    __device__ inline int x_of(int i) const { return (i / HM) * (BM / 2) + ((threadIdx.x >> 6) / WN) * (HM * 16) + (i % HM) * 16 + (tg_lane() >> 4) * 4; }
+    __device__ inline int y_of(int j) const { return (j / HN) * (BN / 2) + ((threadIdx.x >> 6) % WN) * (HN * 16) + (j % HN) * 16 + (tg_lane() & 15); }
 };
 
 // four neighbours of an output row
@@ -256,6 +365,7 @@ __device__ inline void tile_place(uint32_t t, uint32_t nx, uint32_t ny, uint32_t
 {
     const uint32_t per = nx * group, g = t / per, first = g * group;
     const uint32_t high = ny - first < group ? ny - first : group, in = t - g * per;
-    *tx = in / high;
-    *ty = first + in % high;
+    // (the divisions are the vector unit's: the results go back to where the addresses of whole waves are formed)
+    *tx = (uint32_t)__builtin_amdgcn_readfirstlane((int)(in / high));
+    *ty = (uint32_t)__builtin_amdgcn_readfirstlane((int)(first + in % high));
 }

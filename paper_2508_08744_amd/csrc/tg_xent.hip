@@ -23,20 +23,18 @@ __device__ inline void xent_join(float& m, float& l, float m2, float l2)
     m = top;
 }
 
-// x: rows of the table, y: tokens.  parts: for every stretch of BM / WM rows of the table, (maximum, sum) of every token.
+// x: rows of the table, y: tokens.  parts: for every tile and wave along x (BM / WM rows of the table), (maximum, sum) of every token.
 template <class E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
                                                                  float scale, uint32_t nx, uint32_t ny, uint32_t group, float2* __restrict__ parts,
                                                                  int64_t parts_pitch, float* __restrict__ at_target)
 {
     typedef Tile<E, BM, BN, WM, WN> T;
-    __shared__ __align__(1024) char s0[T::STAGE];
-    __shared__ __align__(1024) char s1[T::STAGE];
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
     T t;
-    t.run(X, Y, x0, y0, 0, bytes, s0, s1);
+    t.run(X, Y, x0, y0, 0, bytes);
     const bool whole = x0 + BM <= X.rows;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
@@ -159,13 +157,11 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
                                                               uint32_t ny, uint32_t group, E* __restrict__ p, int64_t pitch)
 {
     typedef Tile<E, BM, BN, WM, WN> T;
-    __shared__ __align__(1024) char s0[T::STAGE];
-    __shared__ __align__(1024) char s1[T::STAGE];
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
     T t;
-    t.run(X, Y, x0, y0, 0, bytes, s0, s1);
+    t.run(X, Y, x0, y0, 0, bytes);
     const float up = c[0];
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
@@ -192,19 +188,18 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
 // dh: x: columns of w (turned), y: tokens, over the rows of the piece from part `s` of `splits`.  sums: splits x n x d, added to but for the
 // first piece
 template <class E, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void xent_dh_kernel(TileRows X, TileRows Y, int64_t bytes, int64_t each, int d, uint32_t nx, uint32_t ny,
+__global__ __launch_bounds__(64 * WM * WN) void xent_dh_kernel(TileRows X, TileRows Y, int bytes, int each, int d, uint32_t nx, uint32_t ny,
                                                                int splits, int first, float* __restrict__ sums)
 {
     typedef Tile<E, BM, BN, WM, WN, true, false> T;
-    __shared__ __align__(1024) char s0[T::STAGE];
-    __shared__ __align__(1024) char s1[T::STAGE];
     const uint32_t b = tile_of_block(blockIdx.x, nx * ny * splits);
-    const uint32_t s = b / (nx * ny), in = b - s * (nx * ny);
-    const uint32_t tx = in % nx, ty = in / nx;
+    const uint32_t s = (uint32_t)__builtin_amdgcn_readfirstlane((int)(b / (nx * ny))), in = b - s * (nx * ny);
+    uint32_t tx, ty;
+    tile_place(in, nx, ny, 1, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
-    const int64_t k0 = s * each, k1 = k0 + each < bytes ? k0 + each : bytes;
+    const int k0 = (int)s * each, k1 = k0 + each < bytes ? k0 + each : bytes;
     T t;
-    t.run(X, Y, x0, y0, k0, k1, s0, s1);
+    t.run(X, Y, x0, y0, k0, k1);
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
         const int64_t y = y0 + t.y_of(j);
@@ -249,17 +244,15 @@ __global__ __launch_bounds__(256) void xent_dh_out_kernel(const float* __restric
 
 // dw: x: columns of h (turned), y: columns of P, rows of the piece (turned), over the tokens
 template <class E, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void xent_dw_kernel(TileRows X, TileRows Y, int64_t rows, int64_t bytes, int d, const float* __restrict__ c,
+__global__ __launch_bounds__(64 * WM * WN) void xent_dw_kernel(TileRows X, TileRows Y, int64_t rows, int bytes, int d, const float* __restrict__ c,
                                                                uint32_t nx, uint32_t ny, E* __restrict__ dw)
 {
     typedef Tile<E, BM, BN, WM, WN, true, true> T;
-    __shared__ __align__(1024) char s0[T::STAGE];
-    __shared__ __align__(1024) char s1[T::STAGE];
-    const uint32_t b = tile_of_block(blockIdx.x, nx * ny);
-    const uint32_t tx = b % nx, ty = b / nx;
+    uint32_t tx, ty;
+    tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, 1, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
     T t;
-    t.run(X, Y, x0, y0, 0, bytes, s0, s1);
+    t.run(X, Y, x0, y0, 0, bytes);
     const float down = c[1];
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
@@ -294,7 +287,7 @@ static void xent_rows(XentRows* r, TgCarve* c, const void* h, int64_t ld_h, cons
 
 // The tile of the logits: 256 x 256 where that leaves every CU one, smaller ones for fewer tokens.  fp32 keeps twice the bytes a
 // value: 128 x 128 there.
-#define XENT_STRETCH 64         // rows of the table that leave one (maximum, sum) in the smallest tile (BM / WM)
+#define XENT_STRETCH 32         // rows of the table that leave one (maximum, sum) at least (BM / WM)
 
 size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready)
 {
@@ -342,8 +335,8 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
     float* at = c.take<float>(n);
     int64_t count = 0;
     TG_WITH_TYPE(dtype, E, {
-        if (n <= 32) count = launch_parts<E, 128, 32, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
-        else if (n <= 64) count = launch_parts<E, 128, 64, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+        if (n <= 32) count = launch_parts<E, 128, 32, 4, 1>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+        else if (n <= 64) count = launch_parts<E, 128, 64, 4, 1>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
         else if (sizeof(E) == 4 || ((n_rows + 255) / 256) * ((n + 255) / 256) < 200)
             count = launch_parts<E, 128, 128, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
         else count = launch_parts<E, 256, 256, 2, 4>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
@@ -358,19 +351,23 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
 
 #define XENT_PIECE_BYTES (256ll << 20)     // of P, where the workspace has them
 #define XENT_LEAST_ROWS 256                // of a piece
+#define XENT_MOST_ROWS (1ll << 28)         // (bytes of a contraction stay within 32 bits)
 
 struct XentGrad {
     int64_t piece;        // rows of the table at a time, a multiple of 256 unless it is all of them
+    bool wide;            // dh in tiles of 256 x 256, of which a CU holds one, else of 128 x 128, of which it holds two
     int splits;           // of dh's contraction
 };
 static int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
-static int xent_splits(int64_t n, int64_t piece, int d, int e)
+static void xent_splits(XentGrad* g, int64_t n, int d, int e)
 {
-    // tiles of 128 x 128 for at least two a CU, each with eight stages of the contraction or more
-    const int64_t tiles = ((n + 127) / 128) * ((d + 127) / 128), stages = (piece * e + TILE_BYTES - 1) / TILE_BYTES;
-    int64_t s = (512 + tiles - 1) / tiles;
-    if (s > stages / 8) s = stages / 8;
-    return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+    g->wide = e == 2 && n > 128 && d > 128;
+    const int64_t side = g->wide ? 256 : 128, fill = g->wide ? 256 : 512;
+    // as many parts as fill the card, each with sixteen stages of the contraction or more
+    const int64_t tiles = ((n + side - 1) / side) * ((d + side - 1) / side), stages = (g->piece * e + TILE_BYTES - 1) / TILE_BYTES;
+    int64_t s = (fill + tiles - 1) / tiles;
+    if (s > stages / 16) s = stages / 16;
+    g->splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
 static size_t carve_xent_grad(XentRows* r, TgCarve* c, const void* h, int64_t ld_h, const void* w, int64_t ld_w, int64_t n, int64_t n_rows, int d,
                               int e, bool ready_w, XentGrad g, float** consts, char** p, float** sums)
@@ -386,13 +383,14 @@ static XentGrad xent_grad_shape(int64_t n, int64_t n_rows, int d, int e, int64_t
     XentGrad g;
     g.piece = p_bytes / ((n > 0 ? n : 1) * e) / 256 * 256;
     if (g.piece < XENT_LEAST_ROWS) g.piece = XENT_LEAST_ROWS;
+    if (g.piece > XENT_MOST_ROWS) g.piece = XENT_MOST_ROWS;
     if (g.piece >= n_rows) g.piece = n_rows;
     else {
         // equal pieces
         const int64_t count = (n_rows + g.piece - 1) / g.piece;
         g.piece = round_up((n_rows + count - 1) / count, 256);
     }
-    g.splits = xent_splits(n, g.piece, d, e);
+    xent_splits(&g, n, d, e);
     return g;
 }
 static size_t xent_grad_bytes(int64_t n, int64_t n_rows, int d, int e, bool ready, int64_t p_bytes)
@@ -429,19 +427,27 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
             hipLaunchKernelGGL(kernel, dim3(nx * ny), dim3(threads), 0, s, W, r.h, (int)W.width, targets, targets64, lse, dloss, (const float*)consts, scale,
                                v0, n_rows, nx, ny, 8u, (E*)p, (int64_t)(pitch / e));
         };
-        if (n <= 64) logits(xent_p_kernel<E, 128, 64, 2, 2>, 128, 64, 256);
-        else if (sizeof(E) == 4 || ((rows + 255) / 256) * ((n + 255) / 256) < 200) logits(xent_p_kernel<E, 128, 128, 2, 2>, 128, 128, 256);
+        const auto tiles = [](int64_t x, int64_t y, int64_t side) { return ((x + side - 1) / side) * ((y + side - 1) / side); };
+        if (n <= 64) logits(xent_p_kernel<E, 128, 64, 4, 1>, 128, 64, 256);
+        else if (e == 4 || tiles(rows, n, 256) < 200) logits(xent_p_kernel<E, 128, 128, 2, 2>, 128, 128, 256);
         else logits(xent_p_kernel<E, 256, 256, 2, 4>, 256, 256, 512);
-        {
-            const int64_t stages = ((int64_t)pitch + TILE_BYTES - 1) / TILE_BYTES, each = (stages + g.splits - 1) / g.splits * TILE_BYTES;
-            const uint32_t nx = (uint32_t)((d + 127) / 128), ny = (uint32_t)((n + 127) / 128);
-            hipLaunchKernelGGL((xent_dh_kernel<E, 128, 128, 2, 2>), dim3(nx * ny * g.splits), dim3(256), 0, s, W, P, (int64_t)pitch, each, d, nx, ny,
-                               g.splits, v0 == 0 ? 1 : 0, sums);
-        }
-        {
-            const uint32_t nx = (uint32_t)((d + 127) / 128), ny = (uint32_t)((rows + 127) / 128);
-            hipLaunchKernelGGL((xent_dw_kernel<E, 128, 128, 2, 2>), dim3(nx * ny), dim3(256), 0, s, r.h, P, rows, n * e, d, (const float*)consts, nx, ny,
-                               dw + v0 * d);
+        const auto product_dh = [&](auto kernel, int side, int threads) {
+            const int stages = (int)((pitch + TILE_BYTES - 1) / TILE_BYTES), each = (stages + g.splits - 1) / g.splits * TILE_BYTES;
+            const uint32_t nx = (uint32_t)((d + side - 1) / side), ny = (uint32_t)((n + side - 1) / side);
+            hipLaunchKernelGGL(kernel, dim3(nx * ny * g.splits), dim3(threads), 0, s, W, P, (int)pitch, each, d, nx, ny, g.splits, v0 == 0 ? 1 : 0, sums);
+        };
+        const auto product_dw = [&](auto kernel, int side, int threads) {
+            const uint32_t nx = (uint32_t)((d + side - 1) / side), ny = (uint32_t)((rows + side - 1) / side);
+            hipLaunchKernelGGL(kernel, dim3(nx * ny), dim3(threads), 0, s, r.h, P, rows, (int)(n * e), d, (const float*)consts, nx, ny, dw + v0 * d);
+        };
+        if constexpr (sizeof(E) == 2) {
+            if (g.wide) product_dh(xent_dh_kernel<E, 256, 256, 2, 4>, 256, 512);
+            else product_dh(xent_dh_kernel<E, 128, 128, 2, 2>, 128, 256);
+            if (tiles(rows, d, 256) >= 200) product_dw(xent_dw_kernel<E, 256, 256, 2, 4>, 256, 512);
+            else product_dw(xent_dw_kernel<E, 128, 128, 2, 2>, 128, 256);
+        } else {
+            product_dh(xent_dh_kernel<E, 128, 128, 2, 2>, 128, 256);
+            product_dw(xent_dw_kernel<E, 128, 128, 2, 2>, 128, 256);
         }
     }
     const int64_t out_wgs = (n * ((d + 3) / 4) + 255) / 256;
