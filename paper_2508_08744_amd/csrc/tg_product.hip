@@ -44,13 +44,14 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(TileRows X, TileR
     }
 }
 
-// Up to 16 FN tokens.  A workgroup has 16 channels, a wave every fourth piece of 64 bytes x STEPS of the contraction.
+// Up to 16 FN tokens.  A workgroup has 16 channels, a wave a quarter of the contraction in one piece, STEPS x 64 bytes of every row in
+// flight.  (16 384 channels of 4096, 4 tokens, fp16: 16 steps 16.1 us, 4.2 TB/s; 4 steps 16.9; 4 steps with the waves' pieces in turn 19.3.)
 template <class O, int FN>
 __global__ __launch_bounds__(256) void product_few_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
                                                           const float* __restrict__ bs, const float* __restrict__ bias, int64_t first,
                                                           O* __restrict__ out)
 {
-    constexpr int STEPS = FN == 1 ? 8 : 4;
+    constexpr int STEPS = 16 / FN;
     __shared__ tg_i32x4 s_part[3][FN][64];
     const int wave = threadIdx.x >> 6, lane = tg_lane(), row = lane & 15, q = lane >> 4;
     const int64_t x0 = first + (int64_t)blockIdx.x * 16;
@@ -67,15 +68,15 @@ __global__ __launch_bounds__(256) void product_few_kernel(TileRows X, TileRows Y
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[j] = tg_i32x4{0, 0, 0, 0};
     const tg_i32x4 none = {0, 0, 0, 0};
-    for (int k = wave * 64 * STEPS; k < bytes; k += 4 * 64 * STEPS) {
+    const int each = ((bytes + 255) / 256) * 64, k1 = (wave + 1) * each < bytes ? (wave + 1) * each : bytes;
+    for (int k = wave * each; k < k1; k += 64 * STEPS) {
         tg_i32x4 x[STEPS], y[STEPS][FN];
 #pragma unroll
-        for (int h = 0; h < STEPS; ++h) {
-            const bool in = k + h * 64 + q * 16 < bytes;
-            x[h] = in && xin ? *reinterpret_cast<const tg_i32x4*>(xp + k + h * 64) : none;
+        for (int h = 0; h < STEPS; ++h) x[h] = k + h * 64 + q * 16 < k1 && xin ? *reinterpret_cast<const tg_i32x4*>(xp + k + h * 64) : none;
 #pragma unroll
-            for (int j = 0; j < FN; ++j) y[h][j] = in && yin[j] ? *reinterpret_cast<const tg_i32x4*>(yp[j] + k + h * 64) : none;
-        }
+        for (int h = 0; h < STEPS; ++h)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) y[h][j] = k + h * 64 + q * 16 < k1 && yin[j] ? *reinterpret_cast<const tg_i32x4*>(yp[j] + k + h * 64) : none;
 #pragma unroll
         for (int h = 0; h < STEPS; ++h)
 #pragma unroll
@@ -101,6 +102,77 @@ __global__ __launch_bounds__(256) void product_few_kernel(TileRows X, TileRows Y
             v[e] = (float)sum[e] * s * (in ? bs[x + e] : 0.0f) + (in && bias ? bias[x + e] : 0.0f);
         }
         if (x < X.rows) tile_put(out + y * X.rows + x, v, X.rows - x);
+    }
+}
+
+// Short rows, of up to STEPS x 64 bytes: the output's bytes bound the product, and a tile would be loaded, multiplied once or twice and stored,
+// each after the other.  A wave keeps the rows of 16 FN tokens in registers, walks over the channels 16 CB at a time with the next ones' rows
+// on their way, and stores as it goes; nothing meets.  (203 tokens, 1 000 000 channels of 128, fp32: STORES.)
+template <class O, int STEPS, int FN, int CB>
+__global__ __launch_bounds__(256) void product_short_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
+                                                            const float* __restrict__ bs, const float* __restrict__ bias, O* __restrict__ out)
+{
+    const int wave = threadIdx.x >> 6, lane = tg_lane(), row = lane & 15, q = lane >> 4;
+    const tg_i32x4 none = {0, 0, 0, 0};
+    const int64_t chunks = (X.rows + 16 * CB - 1) / (16 * CB), step = (int64_t)gridDim.x * 4;
+    tg_i32x4 y[FN][STEPS];
+    float sy[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int64_t r = (int64_t)blockIdx.y * (16 * FN) + j * 16 + row;
+        const bool in = r < Y.rows;
+        sy[j] = in ? as[r] : 0.0f;
+#pragma unroll
+        for (int h = 0; h < STEPS; ++h)
+            y[j][h] = in && h * 64 + q * 16 < bytes ? *reinterpret_cast<const tg_i32x4*>(Y.p + r * Y.pitch + h * 64 + q * 16) : none;
+    }
+    tg_i32x4 x[CB][STEPS], next[CB][STEPS];
+    const auto load = [&](int64_t chunk) {
+#pragma unroll
+        for (int i = 0; i < CB; ++i) {
+            const int64_t r = chunk * (16 * CB) + i * 16 + row;
+            const char* p = X.p + (r < X.rows ? r : 0) * X.pitch + q * 16;
+#pragma unroll
+            for (int h = 0; h < STEPS; ++h) next[i][h] = r < X.rows && h * 64 + q * 16 < bytes ? *reinterpret_cast<const tg_i32x4*>(p + h * 64) : none;
+        }
+    };
+    int64_t chunk = (int64_t)blockIdx.x * 4 + wave;
+    if (chunk < chunks) load(chunk);
+    for (; chunk < chunks; chunk += step) {
+#pragma unroll
+        for (int i = 0; i < CB; ++i)
+#pragma unroll
+            for (int h = 0; h < STEPS; ++h) x[i][h] = next[i][h];
+        if (chunk + step < chunks) load(chunk + step);
+        float c[CB][4], b[CB][4];
+#pragma unroll
+        for (int i = 0; i < CB; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t v = chunk * (16 * CB) + i * 16 + q * 4 + e;
+                c[i][e] = v < X.rows ? bs[v] : 0.0f;
+                b[i][e] = bias && v < X.rows ? bias[v] : 0.0f;
+            }
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int64_t r = (int64_t)blockIdx.y * (16 * FN) + j * 16 + row;
+            tg_i32x4 acc[CB];
+#pragma unroll
+            for (int i = 0; i < CB; ++i) {
+                acc[i] = none;
+#pragma unroll
+                for (int h = 0; h < STEPS; ++h) acc[i] = TileMul<int8_t>::mul(x[i][h], y[j][h], acc[i]);
+            }
+            if (r >= Y.rows) continue;
+#pragma unroll
+            for (int i = 0; i < CB; ++i) {
+                const int64_t v = chunk * (16 * CB) + i * 16 + q * 4;
+                float o[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = (float)acc[i][e] * sy[j] * c[i][e] + b[i][e];
+                if (v < X.rows) tile_put(out + r * X.rows + v, o, X.rows - v);
+            }
+        }
     }
 }
 
@@ -136,6 +208,22 @@ size_t tg_product_space(int64_t m, int64_t n, int k, bool ready)
     return c.used;
 }
 
+template <class O, int STEPS, int FN, int CB>
+static void launch_short(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
+{
+    // (groups of tokens along y: the limit on a grid's y is 65535)
+    const int64_t most = 65535ll * 16 * FN, chunks = (X.rows + 16 * CB - 1) / (16 * CB);
+    for (int64_t y0 = 0; y0 < Y.rows; y0 += most) {
+        const TileRows part{Y.p + y0 * Y.pitch, Y.rows - y0 < most ? Y.rows - y0 : most, Y.pitch, Y.width};
+        const int64_t ny = (part.rows + 16 * FN - 1) / (16 * FN);
+        // waves for all CUs, walking over the channels
+        int64_t nx = (2048 + ny - 1) / ny;
+        if (nx < 64) nx = 64;
+        if (nx > (chunks + 3) / 4) nx = (chunks + 3) / 4;
+        hipLaunchKernelGGL((product_short_kernel<O, STEPS, FN, CB>), dim3((unsigned)nx, (unsigned)ny), dim3(256), 0, s, X, part, bytes, as + y0, bs, bias,
+                           out + y0 * X.rows);
+    }
+}
 template <class O, int BM, int BN, int WM, int WN>
 static void launch_tiles(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
 {
@@ -145,6 +233,19 @@ static void launch_tiles(const TileRows& X, const TileRows& Y, int bytes, const 
 template <class O>
 static void launch_product(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
 {
+    if (bytes <= 128) {
+        if (Y.rows <= 16) launch_short<O, 2, 1, 4>(X, Y, bytes, as, bs, bias, out, s);
+        else if (Y.rows <= 32) launch_short<O, 2, 2, 4>(X, Y, bytes, as, bs, bias, out, s);
+        else if (Y.rows <= 64) launch_short<O, 2, 4, 4>(X, Y, bytes, as, bs, bias, out, s);
+        else launch_short<O, 2, 8, 4>(X, Y, bytes, as, bs, bias, out, s);
+        return;
+    }
+    if (bytes <= 256) {
+        if (Y.rows <= 16) launch_short<O, 4, 1, 2>(X, Y, bytes, as, bs, bias, out, s);
+        else if (Y.rows <= 32) launch_short<O, 4, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
+        else launch_short<O, 4, 4, 2>(X, Y, bytes, as, bs, bias, out, s);
+        return;
+    }
     const auto tiles = [&](int64_t bm, int64_t bn) { return ((X.rows + bm - 1) / bm) * ((Y.rows + bn - 1) / bn); };
     if (bytes > 512 && tiles(256, 256) >= 200) launch_tiles<O, 256, 256, 2, 4>(X, Y, bytes, as, bs, bias, out, s);
     else if (tiles(128, 128) >= 200) launch_tiles<O, 128, 128, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
@@ -168,7 +269,7 @@ void tg_launch_product(const int8_t* a, const float* as, const int8_t* b, const 
         X.p = pb;
     }
     const int bytes = (int)X.pitch;
-    if (m <= PRODUCT_FEW) {
+    if (m <= PRODUCT_FEW && bytes > 256) {
         const int64_t most = TILE_LAUNCH_ITEMS / 256 * 16;
         for (int64_t x0 = 0; x0 < n; x0 += most) {
             const dim3 g((unsigned)(((n - x0 < most ? n - x0 : most) + 15) / 16)), t(256);
