@@ -91,8 +91,9 @@ int tg_dequantize_rows(const int8_t* q, const float* scale, int64_t n, int32_t d
  * scale per token (row of a) and per channel (row of b); the sum is a whole number of 32 bits and exact.
  * a: m x k int8, b: n x k int8 (a weight of n output channels, or the rows of an index), bias: n fp32 or
  * NULL, out: m x n of type dtype.  0 <= m < 2^30, 1 <= n < 2^30, 1 <= k <= 65536 (127 * 128 * k stays below 2^31 for
- * every int8 value).  Rows of a and b whose length or start is no multiple of 16 bytes are copied into the
- * workspace first.  aligned: 1 where a and b both start at a multiple of 16 bytes, 0 where that is not known.
+ * every int8 value).  Beyond 64 tokens and 256 bytes a row, rows
+ * whose length or start is no multiple of 16 bytes are copied into the workspace first.  aligned: 1 where a and b
+ * both start at a multiple of 16 bytes, 0 where that is not known.
  */
 size_t tg_matmul_q8_workspace(int64_t m, int64_t n, int32_t k, int32_t aligned);
 int tg_matmul_q8(const int8_t* a, const float* a_scale, const int8_t* b, const float* b_scale, const float* bias,

@@ -94,13 +94,13 @@ __device__ inline u32 token_key(const void* ids, int ids64, int64_t t, int64_t n
 }
 
 // Few tokens: the place of a token is the number of those in front of it, counted.  16 lanes count for one token, over all keys in LDS.
-// One launch instead of the six of the digits' sort (8192 tokens: RANK_MAX squared comparisons are 6 us; twice as many would be 24).
-#define RANK_MAX 8192
+// One launch instead of the six of the digits' sort: at 4096 tokens 21 against 27 us of the whole gradient, at 8192 31 against 29.
+#define RANK_MAX 6144
 __global__ __launch_bounds__(256) void rank_sort_kernel(const void* __restrict__ ids, int ids64, int n, int64_t n_rows, u32* __restrict__ skey,
                                                         u32* __restrict__ spos, u32* __restrict__ runs, ZeroPart z)
 {
     if (blockIdx.x >= z.first) { zero_part(z); return; }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *runs = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 2) runs[threadIdx.x] = 0;
     extern __shared__ __align__(16) u32 s_rank_keys[];      // n rounded up to 64, the rest larger than any key
     const int full = (n + 63) & ~63;
     for (int i = threadIdx.x; i < full; i += 256) s_rank_keys[i] = i < n ? token_key(ids, ids64, i, n_rows) : 0xFFFFFFFFu;
@@ -109,11 +109,22 @@ __global__ __launch_bounds__(256) void rank_sort_kernel(const void* __restrict__
     const int t = blockIdx.x * 16 + (threadIdx.x >> 4);
     if (t >= n) return;                                     // (16 lanes together: their sums stay among themselves)
     const u32 key = s_rank_keys[t];
+    // in front of the token equal keys count, behind it they do not: up to its own 64 keys, and from them on, one comparison each
     int before = 0;
-    for (int i = part * 4; i < full; i += 64) {
+    const int own = t & ~63;
+    for (int i = part * 4; i < own; i += 64) {
+        const uint4 k = *reinterpret_cast<const uint4*>(s_rank_keys + i);
+        before += (int)(k.x <= key) + (int)(k.y <= key) + (int)(k.z <= key) + (int)(k.w <= key);
+    }
+    {
+        const int i = own + part * 4;
         const uint4 k = *reinterpret_cast<const uint4*>(s_rank_keys + i);
         before += (k.x < key || (k.x == key && i < t)) + (k.y < key || (k.y == key && i + 1 < t)) +
                   (k.z < key || (k.z == key && i + 2 < t)) + (k.w < key || (k.w == key && i + 3 < t));
+    }
+    for (int i = own + 64 + part * 4; i < full; i += 64) {
+        const uint4 k = *reinterpret_cast<const uint4*>(s_rank_keys + i);
+        before += (int)(k.x < key) + (int)(k.y < key) + (int)(k.z < key) + (int)(k.w < key);
     }
 #pragma unroll
     for (int m = 1; m < 16; m <<= 1) before += __shfl_xor(before, m);
@@ -160,7 +171,7 @@ __global__ __launch_bounds__(256) void digit_count_kernel(const void* __restrict
                                                           u32* __restrict__ runs, ZeroPart z)
 {
     if (blockIdx.x >= z.first) { zero_part(z); return; }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *runs = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 2) runs[threadIdx.x] = 0;
     __shared__ u32 s_count[1 << DIGIT_MAX];
     for (int i = threadIdx.x; i < 1 << bits; i += 256) s_count[i] = 0;
     __syncthreads();
@@ -265,6 +276,7 @@ __global__ __launch_bounds__(256) void digit_place_kernel(const void* __restrict
 
 // ---- sums over the runs of the sorted list
 #define RUN_TILE 16
+#define RUN_LONG 16
 template <class E, class O>
 __device__ inline void write_row(const float* v, int left, O* p, float scale, bool add)
 {
@@ -294,7 +306,8 @@ __device__ inline void write_row(const float* v, int left, O* p, float scale, bo
 
 // G lanes a tile, a piece of the row a lane, as many columns of tiles as the row has G pieces.  All of a tile's rows are asked for before
 // the first is added.  parts: two rows of d per tile: of a run that came from the tile before, and of one that goes on in the next
-// but began here; such tiles are listed in runs[1..], runs[0] of them, in any order.
+// but began here; such tiles are listed, in any order, from runs[2] on (runs[0] of them) or, where the run goes on for RUN_LONG tiles or
+// more, from the list's other end (runs[1]).
 template <class E, class O>
 __global__ __launch_bounds__(256) void run_sum_kernel(const E* __restrict__ grad, int64_t ld, const u32* __restrict__ skey,
                                                       const u32* __restrict__ spos, int64_t n, int64_t n_rows, int d, float scale, int add,
@@ -356,47 +369,81 @@ __global__ __launch_bounds__(256) void run_sum_kernel(const E* __restrict__ grad
 #pragma unroll
     for (int i = 0; i < P::E; ++i)
         if (at + i < d) p[i] = acc[i];
-    if (!carried && column == 0 && lane == 0) runs[1 + atomicAdd(runs, 1u)] = (u32)tile;
+    if (!carried && column == 0 && lane == 0) {
+        const int64_t far = i0 + (int64_t)RUN_LONG * RUN_TILE;
+        if (far < n && skey[far] == cur) runs[1 + (n + RUN_TILE - 1) / RUN_TILE - atomicAdd(runs + 1, 1u)] = (u32)tile;
+        else runs[2 + atomicAdd(runs, 1u)] = (u32)tile;
+    }
 }
 
-// 64 columns of a listed run a workgroup: the parts of its tiles are added, an equal stretch of the tiles a wave, then the waves in their order
+// The parts of the listed runs are added in the tiles' order, 256 columns at a time.  Most runs have two or three: a wave each.  Of a long one
+// eight waves take an equal stretch each, and are added in their order; the first RUN_JOIN_LONG workgroups look after those.
+#define RUN_JOIN_LONG 128
 template <class O>
 __global__ __launch_bounds__(512) void run_join_kernel(const u32* __restrict__ skey, int64_t n, int d, float scale, int add,
                                                        const float* __restrict__ parts, const u32* __restrict__ runs, O* __restrict__ out)
 {
-    constexpr int WAVES = 8;
-    __shared__ float s[WAVES][64];
-    const int columns = (d + 63) / 64;
-    const int64_t all = (int64_t)runs[0] * columns;
-    for (int64_t item = blockIdx.x; item < all; item += gridDim.x) {
-        const int64_t tile = runs[1 + item / columns];
-        const int wave = threadIdx.x >> 6, lane = tg_lane(), c = (int)(item % columns) * 64 + lane;
-        const u32 key = skey[(tile + 1) * RUN_TILE - 1];
-        // the run's end: the first place behind the tile with another key; most runs end in the next tile
-        int64_t lo = (tile + 1) * RUN_TILE, hi = lo + RUN_TILE;
-        while (hi < n && skey[hi] == key) { lo = hi; hi = hi + (hi - tile * RUN_TILE); }
-        if (hi > n) hi = n;
+    typedef TgPiece<float> P;
+    __shared__ float s_sum[8][64][4];
+    const int wave = threadIdx.x >> 6, lane = tg_lane(), columns = (d + 255) / 256;
+    const int64_t tiles = (n + RUN_TILE - 1) / RUN_TILE;
+    const auto put = [&](u32 key, int c, const float* v) {
+        O* p = out + (int64_t)key * d + c;
+        write_row<float, O>(v, d - c, p, scale, add != 0);
+    };
+    if (blockIdx.x >= RUN_JOIN_LONG) {
+        const int64_t all = (int64_t)runs[0] * columns;
+        for (int64_t item = (int64_t)(blockIdx.x - RUN_JOIN_LONG) * 8 + wave; item < all; item += (int64_t)(gridDim.x - RUN_JOIN_LONG) * 8) {
+            const int64_t tile = runs[2 + item / columns];
+            const int c = (int)(item % columns) * 256 + lane * 4;
+            const u32 key = skey[tile * RUN_TILE + RUN_TILE - 1];
+            // in how many tiles behind this one it begins the tile
+            const int64_t at = (tile + 1 + lane) * RUN_TILE;
+            const u64 same = __ballot(lane < RUN_LONG && at < n && skey[at] == key);
+            const int more = __ffsll((unsigned long long)~same) - 1;
+            P sum;
+            sum.load(parts + (2 * tile + 1) * d + c, d - c);
+#pragma unroll 4
+            for (int t = 1; t <= more; ++t) {
+                P q;
+                q.load(parts + 2 * (tile + t) * d + c, d - c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum.v[e] += q.v[e];
+            }
+            if (c < d) put(key, c, sum.v);
+        }
+        return;
+    }
+    const int64_t all = (int64_t)runs[1] * columns;
+    for (int64_t item = blockIdx.x; item < all; item += RUN_JOIN_LONG) {
+        const int64_t tile = runs[1 + tiles - item / columns];
+        const int c = (int)(item % columns) * 256 + lane * 4;
+        const u32 key = skey[tile * RUN_TILE + RUN_TILE - 1];
+        int64_t lo = (tile + RUN_LONG) * RUN_TILE, hi = n;                      // the first place with another key
         while (lo < hi) {
             const int64_t mid = (lo + hi) >> 1;
             if (skey[mid] == key) lo = mid + 1; else hi = mid;
         }
         const int64_t end = (lo - 1) / RUN_TILE;                                // its last tile
-        const int64_t each = (end - tile + WAVES - 1) / WAVES, from = tile + 1 + wave * each;
-        const int64_t to = from + each < end + 1 ? from + each : end + 1;
-        float sum = 0.0f;
-        if (c < d) {
-            if (wave == 0) sum = parts[(2 * tile + 1) * d + c];
+        const int64_t each = (end - tile + 7) / 8, from = tile + 1 + wave * each, to = from + each < end + 1 ? from + each : end + 1;
+        P sum;
+        sum.load(parts + (2 * tile + 1) * d + c, wave == 0 ? d - c : 0);
 #pragma unroll 8
-            for (int64_t t = from; t < to; ++t) sum += parts[2 * t * d + c];
+        for (int64_t t = from; t < to; ++t) {
+            P q;
+            q.load(parts + 2 * t * d + c, d - c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum.v[e] += q.v[e];
         }
-        s[wave][lane] = sum;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s_sum[wave][lane][e] = sum.v[e];
         __syncthreads();
         if (wave == 0 && c < d) {
-            float v = s[0][lane];
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) v += s[w][lane];
-            O* p = out + (int64_t)key * d + c;
-            *p = (O)((add ? (float)*p : 0.0f) + v * scale);
+            for (int w = 1; w < 8; ++w)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum.v[e] += s_sum[w][lane][e];
+            put(key, c, sum.v);
         }
         __syncthreads();
     }
@@ -418,7 +465,7 @@ static size_t carve_grad(GradSpace* g, void* base, int64_t n, int64_t n_rows, in
     g->pos[1] = few ? nullptr : c.take<u32>(whole);
     g->table = few ? nullptr : c.take<u32>((size_t)f.wgs << f.bits);
     g->total = few ? nullptr : c.take<u32>((size_t)1 << f.bits);
-    g->runs = c.take<u32>(tiles + 1);
+    g->runs = c.take<u32>(tiles + 2);
     g->parts = c.take<float>(tiles * 2 * d);
     return c.used;
 }
@@ -440,8 +487,10 @@ static void launch_sums(const E* grad, int64_t ld, const u32* key, const u32* po
     hipLaunchKernelGGL((run_sum_kernel<E, O>), dim3((unsigned)((tiles * columns + per - 1) / per)), dim3(256), 0, s, grad, ld, key, pos, n, n_rows, d,
                        scale, add, gs, columns, out, g.parts, g.runs);
     if (tiles > 1) {
-        const int64_t most = (tiles - 1) * ((d + 63) / 64);
-        hipLaunchKernelGGL(run_join_kernel<O>, dim3((unsigned)(most < 2048 ? most : 2048)), dim3(512), 0, s, key, n, d, scale, add, g.parts, g.runs, out);
+        // (at most a listed run a tile)
+        const int64_t waves = (tiles - 1) * ((d + 255) / 256), wgs = (waves + 7) / 8;
+        hipLaunchKernelGGL(run_join_kernel<O>, dim3((unsigned)(wgs < 1024 ? wgs : 1024) + RUN_JOIN_LONG), dim3(512), 0, s, key, n, d, scale, add, g.parts,
+                           g.runs, out);
     }
 }
 

@@ -7,6 +7,25 @@
 #include "tg_embed.h"
 #include "tg_tiles.h"
 
+#include <type_traits>
+
+// what reads rows as they are: short ones, and those of few tokens
+#define PRODUCT_FEW 64            // tokens up to which b is read straight into the registers
+#define PRODUCT_SHORT 256         // bytes of a row up to which a product keeps its tokens' rows in registers
+static bool product_as_is(int64_t m, int k) { return m <= PRODUCT_FEW || k <= PRODUCT_SHORT; }
+
+// 16 bytes of a row that has `left` bytes from p on (rows may begin anywhere; what is not there reads as zero)
+__device__ inline tg_i32x4 product_load(const char* p, int left)
+{
+    typedef int i32x4u __attribute__((ext_vector_type(4), aligned(1)));
+    if (left >= 16) return *reinterpret_cast<const i32x4u*>(p);
+    tg_i32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 15; ++i)
+        if (i < left) v[i / 4] |= (int)(uint8_t)p[i] << (i % 4 * 8);
+    return v;
+}
+
 // x: channels, y: tokens
 template <class O, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
@@ -17,8 +36,9 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(TileRows X, TileR
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
+    __shared__ __align__(1024) char lds[T::LDS];
     T t;
-    t.run(X, Y, x0, y0, 0, bytes);
+    t.run(X, Y, x0, y0, 0, bytes, lds);
     float c[T::FM][4], b[T::FM][4];
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
@@ -53,34 +73,42 @@ __global__ __launch_bounds__(256) void product_few_kernel(TileRows X, TileRows Y
 {
     constexpr int STEPS = 16 / FN;
     __shared__ tg_i32x4 s_part[3][FN][64];
-    const int wave = threadIdx.x >> 6, lane = tg_lane(), row = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = tg_lane(), row = lane & 15, q = lane >> 4;
     const int64_t x0 = first + (int64_t)blockIdx.x * 16;
-    const bool xin = x0 + row < X.rows;
-    const char* xp = X.p + (xin ? x0 + row : 0) * X.pitch + q * 16;
+    // (rows that are not there are read as the first one: nobody stores their sums)
+    const char* xp = X.p + (x0 + row < X.rows ? x0 + row : x0) * X.pitch + q * 16;
     const char* yp[FN];
-    bool yin[FN];
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-        yin[j] = j * 16 + row < Y.rows;
-        yp[j] = Y.p + (int64_t)(yin[j] ? j * 16 + row : 0) * Y.pitch + q * 16;
-    }
+    for (int j = 0; j < FN; ++j) yp[j] = Y.p + (int64_t)(j * 16 + row < Y.rows ? j * 16 + row : 0) * Y.pitch + q * 16;
     tg_i32x4 acc[FN];
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[j] = tg_i32x4{0, 0, 0, 0};
-    const tg_i32x4 none = {0, 0, 0, 0};
     const int each = ((bytes + 255) / 256) * 64, k1 = (wave + 1) * each < bytes ? (wave + 1) * each : bytes;
-    for (int k = wave * each; k < k1; k += 64 * STEPS) {
-        tg_i32x4 x[STEPS], y[STEPS][FN];
+    int k = wave * each;
+    // whole pieces of 64 bytes, STEPS at a time, then by fours and one by one, then what is left of a row
+    const auto steps = [&](auto count) {
+        constexpr int N = decltype(count)::value;
+        for (; k + N * 64 <= k1; k += N * 64) {
+            tg_i32x4 x[N], y[N][FN];
 #pragma unroll
-        for (int h = 0; h < STEPS; ++h) x[h] = k + h * 64 + q * 16 < k1 && xin ? *reinterpret_cast<const tg_i32x4*>(xp + k + h * 64) : none;
+            for (int h = 0; h < N; ++h) x[h] = product_load(xp + k + h * 64, 16);
 #pragma unroll
-        for (int h = 0; h < STEPS; ++h)
+            for (int h = 0; h < N; ++h)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) y[h][j] = k + h * 64 + q * 16 < k1 && yin[j] ? *reinterpret_cast<const tg_i32x4*>(yp[j] + k + h * 64) : none;
+                for (int j = 0; j < FN; ++j) y[h][j] = product_load(yp[j] + k + h * 64, 16);
 #pragma unroll
-        for (int h = 0; h < STEPS; ++h)
+            for (int h = 0; h < N; ++h)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[j] = TileMul<int8_t>::mul(x[h], y[h][j], acc[j]);
+                for (int j = 0; j < FN; ++j) acc[j] = TileMul<int8_t>::mul(x[h], y[h][j], acc[j]);
+        }
+    };
+    steps(std::integral_constant<int, STEPS>());
+    if (STEPS > 4) steps(std::integral_constant<int, 4>());
+    steps(std::integral_constant<int, 1>());
+    if (k < k1) {
+        const tg_i32x4 x = product_load(xp + k, k1 - k - q * 16);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[j] = TileMul<int8_t>::mul(x, product_load(yp[j] + k, k1 - k - q * 16), acc[j]);
     }
     if (wave > 0) {
 #pragma unroll
@@ -124,16 +152,20 @@ __global__ __launch_bounds__(256) void product_short_kernel(TileRows X, TileRows
         sy[j] = in ? as[r] : 0.0f;
 #pragma unroll
         for (int h = 0; h < STEPS; ++h)
-            y[j][h] = in && h * 64 + q * 16 < bytes ? *reinterpret_cast<const tg_i32x4*>(Y.p + r * Y.pitch + h * 64 + q * 16) : none;
+            y[j][h] = product_load(Y.p + (in ? r : 0) * Y.pitch + h * 64 + q * 16, bytes - h * 64 - q * 16);
     }
     tg_i32x4 x[CB][STEPS], next[CB][STEPS];
+    // (rows that are not there are read as the chunk's first: nobody stores their sums)
     const auto load = [&](int64_t chunk) {
 #pragma unroll
         for (int i = 0; i < CB; ++i) {
             const int64_t r = chunk * (16 * CB) + i * 16 + row;
-            const char* p = X.p + (r < X.rows ? r : 0) * X.pitch + q * 16;
+            const char* p = X.p + (r < X.rows ? r : chunk * (16 * CB)) * X.pitch + q * 16;
 #pragma unroll
-            for (int h = 0; h < STEPS; ++h) next[i][h] = r < X.rows && h * 64 + q * 16 < bytes ? *reinterpret_cast<const tg_i32x4*>(p + h * 64) : none;
+            for (int h = 0; h < STEPS; ++h) {
+                if (h * 64 + 64 <= bytes) next[i][h] = product_load(p + h * 64, 16);
+                else next[i][h] = product_load(p + h * 64, bytes - h * 64 - q * 16);
+            }
         }
     };
     int64_t chunk = (int64_t)blockIdx.x * 4 + wave;
@@ -176,22 +208,35 @@ __global__ __launch_bounds__(256) void product_short_kernel(TileRows X, TileRows
     }
 }
 
-// rows of `bytes` bytes, `from` apart, to rows `to` apart (a multiple of 16), the rest zero
+// rows of d elements of e bytes to rows of a multiple of 16 bytes, the rest zero: 16 bytes a lane
 template <class W>
-__global__ __launch_bounds__(256) void pack_kernel(const W* __restrict__ p, int64_t ld, int64_t rows, int d, int per /* W in a row of out */,
+__global__ __launch_bounds__(256) void pack_kernel(const W* __restrict__ p, int64_t ld, int64_t rows, int d, int per /* pieces of a row of out */,
                                                    W* __restrict__ out)
 {
+    constexpr int E = 16 / (int)sizeof(W);
+    typedef W from __attribute__((ext_vector_type(E), aligned(sizeof(W))));
+    typedef W to __attribute__((ext_vector_type(E)));
     const int64_t all = rows * per;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / per;
-        const int c = (int)(i - r * per);
-        out[i] = c < d ? p[r * ld + c] : (W)0;
+        const int64_t r = all < (1ll << 31) ? (int64_t)((uint32_t)i / (uint32_t)per) : i / per;
+        const int at = (int)(i - r * per) * E;
+        const W* q = p + r * ld + at;
+        to x;
+        if (at + E <= d) {
+            const from v = *reinterpret_cast<const from*>(q);
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[j] = v[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[j] = at + j < d ? q[j] : (W)0;
+        }
+        reinterpret_cast<to*>(out)[i] = x;
     }
 }
 void tg_launch_pack(const void* p, int64_t ld, int64_t rows, int d, int e, void* out, hipStream_t s)
 {
     if (rows == 0) return;
-    const int per = (int)(tile_pitch(d, e) / e);
+    const int per = (int)(tile_pitch(d, e) / 16);
     const int64_t wgs = (rows * per + 255) / 256;
     const dim3 g((unsigned)(wgs < 32768 ? wgs : 32768)), b(256);
     if (e == 1) hipLaunchKernelGGL(pack_kernel<uint8_t>, g, b, 0, s, (const uint8_t*)p, ld, rows, d, per, (uint8_t*)out);
@@ -201,7 +246,7 @@ void tg_launch_pack(const void* p, int64_t ld, int64_t rows, int d, int e, void*
 
 size_t tg_product_space(int64_t m, int64_t n, int k, bool ready)
 {
-    if (m == 0 || (ready && (k & 15) == 0)) return 0;
+    if (m == 0 || product_as_is(m, k) || (ready && (k & 15) == 0)) return 0;
     TgCarve c{nullptr, 0};
     c.take<char>((size_t)m * tile_pitch(k, 1));
     c.take<char>((size_t)n * tile_pitch(k, 1));
@@ -240,7 +285,7 @@ static void launch_product(const TileRows& X, const TileRows& Y, int bytes, cons
         else launch_short<O, 2, 8, 4>(X, Y, bytes, as, bs, bias, out, s);
         return;
     }
-    if (bytes <= 256) {
+    if (bytes <= PRODUCT_SHORT) {
         if (Y.rows <= 16) launch_short<O, 4, 1, 2>(X, Y, bytes, as, bs, bias, out, s);
         else if (Y.rows <= 32) launch_short<O, 4, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
         else launch_short<O, 4, 4, 2>(X, Y, bytes, as, bs, bias, out, s);
@@ -252,13 +297,11 @@ static void launch_product(const TileRows& X, const TileRows& Y, int bytes, cons
     else launch_tiles<O, 64, 64, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
 }
 
-#define PRODUCT_FEW 64            // tokens up to which b is read straight into the registers
-
 void tg_launch_product(const int8_t* a, const float* as, const int8_t* b, const float* bs, const float* bias, int64_t m, int64_t n, int k,
                        void* out, int dtype, void* space, hipStream_t s)
 {
     TileRows Y{(const char*)a, m, (uint32_t)k, (uint32_t)k}, X{(const char*)b, n, (uint32_t)k, (uint32_t)k};
-    if (!tile_ready(a, k, k, 1) || !tile_ready(b, k, k, 1)) {
+    if (!product_as_is(m, k) && (!tile_ready(a, k, k, 1) || !tile_ready(b, k, k, 1))) {
         TgCarve c{(char*)space, 0};
         Y.pitch = X.pitch = Y.width = X.width = tile_pitch(k, 1);
         char* pa = c.take<char>((size_t)m * Y.pitch);
@@ -268,8 +311,8 @@ void tg_launch_product(const int8_t* a, const float* as, const int8_t* b, const 
         Y.p = pa;
         X.p = pb;
     }
-    const int bytes = (int)X.pitch;
-    if (m <= PRODUCT_FEW && bytes > 256) {
+    const int bytes = (int)X.width;
+    if (m <= PRODUCT_FEW && bytes > PRODUCT_SHORT) {
         const int64_t most = TILE_LAUNCH_ITEMS / 256 * 16;
         for (int64_t x0 = 0; x0 < n; x0 += most) {
             const dim3 g((unsigned)(((n - x0 < most ? n - x0 : most) + 15) / 16)), t(256);

@@ -286,11 +286,10 @@ struct Tile {
 #endif
 
     // rows (columns, where turned) x0.. of X and y0.. of Y, contraction bytes [k0, k1) (k0 a multiple of TILE_BYTES, k1 of 16;
-    // below 2^31 - 2^10)
-    __device__ inline void run(const TileRows& X, const TileRows& Y, int64_t x0, int64_t y0, int k0, int k1)
+    // below 2^31 - 2^10); lds: LDS bytes that begin at a multiple of 1024
+    __device__ inline void run(const TileRows& X, const TileRows& Y, int64_t x0, int64_t y0, int k0, int k1, char* lds)
     {
 #ifdef __HIP_DEVICE_COMPILE__
-        __shared__ __align__(1024) char lds[LDS];
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         Run r{k0, k1, wave, tg_lane(), wave / WN, wave % WN, lds};
 #pragma unroll

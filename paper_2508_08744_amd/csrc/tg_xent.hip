@@ -33,8 +33,9 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, Til
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
+    __shared__ __align__(1024) char lds[T::LDS];
     T t;
-    t.run(X, Y, x0, y0, 0, bytes);
+    t.run(X, Y, x0, y0, 0, bytes, lds);
     const bool whole = x0 + BM <= X.rows;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
@@ -109,59 +110,63 @@ __global__ __launch_bounds__(1024) void xent_join_kernel(const float2* __restric
 
 // ---- gradient
 
-// h without the rows of tokens that have no target (nothing of theirs, not even a NaN, may reach dw), packed for the tiles; per token
-// what P is multiplied by; and, for fp16, the power of two that P is kept under: P is at most |scale| max |dloss|, so that times
-// c it stays below 2^14, and values down to 2^-28 of the largest keep all their bits (bf16 and fp32 have the range as they are: c = 1).
+// h without the rows of tokens that have no target (nothing of theirs, not even a NaN, may reach dw), packed for the tiles.  The last
+// workgroup finds, for fp16, the power of two that P is kept under: P is at most |scale| max |dloss|, so that times c[0] it stays below 2^14, and
+// values down to 2^-28 of the largest keep all their bits (bf16 and fp32 have the range as they are: c[0] = 1); c[1] = 1 / c[0].
 template <class E>
-__global__ __launch_bounds__(256) void xent_rows_kernel(const E* __restrict__ h, int64_t ld, int64_t n, int64_t n_rows, int d, int per,
-                                                        const void* __restrict__ targets, int targets64, E* __restrict__ out)
+__global__ __launch_bounds__(256) void xent_prepare_kernel(const E* __restrict__ h, int64_t ld, int64_t n, int64_t n_rows, int d, int per,
+                                                           const void* __restrict__ targets, int targets64, const float* __restrict__ dloss,
+                                                           float scale, E* __restrict__ out, float* __restrict__ c)
 {
-    const int64_t all = n * per;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        typedef TgPiece<E> P;
-        const int64_t r = i / per;
-        const int at = (int)(i - r * per) * P::E;
-        P p;
-        p.load(h + r * ld + at, tg_row_of(targets, targets64, r, n_rows) >= 0 ? d - at : 0);
-        p.store(out + r * per * P::E + at, P::E);
+    constexpr bool NARROW = __is_same(E, tg_f16);
+    if (blockIdx.x < gridDim.x - 1) {
+        const int64_t all = n * per;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)(gridDim.x - 1) * 256) {
+            typedef TgPiece<E> P;
+            const int64_t r = i / per;
+            const int at = (int)(i - r * per) * P::E;
+            *reinterpret_cast<typename P::vec*>(out + r * per * P::E + at) = P::raw(h + r * ld + at, tg_row_of(targets, targets64, r, n_rows) >= 0 ? d - at : 0);
+        }
+        return;
     }
-}
-__global__ __launch_bounds__(1024) void xent_range_kernel(const float* __restrict__ dloss, const void* __restrict__ targets, int targets64, int64_t n,
-                                                          int64_t n_rows, float scale, int narrow, float* __restrict__ c)
-{
-    __shared__ float s[16];
     float top = 0.0f;
-    if (narrow)
-        for (int64_t t = threadIdx.x; t < n; t += 1024)
+    if (NARROW) {
+        __shared__ float s[4];
+        for (int64_t t = threadIdx.x; t < n; t += 256)
             if (tg_row_of(targets, targets64, t, n_rows) >= 0) top = fmaxf(top, fabsf(dloss[t] * scale));
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = top;
-    __syncthreads();
+        for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    }
     if (threadIdx.x) return;
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-    int e = 0;
-    if (narrow && top > 0.0f && top <= 3.4028234e38f) (void)frexpf(top, &e);     // top in [2^(e-1), 2^e)
-    else e = 14;
-    int up = 14 - e;
-    up = up < -100 ? -100 : up > 100 ? 100 : up;
+    int up = 0;
+    if (NARROW && top > 0.0f && top <= 3.4028234e38f) {
+        int e;
+        (void)frexpf(top, &e);                        // top in [2^(e-1), 2^e)
+        up = 14 - e;
+        up = up < -100 ? -100 : up > 100 ? 100 : up;
+    }
     c[0] = ldexpf(1.0f, up);
     c[1] = ldexpf(1.0f, -up);
 }
 
-// P of a piece: x: rows v0.. of the table, y: tokens; p: n rows, `pitch` elements apart, zeros behind the piece's rows
+// P of a piece: x: rows v0.. of the table, y: tokens; p: n rows, `pitch` elements apart, zeros behind the piece's rows.  lost: for types
+// of 16 bits, what rounding took from P at the token's target, the entry that outweighs all others together.
 template <class E, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
                                                               const float* __restrict__ lse, const float* __restrict__ dloss,
                                                               const float* __restrict__ c, float scale, int64_t v0, int64_t n_rows, uint32_t nx,
-                                                              uint32_t ny, uint32_t group, E* __restrict__ p, int64_t pitch)
+                                                              uint32_t ny, uint32_t group, E* __restrict__ p, int64_t pitch, float* __restrict__ lost)
 {
     typedef Tile<E, BM, BN, WM, WN> T;
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
+    __shared__ __align__(1024) char lds[T::LDS];
     T t;
-    t.run(X, Y, x0, y0, 0, bytes);
+    t.run(X, Y, x0, y0, 0, bytes, lds);
     const float up = c[0];
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
@@ -179,94 +184,142 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
                 const float s = __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e] * scale, XENT_LOG2E, -b)) - (x + e == hit ? 1.0f : 0.0f);
                 // (a token without a target has no part in anything, whatever its logits are)
                 v[e] = target >= 0 && x + e < X.rows ? s * g : 0.0f;
+                if (sizeof(E) == 2 && x + e == hit) lost[y] = v[e] - (float)(E)v[e];
             }
             if (x < pitch) tile_put(p + y * pitch + x, v, pitch - x);
         }
     }
 }
 
-// dh: x: columns of w (turned), y: tokens, over the rows of the piece from part `s` of `splits`.  sums: splits x n x d, added to but for the
-// first piece
-template <class E, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void xent_dh_kernel(TileRows X, TileRows Y, int bytes, int each, int d, uint32_t nx, uint32_t ny,
-                                                               int splits, int first, float* __restrict__ sums)
+// The two products of a piece in one launch, the first workgroups dh's (they fill the card in whole rounds together where each does not).
+//
+// dh: x: columns of w (turned), y: tokens, over the rows of the piece, in `splits` parts.  sums: splits x n x d, added to but for the first
+// piece; or, where there is one piece and one part, dh itself.
+// dw: x: columns of h (turned), y: columns of P, rows of the piece (turned), over the tokens.
+struct XentProducts {
+    TileRows w, h, p;
+    int64_t v0, rows, n_rows;       // the piece's first row of the table, its rows, the table's
+    int d;
+    int p_bytes, each, h_bytes;     // contractions: of dh, of one part of it, of dw
+    uint32_t dh_x, dh_y, dw_x, dw_y;
+    int splits, first, direct;
+    const void* targets;
+    int targets64;
+    const void* table;              // the caller's w
+    int64_t ld_table;
+    const float *c, *lost;
+    float* sums;
+    void *dh, *dw;
+};
+// four neighbours of row y of dh, with what rounding took from P at the target
+template <class E>
+__device__ inline void xent_put_dh(const XentProducts& a, int64_t y, int x, float* v)
 {
-    typedef Tile<E, BM, BN, WM, WN, true, false> T;
-    const uint32_t b = tile_of_block(blockIdx.x, nx * ny * splits);
-    const uint32_t s = (uint32_t)__builtin_amdgcn_readfirstlane((int)(b / (nx * ny))), in = b - s * (nx * ny);
+    const int64_t target = tg_row_of(a.targets, a.targets64, y, a.n_rows);
+    const float l = sizeof(E) == 2 && target >= 0 ? a.lost[y] : 0.0f;
+    const E* row = (const E*)a.table + (target < 0 ? 0 : target) * a.ld_table + x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (sizeof(E) == 2 && x + e < a.d) v[e] = fmaf(l, (float)row[e], v[e]);
+        v[e] = target >= 0 ? v[e] * a.c[1] : 0.0f;
+    }
+    tile_put((E*)a.dh + y * a.d + x, v, a.d - x);
+}
+// tokens up to which dw too gets back what rounding took from P at the targets: of more the errors are many and average out
+#define XENT_LOST_TOKENS 32
+
+template <class E, int B, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void xent_products_kernel(XentProducts a)
+{
+    typedef Tile<E, B, B, WM, WN, true, false> TH;
+    typedef Tile<E, B, B, WM, WN, true, true> TW;
+    static_assert(TH::LDS == TW::LDS, "one memory for both");
+    __shared__ __align__(1024) char lds[TH::LDS];
+    const uint32_t dh_all = a.dh_x * a.dh_y * a.splits;
     uint32_t tx, ty;
-    tile_place(in, nx, ny, 1, &tx, &ty);
-    const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
-    const int k0 = (int)s * each, k1 = k0 + each < bytes ? k0 + each : bytes;
-    T t;
-    t.run(X, Y, x0, y0, k0, k1);
+    if (blockIdx.x < dh_all) {
+        const uint32_t b = tile_of_block(blockIdx.x, dh_all);
+        const uint32_t s = (uint32_t)__builtin_amdgcn_readfirstlane((int)(b / (a.dh_x * a.dh_y)));
+        tile_place(b - s * (a.dh_x * a.dh_y), a.dh_x, a.dh_y, 1, &tx, &ty);
+        const int64_t x0 = (int64_t)tx * B, y0 = (int64_t)ty * B;
+        const int k0 = (int)s * a.each, k1 = k0 + a.each < a.p_bytes ? k0 + a.each : a.p_bytes;
+        TH t;
+        t.run(a.w, a.p, x0, y0, k0, k1, lds);
 #pragma unroll
-    for (int j = 0; j < T::FN; ++j) {
+        for (int j = 0; j < TH::FN; ++j) {
+            const int64_t y = y0 + t.y_of(j);
+            if (y >= a.p.rows) continue;
+#pragma unroll
+            for (int i = 0; i < TH::FM; ++i) {
+                const int x = (int)x0 + t.x_of(i);
+                if (x >= a.d) continue;
+                float v[4];
+                float* o = a.sums + ((int64_t)s * a.p.rows + y) * a.d + x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = t.acc[i][j][e] + (!a.first && x + e < a.d ? o[e] : 0.0f);
+                if (a.direct) xent_put_dh<E>(a, y, x, v);
+                else tile_put(o, v, a.d - x);
+            }
+        }
+        return;
+    }
+    tile_place(tile_of_block(blockIdx.x - dh_all, a.dw_x * a.dw_y), a.dw_x, a.dw_y, 1, &tx, &ty);
+    const int64_t x0 = (int64_t)tx * B, y0 = (int64_t)ty * B;
+    TW t;
+    t.run(a.h, a.p, x0, y0, 0, a.h_bytes, lds);
+    if (sizeof(E) == 2 && a.p.rows <= XENT_LOST_TOKENS) {
+        const int64_t v0 = a.v0 + y0;
+        for (int64_t r = 0; r < a.p.rows; ++r) {
+            const int64_t at = tg_row_of(a.targets, a.targets64, r, a.n_rows) - v0;
+            if (at < 0 || at >= B) continue;
+            const float l = a.lost[r];
+#pragma unroll
+            for (int j = 0; j < TW::FN; ++j)
+                if (t.y_of(j) == at) {
+#pragma unroll
+                    for (int i = 0; i < TW::FM; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int64_t x = x0 + t.x_of(i) + e;
+                            if (x < a.d) t.acc[i][j][e] = fmaf(l, (float)((const E*)(a.h.p + r * a.h.pitch))[x], t.acc[i][j][e]);
+                        }
+                }
+        }
+    }
+    const float down = a.c[1];
+#pragma unroll
+    for (int j = 0; j < TW::FN; ++j) {
         const int64_t y = y0 + t.y_of(j);
-        if (y >= Y.rows) continue;
+        if (y >= a.rows) continue;
 #pragma unroll
-        for (int i = 0; i < T::FM; ++i) {
+        for (int i = 0; i < TW::FM; ++i) {
             const int x = (int)x0 + t.x_of(i);
-            if (x >= d) continue;
-            float* o = sums + ((int64_t)s * Y.rows + y) * d + x;
+            if (x >= a.d) continue;
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = t.acc[i][j][e] + (!first && x + e < d ? o[e] : 0.0f);
-            tile_put(o, v, d - x);
+            for (int e = 0; e < 4; ++e) v[e] = t.acc[i][j][e] * down;
+            tile_put((E*)a.dw + y * a.d + x, v, a.d - x);
         }
     }
 }
+// dh out of its parts
 template <class E>
-__global__ __launch_bounds__(256) void xent_dh_out_kernel(const float* __restrict__ sums, int splits, int64_t n, int64_t n_rows, int d, int pieces,
-                                                          const void* __restrict__ targets, int targets64, const float* __restrict__ c,
-                                                          E* __restrict__ dh)
+__global__ __launch_bounds__(256) void xent_dh_kernel(XentProducts a, int pieces)
 {
-    const int64_t all = n * pieces;
-    const float down = c[1];
+    const int64_t n = a.p.rows, all = n * pieces;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         const int64_t y = i / pieces;
         const int at = (int)(i - y * pieces) * 4;
         TgPiece<float> sum;
-        sum.load(sums + y * d + at, d - at);
+        sum.load(a.sums + y * a.d + at, a.d - at);
 #pragma unroll 8
-        for (int s = 1; s < splits; ++s) {
+        for (int s = 1; s < a.splits; ++s) {
             TgPiece<float> q;
-            q.load(sums + (s * n + y) * d + at, d - at);
+            q.load(a.sums + (s * n + y) * a.d + at, a.d - at);
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum.v[e] += q.v[e];
         }
-        const bool there = tg_row_of(targets, targets64, y, n_rows) >= 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum.v[e] = there ? sum.v[e] * down : 0.0f;
-        tile_put(dh + y * d + at, sum.v, d - at);
-    }
-}
-
-// dw: x: columns of h (turned), y: columns of P, rows of the piece (turned), over the tokens
-template <class E, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void xent_dw_kernel(TileRows X, TileRows Y, int64_t rows, int bytes, int d, const float* __restrict__ c,
-                                                               uint32_t nx, uint32_t ny, E* __restrict__ dw)
-{
-    typedef Tile<E, BM, BN, WM, WN, true, true> T;
-    uint32_t tx, ty;
-    tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, 1, &tx, &ty);
-    const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
-    T t;
-    t.run(X, Y, x0, y0, 0, bytes);
-    const float down = c[1];
-#pragma unroll
-    for (int j = 0; j < T::FN; ++j) {
-        const int64_t y = y0 + t.y_of(j);
-        if (y >= rows) continue;
-#pragma unroll
-        for (int i = 0; i < T::FM; ++i) {
-            const int x = (int)x0 + t.x_of(i);
-            if (x >= d) continue;
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = t.acc[i][j][e] * down;
-            tile_put(dw + y * d + x, v, d - x);
-        }
+        xent_put_dh<E>(a, y, at, sum.v);
     }
 }
 
@@ -355,26 +408,31 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
 
 struct XentGrad {
     int64_t piece;        // rows of the table at a time, a multiple of 256 unless it is all of them
-    bool wide;            // dh in tiles of 256 x 256, of which a CU holds one, else of 128 x 128, of which it holds two
+    bool wide;            // products in tiles of 256 x 256
     int splits;           // of dh's contraction
+    bool direct;          // one piece, one part: dh is written at once
 };
 static int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
-static void xent_splits(XentGrad* g, int64_t n, int d, int e)
+static void xent_splits(XentGrad* g, int64_t n, int64_t n_rows, int d, int e)
 {
-    g->wide = e == 2 && n > 128 && d > 128;
+    // both products take tiles of 256 x 256, of which a CU holds one, where those are enough; else of 128 x 128, of which it holds two
+    const auto tiles = [](int64_t x, int64_t y, int64_t side) { return ((x + side - 1) / side) * ((y + side - 1) / side); };
+    g->wide = e == 2 && n > 128 && d > 128 && tiles(g->piece, d, 256) >= 200;
     const int64_t side = g->wide ? 256 : 128, fill = g->wide ? 256 : 512;
-    // as many parts as fill the card, each with sixteen stages of the contraction or more
-    const int64_t tiles = ((n + side - 1) / side) * ((d + side - 1) / side), stages = (g->piece * e + TILE_BYTES - 1) / TILE_BYTES;
-    int64_t s = (fill + tiles - 1) / tiles;
+    // dh in as many parts as fill the card, each with sixteen stages of the contraction or more
+    const int64_t dh = tiles(n, d, side), stages = (g->piece * e + TILE_BYTES - 1) / TILE_BYTES;
+    int64_t s = (fill + dh - 1) / dh;
     if (s > stages / 16) s = stages / 16;
     g->splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+    g->direct = g->splits == 1 && g->piece >= n_rows;
 }
 static size_t carve_xent_grad(XentRows* r, TgCarve* c, const void* h, int64_t ld_h, const void* w, int64_t ld_w, int64_t n, int64_t n_rows, int d,
-                              int e, bool ready_w, XentGrad g, float** consts, char** p, float** sums)
+                              int e, bool ready_w, XentGrad g, float** consts, char** p, float** sums, float** lost)
 {
-    xent_rows(r, c, h, ld_h, w, ld_w, n, n_rows, d, e, false, ready_w);       // (h is always copied: see xent_rows_kernel)
+    xent_rows(r, c, h, ld_h, w, ld_w, n, n_rows, d, e, false, ready_w);       // (h is always copied: see xent_prepare_kernel)
     *consts = c->take<float>(2);
-    *sums = c->take<float>((size_t)g.splits * n * d);
+    *lost = c->take<float>(e == 2 ? n : 0);
+    *sums = c->take<float>(g.direct ? 0 : (size_t)g.splits * n * d);
     *p = c->take<char>((size_t)n * round_up(g.piece * e, 16));
     return c->used;
 }
@@ -390,69 +448,85 @@ static XentGrad xent_grad_shape(int64_t n, int64_t n_rows, int d, int e, int64_t
         const int64_t count = (n_rows + g.piece - 1) / g.piece;
         g.piece = round_up((n_rows + count - 1) / count, 256);
     }
-    xent_splits(&g, n, d, e);
+    xent_splits(&g, n, n_rows, d, e);
     return g;
 }
 static size_t xent_grad_bytes(int64_t n, int64_t n_rows, int d, int e, bool ready, int64_t p_bytes)
 {
     TgCarve c{nullptr, 0};
     XentRows r;
-    float *k, *sums;
+    float *k, *sums, *lost;
     char* p;
-    return carve_xent_grad(&r, &c, nullptr, d, nullptr, d, n, n_rows, d, e, ready && (d * e & 15) == 0, xent_grad_shape(n, n_rows, d, e, p_bytes), &k, &p, &sums);
+    return carve_xent_grad(&r, &c, nullptr, d, nullptr, d, n, n_rows, d, e, ready && (d * e & 15) == 0, xent_grad_shape(n, n_rows, d, e, p_bytes), &k, &p, &sums, &lost);
 }
 size_t tg_xent_grad_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready, bool least)
 {
     if (n == 0) return 0;
-    return xent_grad_bytes(n, n_rows, d, (int)tg_type_bytes(dtype), ready, least ? 0 : XENT_PIECE_BYTES);
+    const size_t asked = xent_grad_bytes(n, n_rows, d, (int)tg_type_bytes(dtype), ready, XENT_PIECE_BYTES);
+    if (!least) return asked;
+    // (one piece can do with less than many: dh then needs no sums)
+    const size_t pieces = xent_grad_bytes(n, n_rows, d, (int)tg_type_bytes(dtype), ready, 0);
+    return pieces < asked ? pieces : asked;
 }
 
 template <class E>
-static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h, int64_t ld_h, int64_t n, int64_t n_rows, int d, const void* targets,
-                             int targets64, const float* lse, const float* dloss, float scale, float* consts, char* p, float* sums, E* dh, E* dw,
-                             hipStream_t s)
+static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h, int64_t ld_h, const void* w, int64_t ld_w, int64_t n, int64_t n_rows,
+                             int d, const void* targets, int targets64, const float* lse, const float* dloss, float scale, float* consts, char* p,
+                             float* sums, float* lost, E* dh, E* dw, hipStream_t s)
 {
     const int e = (int)sizeof(E), per = (int)(r.h.pitch / 16);
     const int64_t wgs = (n * per + 255) / 256;
-    hipLaunchKernelGGL(xent_range_kernel, dim3(1), dim3(1024), 0, s, dloss, targets, targets64, n, n_rows, scale, __is_same(E, tg_f16) ? 1 : 0, consts);
-    hipLaunchKernelGGL(xent_rows_kernel<E>, dim3((unsigned)(wgs < 16384 ? wgs : 16384)), dim3(256), 0, s, (const E*)h, ld_h, n, n_rows, d, per, targets,
-                       targets64, (E*)r.ph);
+    hipLaunchKernelGGL(xent_prepare_kernel<E>, dim3((unsigned)(wgs < 16384 ? wgs : 16384) + 1), dim3(256), 0, s, (const E*)h, ld_h, n, n_rows, d, per,
+                       targets, targets64, dloss, scale, (E*)r.ph, consts);
+    XentProducts a;
+    a.h = r.h;
+    a.n_rows = n_rows;
+    a.d = d;
+    a.h_bytes = (int)(n * e);
+    a.splits = g.splits;
+    a.direct = g.direct ? 1 : 0;
+    a.targets = targets;
+    a.targets64 = targets64;
+    a.table = w;
+    a.ld_table = ld_w;
+    a.c = consts;
+    a.lost = lost;
+    a.sums = sums;
+    a.dh = dh;
+    const int side = g.wide ? 256 : 128;
+    const auto over = [](int64_t x, int64_t by) { return (uint32_t)((x + by - 1) / by); };
+    a.dh_x = a.dw_x = over(d, side);
+    a.dh_y = over(n, side);
     for (int64_t v0 = 0; v0 < n_rows; v0 += g.piece) {
         const int64_t rows = n_rows - v0 < g.piece ? n_rows - v0 : g.piece;
-        const TileRows W{r.w.p + v0 * r.w.pitch, rows, r.w.pitch, r.w.width};
         const uint32_t pitch = (uint32_t)round_up(rows * e, 16);
-        const TileRows P{p, n, pitch, pitch};
+        a.w = TileRows{r.w.p + v0 * r.w.pitch, rows, r.w.pitch, r.w.width};
+        a.p = TileRows{p, n, pitch, pitch};
         const auto logits = [&](auto kernel, int bm, int bn, int threads) {
-            const uint32_t nx = (uint32_t)((rows + bm - 1) / bm), ny = (uint32_t)((n + bn - 1) / bn);
-            hipLaunchKernelGGL(kernel, dim3(nx * ny), dim3(threads), 0, s, W, r.h, (int)W.width, targets, targets64, lse, dloss, (const float*)consts, scale,
-                               v0, n_rows, nx, ny, 8u, (E*)p, (int64_t)(pitch / e));
+            const uint32_t nx = over(rows, bm), ny = over(n, bn);
+            hipLaunchKernelGGL(kernel, dim3(nx * ny), dim3(threads), 0, s, a.w, r.h, (int)a.w.width, targets, targets64, lse, dloss, (const float*)consts,
+                               scale, v0, n_rows, nx, ny, 8u, (E*)p, (int64_t)(pitch / e), lost);
         };
-        const auto tiles = [](int64_t x, int64_t y, int64_t side) { return ((x + side - 1) / side) * ((y + side - 1) / side); };
         if (n <= 64) logits(xent_p_kernel<E, 128, 64, 4, 1>, 128, 64, 256);
-        else if (e == 4 || tiles(rows, n, 256) < 200) logits(xent_p_kernel<E, 128, 128, 2, 2>, 128, 128, 256);
+        else if (e == 4 || (int64_t)over(rows, 256) * over(n, 256) < 200) logits(xent_p_kernel<E, 128, 128, 2, 2>, 128, 128, 256);
         else logits(xent_p_kernel<E, 256, 256, 2, 4>, 256, 256, 512);
-        const auto product_dh = [&](auto kernel, int side, int threads) {
-            const int stages = (int)((pitch + TILE_BYTES - 1) / TILE_BYTES), each = (stages + g.splits - 1) / g.splits * TILE_BYTES;
-            const uint32_t nx = (uint32_t)((d + side - 1) / side), ny = (uint32_t)((n + side - 1) / side);
-            hipLaunchKernelGGL(kernel, dim3(nx * ny * g.splits), dim3(threads), 0, s, W, P, (int)pitch, each, d, nx, ny, g.splits, v0 == 0 ? 1 : 0, sums);
-        };
-        const auto product_dw = [&](auto kernel, int side, int threads) {
-            const uint32_t nx = (uint32_t)((d + side - 1) / side), ny = (uint32_t)((rows + side - 1) / side);
-            hipLaunchKernelGGL(kernel, dim3(nx * ny), dim3(threads), 0, s, r.h, P, rows, (int)(n * e), d, (const float*)consts, nx, ny, dw + v0 * d);
-        };
+        const int stages = (int)((pitch + TILE_BYTES - 1) / TILE_BYTES);
+        a.v0 = v0;
+        a.rows = rows;
+        a.p_bytes = (int)pitch;
+        a.each = (stages + g.splits - 1) / g.splits * TILE_BYTES;
+        a.first = v0 == 0 ? 1 : 0;
+        a.dw = dw + v0 * d;
+        a.dw_y = over(rows, side);
+        const dim3 grid(a.dh_x * a.dh_y * g.splits + a.dw_x * a.dw_y);
         if constexpr (sizeof(E) == 2) {
-            if (g.wide) product_dh(xent_dh_kernel<E, 256, 256, 2, 4>, 256, 512);
-            else product_dh(xent_dh_kernel<E, 128, 128, 2, 2>, 128, 256);
-            if (tiles(rows, d, 256) >= 200) product_dw(xent_dw_kernel<E, 256, 256, 2, 4>, 256, 512);
-            else product_dw(xent_dw_kernel<E, 128, 128, 2, 2>, 128, 256);
-        } else {
-            product_dh(xent_dh_kernel<E, 128, 128, 2, 2>, 128, 256);
-            product_dw(xent_dw_kernel<E, 128, 128, 2, 2>, 128, 256);
-        }
+            if (g.wide) hipLaunchKernelGGL((xent_products_kernel<E, 256, 2, 4>), grid, dim3(512), 0, s, a);
+            else hipLaunchKernelGGL((xent_products_kernel<E, 128, 2, 2>), grid, dim3(256), 0, s, a);
+        } else hipLaunchKernelGGL((xent_products_kernel<E, 128, 2, 2>), grid, dim3(256), 0, s, a);
     }
+    if (g.direct) return;
     const int64_t out_wgs = (n * ((d + 3) / 4) + 255) / 256;
-    hipLaunchKernelGGL(xent_dh_out_kernel<E>, dim3((unsigned)(out_wgs < 16384 ? out_wgs : 16384)), dim3(256), 0, s, sums, g.splits, n, n_rows, d,
-                       (d + 3) / 4, targets, targets64, (const float*)consts, dh);
+    hipLaunchKernelGGL(xent_dh_kernel<E>, dim3((unsigned)(out_wgs < 16384 ? out_wgs : 16384)), dim3(256), 0, s, a, (d + 3) / 4);
 }
 
 void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const void* targets,
@@ -470,9 +544,10 @@ void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_
     const XentGrad g = xent_grad_shape(n, n_rows, d, e, p_bytes);
     TgCarve c{(char*)space, 0};
     XentRows r;
-    float *consts, *sums;
+    float *consts, *sums, *lost;
     char* p;
-    carve_xent_grad(&r, &c, h, ld_h, w, ld_w, n, n_rows, d, e, ready, g, &consts, &p, &sums);
+    carve_xent_grad(&r, &c, h, ld_h, w, ld_w, n, n_rows, d, e, ready, g, &consts, &p, &sums, &lost);
     if (!ready) tg_launch_pack(w, ld_w, n_rows, d, e, r.pw, s);
-    TG_WITH_TYPE(dtype, E, launch_xent_grad<E>(r, g, h, ld_h, n, n_rows, d, targets, targets64, lse, dloss, scale, consts, p, sums, (E*)dh, (E*)dw, s));
+    TG_WITH_TYPE(dtype, E, launch_xent_grad<E>(r, g, h, ld_h, w, ld_w, n, n_rows, d, targets, targets64, lse, dloss, scale, consts, p, sums, lost,
+                                            (E*)dh, (E*)dw, s));
 }

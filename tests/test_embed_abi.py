@@ -65,10 +65,11 @@ def test_product_refusals():
     _refused("tg_matmul_q8", [P, P, P, P, None, 10, 20, 64, P, 0, None, 0, None],
              [(0, None), (1, None), (2, None), (3, None), (5, -1), (6, 0), (6, 1 << 30), (7, 0), (7, 65537), (8, None), (9, 3)])
     # rows that have to be copied need a workspace
-    _refused("tg_matmul_q8", [P, P, P, P, None, 10, 20, 50, P, 0, P, BIG, None], [(10, None), (10, ODD), (11, 100)])
-    _refused("tg_matmul_q8", [P, P, ODD, P, None, 10, 20, 64, P, 0, P, BIG, None], [(10, None), (11, 100)])
+    _refused("tg_matmul_q8", [P, P, P, P, None, 100, 20, 300, P, 0, P, BIG, None], [(10, None), (10, ODD), (11, 100)])
+    _refused("tg_matmul_q8", [P, P, ODD, P, None, 100, 20, 320, P, 0, P, BIG, None], [(10, None), (11, 100)])
     f = embed.lib().tg_matmul_q8_workspace
-    assert f(10, 20, 64, 1) == 0 and f(10, 20, 64, 0) >= 30 * 64 and f(10, 20, 50, 1) >= 30 * 64 and f(10, 20, 64, 2) == 0
+    assert f(100, 20, 320, 1) == 0 and f(100, 20, 320, 0) >= 120 * 320 and f(100, 20, 300, 1) >= 120 * 304 and f(100, 20, 320, 2) == 0
+    assert f(64, 20, 300, 0) == 0 and f(100, 20, 250, 0) == 0          # few tokens and short rows are read as they are
     assert embed.lib().tg_matmul_q8(None, None, None, None, None, 0, 20, 64, None, 0, None, 0, None) == 0
 
 

@@ -69,7 +69,7 @@ def test_lookup_shapes_and_far_rows():
     assert embed.lookup(table, ids[:0]).shape == (0, 2, d)
 
 
-GRAD_SHAPES = [(1, 1, 1), (5, 3, 8), (31, 7, 50), (33, 1, 128), (64, 5000, 96), (1000, 37, 127), (4097, 300, 1031), (8192, 70_000, 16), (8193, 70_000, 16),
+GRAD_SHAPES = [(1, 1, 1), (5, 3, 8), (31, 7, 50), (33, 1, 128), (64, 5000, 96), (1000, 37, 127), (4097, 300, 1031), (16_384, 70_000, 16), (16_385, 70_000, 16),
                (20_000, 3, 40), (50_000, 5_000_000, 8)]
 
 
@@ -100,7 +100,7 @@ def test_lookup_grad(t, n, v, d):
         assert torch.equal(out.cpu()[still], before.cpu()[still])
 
 
-@pytest.mark.parametrize("n", [100, 9000])
+@pytest.mark.parametrize("n", [100, 20_000])
 def test_lookup_grad_without_a_token(n):
     ids = torch.full((n,), -1, device=DEV)
     grad = torch.full((n, 33), float("nan"), dtype=BF16, device=DEV)
@@ -489,7 +489,7 @@ def _step_inputs(seed, n, v, d, t=BF16):
             torch.randint(-1, v, (n,), generator=g).to(DEV), (torch.rand(n, generator=g) / n).to(DEV))
 
 
-@pytest.mark.parametrize("n", [48, 9000])
+@pytest.mark.parametrize("n", [48, 20_000])
 def test_a_step_in_a_graph(n):
     state = [x.clone() for x in _step_inputs(0, n, 1500, 64)]
     _step(*state)
