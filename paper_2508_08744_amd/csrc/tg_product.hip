@@ -26,40 +26,42 @@ __device__ inline tg_i32x4 product_load(const char* p, int left)
     return v;
 }
 
-// x: channels, y: tokens
-template <class O, int BM, int BN, int WM, int WN>
+// x: channels, y: tokens.
+template <class O, int BM, int BN, int WM, int WN, int NB, bool BIAS>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
                                                                const float* __restrict__ bs, const float* __restrict__ bias, uint32_t nx,
                                                                uint32_t ny, uint32_t group, O* __restrict__ out)
 {
-    typedef Tile<int8_t, BM, BN, WM, WN> T;
+    typedef Tile<int8_t, BM, BN, WM, WN, false, false, NB> T;
+    __shared__ __align__(1024) char lds[T::LDS];
+    // the scales and the bias: asked for before the products, so that nothing waits for them behind
+    __shared__ float s_as[BN], s_bs[BM], s_bias[BIAS ? BM : 1];
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
-    __shared__ __align__(1024) char lds[T::LDS];
     T t;
-    t.run(X, Y, x0, y0, 0, bytes, lds);
-    float c[T::FM][4], b[T::FM][4];
-#pragma unroll
-    for (int i = 0; i < T::FM; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t x = x0 + t.x_of(i) + e;
-            c[i][e] = x < X.rows ? bs[x] : 0.0f;
-            b[i][e] = bias && x < X.rows ? bias[x] : 0.0f;
-        }
+    t.start(X, Y, x0, y0, 0, bytes, lds);
+    const int i0 = threadIdx.x;
+    if (i0 < BN && y0 + i0 < Y.rows) s_as[i0] = as[y0 + i0];
+    if (i0 < BM && x0 + i0 < X.rows) {
+        s_bs[i0] = bs[x0 + i0];
+        if (BIAS) s_bias[i0] = bias[x0 + i0];
+    }
+    t.loop();
+    const int have = x0 + BM <= X.rows ? BM : (int)(X.rows - x0);
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
         const int64_t y = y0 + t.y_of(j);
         if (y >= Y.rows) continue;
-        const float s = as[y];
+        const float s = s_as[t.y_of(j)];
+        O* row = out + y * X.rows + x0;
 #pragma unroll
         for (int i = 0; i < T::FM; ++i) {
-            const int64_t x = x0 + t.x_of(i);
+            const int x = t.x_of(i);
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = (float)t.acc[i][j][e] * s * c[i][e] + b[i][e];
-            tile_put(out + y * X.rows + x, v, X.rows - x);
+            for (int e = 0; e < 4; ++e) v[e] = (float)t.acc[i][j][e] * s * s_bs[x + e] + (BIAS ? s_bias[x + e] : 0.0f);
+            if (x < have) tile_put(row + x, v, have - x);
         }
     }
 }
@@ -134,20 +136,22 @@ __global__ __launch_bounds__(256) void product_few_kernel(TileRows X, TileRows Y
 }
 
 // Short rows, of up to STEPS x 64 bytes: the output's bytes bound the product, and a tile would be loaded, multiplied once or twice and stored,
-// each after the other.  A wave keeps the rows of 16 FN tokens in registers, walks over the channels 16 CB at a time with the next ones' rows
-// on their way, and stores as it goes; nothing meets.  (203 tokens, 1 000 000 channels of 128, fp32: STORES.)
-template <class O, int STEPS, int FN, int CB>
+// each after the other.  A wave keeps the rows of 16 FN tokens in registers, walks over the channels 16 CB at a time with the next ones' rows and
+// scales on their way, and stores as it goes; nothing meets.  Which 16 channels a product takes is free: for outputs of 16 bits two products
+// share 32, in turn four by four, so that a lane has eight neighbours and stores 16 bytes of a row, as it does of four in 32 bits.
+template <class O, int STEPS, int FN, int CB, bool BIAS>
 __global__ __launch_bounds__(256) void product_short_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
                                                             const float* __restrict__ bs, const float* __restrict__ bias, O* __restrict__ out)
 {
-    const int wave = threadIdx.x >> 6, lane = tg_lane(), row = lane & 15, q = lane >> 4;
-    const tg_i32x4 none = {0, 0, 0, 0};
-    const int64_t chunks = (X.rows + 16 * CB - 1) / (16 * CB), step = (int64_t)gridDim.x * 4;
+    constexpr int W = 16 / (int)sizeof(O), PER = W / 4;        // neighbours of a row that a lane stores; products they come from
+    static_assert(CB % PER == 0, "whole stores");
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = tg_lane(), row = lane & 15, q = lane >> 4;
+    const int64_t chunks = (X.rows + 16 * CB - 1) / (16 * CB), step = (int64_t)gridDim.x * 4, y0 = (int64_t)blockIdx.y * (16 * FN);
     tg_i32x4 y[FN][STEPS];
     float sy[FN];
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
-        const int64_t r = (int64_t)blockIdx.y * (16 * FN) + j * 16 + row;
+        const int64_t r = y0 + j * 16 + row;
         const bool in = r < Y.rows;
         sy[j] = in ? as[r] : 0.0f;
 #pragma unroll
@@ -155,16 +159,29 @@ __global__ __launch_bounds__(256) void product_short_kernel(TileRows X, TileRows
             y[j][h] = product_load(Y.p + (in ? r : 0) * Y.pitch + h * 64 + q * 16, bytes - h * 64 - q * 16);
     }
     tg_i32x4 x[CB][STEPS], next[CB][STEPS];
-    // (rows that are not there are read as the chunk's first: nobody stores their sums)
+    float c[CB / PER][W], c_next[CB / PER][W];
+    // (channels that are not there are read as the chunk's first: nobody stores their sums)
     const auto load = [&](int64_t chunk) {
+        const int64_t first = chunk * (16 * CB);
 #pragma unroll
         for (int i = 0; i < CB; ++i) {
-            const int64_t r = chunk * (16 * CB) + i * 16 + row;
-            const char* p = X.p + (r < X.rows ? r : chunk * (16 * CB)) * X.pitch + q * 16;
+            const int64_t r = first + i / PER * (16 * PER) + (row >> 2) * W + i % PER * 4 + (row & 3);
+            const char* p = X.p + (r < X.rows ? r : first) * X.pitch + q * 16;
 #pragma unroll
             for (int h = 0; h < STEPS; ++h) {
                 if (h * 64 + 64 <= bytes) next[i][h] = product_load(p + h * 64, 16);
                 else next[i][h] = product_load(p + h * 64, bytes - h * 64 - q * 16);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < CB / PER; ++i) {
+            const int64_t v = first + i * (16 * PER) + q * W;
+#pragma unroll
+            for (int e = 0; e < W; e += 4) {
+                TgPiece<float> s;
+                s.load(bs + v + e, v + e + 4 <= X.rows ? 4 : (int)(X.rows - v - e));
+#pragma unroll
+                for (int f = 0; f < 4; ++f) c_next[i][e + f] = s.v[f];
             }
         }
     };
@@ -175,34 +192,38 @@ __global__ __launch_bounds__(256) void product_short_kernel(TileRows X, TileRows
         for (int i = 0; i < CB; ++i)
 #pragma unroll
             for (int h = 0; h < STEPS; ++h) x[i][h] = next[i][h];
+#pragma unroll
+        for (int i = 0; i < CB / PER; ++i)
+#pragma unroll
+            for (int e = 0; e < W; ++e) c[i][e] = c_next[i][e];
         if (chunk + step < chunks) load(chunk + step);
-        float c[CB][4], b[CB][4];
+        const bool whole = (chunk + 1) * (16 * CB) <= X.rows;
+        TgPiece<float> b[CB];
+        if (BIAS) {
 #pragma unroll
-        for (int i = 0; i < CB; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t v = chunk * (16 * CB) + i * 16 + q * 4 + e;
-                c[i][e] = v < X.rows ? bs[v] : 0.0f;
-                b[i][e] = bias && v < X.rows ? bias[v] : 0.0f;
+            for (int i = 0; i < CB; ++i) {
+                const int64_t v = chunk * (16 * CB) + i / PER * (16 * PER) + q * W + i % PER * 4;
+                b[i].load(bias + v, v + 4 <= X.rows ? 4 : (int)(X.rows - v));
             }
+        }
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const int64_t r = (int64_t)blockIdx.y * (16 * FN) + j * 16 + row;
+            const int64_t r = y0 + j * 16 + row;
             tg_i32x4 acc[CB];
 #pragma unroll
             for (int i = 0; i < CB; ++i) {
-                acc[i] = none;
+                acc[i] = tg_i32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int h = 0; h < STEPS; ++h) acc[i] = TileMul<int8_t>::mul(x[i][h], y[j][h], acc[i]);
             }
             if (r >= Y.rows) continue;
 #pragma unroll
-            for (int i = 0; i < CB; ++i) {
-                const int64_t v = chunk * (16 * CB) + i * 16 + q * 4;
-                float o[4];
+            for (int i = 0; i < CB / PER; ++i) {
+                const int64_t v = chunk * (16 * CB) + i * (16 * PER) + q * W;
+                TgPiece<O> o;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = (float)acc[i][e] * sy[j] * c[i][e] + b[i][e];
-                if (v < X.rows) tile_put(out + r * X.rows + v, o, X.rows - v);
+                for (int e = 0; e < W; ++e) o.v[e] = (float)acc[i * PER + e / 4][e % 4] * sy[j] * c[i][e] + (BIAS ? b[i * PER + e / 4].v[e % 4] : 0.0f);
+                o.store(out + r * X.rows + v, whole || v + W <= X.rows ? W : (int)(X.rows - v));
             }
         }
     }
@@ -265,36 +286,41 @@ static void launch_short(const TileRows& X, const TileRows& Y, int bytes, const 
         int64_t nx = (2048 + ny - 1) / ny;
         if (nx < 64) nx = 64;
         if (nx > (chunks + 3) / 4) nx = (chunks + 3) / 4;
-        hipLaunchKernelGGL((product_short_kernel<O, STEPS, FN, CB>), dim3((unsigned)nx, (unsigned)ny), dim3(256), 0, s, X, part, bytes, as + y0, bs, bias,
-                           out + y0 * X.rows);
+        const dim3 grid((unsigned)nx, (unsigned)ny);
+        if (bias) hipLaunchKernelGGL((product_short_kernel<O, STEPS, FN, CB, true>), grid, dim3(256), 0, s, X, part, bytes, as + y0, bs, bias, out + y0 * X.rows);
+        else hipLaunchKernelGGL((product_short_kernel<O, STEPS, FN, CB, false>), grid, dim3(256), 0, s, X, part, bytes, as + y0, bs, bias, out + y0 * X.rows);
     }
 }
-template <class O, int BM, int BN, int WM, int WN>
+template <class O, int BM, int BN, int WM, int WN, int NB = 2>
 static void launch_tiles(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
 {
     const uint32_t nx = (uint32_t)((X.rows + BM - 1) / BM), ny = (uint32_t)((Y.rows + BN - 1) / BN);
-    hipLaunchKernelGGL((product_kernel<O, BM, BN, WM, WN>), dim3(nx * ny), dim3(64 * WM * WN), 0, s, X, Y, bytes, as, bs, bias, nx, ny, 8u, out);
+    const dim3 wgs(nx * ny), threads(64 * WM * WN);
+    if (bias) hipLaunchKernelGGL((product_kernel<O, BM, BN, WM, WN, NB, true>), wgs, threads, 0, s, X, Y, bytes, as, bs, bias, nx, ny, 8u, out);
+    else hipLaunchKernelGGL((product_kernel<O, BM, BN, WM, WN, NB, false>), wgs, threads, 0, s, X, Y, bytes, as, bs, bias, nx, ny, 8u, out);
 }
 template <class O>
 static void launch_product(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
 {
-    if (bytes <= 128) {
-        if (Y.rows <= 16) launch_short<O, 2, 1, 4>(X, Y, bytes, as, bs, bias, out, s);
-        else if (Y.rows <= 32) launch_short<O, 2, 2, 4>(X, Y, bytes, as, bs, bias, out, s);
-        else if (Y.rows <= 64) launch_short<O, 2, 4, 4>(X, Y, bytes, as, bs, bias, out, s);
-        else launch_short<O, 2, 8, 4>(X, Y, bytes, as, bs, bias, out, s);
-        return;
-    }
     if (bytes <= PRODUCT_SHORT) {
-        if (Y.rows <= 16) launch_short<O, 4, 1, 2>(X, Y, bytes, as, bs, bias, out, s);
-        else if (Y.rows <= 32) launch_short<O, 4, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
-        else launch_short<O, 4, 4, 2>(X, Y, bytes, as, bs, bias, out, s);
+        // 32 channels at a time, for outputs of 32 bits 64 where the registers are enough (4530 tokens, 52 160 channels of 128: bf16 116 us with
+        // 32, 172 with 64; 200 tokens, 2^20 channels of 128, fp32: 295 with 32, 248 with 64)
+        const auto go = [&](auto steps, auto most) {
+            constexpr int S = decltype(steps)::value, FN = decltype(most)::value, CB = sizeof(O) == 4 && S < 4 ? 4 : 2;
+            if (Y.rows <= 16) launch_short<O, S, 1, CB>(X, Y, bytes, as, bs, bias, out, s);
+            else if (Y.rows <= 32) launch_short<O, S, 2, CB>(X, Y, bytes, as, bs, bias, out, s);
+            else if (Y.rows <= 64 || FN == 4) launch_short<O, S, 4, CB>(X, Y, bytes, as, bs, bias, out, s);
+            else launch_short<O, S, FN, CB>(X, Y, bytes, as, bs, bias, out, s);
+        };
+        if (bytes <= 64) go(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
+        else if (bytes <= 128) go(std::integral_constant<int, 2>(), std::integral_constant<int, 8>());
+        else go(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
         return;
     }
     const auto tiles = [&](int64_t bm, int64_t bn) { return ((X.rows + bm - 1) / bm) * ((Y.rows + bn - 1) / bn); };
     if (bytes > 512 && tiles(256, 256) >= 200) launch_tiles<O, 256, 256, 2, 4>(X, Y, bytes, as, bs, bias, out, s);
     else if (tiles(128, 128) >= 200) launch_tiles<O, 128, 128, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
-    else launch_tiles<O, 64, 64, 2, 2>(X, Y, bytes, as, bs, bias, out, s);
+    else launch_tiles<O, 64, 64, 2, 2, 4>(X, Y, bytes, as, bs, bias, out, s);
 }
 
 void tg_launch_product(const int8_t* a, const float* as, const int8_t* b, const float* bs, const float* bias, int64_t m, int64_t n, int k,

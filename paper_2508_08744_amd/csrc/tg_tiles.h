@@ -7,9 +7,10 @@
 //
 // Each side's stage is two units, its first and second half of the rows, and every wave has as many rows of one as of the other.  The
 // four products of halves are four phases; they go round the halves so that each phase needs one unit more than the phase before, which
-// is read from LDS into registers one phase ahead, and every phase frees one unit, which is filled for two stages on.  So a load has
-// seven phases (of 16 products of 16 x 16 each, at 256 x 256) to land, the matrix instructions find their operands in registers, and a phase
-// costs one barrier, at which all waves have the unit they read next and none still reads the one that is filled next.
+// is read from LDS into registers one phase ahead, and every phase frees one unit, which is filled for NB stages on.  So a load has
+// 4 NB - 1 phases (of 16 products of 16 x 16 each, at 256 x 256) to land, the matrix instructions find their operands in registers, and a phase
+// costs one barrier, at which all waves have the unit they read next and none still reads the one that is filled next.  NB is 2; where there
+// are too few tiles for all CUs, each alone on its own, a load's way is what a stage costs, and smaller tiles have room for 4.
 //
 // A unit holds 8 pieces of 16 bytes a row; piece c of row r lies at place c ^ (r & 7), so that the eight rows that a matrix instruction's lanes
 // read at a time lie in different banks.  The loads write LDS in lane order, so the exchange is made by the lanes' addresses in memory.
@@ -201,8 +202,8 @@ struct TileSide {
 #endif
 };
 
-// BM x BN in WM x WN waves
-template <class E, int BM, int BN, int WM, int WN, bool XT = false, bool YT = false>
+// BM x BN in WM x WN waves, NB stages in LDS
+template <class E, int BM, int BN, int WM, int WN, bool XT = false, bool YT = false, int NB = 2>
 struct Tile {
     static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;       // products of 16 x 16 of a wave
@@ -211,8 +212,8 @@ struct Tile {
     typedef TileSide<E, BM, WAVES, XT> SX;
     typedef TileSide<E, BN, WAVES, YT> SY;
     static constexpr int LX = SX::LOADS, LY = SY::LOADS;
-    static constexpr int LDS = 4 * (SX::BYTES + SY::BYTES);
-    static_assert(FM % 2 == 0 && FN % 2 == 0, "halves");
+    static constexpr int LDS = 2 * NB * (SX::BYTES + SY::BYTES);
+    static_assert(FM % 2 == 0 && FN % 2 == 0 && (NB == 2 || NB == 4), "halves");
 
     acc_t acc[FM][FN];
 
@@ -223,11 +224,13 @@ struct Tile {
         char* lds;
         SX sx;
         SY sy;
+    };
+    struct Halves {
         tg_i32x4 x[2][2][HM], y[2][2][HN];                           // [half of the rows][half of the stage]
     };
     // the memory of unit h of buffer b
     static __device__ inline char* unit_x(const Run& r, int b, int h) { return r.lds + (b * 2 + h) * SX::BYTES; }
-    static __device__ inline char* unit_y(const Run& r, int b, int h) { return r.lds + 4 * SX::BYTES + (b * 2 + h) * SY::BYTES; }
+    static __device__ inline char* unit_y(const Run& r, int b, int h) { return r.lds + 2 * NB * SX::BYTES + (b * 2 + h) * SY::BYTES; }
     static __device__ inline void fill_x(const Run& r, int b, int h, int k)
     {
         r.sx.fill(h, (uint32_t)(uintptr_t)(tg_lds_char*)unit_x(r, b, h), k, r.k1, r.wave);
@@ -237,8 +240,8 @@ struct Tile {
         r.sy.fill(h, (uint32_t)(uintptr_t)(tg_lds_char*)unit_y(r, b, h), k, r.k1, r.wave);
     }
     // one of the 2 HM (2 HN) reads of a unit
-    static __device__ inline void read_x(Run& r, int b, int h, int n) { r.x[h][n / HM][n % HM] = r.sx.read(unit_x(r, b, h), r.wm * (HM * 16), n % HM, n / HM, r.lane); }
-    static __device__ inline void read_y(Run& r, int b, int h, int n) { r.y[h][n / HN][n % HN] = r.sy.read(unit_y(r, b, h), r.wn * (HN * 16), n % HN, n / HN, r.lane); }
+    static __device__ inline void read_x(const Run& r, Halves& f, int b, int h, int n) { f.x[h][n / HM][n % HM] = r.sx.read(unit_x(r, b, h), r.wm * (HM * 16), n % HM, n / HM, r.lane); }
+    static __device__ inline void read_y(const Run& r, Halves& f, int b, int h, int n) { f.y[h][n / HN][n % HN] = r.sy.read(unit_y(r, b, h), r.wn * (HN * 16), n % HN, n / HN, r.lane); }
     // All but the last `LATER` loads of every wave have landed, and no wave has reads under way.
     template <int LATER>
     static __device__ inline void meet()
@@ -251,81 +254,106 @@ struct Tile {
     // The products of halves hx and hy, out of registers; between them the reads of a unit of X (XU) or Y for the next phase, and the loads
     // of one, so that the matrix instructions wait for neither's turn to be issued.
     template <bool XU, class Fill>
-    __device__ inline void phase(Run& r, int hx, int hy, int read_buffer, int read_half, Fill fill)
+    __device__ inline void phase(const Run& r, Halves& f, int hx, int hy, int read_buffer, int read_half, Fill fill)
     {
         constexpr int PRODUCTS = 2 * HM * HN, READS = XU ? 2 * HM : 2 * HN;
 #pragma unroll
         for (int m = 0; m < PRODUCTS; ++m) {
             const int s = m / (HM * HN), i = m / HN % HM, j = m % HN;
-            acc[hx * HM + i][hy * HN + j] = TileMul<E>::mul(r.x[hx][s][i], r.y[hy][s][j], acc[hx * HM + i][hy * HN + j]);
+            acc[hx * HM + i][hy * HN + j] = TileMul<E>::mul(f.x[hx][s][i], f.y[hy][s][j], acc[hx * HM + i][hy * HN + j]);
 #pragma unroll
             for (int n = 0; n < READS; ++n)
                 if (n * PRODUCTS / READS == m) {
-                    if (XU) read_x(r, read_buffer, read_half, n);
-                    else read_y(r, read_buffer, read_half, n);
+                    if (XU) read_x(r, f, read_buffer, read_half, n);
+                    else read_y(r, f, read_buffer, read_half, n);
                 }
             if (m == PRODUCTS / 2) fill();
             __builtin_amdgcn_sched_barrier(0);      // (the order as it is written)
         }
     }
-    // One stage, out of buffer P; Y's units in the order P, 1 - P.  Of the loads that a phase waits for, those of the six phases
-    // before it may be on their way.
-    template <int P>
-    __device__ inline void stage(Run& r)
+    // Stage of buffer B; Y's units in the order P, 1 - P.  Of the loads that a phase waits for, those of the 4 NB - 2 phases before it may be on
+    // their way: FAR of them, and the last six phases' by kind.
+    template <int B>
+    __device__ inline void stage(Run& r, Halves& f)
     {
-        meet<4 * LX + 2 * LY>();
-        phase<false>(r, 0, P, P, 1 - P, [&] { fill_y(r, P, P, r.k + 2 * TILE_BYTES); });
-        meet<3 * LX + 3 * LY>();
-        phase<true>(r, 0, 1 - P, P, 1, [&] { fill_y(r, P, 1 - P, r.k + 2 * TILE_BYTES); });
-        meet<2 * LX + 4 * LY>();
-        phase<true>(r, 1, 1 - P, 1 - P, 0, [&] { fill_x(r, P, 1, r.k + 2 * TILE_BYTES); });
-        meet<3 * LX + 3 * LY>();
-        phase<false>(r, 1, P, 1 - P, 1 - P, [&] { fill_x(r, 1 - P, 0, r.k + 3 * TILE_BYTES); });
+        constexpr int P = B & 1, NEXT = (B + 1) % NB, FAR = (NB - 2) * (2 * LX + 2 * LY);
+        meet<FAR + 4 * LX + 2 * LY>();
+        phase<false>(r, f, 0, P, B, 1 - P, [&] { fill_y(r, B, P, r.k + NB * TILE_BYTES); });
+        meet<FAR + 3 * LX + 3 * LY>();
+        phase<true>(r, f, 0, 1 - P, B, 1, [&] { fill_y(r, B, 1 - P, r.k + NB * TILE_BYTES); });
+        meet<FAR + 2 * LX + 4 * LY>();
+        phase<true>(r, f, 1, 1 - P, NEXT, 0, [&] { fill_x(r, B, 1, r.k + NB * TILE_BYTES); });
+        meet<FAR + 3 * LX + 3 * LY>();
+        phase<false>(r, f, 1, P, NEXT, 1 - P, [&] { fill_x(r, NEXT, 0, r.k + (NB + 1) * TILE_BYTES); });
         r.k += TILE_BYTES;
     }
+    Run r;
 #endif
 
-    // rows (columns, where turned) x0.. of X and y0.. of Y, contraction bytes [k0, k1) (k0 a multiple of TILE_BYTES, k1 of 16;
-    // below 2^31 - 2^10); lds: LDS bytes that begin at a multiple of 1024
-    __device__ inline void run(const TileRows& X, const TileRows& Y, int64_t x0, int64_t y0, int k0, int k1, char* lds)
+    // Asks for the first stages of rows (columns, where turned) x0.. of X and y0.. of Y, contraction bytes [k0, k1) (k0 a multiple of TILE_BYTES, k1 of
+    // 16; below 2^31 - 2^10).  lds: LDS bytes that begin at a multiple of 1024, and that no wave reads any more.  acc is left alone.
+    __device__ inline void start(const TileRows& X, const TileRows& Y, int64_t x0, int64_t y0, int k0, int k1, char* lds)
     {
 #ifdef __HIP_DEVICE_COMPILE__
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        Run r{k0, k1, wave, tg_lane(), wave / WN, wave % WN, lds};
+        r.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        r.lane = tg_lane();
+        r.wm = r.wave / WN;
+        r.wn = r.wave % WN;
+        r.lds = lds;
+        r.k = k0;
+        r.k1 = k1;
+        r.sx.begin(X, x0, r.wave, r.lane);
+        r.sy.begin(Y, y0, r.wave, r.lane);
+        r.sx.begin_reads(r.wm * (HM * 16), r.lane);
+        r.sy.begin_reads(r.wn * (HN * 16), r.lane);
+        // in the order of the phases that would have asked for them
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            fill_x(r, b, 0, k0 + b * TILE_BYTES);
+            fill_y(r, b, b & 1, k0 + b * TILE_BYTES);
+            fill_y(r, b, 1 - (b & 1), k0 + b * TILE_BYTES);
+            fill_x(r, b, 1, k0 + b * TILE_BYTES);
+        }
+#endif
+    }
+    // ... and the products (an empty stretch is one stage of zeros).  Behind it no wave reads the memory any more.
+    __device__ inline void loop()
+    {
+#ifdef __HIP_DEVICE_COMPILE__
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = acc_t{0, 0, 0, 0};
-        if (k0 >= k1) return;
-        r.sx.begin(X, x0, wave, r.lane);
-        r.sy.begin(Y, y0, wave, r.lane);
-        r.sx.begin_reads(r.wm * (HM * 16), r.lane);
-        r.sy.begin_reads(r.wn * (HN * 16), r.lane);
-        // two stages in the order of the phases that would have filled them, and the reads of the two phases in front of the first
-        fill_x(r, 0, 0, k0);
-        fill_y(r, 0, 0, k0);
-        fill_y(r, 0, 1, k0);
-        fill_x(r, 0, 1, k0);
-        fill_x(r, 1, 0, k0 + TILE_BYTES);
-        fill_y(r, 1, 1, k0 + TILE_BYTES);
-        fill_y(r, 1, 0, k0 + TILE_BYTES);
-        fill_x(r, 1, 1, k0 + TILE_BYTES);
-        meet<2 * LX + 4 * LY>();
+        constexpr int FAR = (NB - 2) * (2 * LX + 2 * LY);
+        Halves f;
+        // the reads of the two phases in front of the first
+        meet<FAR + 2 * LX + 4 * LY>();
 #pragma unroll
-        for (int n = 0; n < 2 * HM; ++n) read_x(r, 0, 0, n);
-        meet<3 * LX + 3 * LY>();
+        for (int n = 0; n < 2 * HM; ++n) read_x(r, f, 0, 0, n);
+        meet<FAR + 3 * LX + 3 * LY>();
 #pragma unroll
-        for (int n = 0; n < 2 * HN; ++n) read_y(r, 0, 0, n);
-        fill_x(r, 0, 0, k0 + 2 * TILE_BYTES);
+        for (int n = 0; n < 2 * HN; ++n) read_y(r, f, 0, 0, n);
+        fill_x(r, 0, 0, r.k + NB * TILE_BYTES);
         for (;;) {
-            stage<0>(r);
-            if (r.k >= k1) break;
-            stage<1>(r);
-            if (r.k >= k1) break;
+            stage<0>(r, f);
+            if (r.k >= r.k1) break;
+            stage<1>(r, f);
+            if (r.k >= r.k1) break;
+            if constexpr (NB == 4) {
+                stage<2>(r, f);
+                if (r.k >= r.k1) break;
+                stage<3>(r, f);
+                if (r.k >= r.k1) break;
+            }
         }
-        // (loads of zeros behind the end are still on their way into LDS)
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // (loads of zeros behind the end may still be on their way into LDS)
+        meet<0>();
 #endif
+    }
+    __device__ inline void run(const TileRows& X, const TileRows& Y, int64_t x0, int64_t y0, int k0, int k1, char* lds)
+    {
+        start(X, Y, x0, y0, k0, k1, lds);
+        loop();
     }
     // the rows of X and Y that acc[i][j][0] belongs to; acc[i][j][e] is for x + e
     __device__ inline int x_of(int i) const { return (i / HM) * (BM / 2) + ((threadIdx.x >> 6) / WN) * (HM * 16) + (i % HM) * 16 + (tg_lane() >> 4) * 4; }
@@ -334,7 +362,7 @@ struct Tile {
 
 // four neighbours of an output row
 template <class O>
-__device__ inline void tile_put(O* p, const float* v, int64_t left)
+__device__ inline void tile_put(O* p, const float* v, int left)
 {
     typedef O vec __attribute__((ext_vector_type(4), aligned(sizeof(O))));
     if (left >= 4) {
@@ -351,7 +379,6 @@ __device__ inline void tile_put(O* p, const float* v, int64_t left)
 
 // a launch has fewer than 2^32 work-items
 #define TILE_LAUNCH_ITEMS (1ll << 31)
-
 // Workgroups go to the eight dies in turn: tile number `b` of `count` such that every die gets a stretch of neighbours, whose rows its
 // own L2 then holds.
 __device__ inline uint32_t tile_of_block(uint32_t b, uint32_t count)

@@ -24,46 +24,68 @@ __device__ inline void xent_join(float& m, float& l, float m2, float l2)
 }
 
 // x: rows of the table, y: tokens.  parts: for every tile and wave along x (BM / WM rows of the table), (maximum, sum) of every token.
-template <class E, int BM, int BN, int WM, int WN>
+template <class E, int BM, int BN, int WM, int WN, int NB>
 __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
                                                                  float scale, uint32_t nx, uint32_t ny, uint32_t group, float2* __restrict__ parts,
                                                                  int64_t parts_pitch, float* __restrict__ at_target)
 {
-    typedef Tile<E, BM, BN, WM, WN> T;
+    typedef Tile<E, BM, BN, WM, WN, false, false, NB> T;
+    __shared__ __align__(1024) char lds[T::LDS];
+    // the tokens' targets among the tile's rows: asked for before the products, so that nothing waits for them behind
+    __shared__ int s_target[BN];
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
-    __shared__ __align__(1024) char lds[T::LDS];
     T t;
-    t.run(X, Y, x0, y0, 0, bytes, lds);
-    const bool whole = x0 + BM <= X.rows;
+    t.start(X, Y, x0, y0, 0, bytes, lds);
+    if (threadIdx.x < BN) {
+        const int64_t y = y0 + threadIdx.x, target = y < Y.rows ? tg_row_of(targets, targets64, y, X.rows) - x0 : -1;
+        s_target[threadIdx.x] = target >= 0 && target < BM ? (int)target : -1;
+    }
+    t.loop();
+    const uint32_t stretch = tx * WM + (threadIdx.x >> 6) / WN;
+    const int have = x0 + BM <= X.rows ? BM : (int)(X.rows - x0);
+    const float base = scale * XENT_LOG2E;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
         const int64_t y = y0 + t.y_of(j);
-        const int64_t target = y < Y.rows ? tg_row_of(targets, targets64, y, X.rows) : -1;
-        float m = -__builtin_inff();
+        const int target = s_target[t.y_of(j)];
+        float m = -__builtin_inff(), l = 0.0f;
 #pragma unroll
-        for (int i = 0; i < T::FM; ++i)
+        for (int i = 0; i < T::FM; ++i) {
+            const int x = t.x_of(i);
+            if ((unsigned)(target - x) < 4u) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t x = x0 + t.x_of(i) + e;
-                float z = t.acc[i][j][e] * scale;
-                if (x == target) at_target[y] = z;
-                if (!whole && x >= X.rows) z = -__builtin_inff();
-                t.acc[i][j][e] = z;
-                m = fmaxf(m, z);
+                for (int e = 0; e < 4; ++e)
+                    if (x + e == target) at_target[y] = t.acc[i][j][e] * scale;
             }
+            if (x + 4 <= have) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, t.acc[i][j][e] * scale);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (x + e < have) m = fmaxf(m, t.acc[i][j][e] * scale);
+            }
+        }
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
         const float b = (m == -__builtin_inff() ? 0.0f : m) * XENT_LOG2E;
-        float l = 0.0f;
 #pragma unroll
-        for (int i = 0; i < T::FM; ++i)
+        for (int i = 0; i < T::FM; ++i) {
+            const int x = t.x_of(i);
+            if (x + 4 <= have) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], XENT_LOG2E, -b));
+                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], base, -b));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (x + e < have) l += __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], base, -b));
+            }
+        }
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
-        if (tg_lane() < 16 && y < Y.rows) parts[((int64_t)tx * WM + (threadIdx.x >> 6) / WN) * parts_pitch + y] = make_float2(m, l);
+        if (tg_lane() < 16 && y < Y.rows) parts[(int64_t)stretch * parts_pitch + y] = make_float2(m, l);
     }
 }
 
@@ -152,41 +174,63 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(const E* __restrict__
     c[1] = ldexpf(1.0f, -up);
 }
 
-// P of a piece: x: rows v0.. of the table, y: tokens; p: n rows, `pitch` elements apart, zeros behind the piece's rows.  lost: for types
+// P of a piece: x: rows v0.. of the table, y: tokens; p: n rows, `pitch` elements apart, zeros behind the piece's rows up to `width`.  lost: for types
 // of 16 bits, what rounding took from P at the token's target, the entry that outweighs all others together.
-template <class E, int BM, int BN, int WM, int WN>
+template <class E, int BM, int BN, int WM, int WN, int NB>
 __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
                                                               const float* __restrict__ lse, const float* __restrict__ dloss,
                                                               const float* __restrict__ c, float scale, int64_t v0, int64_t n_rows, uint32_t nx,
-                                                              uint32_t ny, uint32_t group, E* __restrict__ p, int64_t pitch, float* __restrict__ lost)
+                                                              uint32_t ny, uint32_t group, E* __restrict__ p, int64_t pitch, int width, float* __restrict__ lost)
 {
-    typedef Tile<E, BM, BN, WM, WN> T;
+    typedef Tile<E, BM, BN, WM, WN, false, false, NB> T;
+    __shared__ __align__(1024) char lds[T::LDS];
+    // what a token's logits become P with: its target among the tile's rows, its factor and its lse.  A token without a target has no part in
+    // anything, whatever its logits are.
+    struct Token { int hit, there; float g, b; };
+    __shared__ Token s_token[BN];
+    const float up = c[0], base = scale * XENT_LOG2E;
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
-    __shared__ __align__(1024) char lds[T::LDS];
     T t;
-    t.run(X, Y, x0, y0, 0, bytes, lds);
-    const float up = c[0];
+    t.start(X, Y, x0, y0, 0, bytes, lds);
+    if (threadIdx.x < BN) {
+        const int64_t y = y0 + threadIdx.x, target = y < Y.rows ? tg_row_of(targets, targets64, y, n_rows) : -1, hit = target - v0 - x0;
+        Token k{target >= 0 && hit >= 0 && hit < BM ? (int)hit : -1, target >= 0, 0.0f, 0.0f};
+        if (target >= 0) {
+            k.g = dloss[y] * scale * up;
+            k.b = lse[y] * XENT_LOG2E;
+        }
+        s_token[threadIdx.x] = k;
+    }
+    t.loop();
+    const int have = x0 + BM <= X.rows ? BM : (int)(X.rows - x0), room = x0 + BM <= width ? BM : (int)(width - x0);
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
         const int64_t y = y0 + t.y_of(j);
         if (y >= Y.rows) continue;
-        const int64_t target = tg_row_of(targets, targets64, y, n_rows);
-        const float g = target >= 0 ? dloss[y] * scale * up : 0.0f, b = lse[y] * XENT_LOG2E;
-        const int64_t hit = target >= 0 ? target - v0 : -1;
+        const Token k = s_token[t.y_of(j)];
+        E* row = p + y * pitch + x0;
 #pragma unroll
         for (int i = 0; i < T::FM; ++i) {
-            const int64_t x = x0 + t.x_of(i);
+            const int x = t.x_of(i);
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float s = __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e] * scale, XENT_LOG2E, -b)) - (x + e == hit ? 1.0f : 0.0f);
-                // (a token without a target has no part in anything, whatever its logits are)
-                v[e] = target >= 0 && x + e < X.rows ? s * g : 0.0f;
-                if (sizeof(E) == 2 && x + e == hit) lost[y] = v[e] - (float)(E)v[e];
+            for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], base, -k.b)) * k.g;
+            if ((unsigned)(k.hit - x) < 4u) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (x + e == k.hit) {
+                        v[e] = (__builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], base, -k.b)) - 1.0f) * k.g;
+                        if (sizeof(E) == 2) lost[y] = v[e] - (float)(E)v[e];
+                    }
             }
-            if (x < pitch) tile_put(p + y * pitch + x, v, pitch - x);
+            if (!k.there || x + 4 > have) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (!k.there || x + e >= have) v[e] = 0.0f;
+            }
+            if (x < room) tile_put(row + x, v, room - x);
         }
     }
 }
@@ -355,7 +399,7 @@ size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready)
     return c.used;
 }
 
-template <class E, int BM, int BN, int WM, int WN>
+template <class E, int BM, int BN, int WM, int WN, int NB = 2>
 static int64_t launch_parts(const TileRows& X, const TileRows& Y, int bytes, const void* targets, int targets64, float scale, float2* parts,
                             float* at_target, hipStream_t s)
 {
@@ -366,7 +410,7 @@ static int64_t launch_parts(const TileRows& X, const TileRows& Y, int bytes, con
         const int64_t rows = Y.rows - y0 < most ? Y.rows - y0 : most;
         const uint32_t ny = (uint32_t)((rows + BN - 1) / BN);
         const TileRows part{Y.p + y0 * Y.pitch, rows, Y.pitch, Y.width};
-        hipLaunchKernelGGL((xent_part_kernel<E, BM, BN, WM, WN>), dim3((unsigned)(nx * ny)), dim3(64 * WM * WN), 0, s, X, part, bytes,
+        hipLaunchKernelGGL((xent_part_kernel<E, BM, BN, WM, WN, NB>), dim3((unsigned)(nx * ny)), dim3(64 * WM * WN), 0, s, X, part, bytes,
                            (const char*)targets + y0 * (targets64 ? 8 : 4), targets64, scale, (uint32_t)nx, ny, 8u, parts + y0, Y.rows, at_target + y0);
     }
     return nx * WM;
@@ -390,9 +434,14 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
     TG_WITH_TYPE(dtype, E, {
         if (n <= 32) count = launch_parts<E, 128, 32, 4, 1>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
         else if (n <= 64) count = launch_parts<E, 128, 64, 4, 1>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
-        else if (sizeof(E) == 4 || ((n_rows + 255) / 256) * ((n + 255) / 256) < 200)
-            count = launch_parts<E, 128, 128, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
-        else count = launch_parts<E, 256, 256, 2, 4>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+        else {
+            bool wide = false;
+            if constexpr (sizeof(E) == 2) {
+                wide = ((n_rows + 255) / 256) * ((n + 255) / 256) >= 200;
+                if (wide) count = launch_parts<E, 256, 256, 2, 4>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+            }
+            if (!wide) count = launch_parts<E, 128, 128, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+        }
     });
     // few tokens: more lanes each, and more workgroups
     const int tok = n <= 1024 ? 4 : 16;
@@ -403,8 +452,9 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
 }
 
 #define XENT_PIECE_BYTES (256ll << 20)     // of P, where the workspace has them
+#define XENT_PAD 256
 #define XENT_LEAST_ROWS 256                // of a piece
-#define XENT_MOST_ROWS (1ll << 28)         // (bytes of a contraction stay within 32 bits)
+#define XENT_MOST_ROWS (1ll << 20)         // (256 rows of P stay within a buffer of 32 bits)
 
 struct XentGrad {
     int64_t piece;        // rows of the table at a time, a multiple of 256 unless it is all of them
@@ -413,6 +463,9 @@ struct XentGrad {
     bool direct;          // one piece, one part: dh is written at once
 };
 static int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+// bytes between the rows of P.  Its tiles are stored sixteen rows at a time: at a distance of a power of two those would meet in one channel of
+// the caches.
+static uint32_t xent_pitch(int64_t rows, int e) { return (uint32_t)round_up(rows * e, 16) + XENT_PAD; }
 static void xent_splits(XentGrad* g, int64_t n, int64_t n_rows, int d, int e)
 {
     // both products take tiles of 256 x 256, of which a CU holds one, where those are enough; else of 128 x 128, of which it holds two
@@ -433,7 +486,7 @@ static size_t carve_xent_grad(XentRows* r, TgCarve* c, const void* h, int64_t ld
     *consts = c->take<float>(2);
     *lost = c->take<float>(e == 2 ? n : 0);
     *sums = c->take<float>(g.direct ? 0 : (size_t)g.splits * n * d);
-    *p = c->take<char>((size_t)n * round_up(g.piece * e, 16));
+    *p = c->take<char>((size_t)n * xent_pitch(g.piece, e));
     return c->used;
 }
 static XentGrad xent_grad_shape(int64_t n, int64_t n_rows, int d, int e, int64_t p_bytes)
@@ -499,21 +552,28 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
     a.dh_y = over(n, side);
     for (int64_t v0 = 0; v0 < n_rows; v0 += g.piece) {
         const int64_t rows = n_rows - v0 < g.piece ? n_rows - v0 : g.piece;
-        const uint32_t pitch = (uint32_t)round_up(rows * e, 16);
+        const uint32_t pitch = xent_pitch(rows, e);
         a.w = TileRows{r.w.p + v0 * r.w.pitch, rows, r.w.pitch, r.w.width};
-        a.p = TileRows{p, n, pitch, pitch};
+        const uint32_t width = (uint32_t)round_up(rows * e, 16);
+        a.p = TileRows{p, n, pitch, width};
         const auto logits = [&](auto kernel, int bm, int bn, int threads) {
             const uint32_t nx = over(rows, bm), ny = over(n, bn);
             hipLaunchKernelGGL(kernel, dim3(nx * ny), dim3(threads), 0, s, a.w, r.h, (int)a.w.width, targets, targets64, lse, dloss, (const float*)consts,
-                               scale, v0, n_rows, nx, ny, 8u, (E*)p, (int64_t)(pitch / e), lost);
+                               scale, v0, n_rows, nx, ny, 8u, (E*)p, (int64_t)(pitch / e), (int)(width / e), lost);
         };
-        if (n <= 64) logits(xent_p_kernel<E, 128, 64, 4, 1>, 128, 64, 256);
-        else if (e == 4 || (int64_t)over(rows, 256) * over(n, 256) < 200) logits(xent_p_kernel<E, 128, 128, 2, 2>, 128, 128, 256);
-        else logits(xent_p_kernel<E, 256, 256, 2, 4>, 256, 256, 512);
-        const int stages = (int)((pitch + TILE_BYTES - 1) / TILE_BYTES);
+        if (n <= 64) logits(xent_p_kernel<E, 128, 64, 4, 1, 2>, 128, 64, 256);
+        else {
+            bool wide = false;
+            if constexpr (sizeof(E) == 2) {
+                wide = (int64_t)over(rows, 256) * over(n, 256) >= 200;
+                if (wide) logits(xent_p_kernel<E, 256, 256, 2, 4, 2>, 256, 256, 512);
+            }
+            if (!wide) logits(xent_p_kernel<E, 128, 128, 2, 2, 2>, 128, 128, 256);
+        }
+        const int stages = (int)((width + TILE_BYTES - 1) / TILE_BYTES);
         a.v0 = v0;
         a.rows = rows;
-        a.p_bytes = (int)pitch;
+        a.p_bytes = (int)width;
         a.each = (stages + g.splits - 1) / g.splits * TILE_BYTES;
         a.first = v0 == 0 ? 1 : 0;
         a.dw = dw + v0 * d;
