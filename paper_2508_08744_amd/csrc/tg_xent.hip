@@ -272,11 +272,11 @@ __device__ inline void xent_put_dh(const XentProducts& a, int64_t y, int x, floa
 // tokens up to which dw too gets back what rounding took from P at the targets: of more the errors are many and average out
 #define XENT_LOST_TOKENS 32
 
-template <class E, int B, int WM, int WN>
+template <class E, int B, int WM, int WN, int NB>
 __global__ __launch_bounds__(64 * WM * WN) void xent_products_kernel(XentProducts a)
 {
-    typedef Tile<E, B, B, WM, WN, true, false> TH;
-    typedef Tile<E, B, B, WM, WN, true, true> TW;
+    typedef Tile<E, B, B, WM, WN, true, false, NB> TH;
+    typedef Tile<E, B, B, WM, WN, true, true, NB> TW;
     static_assert(TH::LDS == TW::LDS, "one memory for both");
     __shared__ __align__(1024) char lds[TH::LDS];
     const uint32_t dh_all = a.dh_x * a.dh_y * a.splits;
@@ -399,6 +399,9 @@ size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready)
     return c.used;
 }
 
+// Logits of so few tiles that each has a CU of its own: what counts is then how long a stage is on its way, and tiles of 64 x 64 (or of 32 tokens)
+// have four of them in flight.
+static bool xent_small(int64_t rows, int64_t n) { return ((rows + 127) / 128) * ((n + 127) / 128) <= 128; }
 template <class E, int BM, int BN, int WM, int WN, int NB = 2>
 static int64_t launch_parts(const TileRows& X, const TileRows& Y, int bytes, const void* targets, int targets64, float scale, float2* parts,
                             float* at_target, hipStream_t s)
@@ -432,7 +435,10 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
     float* at = c.take<float>(n);
     int64_t count = 0;
     TG_WITH_TYPE(dtype, E, {
-        if (n <= 32) count = launch_parts<E, 128, 32, 4, 1>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+        const bool small = xent_small(n_rows, n);
+        if (n <= 32 && small) count = launch_parts<E, 128, 32, 4, 1, 4>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+        else if (n <= 32) count = launch_parts<E, 128, 32, 4, 1>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+        else if (small) count = launch_parts<E, 64, 64, 2, 2, 4>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
         else if (n <= 64) count = launch_parts<E, 128, 64, 4, 1>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
         else {
             bool wide = false;
@@ -459,6 +465,7 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
 struct XentGrad {
     int64_t piece;        // rows of the table at a time, a multiple of 256 unless it is all of them
     bool wide;            // products in tiles of 256 x 256
+    bool small;           // so few tiles that each has a CU of its own: four stages in flight
     int splits;           // of dh's contraction
     bool direct;          // one piece, one part: dh is written at once
 };
@@ -471,11 +478,13 @@ static void xent_splits(XentGrad* g, int64_t n, int64_t n_rows, int d, int e)
     // both products take tiles of 256 x 256, of which a CU holds one, where those are enough; else of 128 x 128, of which it holds two
     const auto tiles = [](int64_t x, int64_t y, int64_t side) { return ((x + side - 1) / side) * ((y + side - 1) / side); };
     g->wide = e == 2 && n > 128 && d > 128 && tiles(g->piece, d, 256) >= 200;
-    const int64_t side = g->wide ? 256 : 128, fill = g->wide ? 256 : 512;
-    // dh in as many parts as fill the card, each with sixteen stages of the contraction or more
+    const int64_t side = g->wide ? 256 : 128;
+    g->small = !g->wide && tiles(n, d, 128) + tiles(g->piece, d, 128) <= 128;
+    // dh in as many parts as fill the card, each with sixteen stages of the contraction or more (four where a stage is a load's way)
+    const int64_t fill = g->wide || g->small ? 256 : 512, least = g->small ? 4 : 16;
     const int64_t dh = tiles(n, d, side), stages = (g->piece * e + TILE_BYTES - 1) / TILE_BYTES;
     int64_t s = (fill + dh - 1) / dh;
-    if (s > stages / 16) s = stages / 16;
+    if (s > stages / least) s = stages / least;
     g->splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
     g->direct = g->splits == 1 && g->piece >= n_rows;
 }
@@ -561,7 +570,8 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
             hipLaunchKernelGGL(kernel, dim3(nx * ny), dim3(threads), 0, s, a.w, r.h, (int)a.w.width, targets, targets64, lse, dloss, (const float*)consts,
                                scale, v0, n_rows, nx, ny, 8u, (E*)p, (int64_t)(pitch / e), (int)(width / e), lost);
         };
-        if (n <= 64) logits(xent_p_kernel<E, 128, 64, 4, 1, 2>, 128, 64, 256);
+        if (xent_small(rows, n)) logits(xent_p_kernel<E, 64, 64, 2, 2, 4>, 64, 64, 256);
+        else if (n <= 64) logits(xent_p_kernel<E, 128, 64, 4, 1, 2>, 128, 64, 256);
         else {
             bool wide = false;
             if constexpr (sizeof(E) == 2) {
@@ -580,9 +590,13 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
         a.dw_y = over(rows, side);
         const dim3 grid(a.dh_x * a.dh_y * g.splits + a.dw_x * a.dw_y);
         if constexpr (sizeof(E) == 2) {
-            if (g.wide) hipLaunchKernelGGL((xent_products_kernel<E, 256, 2, 4>), grid, dim3(512), 0, s, a);
-            else hipLaunchKernelGGL((xent_products_kernel<E, 128, 2, 2>), grid, dim3(256), 0, s, a);
-        } else hipLaunchKernelGGL((xent_products_kernel<E, 128, 2, 2>), grid, dim3(256), 0, s, a);
+            if (g.wide) {
+                hipLaunchKernelGGL((xent_products_kernel<E, 256, 2, 4, 2>), grid, dim3(512), 0, s, a);
+                continue;
+            }
+        }
+        if (g.small) hipLaunchKernelGGL((xent_products_kernel<E, 128, 2, 2, 4>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((xent_products_kernel<E, 128, 2, 2, 2>), grid, dim3(256), 0, s, a);
     }
     if (g.direct) return;
     const int64_t out_wgs = (n * ((d + 3) / 4) + 255) / 256;
