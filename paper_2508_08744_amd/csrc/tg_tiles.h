@@ -95,13 +95,14 @@ struct TileSide {
     static constexpr int LOADS = (UNIT * TILE_BYTES / 1024 + WAVES - 1) / WAVES;   // of a wave and unit, 1024 bytes each
     static constexpr int BYTES = LOADS * WAVES * 1024;                 // of a unit, behind its end what surplus loads write
     static_assert(ROW <= 1024, "a load has whole rows");
-    static_assert(!TURNED || (sizeof(E) > 1 && ROW >= 128 && LOADS * WAVES * 1024 == UNIT * TILE_BYTES), "turned bytes, short or odd rows are not read");
+    static_assert(!TURNED || (sizeof(E) > 1 && ROW >= 64 && LOADS * WAVES * 1024 == UNIT * TILE_BYTES), "turned bytes, short or odd rows are not read");
 
     // which piece of row r lies at place 0: place c holds piece c ^ that
     static __device__ inline int exchange(int r)
     {
         if (!TURNED) return r & 7;
-        if (sizeof(E) == 4) return ((r >> 2) & 3) << 2;
+        if (sizeof(E) == 4) return ((r >> 2) & (PIECES >= 16 ? 3 : 1)) << 2;
+        if (PIECES == 4) return (r & 1) << 1;
         return ((r & 3) | (PIECES >= 16 ? ((r >> 3) & 1) << 2 : 0)) << 1;
     }
 

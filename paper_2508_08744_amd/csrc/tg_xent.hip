@@ -313,10 +313,14 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_products_kernel(XentProduct
     t.run(a.h, a.p, x0, y0, 0, a.h_bytes, lds);
     if (sizeof(E) == 2 && a.p.rows <= XENT_LOST_TOKENS) {
         const int64_t v0 = a.v0 + y0;
-        for (int64_t r = 0; r < a.p.rows; ++r) {
-            const int64_t at = tg_row_of(a.targets, a.targets64, r, a.n_rows) - v0;
-            if (at < 0 || at >= B) continue;
-            const float l = a.lost[r];
+        // (a lane a token: they are asked for at once)
+        const int lane = tg_lane();
+        const int64_t target = lane < a.p.rows ? tg_row_of(a.targets, a.targets64, lane, a.n_rows) - v0 : -1;
+        const int mine = target >= 0 && target < B ? (int)target : -1;
+        const float rounded = mine >= 0 ? a.lost[lane] : 0.0f;
+        for (uint64_t left = __ballot(mine >= 0); left; left &= left - 1) {
+            const int r = __builtin_ctzll(left), at = __builtin_amdgcn_readlane(mine, r);
+            const float l = __shfl(rounded, r);
 #pragma unroll
             for (int j = 0; j < TW::FN; ++j)
                 if (t.y_of(j) == at) {
@@ -464,8 +468,7 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
 
 struct XentGrad {
     int64_t piece;        // rows of the table at a time, a multiple of 256 unless it is all of them
-    bool wide;            // products in tiles of 256 x 256
-    bool small;           // so few tiles that each has a CU of its own: four stages in flight
+    int side;             // products in tiles of 256 x 256, 128 x 128 or 64 x 64
     int splits;           // of dh's contraction
     bool direct;          // one piece, one part: dh is written at once
 };
@@ -475,14 +478,13 @@ static int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 static uint32_t xent_pitch(int64_t rows, int e) { return (uint32_t)round_up(rows * e, 16) + XENT_PAD; }
 static void xent_splits(XentGrad* g, int64_t n, int64_t n_rows, int d, int e)
 {
-    // both products take tiles of 256 x 256, of which a CU holds one, where those are enough; else of 128 x 128, of which it holds two
+    // both products take tiles of 256 x 256, of which a CU holds one, where those are enough; else of 128 x 128, of which it holds two; and of
+    // 64 x 64, with four stages in flight, where each of 128 x 128 would have a CU of its own
     const auto tiles = [](int64_t x, int64_t y, int64_t side) { return ((x + side - 1) / side) * ((y + side - 1) / side); };
-    g->wide = e == 2 && n > 128 && d > 128 && tiles(g->piece, d, 256) >= 200;
-    const int64_t side = g->wide ? 256 : 128;
-    g->small = !g->wide && tiles(n, d, 128) + tiles(g->piece, d, 128) <= 128;
+    g->side = e == 2 && n > 128 && d > 128 && tiles(g->piece, d, 256) >= 200 ? 256 : tiles(n, d, 128) + tiles(g->piece, d, 128) <= 128 ? 64 : 128;
     // dh in as many parts as fill the card, each with sixteen stages of the contraction or more (four where a stage is a load's way)
-    const int64_t fill = g->wide || g->small ? 256 : 512, least = g->small ? 4 : 16;
-    const int64_t dh = tiles(n, d, side), stages = (g->piece * e + TILE_BYTES - 1) / TILE_BYTES;
+    const int64_t fill = g->side == 256 ? 256 : 512, least = g->side == 64 ? 4 : 16;
+    const int64_t dh = tiles(n, d, g->side), stages = (g->piece * e + TILE_BYTES - 1) / TILE_BYTES;
     int64_t s = (fill + dh - 1) / dh;
     if (s > stages / least) s = stages / least;
     g->splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
@@ -555,7 +557,7 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
     a.lost = lost;
     a.sums = sums;
     a.dh = dh;
-    const int side = g.wide ? 256 : 128;
+    const int side = g.side;
     const auto over = [](int64_t x, int64_t by) { return (uint32_t)((x + by - 1) / by); };
     a.dh_x = a.dw_x = over(d, side);
     a.dh_y = over(n, side);
@@ -589,14 +591,12 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
         a.dw = dw + v0 * d;
         a.dw_y = over(rows, side);
         const dim3 grid(a.dh_x * a.dh_y * g.splits + a.dw_x * a.dw_y);
+        const auto products = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a); };
         if constexpr (sizeof(E) == 2) {
-            if (g.wide) {
-                hipLaunchKernelGGL((xent_products_kernel<E, 256, 2, 4, 2>), grid, dim3(512), 0, s, a);
-                continue;
-            }
+            if (g.side == 256) products(xent_products_kernel<E, 256, 2, 4, 2>, 512);
         }
-        if (g.small) hipLaunchKernelGGL((xent_products_kernel<E, 128, 2, 2, 4>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((xent_products_kernel<E, 128, 2, 2, 2>), grid, dim3(256), 0, s, a);
+        if (g.side == 128) products(xent_products_kernel<E, 128, 2, 2, 2>, 256);
+        if (g.side == 64) products(xent_products_kernel<E, 64, 2, 2, 4>, 256);
     }
     if (g.direct) return;
     const int64_t out_wgs = (n * ((d + 3) / 4) + 255) / 256;
