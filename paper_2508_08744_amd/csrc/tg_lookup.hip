@@ -73,7 +73,7 @@ static ZeroPart zero_of(void* p, size_t bytes)
     if (z.head > z.halves) z.head = z.halves;
     return z;
 }
-// workgroups of 256 that clear a part: 16 KB each, up to 2048
+// workgroups that clear a part: 16 KB each, up to 2048
 static unsigned zero_wgs(const ZeroPart& z)
 {
     if (z.halves == 0) return 0;
@@ -94,7 +94,8 @@ __device__ inline u32 token_key(const void* ids, int ids64, int64_t t, int64_t n
 }
 
 // Few tokens: the place of a token is the number of those in front of it, counted.  16 lanes count for one token, over all keys in LDS.
-// One launch instead of the six of the digits' sort: at 4096 tokens 21 against 27 us of the whole gradient, at 8192 31 against 29.
+// One launch instead of the four of the digits' sort: at 4000 tokens and rows of 50 fp32 20 against 26 us of the whole gradient, at 6000 25 against 27,
+// at 8000 30 against 26.
 #define RANK_MAX 6144
 __global__ __launch_bounds__(256) void rank_sort_kernel(const void* __restrict__ ids, int ids64, int n, int64_t n_rows, u32* __restrict__ skey,
                                                         u32* __restrict__ spos, u32* __restrict__ runs, ZeroPart z)
@@ -134,13 +135,17 @@ __global__ __launch_bounds__(256) void rank_sort_kernel(const void* __restrict__
     }
 }
 
-// Many tokens: by digits of up to 11 bits, the lowest first, every pass keeping the order of equal digits.  A workgroup takes a
-// chunk of the tokens, each of its four waves a quarter of it in one piece.
-#define DIGIT_MAX 11
+// Many tokens: by digits of up to 10 bits, the lowest first, every pass keeping the order of equal digits.  A workgroup takes a
+// chunk of the tokens, each of its sixteen waves a sixteenth of it in one piece.  Up to SORT_FUSED chunks a workgroup adds up the counts of those
+// before it by itself; of more that would be as much work as the sort, and a launch in between does it once for all.
+#define DIGIT_MAX 10
+#define SORT_WAVES 16
+#define SORT_FUSED 64
 #define SORT_WGS 256
 struct SortShape {
     int passes, bits;        // digits, and bits of one
-    int64_t wgs, chunk;      // workgroups, and tokens of one (a multiple of 256)
+    int64_t wgs, chunk;      // workgroups, and tokens of one (a multiple of 1024)
+    bool fused;
 };
 static SortShape sort_shape(int64_t n, int64_t n_rows)
 {
@@ -149,10 +154,10 @@ static SortShape sort_shape(int64_t n, int64_t n_rows)
     while (b < 31 && (n_rows >> b) != 0) ++b;               // bits of the largest key, n_rows
     f.passes = (b + DIGIT_MAX - 1) / DIGIT_MAX;
     f.bits = (b + f.passes - 1) / f.passes;
-    int64_t chunk = (n + SORT_WGS - 1) / SORT_WGS;
-    chunk = (chunk + 255) & ~(int64_t)255;
-    f.chunk = chunk;
-    f.wgs = (n + chunk - 1) / chunk;
+    f.fused = n <= (int64_t)SORT_FUSED * 4096;
+    const int64_t wgs = f.fused ? SORT_FUSED : SORT_WGS;
+    f.chunk = ((n + wgs - 1) / wgs + 1023) & ~(int64_t)1023;
+    f.wgs = (n + f.chunk - 1) / f.chunk;
     return f;
 }
 // how many of the wave's tokens have which digit: s_count[wave][digit]
@@ -165,88 +170,101 @@ __device__ inline void count_digits(const void* ids, int ids64, const u32* key_i
         atomicAdd(count + digit_of(key, shift, bits), 1u);
     }
 }
-// per workgroup and digit: how many.  table: digit-major, wgs a digit
-__global__ __launch_bounds__(256) void digit_count_kernel(const void* __restrict__ ids, int ids64, const u32* __restrict__ key_in, int64_t n,
-                                                          int64_t n_rows, int64_t chunk, int shift, int bits, u32* __restrict__ table,
-                                                          u32* __restrict__ runs, ZeroPart z)
+// per workgroup and digit: how many.  table: the counts of a workgroup back to back
+__global__ __launch_bounds__(64 * SORT_WAVES) void digit_count_kernel(const void* __restrict__ ids, int ids64, const u32* __restrict__ key_in, int64_t n,
+                                                                      int64_t n_rows, int64_t chunk, int shift, int bits, u32* __restrict__ table,
+                                                                      u32* __restrict__ runs, ZeroPart z)
 {
     if (blockIdx.x >= z.first) { zero_part(z); return; }
     if (blockIdx.x == 0 && threadIdx.x < 2) runs[threadIdx.x] = 0;
     __shared__ u32 s_count[1 << DIGIT_MAX];
-    for (int i = threadIdx.x; i < 1 << bits; i += 256) s_count[i] = 0;
+    const int digits = 1 << bits;
+    for (int i = threadIdx.x; i < digits; i += 64 * SORT_WAVES) s_count[i] = 0;
     __syncthreads();
-    const int64_t from = (int64_t)blockIdx.x * chunk + (threadIdx.x >> 6) * (chunk / 4);
-    int64_t to = from + chunk / 4;
+    const int64_t from = (int64_t)blockIdx.x * chunk + (threadIdx.x >> 6) * (chunk / SORT_WAVES);
+    int64_t to = from + chunk / SORT_WAVES;
     if (to > n) to = n;
     count_digits(ids, ids64, key_in, n, n_rows, from, to, shift, bits, s_count);
     __syncthreads();
-    for (int i = threadIdx.x; i < 1 << bits; i += 256) table[(int64_t)i * z.first + blockIdx.x] = s_count[i];
+    for (int i = threadIdx.x; i < digits; i += 64 * SORT_WAVES) table[(int64_t)blockIdx.x * digits + i] = s_count[i];
 }
-// a wave a digit: its counts become the number of tokens in workgroups before, their sum goes to total[digit]
+// a thread a digit: its counts become the number of tokens in workgroups before, their sum goes to total[digit]
 __global__ __launch_bounds__(256) void digit_scan_kernel(u32* __restrict__ table, int wgs, int digits, u32* __restrict__ total, ZeroPart z)
 {
     if (blockIdx.x >= z.first) { zero_part(z); return; }
-    const int digit = blockIdx.x * 4 + (threadIdx.x >> 6), lane = tg_lane();
+    const int digit = blockIdx.x * 256 + threadIdx.x;
     if (digit >= digits) return;
-    u32 base = 0;
-    for (int i0 = 0; i0 < wgs; i0 += 64) {
-        const int i = i0 + lane;
-        const u32 c = i < wgs ? table[(int64_t)digit * wgs + i] : 0u;
-        u32 x = c;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const u32 y = (u32)__shfl_up((int)x, m);
-            if (lane >= m) x += y;
-        }
-        if (i < wgs) table[(int64_t)digit * wgs + i] = base + x - c;
-        base += (u32)__shfl((int)x, 63);
+    u32 sum = 0;
+#pragma unroll 16
+    for (int w = 0; w < wgs; ++w) {
+        const u32 c = table[(int64_t)w * digits + digit];
+        table[(int64_t)w * digits + digit] = sum;
+        sum += c;
     }
-    if (lane == 0) total[digit] = base;
+    total[digit] = sum;
 }
 // every token to its place: the smaller digits' tokens, those of its digit in workgroups before, in waves before, and in its wave before
-__global__ __launch_bounds__(256) void digit_place_kernel(const void* __restrict__ ids, int ids64, const u32* __restrict__ key_in,
-                                                          const u32* __restrict__ pos_in, int64_t n, int64_t n_rows, int64_t chunk, int shift,
-                                                          int bits, const u32* __restrict__ table, const u32* __restrict__ total,
-                                                          u32* __restrict__ key_out, u32* __restrict__ pos_out, ZeroPart z)
+template <bool FUSED>
+__global__ __launch_bounds__(64 * SORT_WAVES) void digit_place_kernel(const void* __restrict__ ids, int ids64, const u32* __restrict__ key_in,
+                                                                      const u32* __restrict__ pos_in, int64_t n, int64_t n_rows, int64_t chunk,
+                                                                      int shift, int bits, const u32* __restrict__ table,
+                                                                      const u32* __restrict__ total, u32* __restrict__ key_out,
+                                                                      u32* __restrict__ pos_out, ZeroPart z)
 {
     if (blockIdx.x >= z.first) { zero_part(z); return; }
-    __shared__ u32 s_next[4][1 << DIGIT_MAX];
-    __shared__ u32 s_wave[4];
-    const int wave = threadIdx.x >> 6, lane = tg_lane(), digits = 1 << bits;
-    for (int i = threadIdx.x; i < digits; i += 256) s_next[0][i] = s_next[1][i] = s_next[2][i] = s_next[3][i] = 0;
+    static_assert(1 << DIGIT_MAX <= 64 * SORT_WAVES, "a thread a digit");
+    __shared__ u32 s_next[SORT_WAVES][1 << DIGIT_MAX];
+    __shared__ u32 s_wave[SORT_WAVES];
+    const int wave = threadIdx.x >> 6, lane = tg_lane(), digits = 1 << bits, i = threadIdx.x;
+    if (i < digits) {
+#pragma unroll
+        for (int w = 0; w < SORT_WAVES; ++w) s_next[w][i] = 0;
+    }
     __syncthreads();
-    const int64_t from = (int64_t)blockIdx.x * chunk + wave * (chunk / 4);
-    int64_t to = from + chunk / 4;
+    const int64_t from = (int64_t)blockIdx.x * chunk + wave * (chunk / SORT_WAVES);
+    int64_t to = from + chunk / SORT_WAVES;
     if (to > n) to = n;
     count_digits(ids, ids64, key_in, n, n_rows, from, to, shift, bits, s_next[wave]);
-    __syncthreads();
-    // sum of the totals before a digit: 256 threads a stretch, in order
-    u32 base = 0;
-    for (int i0 = 0; i0 < digits; i0 += 256) {
-        const int i = i0 + threadIdx.x;
-        const u32 c = i < digits ? total[i] : 0u;
-        u32 x = c;
+    // the thread's digit: how many tokens have it, and how many of them are in workgroups before
+    u32 all = 0, here = 0;
+    if (i < digits) {
+        if (FUSED) {
+            const int wgs = (int)z.first, me = (int)blockIdx.x;
+            u32 c[16];
+            for (int w0 = 0; w0 < wgs; w0 += 16) {
 #pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const u32 y = (u32)__shfl_up((int)x, m);
-            if (lane >= m) x += y;
-        }
-        if (lane == 63) s_wave[wave] = x;
-        __syncthreads();
-        u32 before = base;
-        for (int j = 0; j < wave; ++j) before += s_wave[j];
-        base += s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
-        if (i < digits) {
-            u32 at = before + x - c + table[(int64_t)i * z.first + blockIdx.x];
+                for (int w = 0; w < 16; ++w) c[w] = w0 + w < wgs ? table[(w0 + w) * digits + i] : 0u;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const u32 k = s_next[j][i];
-                s_next[j][i] = at;
-                at += k;
+                for (int w = 0; w < 16; ++w) {
+                    all += c[w];
+                    here += w0 + w < me ? c[w] : 0u;
+                }
             }
+        } else {
+            all = total[i];
+            here = table[(int64_t)blockIdx.x * digits + i];
         }
-        __syncthreads();
     }
+    // ... and how many have a smaller one
+    u32 x = all;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const u32 y = (u32)__shfl_up((int)x, m);
+        if (lane >= m) x += y;
+    }
+    if (lane == 63) s_wave[wave] = x;
+    __syncthreads();                                        // (the waves' counts are there as well)
+    if (i < digits) {
+        u32 at = x - all + here;
+        for (int j = 0; j < wave; ++j) at += s_wave[j];
+#pragma unroll
+        for (int j = 0; j < SORT_WAVES; ++j) {
+            const u32 k = s_next[j][i];
+            s_next[j][i] = at;
+            at += k;
+        }
+    }
+    __syncthreads();
     // (the wave's own words from here on; a row of tokens is placed before the next one reads them)
     for (int64_t t0 = from; t0 < to; t0 += 64) {
         const int64_t t = t0 + lane;
@@ -305,23 +323,30 @@ __device__ inline void write_row(const float* v, int left, O* p, float scale, bo
 }
 
 // G lanes a tile, a piece of the row a lane, as many columns of tiles as the row has G pieces.  All of a tile's rows are asked for before
-// the first is added.  parts: two rows of d per tile: of a run that came from the tile before, and of one that goes on in the next
+// the first is added.  The end of a run stands in the code sixteen times, and its length is what the waves fetch: so pieces are whole (WHOLE, rows of a
+// piece or more: the last one ends where the row does, and shares columns with the one before, which has the same sums) and a run's end
+// is a store or two.  (131 072 rows of 1024 bf16, 65 536 tokens: 64 us with pieces of any length, 60 whole; 20 011 tokens, rows of 50 fp32: 11.8 and 8.8.)
+// parts: two rows of d per tile: of a run that came from the tile before, and of one that goes on in the next
 // but began here; such tiles are listed, in any order, from runs[2] on (runs[0] of them) or, where the run goes on for RUN_LONG tiles or
 // more, from the list's other end (runs[1]).
-template <class E, class O>
+template <class E, class O, bool ADD, bool WHOLE>
 __global__ __launch_bounds__(256) void run_sum_kernel(const E* __restrict__ grad, int64_t ld, const u32* __restrict__ skey,
-                                                      const u32* __restrict__ spos, int64_t n, int64_t n_rows, int d, float scale, int add,
+                                                      const u32* __restrict__ spos, int64_t n, int64_t n_rows, int d, float scale,
                                                       int gshift, int columns, O* __restrict__ out, float* __restrict__ parts,
                                                       u32* __restrict__ runs)
 {
     typedef TgPiece<E> P;
+    typedef float part __attribute__((ext_vector_type(4), aligned(4)));
     const int lane = threadIdx.x & ((1 << gshift) - 1);
     const int64_t unit = (int64_t)blockIdx.x * (256 >> gshift) + (threadIdx.x >> gshift);
     const int64_t tile = unit / columns;
     const int column = (int)(unit - tile * columns);
-    const int at = ((column << gshift) + lane) * P::E;
+    const int piece = ((column << gshift) + lane) * P::E;
     const int64_t i0 = tile * RUN_TILE;
-    if (i0 >= n || at >= d) return;
+    if (i0 >= n || piece >= d) return;
+    const int at = WHOLE && piece + P::E > d ? d - P::E : piece;
+    // (what is added to has to be added once: the shared columns are the piece's before)
+    const int skip = ADD ? piece - at : 0, left = WHOLE ? P::E : d;
     const int count = (int)(n - i0 < RUN_TILE ? n - i0 : RUN_TILE);
     const u32 none = (u32)n_rows;
     u32 key[RUN_TILE];
@@ -337,7 +362,8 @@ __global__ __launch_bounds__(256) void run_sum_kernel(const E* __restrict__ grad
 #pragma unroll
         for (int j = 0; j < RUN_TILE; ++j) {
             if (j >= count) key[j] = none;
-            g[j] = P::raw(grad + (int64_t)(key[j] == none ? 0u : pos[j]) * ld + at, key[j] == none ? 0 : d - at);
+            // (a token without a row: the first token's values, which no run takes in)
+            g[j] = P::raw(grad + (int64_t)(key[j] == none ? 0u : pos[j]) * ld + at, left);
         }
     }
     u32 cur = key[0];
@@ -347,14 +373,30 @@ __global__ __launch_bounds__(256) void run_sum_kernel(const E* __restrict__ grad
     float acc[P::E];
 #pragma unroll
     for (int i = 0; i < P::E; ++i) acc[i] = 0.0f;
+    const auto put_part = [&](int which) {
+        float* p = parts + (2 * tile + which) * (int64_t)d + at;
+        if (WHOLE) {
+#pragma unroll
+            for (int i = 0; i < P::E; i += 4) *reinterpret_cast<part*>(p + i) = part{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < P::E; ++i)
+                if (i < left) p[i] = acc[i];
+        }
+    };
+    const auto put = [&] {
+        O* p = out + (int64_t)cur * d + at;
+        if (ADD && skip) {
+#pragma unroll
+            for (int i = 0; i < P::E; ++i)
+                if (i >= skip) p[i] = (O)((float)p[i] + acc[i] * scale);
+        } else write_row<E, O>(acc, left, p, scale, ADD);
+    };
 #pragma unroll
     for (int j = 0; j < RUN_TILE; ++j) {
         if (key[j] != cur) {
-            if (carried) {
-#pragma unroll
-                for (int i = 0; i < P::E; ++i)
-                    if (at + i < d) parts[2 * tile * d + at + i] = acc[i];
-            } else write_row<E, O>(acc, d - at, out + (int64_t)cur * d + at, scale, add != 0);
+            if (carried) put_part(0);
+            else put();
             carried = false;
             cur = key[j];
             if (cur == none) return;
@@ -364,11 +406,8 @@ __global__ __launch_bounds__(256) void run_sum_kernel(const E* __restrict__ grad
 #pragma unroll
         for (int i = 0; i < P::E; ++i) acc[i] += (float)g[j][i];
     }
-    if (!carried && !goes_on) { write_row<E, O>(acc, d - at, out + (int64_t)cur * d + at, scale, add != 0); return; }
-    float* p = parts + (2 * tile + (carried ? 0 : 1)) * (int64_t)d + at;
-#pragma unroll
-    for (int i = 0; i < P::E; ++i)
-        if (at + i < d) p[i] = acc[i];
+    if (!carried && !goes_on) { put(); return; }
+    put_part(carried ? 0 : 1);
     if (!carried && column == 0 && lane == 0) {
         const int64_t far = i0 + (int64_t)RUN_LONG * RUN_TILE;
         if (far < n && skey[far] == cur) runs[1 + (n + RUN_TILE - 1) / RUN_TILE - atomicAdd(runs + 1, 1u)] = (u32)tile;
@@ -377,14 +416,15 @@ __global__ __launch_bounds__(256) void run_sum_kernel(const E* __restrict__ grad
 }
 
 // The parts of the listed runs are added in the tiles' order, 256 columns at a time.  Most runs have two or three: a wave each.  Of a long one
-// eight waves take an equal stretch each, and are added in their order; the first RUN_JOIN_LONG workgroups look after those.
+// sixteen waves take an equal stretch each, and are added in their order; the first RUN_JOIN_LONG workgroups look after those.
 #define RUN_JOIN_LONG 128
+#define RUN_JOIN_WAVES 16
 template <class O>
-__global__ __launch_bounds__(512) void run_join_kernel(const u32* __restrict__ skey, int64_t n, int d, float scale, int add,
+__global__ __launch_bounds__(64 * RUN_JOIN_WAVES) void run_join_kernel(const u32* __restrict__ skey, int64_t n, int d, float scale, int add,
                                                        const float* __restrict__ parts, const u32* __restrict__ runs, O* __restrict__ out)
 {
     typedef TgPiece<float> P;
-    __shared__ float s_sum[8][64][4];
+    __shared__ float s_sum[RUN_JOIN_WAVES][64][4];
     const int wave = threadIdx.x >> 6, lane = tg_lane(), columns = (d + 255) / 256;
     const int64_t tiles = (n + RUN_TILE - 1) / RUN_TILE;
     const auto put = [&](u32 key, int c, const float* v) {
@@ -393,7 +433,8 @@ __global__ __launch_bounds__(512) void run_join_kernel(const u32* __restrict__ s
     };
     if (blockIdx.x >= RUN_JOIN_LONG) {
         const int64_t all = (int64_t)runs[0] * columns;
-        for (int64_t item = (int64_t)(blockIdx.x - RUN_JOIN_LONG) * 8 + wave; item < all; item += (int64_t)(gridDim.x - RUN_JOIN_LONG) * 8) {
+        for (int64_t item = (int64_t)(blockIdx.x - RUN_JOIN_LONG) * RUN_JOIN_WAVES + wave; item < all;
+             item += (int64_t)(gridDim.x - RUN_JOIN_LONG) * RUN_JOIN_WAVES) {
             const int64_t tile = runs[2 + item / columns];
             const int c = (int)(item % columns) * 256 + lane * 4;
             const u32 key = skey[tile * RUN_TILE + RUN_TILE - 1];
@@ -425,7 +466,7 @@ __global__ __launch_bounds__(512) void run_join_kernel(const u32* __restrict__ s
             if (skey[mid] == key) lo = mid + 1; else hi = mid;
         }
         const int64_t end = (lo - 1) / RUN_TILE;                                // its last tile
-        const int64_t each = (end - tile + 7) / 8, from = tile + 1 + wave * each, to = from + each < end + 1 ? from + each : end + 1;
+        const int64_t each = (end - tile + RUN_JOIN_WAVES - 1) / RUN_JOIN_WAVES, from = tile + 1 + wave * each, to = from + each < end + 1 ? from + each : end + 1;
         P sum;
         sum.load(parts + (2 * tile + 1) * d + c, wave == 0 ? d - c : 0);
 #pragma unroll 8
@@ -440,7 +481,7 @@ __global__ __launch_bounds__(512) void run_join_kernel(const u32* __restrict__ s
         __syncthreads();
         if (wave == 0 && c < d) {
 #pragma unroll
-            for (int w = 1; w < 8; ++w)
+            for (int w = 1; w < RUN_JOIN_WAVES; ++w)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum.v[e] += s_sum[w][lane][e];
             put(key, c, sum.v);
@@ -484,12 +525,17 @@ static void launch_sums(const E* grad, int64_t ld, const u32* key, const u32* po
     const int gs = lanes_shift(pieces), columns = (pieces + (1 << gs) - 1) >> gs;
     const int64_t per = 256 >> gs;
     // (fewer than 2^32 work-items: 64 of them stand for 16 KB of a gradient that fits the card, or for 16 tokens of a short row)
-    hipLaunchKernelGGL((run_sum_kernel<E, O>), dim3((unsigned)((tiles * columns + per - 1) / per)), dim3(256), 0, s, grad, ld, key, pos, n, n_rows, d,
-                       scale, add, gs, columns, out, g.parts, g.runs);
+    const auto sums = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles * columns + per - 1) / per)), dim3(256), 0, s, grad, ld, key, pos, n, n_rows, d, scale, gs,
+                           columns, out, g.parts, g.runs);
+    };
+    const bool whole = d >= TgPiece<E>::E;
+    if (add) whole ? sums(run_sum_kernel<E, O, true, true>) : sums(run_sum_kernel<E, O, true, false>);
+    else whole ? sums(run_sum_kernel<E, O, false, true>) : sums(run_sum_kernel<E, O, false, false>);
     if (tiles > 1) {
         // (at most a listed run a tile)
-        const int64_t waves = (tiles - 1) * ((d + 255) / 256), wgs = (waves + 7) / 8;
-        hipLaunchKernelGGL(run_join_kernel<O>, dim3((unsigned)(wgs < 1024 ? wgs : 1024) + RUN_JOIN_LONG), dim3(512), 0, s, key, n, d, scale, add, g.parts,
+        const int64_t waves = (tiles - 1) * ((d + 255) / 256), wgs = (waves + RUN_JOIN_WAVES - 1) / RUN_JOIN_WAVES;
+        hipLaunchKernelGGL(run_join_kernel<O>, dim3((unsigned)(wgs < 512 ? wgs : 512) + RUN_JOIN_LONG), dim3(64 * RUN_JOIN_WAVES), 0, s, key, n, d, scale, add, g.parts,
                            g.runs, out);
     }
 }
@@ -512,23 +558,26 @@ void tg_launch_lookup_grad(const void* grad, int64_t ld, int dtype, const void* 
         hipLaunchKernelGGL(rank_sort_kernel, dim3(z.first + zero_wgs(z)), dim3(256), full * 4, s, ids, ids64, (int)n, n_rows, g.key[0], g.pos[0], g.runs, z);
     } else {
         const SortShape f = sort_shape(n, n_rows);
-        const int digits = 1 << f.bits;
-        z.parts = 3 * f.passes;
+        const int digits = 1 << f.bits, each = f.fused ? 2 : 3;
+        const dim3 threads(64 * SORT_WAVES);
+        z.parts = each * f.passes;
+        const unsigned zw = zero_wgs(z);
         for (int p = 0; p < f.passes; ++p) {
             const u32* ki = p ? g.key[at] : nullptr;
             const u32* pi = p ? g.pos[at] : nullptr;
             const int to = p ? at ^ 1 : 0, shift = p * f.bits;
-            const unsigned zw = zero_wgs(z);
-            z.part = 3 * p;
+            z.part = each * p;
             z.first = (uint32_t)f.wgs;
-            hipLaunchKernelGGL(digit_count_kernel, dim3(z.first + zw), dim3(256), 0, s, ids, ids64, ki, n, n_rows, f.chunk, shift, f.bits, g.table, g.runs, z);
-            z.part = 3 * p + 1;
-            z.first = (uint32_t)((digits + 3) / 4);
-            hipLaunchKernelGGL(digit_scan_kernel, dim3(z.first + zw), dim3(256), 0, s, g.table, (int)f.wgs, digits, g.total, z);
-            z.part = 3 * p + 2;
+            hipLaunchKernelGGL(digit_count_kernel, dim3(z.first + zw), threads, 0, s, ids, ids64, ki, n, n_rows, f.chunk, shift, f.bits, g.table, g.runs, z);
+            if (!f.fused) {
+                z.part = each * p + 1;
+                z.first = (uint32_t)((digits + 255) / 256);
+                hipLaunchKernelGGL(digit_scan_kernel, dim3(z.first + zw), dim3(256), 0, s, g.table, (int)f.wgs, digits, g.total, z);
+            }
+            z.part = each * p + each - 1;
             z.first = (uint32_t)f.wgs;
-            hipLaunchKernelGGL(digit_place_kernel, dim3(z.first + zw), dim3(256), 0, s, ids, ids64, ki, pi, n, n_rows, f.chunk, shift, f.bits, g.table, g.total,
-                               g.key[to], g.pos[to], z);
+            hipLaunchKernelGGL(f.fused ? digit_place_kernel<true> : digit_place_kernel<false>, dim3(z.first + zw), threads, 0, s, ids, ids64, ki, pi, n,
+                               n_rows, f.chunk, shift, f.bits, g.table, g.total, g.key[to], g.pos[to], z);
             at = to;
         }
     }

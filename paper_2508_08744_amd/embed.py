@@ -123,7 +123,7 @@ def lookup(table, ids, scale=1.0):
     """tg_embed_lookup: scale * table[ids], zeros where an id is no row of the table; the shape of ids and the rows' length."""
     ld, v, d = _rows("table", table)
     wide = _ids("ids", ids)
-    out = table.new_empty(ids.shape + (d,))
+    out = table.new_empty(*ids.shape, d)
     _check(lib().tg_embed_lookup(table.data_ptr(), ld, DTYPES[table.dtype], v, d, ids.data_ptr(), wide, ids.numel(), scale, out.data_ptr(),
                                  _stream(table, ids)))
     return out
