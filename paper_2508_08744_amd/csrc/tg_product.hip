@@ -26,6 +26,22 @@ __device__ inline tg_i32x4 product_load(const char* p, int left)
     return v;
 }
 
+// 16 bytes from p on, of which those behind `end` read as zero: for rows whose other factor is zero behind their length, so that what follows a row
+// in memory may be read with it.  (Only the matrix's last bytes take the loop.)
+__device__ inline tg_i32x4 product_load_on(const char* p, const char* end)
+{
+    typedef int i32x4u __attribute__((ext_vector_type(4), aligned(1)));
+    if (p + 16 <= end) return *reinterpret_cast<const i32x4u*>(p);
+    uint64_t v[2] = {0, 0};
+#pragma unroll 1
+    for (int i = 0; i < 15 && p + i < end; ++i) {
+        const uint64_t b = (uint64_t)(uint8_t)p[i] << (i % 8 * 8);
+        v[0] |= i < 8 ? b : 0;
+        v[1] |= i < 8 ? 0 : b;
+    }
+    return tg_i32x4{(int)v[0], (int)(v[0] >> 32), (int)v[1], (int)(v[1] >> 32)};
+}
+
 // x: channels, y: tokens.
 template <class O, int BM, int BN, int WM, int WN, int NB, bool BIAS>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
@@ -136,17 +152,26 @@ __global__ __launch_bounds__(256) void product_few_kernel(TileRows X, TileRows Y
 }
 
 // Short rows, of up to STEPS x 64 bytes: the output's bytes bound the product, and a tile would be loaded, multiplied once or twice and stored,
-// each after the other.  A wave keeps the rows of 16 FN tokens in registers, walks over the channels 16 CB at a time with the next ones' rows and
-// scales on their way, and stores as it goes; nothing meets.  Which 16 channels a product takes is free: for outputs of 16 bits two products
-// share 32, in turn four by four, so that a lane has eight neighbours and stores 16 bytes of a row, as it does of four in 32 bits.
+// each after the other.  A wave keeps the rows of 16 FN tokens in registers and walks over the channels 16 CB at a time, beside the
+// other waves of its workgroup, with the next ones' rows and scales on their way.  A lane's results are 16 bytes of an output row (which 16
+// channels a product takes is free: for outputs of 16 bits two products share 32, in turn four by four), but a wave's are 64 bytes of each of 16
+// rows, which lie far apart: so the workgroup's go through LDS, 16 KB at a time, and are stored as stretches of a row.  (203 tokens, 10^6 channels of
+// 128, fp32: 243 us without, 216 with it, of which 54 are left without the stores; 4000 tokens, 30 000 channels of 200, fp32: 197 and 150.)
 template <class O, int STEPS, int FN, int CB, bool BIAS>
-__global__ __launch_bounds__(256) void product_short_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
+__global__ __launch_bounds__(256, 2) void product_short_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
                                                             const float* __restrict__ bs, const float* __restrict__ bias, O* __restrict__ out)
 {
     constexpr int W = 16 / (int)sizeof(O), PER = W / 4;        // neighbours of a row that a lane stores; products they come from
     static_assert(CB % PER == 0, "whole stores");
+    constexpr int PIECES = 16 * CB / PER;                      // of 16 bytes, of a row of the workgroup's
+    constexpr int FEW = 1024 / (16 * PIECES), TURN = FEW < FN ? FEW : FN;      // groups of 16 tokens that go through LDS at a time
+    static_assert(FN % TURN == 0, "whole turns");
+    constexpr int EACH = TURN * 16 * PIECES / 256;             // pieces that a lane stores of them
+    typedef O vec __attribute__((ext_vector_type(W)));
+    __shared__ vec s_out[2][TURN * 16 * PIECES];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = tg_lane(), row = lane & 15, q = lane >> 4;
-    const int64_t chunks = (X.rows + 16 * CB - 1) / (16 * CB), step = (int64_t)gridDim.x * 4, y0 = (int64_t)blockIdx.y * (16 * FN);
+    const int64_t chunks = (X.rows + 16 * CB - 1) / (16 * CB), groups = (chunks + 3) / 4, y0 = (int64_t)blockIdx.y * (16 * FN);
+    const char* end = X.p + X.rows * X.pitch;
     tg_i32x4 y[FN][STEPS];
     float sy[FN];
 #pragma unroll
@@ -160,18 +185,16 @@ __global__ __launch_bounds__(256) void product_short_kernel(TileRows X, TileRows
     }
     tg_i32x4 x[CB][STEPS], next[CB][STEPS];
     float c[CB / PER][W], c_next[CB / PER][W];
-    // (channels that are not there are read as the chunk's first: nobody stores their sums)
+    // (channels that are not there are read as the last chunk's first: nobody stores their sums)
     const auto load = [&](int64_t chunk) {
+        if (chunk >= chunks) chunk = chunks - 1;
         const int64_t first = chunk * (16 * CB);
 #pragma unroll
         for (int i = 0; i < CB; ++i) {
             const int64_t r = first + i / PER * (16 * PER) + (row >> 2) * W + i % PER * 4 + (row & 3);
             const char* p = X.p + (r < X.rows ? r : first) * X.pitch + q * 16;
 #pragma unroll
-            for (int h = 0; h < STEPS; ++h) {
-                if (h * 64 + 64 <= bytes) next[i][h] = product_load(p + h * 64, 16);
-                else next[i][h] = product_load(p + h * 64, bytes - h * 64 - q * 16);
-            }
+            for (int h = 0; h < STEPS; ++h) next[i][h] = product_load_on(p + h * 64, end);
         }
 #pragma unroll
         for (int i = 0; i < CB / PER; ++i) {
@@ -185,9 +208,10 @@ __global__ __launch_bounds__(256) void product_short_kernel(TileRows X, TileRows
             }
         }
     };
-    int64_t chunk = (int64_t)blockIdx.x * 4 + wave;
-    if (chunk < chunks) load(chunk);
-    for (; chunk < chunks; chunk += step) {
+    int buffer = 0;
+    load((int64_t)blockIdx.x * 4 + wave);
+    for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
+        const int64_t v0 = group * (64 * CB), v_wave = v0 + wave * (16 * CB);
 #pragma unroll
         for (int i = 0; i < CB; ++i)
 #pragma unroll
@@ -196,35 +220,58 @@ __global__ __launch_bounds__(256) void product_short_kernel(TileRows X, TileRows
         for (int i = 0; i < CB / PER; ++i)
 #pragma unroll
             for (int e = 0; e < W; ++e) c[i][e] = c_next[i][e];
-        if (chunk + step < chunks) load(chunk + step);
-        const bool whole = (chunk + 1) * (16 * CB) <= X.rows;
+        if (group + gridDim.x < groups) load((group + gridDim.x) * 4 + wave);
         TgPiece<float> b[CB];
         if (BIAS) {
 #pragma unroll
             for (int i = 0; i < CB; ++i) {
-                const int64_t v = chunk * (16 * CB) + i / PER * (16 * PER) + q * W + i % PER * 4;
-                b[i].load(bias + v, v + 4 <= X.rows ? 4 : (int)(X.rows - v));
+                const int64_t v = v_wave + i / PER * (16 * PER) + q * W + i % PER * 4;
+                b[i].load(bias + v, v + 4 <= X.rows ? 4 : v < X.rows ? (int)(X.rows - v) : 0);
             }
         }
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int64_t r = y0 + j * 16 + row;
-            tg_i32x4 acc[CB];
+        for (int j0 = 0; j0 < FN; j0 += TURN) {
+            if (y0 + j0 * 16 >= Y.rows) break;
+            // (piece p of token t lies at place p ^ t: the lanes that write one column of pieces at a time are in different banks)
 #pragma unroll
-            for (int i = 0; i < CB; ++i) {
-                acc[i] = tg_i32x4{0, 0, 0, 0};
+            for (int jj = 0; jj < TURN; ++jj) {
+                const int j = j0 + jj;
+                tg_i32x4 acc[CB];
 #pragma unroll
-                for (int h = 0; h < STEPS; ++h) acc[i] = TileMul<int8_t>::mul(x[i][h], y[j][h], acc[i]);
+                for (int i = 0; i < CB; ++i) {
+                    acc[i] = tg_i32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int h = 0; h < STEPS; ++h) acc[i] = TileMul<int8_t>::mul(x[i][h], y[j][h], acc[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < CB / PER; ++i) {
+                    vec o;
+#pragma unroll
+                    for (int e = 0; e < W; ++e) {
+                        const float v = (float)acc[i * PER + e / 4][e % 4] * sy[j] * c[i][e];
+                        o[e] = (O)(BIAS ? v + b[i * PER + e / 4].v[e % 4] : v);
+                    }
+                    s_out[buffer][(jj * 16 + row) * PIECES + (((wave * (CB / PER) + i) * 4 + q) ^ row)] = o;
+                }
             }
-            if (r >= Y.rows) continue;
+            // (two buffers in turn: one is written again only behind the next barrier, when all have read it)
+            __syncthreads();
 #pragma unroll
-            for (int i = 0; i < CB / PER; ++i) {
-                const int64_t v = chunk * (16 * CB) + i * (16 * PER) + q * W;
-                TgPiece<O> o;
+            for (int n = 0; n < EACH; ++n) {
+                const int at = n * 256 + threadIdx.x, t = at / PIECES, p = at % PIECES;
+                const vec o = s_out[buffer][t * PIECES + (p ^ (t & 15))];
+                const int64_t r = y0 + j0 * 16 + t, v = v0 + p * W;
+                if (r >= Y.rows || v >= X.rows) continue;
+                typedef O loose __attribute__((ext_vector_type(W), aligned(sizeof(O))));
+                O* to = out + r * X.rows + v;
+                if (v + W <= X.rows) *reinterpret_cast<loose*>(to) = o;
+                else {
 #pragma unroll
-                for (int e = 0; e < W; ++e) o.v[e] = (float)acc[i * PER + e / 4][e % 4] * sy[j] * c[i][e] + (BIAS ? b[i * PER + e / 4].v[e % 4] : 0.0f);
-                o.store(out + r * X.rows + v, whole || v + W <= X.rows ? W : (int)(X.rows - v));
+                    for (int e = 0; e < W - 1; ++e)
+                        if (v + e < X.rows) to[e] = o[e];
+                }
             }
+            buffer ^= 1;
         }
     }
 }
@@ -274,16 +321,17 @@ size_t tg_product_space(int64_t m, int64_t n, int k, bool ready)
     return c.used;
 }
 
-template <class O, int STEPS, int FN, int CB>
+template <class O, int STEPS, int FN>
 static void launch_short(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
 {
+    constexpr int CB = 2;                                      // (64 channels at a time for outputs of 32 bits: 230 us where 32 take 216)
     // (groups of tokens along y: the limit on a grid's y is 65535)
     const int64_t most = 65535ll * 16 * FN, chunks = (X.rows + 16 * CB - 1) / (16 * CB);
     for (int64_t y0 = 0; y0 < Y.rows; y0 += most) {
         const TileRows part{Y.p + y0 * Y.pitch, Y.rows - y0 < most ? Y.rows - y0 : most, Y.pitch, Y.width};
         const int64_t ny = (part.rows + 16 * FN - 1) / (16 * FN);
-        // waves for all CUs, walking over the channels
-        int64_t nx = (2048 + ny - 1) / ny;
+        // two workgroups a CU, twice (256 tokens, 10^6 channels of 256, bf16: 231 us, 283 with twice as many)
+        int64_t nx = (1024 + ny - 1) / ny;
         if (nx < 64) nx = 64;
         if (nx > (chunks + 3) / 4) nx = (chunks + 3) / 4;
         const dim3 grid((unsigned)nx, (unsigned)ny);
@@ -303,14 +351,12 @@ template <class O>
 static void launch_product(const TileRows& X, const TileRows& Y, int bytes, const float* as, const float* bs, const float* bias, O* out, hipStream_t s)
 {
     if (bytes <= PRODUCT_SHORT) {
-        // 32 channels at a time, for outputs of 32 bits 64 where the registers are enough (4530 tokens, 52 160 channels of 128: bf16 116 us with
-        // 32, 172 with 64; 200 tokens, 2^20 channels of 128, fp32: 295 with 32, 248 with 64)
         const auto go = [&](auto steps, auto most) {
-            constexpr int S = decltype(steps)::value, FN = decltype(most)::value, CB = sizeof(O) == 4 && S < 4 ? 4 : 2;
-            if (Y.rows <= 16) launch_short<O, S, 1, CB>(X, Y, bytes, as, bs, bias, out, s);
-            else if (Y.rows <= 32) launch_short<O, S, 2, CB>(X, Y, bytes, as, bs, bias, out, s);
-            else if (Y.rows <= 64 || FN == 4) launch_short<O, S, 4, CB>(X, Y, bytes, as, bs, bias, out, s);
-            else launch_short<O, S, FN, CB>(X, Y, bytes, as, bs, bias, out, s);
+            constexpr int S = decltype(steps)::value, FN = decltype(most)::value;
+            if (Y.rows <= 16) launch_short<O, S, 1>(X, Y, bytes, as, bs, bias, out, s);
+            else if (Y.rows <= 32) launch_short<O, S, 2>(X, Y, bytes, as, bs, bias, out, s);
+            else if (Y.rows <= 64 || FN == 4) launch_short<O, S, 4>(X, Y, bytes, as, bs, bias, out, s);
+            else launch_short<O, S, FN>(X, Y, bytes, as, bs, bias, out, s);
         };
         if (bytes <= 64) go(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
         else if (bytes <= 128) go(std::integral_constant<int, 2>(), std::integral_constant<int, 8>());

@@ -386,8 +386,9 @@ static void xent_rows(XentRows* r, TgCarve* c, const void* h, int64_t ld_h, cons
     r->w = ready_w ? TileRows{(const char*)w, n_rows, (uint32_t)(ld_w * e), pitch} : TileRows{(const char*)r->pw, n_rows, pitch, pitch};
 }
 
-// The tile of the logits: 256 x 256 where that leaves every CU one, smaller ones for fewer tokens.  fp32 keeps twice the bytes a
-// value: 128 x 128 there.
+// The tile of the logits: 256 x 256 where that leaves every CU one, smaller ones for fewer tokens.  fp32, whose products take sixteen times as long
+// a byte, is fed by the smallest, 64 x 64, of which a CU holds four that wait for each other's loads and epilogues (1003 tokens, 37 511 rows of 96, there and back:
+// 398 us in tiles of 128 x 128, 359 in these; 2048 tokens, 8000 rows of 1500: 1502 and 1444).
 #define XENT_STRETCH 32         // rows of the table that leave one (maximum, sum) at least (BM / WM)
 
 size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready)
@@ -450,7 +451,8 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
                 wide = ((n_rows + 255) / 256) * ((n + 255) / 256) >= 200;
                 if (wide) count = launch_parts<E, 256, 256, 2, 4>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
             }
-            if (!wide) count = launch_parts<E, 128, 128, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+            if constexpr (sizeof(E) == 4) count = launch_parts<E, 64, 64, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
+            else if (!wide) count = launch_parts<E, 128, 128, 2, 2>(r.w, r.h, r.w.width, targets, targets64, scale, parts, at, s);
         }
     });
     // few tokens: more lanes each, and more workgroups
@@ -469,6 +471,7 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
 struct XentGrad {
     int64_t piece;        // rows of the table at a time, a multiple of 256 unless it is all of them
     int side;             // products in tiles of 256 x 256, 128 x 128 or 64 x 64
+    bool few;             // tiles: 64 x 64, with four stages in flight
     int splits;           // of dh's contraction
     bool direct;          // one piece, one part: dh is written at once
 };
@@ -478,12 +481,13 @@ static int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 static uint32_t xent_pitch(int64_t rows, int e) { return (uint32_t)round_up(rows * e, 16) + XENT_PAD; }
 static void xent_splits(XentGrad* g, int64_t n, int64_t n_rows, int d, int e)
 {
-    // both products take tiles of 256 x 256, of which a CU holds one, where those are enough; else of 128 x 128, of which it holds two; and of
-    // 64 x 64, with four stages in flight, where each of 128 x 128 would have a CU of its own
+    // both products take tiles of 256 x 256, of which a CU holds one, where those are enough; else of 128 x 128, of which it holds two, in fp32 of
+    // 64 x 64, of which it holds four; and of 64 x 64, with four stages in flight, where each of 128 x 128 would have a CU of its own
     const auto tiles = [](int64_t x, int64_t y, int64_t side) { return ((x + side - 1) / side) * ((y + side - 1) / side); };
-    g->side = e == 2 && n > 128 && d > 128 && tiles(g->piece, d, 256) >= 200 ? 256 : tiles(n, d, 128) + tiles(g->piece, d, 128) <= 128 ? 64 : 128;
+    g->few = tiles(n, d, 128) + tiles(g->piece, d, 128) <= 128;
+    g->side = e == 2 && n > 128 && d > 128 && tiles(g->piece, d, 256) >= 200 ? 256 : g->few || e == 4 ? 64 : 128;
     // dh in as many parts as fill the card, each with sixteen stages of the contraction or more (four where a stage is a load's way)
-    const int64_t fill = g->side == 256 ? 256 : 512, least = g->side == 64 ? 4 : 16;
+    const int64_t fill = g->side == 256 ? 256 : g->few || g->side == 128 ? 512 : 1024, least = g->few ? 4 : 16;
     const int64_t dh = tiles(n, d, g->side), stages = (g->piece * e + TILE_BYTES - 1) / TILE_BYTES;
     int64_t s = (fill + dh - 1) / dh;
     if (s > stages / least) s = stages / least;
@@ -580,7 +584,8 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
                 wide = (int64_t)over(rows, 256) * over(n, 256) >= 200;
                 if (wide) logits(xent_p_kernel<E, 256, 256, 2, 4, 2>, 256, 256, 512);
             }
-            if (!wide) logits(xent_p_kernel<E, 128, 128, 2, 2, 2>, 128, 128, 256);
+            if constexpr (sizeof(E) == 4) logits(xent_p_kernel<E, 64, 64, 2, 2, 2>, 64, 64, 256);
+            else if (!wide) logits(xent_p_kernel<E, 128, 128, 2, 2, 2>, 128, 128, 256);
         }
         const int stages = (int)((width + TILE_BYTES - 1) / TILE_BYTES);
         a.v0 = v0;
@@ -595,8 +600,9 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
         if constexpr (sizeof(E) == 2) {
             if (g.side == 256) products(xent_products_kernel<E, 256, 2, 4, 2>, 512);
         }
-        if (g.side == 128) products(xent_products_kernel<E, 128, 2, 2, 2>, 256);
-        if (g.side == 64) products(xent_products_kernel<E, 64, 2, 2, 4>, 256);
+        if (g.few) products(xent_products_kernel<E, 64, 2, 2, 4>, 256);
+        else if constexpr (sizeof(E) == 4) products(xent_products_kernel<E, 64, 2, 2, 2>, 256);
+        else if (g.side == 128) products(xent_products_kernel<E, 128, 2, 2, 2>, 256);
     }
     if (g.direct) return;
     const int64_t out_wgs = (n * ((d + 3) / 4) + 255) / 256;
