@@ -8,17 +8,16 @@
 // T lanes of a workgroup share a row; CH pieces of 16 bytes of it a lane.
 template <int T> struct NormShare { static constexpr int ROWS = T < 256 ? 256 / T : 1, THREADS = T < 256 ? 256 : T; };
 
+// What is left of a row from a lane's piece on.  Rows of whole pieces (WHOLE) have one or none: the kernels then hold no code for parts
+// of a piece, which is most of it otherwise.
+template <class E, bool WHOLE>
+__device__ inline int norm_left(int left) { return !WHOLE ? left : left > 0 ? TgPiece<E>::E : 0; }
+
 template <class V>
 __device__ inline V wave_sum(V x)
 {
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    return x;
-}
-__device__ inline float wave_max(float x)
-{
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x = fmaxf(x, __shfl_xor(x, m));
     return x;
 }
 // sum over the T lanes of a row, the same in all of them; `s`: a word per wave, not used by the sum before
@@ -34,20 +33,21 @@ __device__ inline V row_sum(V x, V* s)
     for (int i = 1; i < T / 64; ++i) y += s[i];
     return y;
 }
+// their maximum
 template <int T>
-__device__ inline float row_max(float x, float* s)
+__device__ inline double row_max64(double x, double* s)
 {
-    x = wave_max(x);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x = fmax(x, __shfl_xor(x, m));
     if (T == 64) return x;
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
     __syncthreads();
-    float y = s[0];
 #pragma unroll
-    for (int i = 1; i < T / 64; ++i) y = fmaxf(y, s[i]);
-    return y;
+    for (int i = 0; i < T / 64; ++i) x = fmax(x, s[i]);
+    return x;
 }
 
-template <class E, int T, int CH>
+template <class E, int T, int CH, bool WHOLE>
 __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_kernel(const E* x, int64_t ld_x, const E* res, int64_t ld_res,
                                                                      const E* __restrict__ w, int64_t n, int d, float eps, E* __restrict__ y,
                                                                      E* r, float* __restrict__ rstd_out)
@@ -60,19 +60,19 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_kernel(const E* x,
     P p[CH];
     float sum = 0.0f;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) p[c].load(x + row * ld_x + (lane + c * T) * P::E, d - (lane + c * T) * P::E);
+    for (int c = 0; c < CH; ++c) p[c].load(x + row * ld_x + (lane + c * T) * P::E, norm_left<E, WHOLE>(d - (lane + c * T) * P::E));
     if (res) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int at = (lane + c * T) * P::E;
             P q;
-            q.load(res + row * ld_res + at, d - at);
+            q.load(res + row * ld_res + at, norm_left<E, WHOLE>(d - at));
 #pragma unroll
             for (int i = 0; i < P::E; ++i) p[c].v[i] += q.v[i];
             p[c].round();
         }
 #pragma unroll
-        for (int c = 0; c < CH; ++c) p[c].store(r + row * d + (lane + c * T) * P::E, d - (lane + c * T) * P::E);
+        for (int c = 0; c < CH; ++c) p[c].store(r + row * d + (lane + c * T) * P::E, norm_left<E, WHOLE>(d - (lane + c * T) * P::E));
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c)
@@ -84,18 +84,38 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_kernel(const E* x,
     for (int c = 0; c < CH; ++c) {
         const int at = (lane + c * T) * P::E;
         P g;
-        g.load(w + at, d - at);
+        g.load(w + at, norm_left<E, WHOLE>(d - at));
 #pragma unroll
         for (int i = 0; i < P::E; ++i) g.v[i] *= p[c].v[i] * rstd;
-        g.store(y + row * d + at, d - at);
+        g.store(y + row * d + at, norm_left<E, WHOLE>(d - at));
     }
 }
 
+// 1 / sqrt(x) and 1 / x in 64 bits from the instructions' estimates, to a few units in the last place: each step of Newton's doubles the bits, of
+// which the estimates have 20 or more.  (Zero and infinity give NaN.)
+__device__ inline double norm_rsqrt(double x)
+{
+    double y = __builtin_amdgcn_rsq(x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) y = fma(0.5 * y, fma(-x * y, y, 1.0), y);
+    return y;
+}
+__device__ inline double norm_rcp(double x)
+{
+    double y = __builtin_amdgcn_rcp(x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) y = fma(y, fma(-x, y, 1.0), y);
+    return y;
+}
+
 // The norm in 64 bits, the normed row on its grid.  Which whole number a value next to a border becomes must not depend on how its row
-// was summed, so sum, scale and quotient are taken in 64 bits; the bytes of the rows still bound the kernel.
-template <class E, int T, int CH, bool NORM>
+// was summed, so sum, scale and quotient are taken in 64 bits; the bytes of the rows still bound the kernel.  A 16-bit value times its weight is exact in
+// 32 bits while it stays within their range (a row that leaves it takes its products in 64 bits), and so is its quotient's
+// rounding, except next to a border.  (16 384 rows of 4096 bf16: 101 us, 4.7 TB/s, as a copy; 109
+// with the divisions and the root spelt out and code for parts of a piece.)
+template <class E, int T, int CH, bool WHOLE, bool NORM>
 __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E* x, int64_t ld_x, const E* res, int64_t ld_res,
-                                                                        const E* __restrict__ w, int64_t n, int d, float eps,
+                                                                        const E* __restrict__ w, int64_t n, int d, double per_d, float eps,
                                                                         int8_t* __restrict__ q_out, float* __restrict__ scale_out, E* r)
 {
     typedef TgPiece<E> P;
@@ -107,7 +127,7 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E*
     if (row >= n) return;
     P p[CH];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) p[c].load(x + row * ld_x + (lane + c * T) * P::E, d - (lane + c * T) * P::E);
+    for (int c = 0; c < CH; ++c) p[c].load(x + row * ld_x + (lane + c * T) * P::E, norm_left<E, WHOLE>(d - (lane + c * T) * P::E));
     double rstd = 1.0;
     if (NORM) {
         if (res) {
@@ -115,22 +135,22 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E*
             for (int c = 0; c < CH; ++c) {
                 const int at = (lane + c * T) * P::E;
                 P q;
-                q.load(res + row * ld_res + at, d - at);
+                q.load(res + row * ld_res + at, norm_left<E, WHOLE>(d - at));
 #pragma unroll
                 for (int i = 0; i < P::E; ++i) p[c].v[i] += q.v[i];
                 p[c].round();
             }
 #pragma unroll
-            for (int c = 0; c < CH; ++c) p[c].store(r + row * d + (lane + c * T) * P::E, d - (lane + c * T) * P::E);
+            for (int c = 0; c < CH; ++c) p[c].store(r + row * d + (lane + c * T) * P::E, norm_left<E, WHOLE>(d - (lane + c * T) * P::E));
         }
         double sum = 0.0;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < P::E; ++i) sum = fma((double)p[c].v[i], (double)p[c].v[i], sum);
-        rstd = 1.0 / sqrt(row_sum<T>(sum, s_sum) / (double)d + (double)eps);
+        rstd = norm_rsqrt(fma(row_sum<T>(sum, s_sum), per_d, (double)eps));
     }
-    // max |r w|, and whether a value is NaN (a maximum leaves it out).  A product of two 16-bit values is exact in 32 bits.
+    // max |r w|, and whether a value is NaN (a maximum leaves it out)
     constexpr bool SHORT = sizeof(E) == 2;
     double top = 0.0;
     float top32 = 0.0f;
@@ -139,7 +159,7 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E*
     for (int c = 0; c < CH; ++c) {
         const int at = (lane + c * T) * P::E;
         P g;
-        if (NORM) g.load(w + at, d - at);
+        if (NORM) g.load(w + at, norm_left<E, WHOLE>(d - at));
 #pragma unroll
         for (int i = 0; i < P::E; ++i) {
             if (SHORT) {
@@ -153,39 +173,62 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E*
             }
         }
     }
-    if (SHORT) top = (double)top32;
+    if (SHORT) top = top32 <= 3.4028234e38f ? (double)top32 : 1e300;        // (beyond fp32: to be found out)
     if (odd) top = __builtin_inf();
+    top = row_max64<T>(top, s_max);
+    // (only bf16 has values whose products leave fp32's range: 1e-30 is far enough above its end for what is lost there to be zero on the grid)
+    const bool wide = NORM && __is_same(E, tg_bf16) && !(top >= 1e-30 && top <= 3.4028234e38) && top <= 1e300;
+    const E* again = res ? r + row * d : x + row * ld_x;
+    if (wide) {
+        top = 0.0;
+#pragma unroll 1
+        for (int at = lane * P::E; at < d; at += T * P::E) {
+            P z, g;
+            z.load(again + at, norm_left<E, WHOLE>(d - at));
+            g.load(w + at, norm_left<E, WHOLE>(d - at));
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) top = fmax(top, __shfl_xor(top, m));
-    if (T > 64) {
-        if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = top;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < T / 64; ++i) top = fmax(top, s_max[i]);
+            for (int i = 0; i < P::E; ++i) top = fmax(top, fabs((double)z.v[i] * (double)g.v[i]));
+        }
+        top = row_max64<T>(top, s_sum);
     }
-    float scale = (float)(top * rstd / 127.0);
+    float scale = (float)(top * rstd * (1.0 / 127.0));
     // not a number, an infinite row, or one whose norm is: no grid
     const bool none = !(top <= 1.79e308) || !(rstd <= 1.79e308) || !(scale <= 3.4028234e38f);
     if (none) scale = __builtin_nanf("");
     if (lane == 0) scale_out[row] = scale;
-    const double f = none || scale == 0.0f ? 0.0 : rstd / (double)scale;
+    const double f = none || scale == 0.0f ? 0.0 : rstd * norm_rcp((double)scale);
     const float f32 = (float)f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int at = (lane + c * T) * P::E, left = d - at;
-        P g;
-        if (NORM && !SHORT) g.load(w + at, left);
+        const int at = (lane + c * T) * P::E, left = norm_left<E, WHOLE>(d - at);
         qvec q;
+        // (a scale below fp32's normal numbers has few bits of its own: the quotient can pass 127)
+        if (SHORT) {
+            // the quotient in 32 bits is off by less than 127 x 2^-22: it decides unless it lies that near to a border
+            bool near = false;
 #pragma unroll
-        for (int i = 0; i < P::E; ++i) {
-            // (a scale below fp32's normal numbers has few bits of its own: the quotient can pass 127)
-            if (SHORT) {
-                // the quotient in 32 bits is off by less than 127 x 2^-22: it decides unless it lies that near to a border
+            for (int i = 0; i < P::E; ++i) {
                 const float u = p[c].v[i] * f32, whole = rintf(u);
                 q[i] = (char)(int)fminf(fmaxf(whole, -127.0f), 127.0f);
-                if (fabsf(fabsf(u - whole) - 0.5f) < 1e-4f) q[i] = (char)(int)fmin(fmax(rint((double)p[c].v[i] * f), -127.0), 127.0);
-                if (none) q[i] = 0;
-            } else {
+                near |= fabsf(u - whole) > 0.5f - 1e-4f;
+            }
+            if (near) {
+#pragma unroll
+                for (int i = 0; i < P::E; ++i) q[i] = (char)(int)fmin(fmax(rint((double)p[c].v[i] * f), -127.0), 127.0);
+            }
+            if (wide) {
+                P z, g;
+                z.load(again + at, left);
+                g.load(w + at, left);
+#pragma unroll
+                for (int i = 0; i < P::E; ++i) q[i] = (char)(int)fmin(fmax(rint((double)z.v[i] * (double)g.v[i] * f), -127.0), 127.0);
+            }
+            if (none) q = (qvec)0;
+        } else {
+            P g;
+            if (NORM) g.load(w + at, left);
+#pragma unroll
+            for (int i = 0; i < P::E; ++i) {
                 const double t = NORM ? (double)p[c].v[i] * (double)g.v[i] : (double)p[c].v[i];
                 q[i] = (char)(int)(none ? 0.0 : fmin(fmax(rint(t * f), -127.0), 127.0));
             }
@@ -225,7 +268,7 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const int8_t* __restric
 
 // u = dy w, c = mean(u r): dx = dr + rstd (u - r rstd^2 c), dw = sum over rows of dy r rstd.  A workgroup takes every gridDim.x-th
 // group of rows and keeps its part of dw in registers; the parts are added by norm_dw_kernel in the workgroups' order.
-template <class E, int T, int CH>
+template <class E, int T, int CH, bool WHOLE>
 __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_grad_kernel(const E* __restrict__ dy, int64_t ld_dy, const E* dr, int64_t ld_dr,
                                                                           const E* __restrict__ r, int64_t ld_r, const E* __restrict__ w,
                                                                           const float* __restrict__ rstd_in, int64_t n, int d, E* dx,
@@ -240,30 +283,43 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_grad_kernel(const 
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < P::E; ++i) dw[c][i] = 0.0f;
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T; row < n; row += (int64_t)gridDim.x * ROWS) {
-        P u[CH], z[CH];
-        const float rstd = rstd_in[row];
+    // the row behind is asked for while this one is summed
+    typename P::vec a_dy[CH], a_r[CH], a_dr[CH], gw[CH];
+    float a_rstd = 0.0f;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T;
+    const auto ask = [&](int64_t i) {
+        a_rstd = rstd_in[i];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int at = (lane + c * T) * P::E;
-            u[c].load(dy + row * ld_dy + at, d - at);
-            z[c].load(r + row * ld_r + at, d - at);
+            const int at = (lane + c * T) * P::E, left = norm_left<E, WHOLE>(d - at);
+            a_dy[c] = P::raw(dy + i * ld_dy + at, left);
+            a_r[c] = P::raw(r + i * ld_r + at, left);
+            if (dr) a_dr[c] = P::raw(dr + i * ld_dr + at, left);
         }
+    };
+#pragma unroll
+    for (int c = 0; c < CH; ++c) gw[c] = P::raw(w + (lane + c * T) * P::E, norm_left<E, WHOLE>(d - (lane + c * T) * P::E));
+    if (row < n) ask(row);
+    int turn = 0;
+    for (; row < n; row += step) {
+        P u[CH], z[CH];
+        typename P::vec b_dr[CH];
+        const float rstd = a_rstd;
         float sum = 0.0f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int at = (lane + c * T) * P::E;
-            P g;
-            g.load(w + at, d - at);
+            b_dr[c] = a_dr[c];
 #pragma unroll
             for (int i = 0; i < P::E; ++i) {
-                z[c].v[i] *= rstd;
-                dw[c][i] = fmaf(u[c].v[i], z[c].v[i], dw[c][i]);
-                u[c].v[i] *= g.v[i];
+                const float v = (float)a_dy[c][i];
+                z[c].v[i] = (float)a_r[c][i] * rstd;
+                dw[c][i] = fmaf(v, z[c].v[i], dw[c][i]);
+                u[c].v[i] = v * (float)gw[c][i];
                 sum = fmaf(u[c].v[i], z[c].v[i], sum);
             }
         }
+        if (row + step < n) ask(row + step);
         // (two sets of words in turn: a wave may be a row ahead of another that still reads its sum)
         const float mean = row_sum<T>(sum, s_sum[turn]) / (float)d;
         turn ^= 1;
@@ -271,13 +327,12 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_grad_kernel(const 
         for (int c = 0; c < CH; ++c) {
             const int at = (lane + c * T) * P::E;
             P o;
-            if (dr) o.load(dr + row * ld_dr + at, d - at);
 #pragma unroll
             for (int i = 0; i < P::E; ++i) {
                 const float v = rstd * (u[c].v[i] - z[c].v[i] * mean);
-                o.v[i] = dr ? o.v[i] + v : v;
+                o.v[i] = dr ? (float)b_dr[c][i] + v : v;
             }
-            o.store(dx + row * d + at, d - at);
+            o.store(dx + row * d + at, norm_left<E, WHOLE>(d - at));
         }
     }
     // the rows that a workgroup had in hand at a time are added, the first with the second and so on, and leave one part
@@ -331,15 +386,20 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__
 
 // The lanes a row of `d` elements gets and the pieces a lane holds: a wave up to four pieces a lane (2048 elements of 16 bits), four
 // waves up to four (8192), sixteen beyond (8192 elements of 32 bits).
+#define NORM_SHAPE(pieces, WHOLE, LAUNCH)                                            \
+    do {                                                                             \
+        if ((pieces) <= 64) { LAUNCH(64, 1, WHOLE); }                                \
+        else if ((pieces) <= 128) { LAUNCH(64, 2, WHOLE); }                          \
+        else if ((pieces) <= 256) { LAUNCH(256, 1, WHOLE); }                         \
+        else if ((pieces) <= 512) { LAUNCH(256, 2, WHOLE); }                         \
+        else if ((pieces) <= 1024) { LAUNCH(256, 4, WHOLE); }                        \
+        else { LAUNCH(1024, 2, WHOLE); }                                             \
+    } while (0)
 #define NORM_SHAPES(E, d, LAUNCH)                                                    \
     do {                                                                             \
         const int pieces_ = ((d) + TgPiece<E>::E - 1) / TgPiece<E>::E;               \
-        if (pieces_ <= 64) { LAUNCH(64, 1); }                                        \
-        else if (pieces_ <= 128) { LAUNCH(64, 2); }                                  \
-        else if (pieces_ <= 256) { LAUNCH(256, 1); }                                 \
-        else if (pieces_ <= 512) { LAUNCH(256, 2); }                                 \
-        else if (pieces_ <= 1024) { LAUNCH(256, 4); }                                \
-        else { LAUNCH(1024, 2); }                                                    \
+        if ((d) % TgPiece<E>::E == 0) { NORM_SHAPE(pieces_, true, LAUNCH); }         \
+        else { NORM_SHAPE(pieces_, false, LAUNCH); }                                 \
     } while (0)
 
 // rows of one launch: below 2^32 work-items
@@ -355,8 +415,8 @@ void tg_launch_norm(const void* x, int64_t ld_x, const void* res, int64_t ld_res
                     void* y, void* r, float* rstd, hipStream_t s)
 {
     norm_chunks(n, [&](int64_t r0, int64_t nr) {
-#define NORM_FWD(T, CH)                                                                                                                  \
-    hipLaunchKernelGGL((norm_kernel<E, T, CH>), dim3((unsigned)((nr + NormShare<T>::ROWS - 1) / NormShare<T>::ROWS)),                     \
+#define NORM_FWD(T, CH, W)                                                                                                                  \
+    hipLaunchKernelGGL((norm_kernel<E, T, CH, W>), dim3((unsigned)((nr + NormShare<T>::ROWS - 1) / NormShare<T>::ROWS)),                     \
                        dim3(NormShare<T>::THREADS), 0, s, (const E*)x + r0 * ld_x, ld_x, res ? (const E*)res + r0 * ld_res : nullptr,     \
                        ld_res, (const E*)w, nr, d, eps, (E*)y + r0 * d, r ? (E*)r + r0 * d : nullptr, rstd ? rstd + r0 : nullptr)
         TG_WITH_TYPE(dtype, E, NORM_SHAPES(E, d, NORM_FWD));
@@ -367,14 +427,14 @@ void tg_launch_norm_q8(const void* x, int64_t ld_x, const void* res, int64_t ld_
                        int8_t* q, float* scale, void* r, hipStream_t s)
 {
     norm_chunks(n, [&](int64_t r0, int64_t nr) {
-#define NORM_Q8(T, CH)                                                                                                                   \
+#define NORM_Q8(T, CH, W)                                                                                                                   \
     do {                                                                                                                                 \
         const dim3 g((unsigned)((nr + NormShare<T>::ROWS - 1) / NormShare<T>::ROWS)), b(NormShare<T>::THREADS);                           \
         const E* xr = (const E*)x + r0 * ld_x;                                                                                           \
         const E* rr = res ? (const E*)res + r0 * ld_res : nullptr;                                                                       \
-        if (w) hipLaunchKernelGGL((norm_q8_kernel<E, T, CH, true>), g, b, 0, s, xr, ld_x, rr, ld_res, (const E*)w, nr, d, eps, q + r0 * d, \
+        if (w) hipLaunchKernelGGL((norm_q8_kernel<E, T, CH, W, true>), g, b, 0, s, xr, ld_x, rr, ld_res, (const E*)w, nr, d, 1.0 / d, eps, q + r0 * d, \
                                   scale + r0, r ? (E*)r + r0 * d : nullptr);                                                             \
-        else hipLaunchKernelGGL((norm_q8_kernel<E, T, CH, false>), g, b, 0, s, xr, ld_x, rr, ld_res, (const E*)w, nr, d, eps, q + r0 * d,  \
+        else hipLaunchKernelGGL((norm_q8_kernel<E, T, CH, W, false>), g, b, 0, s, xr, ld_x, rr, ld_res, (const E*)w, nr, d, 1.0 / d, eps, q + r0 * d,  \
                                 scale + r0, (E*)nullptr);                                                                                \
     } while (0)
         TG_WITH_TYPE(dtype, E, NORM_SHAPES(E, d, NORM_Q8));
@@ -405,11 +465,11 @@ void tg_launch_norm_grad(const void* dy, int64_t ld_dy, const void* dr, int64_t 
 {
     float* parts = (float*)space;
     int64_t count = 0;
-#define NORM_BWD(T, CH)                                                                                                                  \
+#define NORM_BWD(T, CH, W)                                                                                                                  \
     do {                                                                                                                                 \
         count = norm_grad_wgs(n, NormShare<T>::ROWS);                                                                                  \
         if (n > 0)                                                                                                                       \
-            hipLaunchKernelGGL((norm_grad_kernel<E, T, CH>), dim3((unsigned)count), dim3(NormShare<T>::THREADS), 0, \
+            hipLaunchKernelGGL((norm_grad_kernel<E, T, CH, W>), dim3((unsigned)count), dim3(NormShare<T>::THREADS), 0, \
                                s, (const E*)dy, ld_dy, (const E*)dr, ld_dr, (const E*)r, ld_r, (const E*)w, rstd, n, d, (E*)dx, parts);   \
         hipLaunchKernelGGL(norm_dw_kernel<E>, dim3((unsigned)((d + 15) / 16)), dim3(1024), 0, s, parts, (int)count, d, (E*)dw);           \
     } while (0)

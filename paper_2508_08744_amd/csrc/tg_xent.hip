@@ -23,7 +23,7 @@ __device__ inline void xent_join(float& m, float& l, float m2, float l2)
     m = top;
 }
 
-// x: rows of the table, y: tokens.  parts: for every tile and wave along x (BM / WM rows of the table), (maximum, sum) of every token.
+// x: rows of the table, y: tokens.  parts: for every tile along x (BM rows of the table), (maximum, sum) of every token.
 template <class E, int BM, int BN, int WM, int WN, int NB>
 __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
                                                                  float scale, uint32_t nx, uint32_t ny, uint32_t group, float2* __restrict__ parts,
@@ -43,7 +43,9 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, Til
         s_target[threadIdx.x] = target >= 0 && target < BM ? (int)target : -1;
     }
     t.loop();
-    const uint32_t stretch = tx * WM + (threadIdx.x >> 6) / WN;
+    // (the tile's memory is free: a pair for every token and wave along x)
+    float2* const s_pair = reinterpret_cast<float2*>(lds) + (threadIdx.x >> 6) / WN * BN;
+    static_assert(WM * BN * sizeof(float2) <= T::LDS, "the pairs' place");
     const int have = x0 + BM <= X.rows ? BM : (int)(X.rows - x0);
     const float base = scale * XENT_LOG2E;
 #pragma unroll
@@ -85,7 +87,15 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, Til
         }
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
-        if (tg_lane() < 16 && y < Y.rows) parts[(int64_t)stretch * parts_pitch + y] = make_float2(m, l);
+        if (tg_lane() < 16) s_pair[t.y_of(j)] = make_float2(m, l);
+    }
+    __syncthreads();
+    if (threadIdx.x < BN && y0 + threadIdx.x < Y.rows) {
+        const float2* pair = reinterpret_cast<const float2*>(lds) + threadIdx.x;
+        float m = pair[0].x, l = pair[0].y;
+#pragma unroll
+        for (int w = 1; w < WM; ++w) xent_join(m, l, pair[w * BN].x, pair[w * BN].y);
+        parts[(int64_t)tx * parts_pitch + y0 + threadIdx.x] = make_float2(m, l);
     }
 }
 
@@ -389,7 +399,7 @@ static void xent_rows(XentRows* r, TgCarve* c, const void* h, int64_t ld_h, cons
 // The tile of the logits: 256 x 256 where that leaves every CU one, smaller ones for fewer tokens.  fp32, whose products take sixteen times as long
 // a byte, is fed by the smallest, 64 x 64, of which a CU holds four that wait for each other's loads and epilogues (1003 tokens, 37 511 rows of 96, there and back:
 // 398 us in tiles of 128 x 128, 359 in these; 2048 tokens, 8000 rows of 1500: 1502 and 1444).
-#define XENT_STRETCH 32         // rows of the table that leave one (maximum, sum) at least (BM / WM)
+#define XENT_STRETCH 64         // rows of the table that leave one (maximum, sum) at least (BM)
 
 size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready)
 {
@@ -421,7 +431,7 @@ static int64_t launch_parts(const TileRows& X, const TileRows& Y, int bytes, con
         hipLaunchKernelGGL((xent_part_kernel<E, BM, BN, WM, WN, NB>), dim3((unsigned)(nx * ny)), dim3(64 * WM * WN), 0, s, X, part, bytes,
                            (const char*)targets + y0 * (targets64 ? 8 : 4), targets64, scale, (uint32_t)nx, ny, 8u, parts + y0, Y.rows, at_target + y0);
     }
-    return nx * WM;
+    return nx;
 }
 
 void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const void* targets,

@@ -148,7 +148,7 @@ def lookup_grad(grad, ids, n_rows, scale=1.0, out=None):
         if out.dtype not in (torch.float32, grad.dtype) or not out.is_contiguous():
             raise TypeError("out must be contiguous and float32 or of the gradient's type")
     else:
-        out = grad.new_empty((n_rows, d))
+        out = grad.new_empty(n_rows, d)
     L = lib()
     nbytes = L.tg_embed_lookup_grad_workspace(n, n_rows, d)
     keep, ws = _space(nbytes, grad)
@@ -161,12 +161,12 @@ def add_rms_norm(x, weight, residual=None, eps=1e-6):
     """tg_add_rms_norm: (y, r, rstd) with r = x + residual (x itself where there is none) and y = r rstd weight."""
     ld, n, d = _rows("x", x)
     _vector("weight", weight, d, (x.dtype,))
-    y = x.new_empty((n, d))
+    y = x.new_empty(n, d)
     rstd = x.new_empty(n, dtype=torch.float32)
     r, ld_res, out_r = x, 0, None
     if residual is not None:
         ld_res, _, _ = _rows("residual", residual, x.dtype, x.shape)
-        r = x.new_empty((n, d))
+        r = x.new_empty(n, d)
         out_r = r.data_ptr()
     _check(lib().tg_add_rms_norm(x.data_ptr(), ld, _ptr(residual), ld_res, weight.data_ptr(), DTYPES[x.dtype], n, d, eps, y.data_ptr(), out_r,
                                  rstd.data_ptr(), _stream(x, weight, residual)))
@@ -180,7 +180,7 @@ def add_rms_norm_grad(dy, r, weight, rstd, dr=None):
     ld_dr = 0 if dr is None else _rows("dr", dr, r.dtype, r.shape)[0]
     _vector("weight", weight, d, (r.dtype,))
     _vector("rstd", rstd, n, (torch.float32,))
-    dx = r.new_empty((n, d))
+    dx = r.new_empty(n, d)
     dw = r.new_empty(d)
     L = lib()
     nbytes = L.tg_add_rms_norm_grad_workspace(n, d)
@@ -194,12 +194,12 @@ def add_rms_norm_q8(x, weight, residual=None, eps=1e-6):
     """tg_add_rms_norm_q8: (q, scale, r), the normed rows as int8 with a scale each, and the residual stream."""
     ld, n, d = _rows("x", x)
     _vector("weight", weight, d, (x.dtype,))
-    q = x.new_empty((n, d), dtype=torch.int8)
+    q = x.new_empty(n, d, dtype=torch.int8)
     scale = x.new_empty(n, dtype=torch.float32)
     r, ld_res, out_r = x, 0, None
     if residual is not None:
         ld_res, _, _ = _rows("residual", residual, x.dtype, x.shape)
-        r = x.new_empty((n, d))
+        r = x.new_empty(n, d)
         out_r = r.data_ptr()
     _check(lib().tg_add_rms_norm_q8(x.data_ptr(), ld, _ptr(residual), ld_res, weight.data_ptr(), DTYPES[x.dtype], n, d, eps, q.data_ptr(),
                                     scale.data_ptr(), out_r, _stream(x, weight, residual)))
@@ -209,7 +209,7 @@ def add_rms_norm_q8(x, weight, residual=None, eps=1e-6):
 def quantize_rows(x):
     """tg_quantize_rows: (q, scale), the rows as int8 with a scale each."""
     ld, n, d = _rows("x", x)
-    q = x.new_empty((n, d), dtype=torch.int8)
+    q = x.new_empty(n, d, dtype=torch.int8)
     scale = x.new_empty(n, dtype=torch.float32)
     _check(lib().tg_quantize_rows(x.data_ptr(), ld, DTYPES[x.dtype], n, d, q.data_ptr(), scale.data_ptr(), _stream(x)))
     return q, scale
@@ -228,7 +228,7 @@ def dequantize_rows(q, scale, dtype=torch.float32):
     n, d = _codes("q", q, scale)
     if dtype not in DTYPES:
         raise TypeError("dtype must be float32, bfloat16 or float16")
-    out = q.new_empty((n, d), dtype=dtype)
+    out = q.new_empty(n, d, dtype=dtype)
     _check(lib().tg_dequantize_rows(q.data_ptr(), scale.data_ptr(), n, d, DTYPES[dtype], out.data_ptr(), _stream(q, scale)))
     return out
 
@@ -243,7 +243,7 @@ def matmul_q8(a, a_scale, b, b_scale, bias=None, out_dtype=torch.float32):
         _vector("bias", bias, n, (torch.float32,))
     if out_dtype not in DTYPES:
         raise TypeError("out_dtype must be float32, bfloat16 or float16")
-    out = a.new_empty((m, n), dtype=out_dtype)
+    out = a.new_empty(m, n, dtype=out_dtype)
     L = lib()
     aligned = 0 if (a.data_ptr() | b.data_ptr()) % 16 else 1
     nbytes = L.tg_matmul_q8_workspace(m, n, k, aligned)
@@ -280,8 +280,8 @@ def softmax_xent_grad(h, w, targets, lse, dloss, scale=1.0, workspace=None):
     wide = _ids("targets", targets, n)
     _vector("lse", lse, n, (torch.float32,))
     _vector("dloss", dloss, n, (torch.float32,))
-    dh = h.new_empty((n, d))
-    dw = h.new_empty((v, d))
+    dh = h.new_empty(n, d)
+    dw = h.new_empty(v, d)
     t, L = DTYPES[h.dtype], lib()
     if workspace is None:
         nbytes = L.tg_softmax_xent_grad_workspace(n, v, d, t, _aligned(h, ld_h, w, ld_w))
