@@ -215,12 +215,23 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
     }
     t.loop();
     const int have = x0 + BM <= X.rows ? BM : (int)(X.rows - x0), room = x0 + BM <= width ? BM : (int)(width - x0);
+    // A lane has four neighbours of 16 rows at a time; the tile goes through its memory, which is free, to be stored as whole rows.  Piece c of row r lies at
+    // place c ^ (r & SWAP): the lanes that write one column of pieces at a time are in different banks.
+    constexpr int W = 16 / (int)sizeof(E), PIECES = BM / W, SWAP = PIECES < 16 ? PIECES - 1 : 15;
+    static_assert(BM * BN * sizeof(E) <= T::LDS && (PIECES & (PIECES - 1)) == 0, "the tile's place");
+    typedef E four __attribute__((ext_vector_type(4)));
+    typedef E vec __attribute__((ext_vector_type(W)));
+    // (r & SWAP, whatever j)
+    int swap = threadIdx.x & SWAP;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
-        const int64_t y = y0 + t.y_of(j);
-        if (y >= Y.rows) continue;
-        const Token k = s_token[t.y_of(j)];
-        E* row = p + y * pitch + x0;
+        // (nothing of this is made out in front of the products, in whose loop no register is free)
+        asm volatile("" : "+v"(swap) : : "memory");
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) asm volatile("" : "+v"(t.acc[i][j]));
+        const int r = t.y_of(j);
+        const Token k = s_token[r];
+        char* const row = lds + r * (PIECES * 16);
 #pragma unroll
         for (int i = 0; i < T::FM; ++i) {
             const int x = t.x_of(i);
@@ -232,7 +243,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
                 for (int e = 0; e < 4; ++e)
                     if (x + e == k.hit) {
                         v[e] = (__builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], base, -k.b)) - 1.0f) * k.g;
-                        if (sizeof(E) == 2) lost[y] = v[e] - (float)(E)v[e];
+                        if (sizeof(E) == 2) lost[y0 + r] = v[e] - (float)(E)v[e];
                     }
             }
             if (!k.there || x + 4 > have) {
@@ -240,8 +251,17 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
                 for (int e = 0; e < 4; ++e)
                     if (!k.there || x + e >= have) v[e] = 0.0f;
             }
-            if (x < room) tile_put(row + x, v, room - x);
+            *reinterpret_cast<four*>(row + ((x / W) ^ swap) * 16 + x % W * (int)sizeof(E)) = four{(E)v[0], (E)v[1], (E)v[2], (E)v[3]};
         }
+    }
+    __syncthreads();
+    // (a row's room is whole pieces)
+    constexpr int THREADS = 64 * WM * WN;
+#pragma unroll 4
+    for (int at = threadIdx.x; at < BN * PIECES; at += THREADS) {
+        const int r = at / PIECES, piece = at % PIECES;
+        if (y0 + r < Y.rows && piece * W < room)
+            *reinterpret_cast<vec*>(p + (y0 + r) * pitch + x0 + piece * W) = *reinterpret_cast<const vec*>(lds + (r * PIECES + (piece ^ (r & SWAP))) * 16);
     }
 }
 
