@@ -516,11 +516,21 @@ static void xent_splits(XentGrad* g, int64_t n, int64_t n_rows, int d, int e)
     const auto tiles = [](int64_t x, int64_t y, int64_t side) { return ((x + side - 1) / side) * ((y + side - 1) / side); };
     g->few = tiles(n, d, 128) + tiles(g->piece, d, 128) <= 128;
     g->side = e == 2 && n > 128 && d > 128 && tiles(g->piece, d, 256) >= 200 ? 256 : g->few || e == 4 ? 64 : 128;
-    // dh in as many parts as fill the card, each with sixteen stages of the contraction or more (four where a stage is a load's way)
-    const int64_t fill = g->side == 256 ? 256 : g->few || g->side == 128 ? 512 : 1024, least = g->few ? 4 : 16;
+    // dh in as many parts as fill the card, each with sixteen stages of the contraction or more; where dw, beside it, has fewer, with as many as
+    // that, but four, up to 32 parts whose bytes are half of the table's (there and back, bf16: 7 tokens, 6938 rows of 688: 39.8 us with sixteen, 37.2;
+    // 900 tokens, 5000 rows of 700: 77.7 and 75.2)
+    const int64_t fill = g->side == 256 ? 256 : g->few || g->side == 128 ? 512 : 1024, dw_stages = (n * e + TILE_BYTES - 1) / TILE_BYTES;
+    const int64_t least = g->few || dw_stages < 4 ? 4 : dw_stages < 16 ? dw_stages : 16, light = g->piece * e / (8 * n);
     const int64_t dh = tiles(n, d, g->side), stages = (g->piece * e + TILE_BYTES - 1) / TILE_BYTES;
     int64_t s = (fill + dh - 1) / dh;
-    if (s > stages / least) s = stages / least;
+    const int64_t long_parts = stages / 16;
+    if (s > long_parts) {
+        int64_t more = stages / least;
+        if (!g->few && more > light) more = light;
+        if (!g->few && more > 32) more = 32;
+        if (more < long_parts) more = long_parts;
+        if (s > more) s = more;
+    }
     g->splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
     g->direct = g->splits == 1 && g->piece >= n_rows;
 }
