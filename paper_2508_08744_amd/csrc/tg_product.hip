@@ -4,7 +4,7 @@
 // tokens: tiles in LDS (tg_tiles.h), bound by the matrix instructions, or by the bytes of the output where rows are short.  A few
 // tokens: every byte of b is needed once and nothing else counts, so a wave reads its rows of b straight into the matrix
 // instructions' registers, with several loads in flight, and the waves of a workgroup share the contraction between them.
-// (8192 x 8192 x 4096: 240 us, 2.3 POP/s; 4 x 16 384 x 4096: 13 us, 5.2 TB/s.)
+// (8192 x 8192 x 4096 to bf16: 220 us, 2.5 POP/s; 4 x 16 384 x 4096: 13 us, 5.2 TB/s.)
 #include "tg_embed.h"
 #include "tg_tiles.h"
 
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(TileRows X, TileR
     if constexpr (sizeof(O) == 2) {
         // A lane has four neighbours, 8 bytes, of 16 rows at a time; the tile goes through its memory, which is free, to be stored as whole rows.  Piece c of
         // row r lies at place c ^ (r & SWAP): the lanes that write one column of pieces at a time are in different banks.
-        // (8192 x 8192 x 4096 to bf16: 267 us stored as the lanes have them, 254 so; 8000 x 4001 x 1024: 56 and 45.  Of fp32 a lane has 16 bytes.)
+        // (8192 x 8192 x 4096 to bf16: 236 us stored as the lanes have them, 222 so; 8000 x 4001 x 1024: 56 and 45.  Of fp32 a lane has 16 bytes.)
         constexpr int W = 8, PIECES = BM / W, SWAP = PIECES < 16 ? PIECES - 1 : 15;
         static_assert(BM * BN * sizeof(O) <= T::LDS && (PIECES & (PIECES - 1)) == 0, "the tile's place");
         typedef O four __attribute__((ext_vector_type(4)));
