@@ -205,13 +205,14 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E*
         qvec q;
         // (a scale below fp32's normal numbers has few bits of its own: the quotient can pass 127)
         if (SHORT) {
-            // the quotient in 32 bits is off by less than 127 x 2^-22: it decides unless it lies that near to a border
+            // the quotient in 32 bits is off by less than 127 x 2^-22: it decides unless it lies that near to a border, or is no finite number (a
+            // factor that fp32 does not hold, of rows that stay below 127 / 3.4e38)
             bool near = false;
 #pragma unroll
             for (int i = 0; i < P::E; ++i) {
                 const float u = p[c].v[i] * f32, whole = rintf(u);
                 q[i] = (char)(int)fminf(fmaxf(whole, -127.0f), 127.0f);
-                near |= fabsf(u - whole) > 0.5f - 1e-4f;
+                near |= !(fabsf(u - whole) <= 0.5f - 1e-4f);
             }
             if (near) {
 #pragma unroll
