@@ -25,11 +25,11 @@ __device__ inline void xent_join(float& m, float& l, float m2, float l2)
     m = top;
 }
 
-// x: rows of the table, y: tokens.  parts: for every tile along x (BM rows of the table), (maximum, sum) of every token.
+// x: rows of the table from v0 on, y: tokens.  parts: for every tile along x (BM rows of the table), (maximum, sum) of every token.
 template <class E, int BM, int BN, int WM, int WN, int NB>
 __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
-                                                                 float scale, uint32_t nx, uint32_t ny, uint32_t group, float2* __restrict__ parts,
-                                                                 int64_t parts_pitch, float* __restrict__ at_target)
+                                                                 float scale, int64_t v0, int64_t n_rows, uint32_t nx, uint32_t ny, uint32_t group,
+                                                                 float2* __restrict__ parts, int64_t parts_pitch, float* __restrict__ at_target)
 {
     typedef Tile<E, BM, BN, WM, WN, false, false, NB> T;
     __shared__ __align__(1024) char lds[T::LDS];
@@ -41,7 +41,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, Til
     T t;
     t.start(X, Y, x0, y0, 0, bytes, lds);
     if (threadIdx.x < BN) {
-        const int64_t y = y0 + threadIdx.x, target = y < Y.rows ? tg_row_of(targets, targets64, y, X.rows) - x0 : -1;
+        const int64_t y = y0 + threadIdx.x, target = y < Y.rows ? tg_row_of(targets, targets64, y, n_rows) - v0 - x0 : -1;
         s_target[threadIdx.x] = target >= 0 && target < BM ? (int)target : -1;
     }
     t.loop();
@@ -444,14 +444,19 @@ static int64_t launch_parts(const TileRows& X, const TileRows& Y, int bytes, con
                             float* at_target, hipStream_t s)
 {
     const int64_t nx = (X.rows + BM - 1) / BM;
-    // (as many tokens a launch as its work-items allow)
-    const int64_t most = TILE_LAUNCH_ITEMS / (64 * WM * WN) / nx * BN;
-    for (int64_t y0 = 0; y0 < Y.rows; y0 += most) {
-        const int64_t rows = Y.rows - y0 < most ? Y.rows - y0 : most;
-        const uint32_t ny = (uint32_t)((rows + BN - 1) / BN);
-        const TileRows part{Y.p + y0 * Y.pitch, rows, Y.pitch, Y.width};
-        hipLaunchKernelGGL((xent_part_kernel<E, BM, BN, WM, WN, NB>), dim3((unsigned)(nx * ny)), dim3(64 * WM * WN), 0, s, X, part, bytes,
-                           (const char*)targets + y0 * (targets64 ? 8 : 4), targets64, scale, (uint32_t)nx, ny, 8u, parts + y0, Y.rows, at_target + y0);
+    // as many tiles along the table as a launch's work-items allow (all of them up to 2^29 rows), then as many tokens
+    constexpr int64_t TILES = TILE_LAUNCH_ITEMS / (64 * WM * WN);
+    for (int64_t t0 = 0; t0 < nx; t0 += TILES) {
+        const int64_t tiles = nx - t0 < TILES ? nx - t0 : TILES, v0 = t0 * BM, most = TILES / tiles * BN;
+        const TileRows table{X.p + v0 * X.pitch, X.rows - v0 < tiles * BM ? X.rows - v0 : tiles * BM, X.pitch, X.width};
+        for (int64_t y0 = 0; y0 < Y.rows; y0 += most) {
+            const int64_t rows = Y.rows - y0 < most ? Y.rows - y0 : most;
+            const uint32_t ny = (uint32_t)((rows + BN - 1) / BN);
+            const TileRows part{Y.p + y0 * Y.pitch, rows, Y.pitch, Y.width};
+            hipLaunchKernelGGL((xent_part_kernel<E, BM, BN, WM, WN, NB>), dim3((unsigned)(tiles * ny)), dim3(64 * WM * WN), 0, s, table, part, bytes,
+                               (const char*)targets + y0 * (targets64 ? 8 : 4), targets64, scale, v0, X.rows, (uint32_t)tiles, ny, 8u,
+                               parts + t0 * Y.rows + y0, Y.rows, at_target + y0);
+        }
     }
     return nx;
 }

@@ -37,3 +37,25 @@ def test_rows_of_small_numbers_on_the_grid(t, tops, d):
     assert ((scale - top).abs() <= top * 2 * U + 2.0 ** -150).all() and (scale > 0).all()
     assert ((z / scale[:, None]).clamp(-127, 127) - q).abs().max() <= 0.5 + 1e-9
     assert (q[z == 0] == 0).all() and (q.abs().amax(1) == 127).all()
+
+
+# ---- many rows
+
+
+@pytest.mark.parametrize("n", [7, 70])
+def test_losses_over_more_than_half_of_2_to_the_30_rows(n):
+    """fp32 rows in tiles of 64: more tiles along the table than one launch has."""
+    v, d = (1 << 29) + 1000, 4
+    w = torch.zeros(v, d, device=DEV)
+    far = torch.tensor([0, 63, 1 << 28, (1 << 29) - 1, 1 << 29, (1 << 29) + 64, v - 1], device=DEV)
+    w[far] = torch.tensor([[20.0, 0, 0, 0], [21, 1, 0, 0], [0, 22, 0, 0], [21, 1, 1, 1], [22, 2, 0, 1], [0, 0, 24, 0], [0, 0, 0, 25]], device=DEV)
+    h = torch.rand(n, d, generator=torch.Generator().manual_seed(n)).to(DEV)
+    targets = far[torch.arange(n, device=DEV) % 7]
+    targets[5] = 12345
+    loss, lse = embed.softmax_xent(h, w, targets)
+    z = h.double() @ w[far].double().t().contiguous()
+    want = torch.log(torch.exp(z).sum(1) + (v - 7))
+    z_t = (h.double() * w[targets].double()).sum(1)
+    # a tile of equal terms is exact; a lane of the join adds a 256th of the tiles one after another; the far rows' logits and exponents: 400
+    tol = (v / 64 / 256 + 400) * U
+    assert ((lse.double() - want).abs() <= tol).all() and ((loss.double() - (want - z_t)).abs() <= 2 * tol).all()
