@@ -17,7 +17,7 @@
  * dtype: a tg_dtype.  Matrices are row-major; `ld` is the distance of two rows in elements, at least
  * the row length (a matrix without `ld` has its rows back to back); rows need no alignment beyond their
  * element's, 16-byte aligned ones are faster.  Sums, norms and softmax statistics are held in 32 bits or
- * more, results are rounded once.  Equal inputs give equal results, bit for bit: no sum depends on the
+ * more, results are rounded once (the softmax's gradient rounds an intermediate as well, see there).  Equal inputs give equal results, bit for bit: no sum depends on the
  * order in which workgroups arrive.
  */
 #ifndef TAGORE_EMBED_H
@@ -120,6 +120,9 @@ int tg_softmax_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
  * out_dh = P w (n x d) and out_dw = P^T h (n_rows x d), both of type dtype.  lse: what tg_softmax_xent gave, dloss: n
  * fp32, the gradient of every token's loss.  The table is taken in pieces, for each of which P is formed
  * (from the logits, computed again) in the type of the inputs and multiplied twice; a larger workspace than asked for makes larger pieces.
+ * So in 16 bits an entry of P is off by up to half a step of the type, except at a token's target, where what was rounded off is given back to
+ * both gradients; the result's own rounding comes on top.  In fp16 the P of all tokens is kept under one power of two: entries
+ * below 2^-27 of the largest |scale dloss| have steps of 2^-37 of it.
  */
 size_t tg_softmax_xent_grad_workspace(int64_t n, int64_t n_rows, int32_t d, int32_t dtype, int32_t aligned);
 int tg_softmax_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32_t dtype, int64_t n,

@@ -8,8 +8,9 @@
 // inputs' type, which goes to memory once (a piece is small enough to be read again while the last-level cache holds it) and into two products:
 // dh += P w over the piece's rows, dw = P^T h over the tokens.  The products read w, h and, for dw, P across their rows, through LDS
 // reads that turn them; no transposed copy is made.  dh is kept in fp32 over the pieces.  (The same step: 8 pieces of 285 us for P and 419 for both
-// products, 1.31 PFLOP/s.)  P in 16 bits is a choice for its bytes: its roundings are half a step of the type each and average out over a sum; the one
-// at the target, which outweighs the others, is given back.
+// products, 1.31 PFLOP/s.)  P in 16 bits is a choice for its bytes.  Its roundings are half a step of the type each; the one at a token's target,
+// the entry that outweighs the others together, is given back to both gradients.  Of the other entries' roundings as much remains in a sum as the sum keeps of the
+// entries themselves: a relative error like that of rounding the result, which comes on top.
 #include "tg_embed.h"
 #include "tg_tiles.h"
 
@@ -301,8 +302,150 @@ __device__ inline void xent_put_dh(const XentProducts& a, int64_t y, int x, floa
     }
     tile_put((E*)a.dh + y * a.d + x, v, a.d - x);
 }
-// tokens up to which dw too gets back what rounding took from P at the targets: of more the errors are many and average out
-#define XENT_LOST_TOKENS 32
+// What rounding took from P at the targets among a tile's rows, given back to dw's tile of 16-bit values: a row that is the target of few tokens is mostly
+// theirs, and their roundings are whole in it, whatever the number of tokens.  The tokens are looked through for targets among the rows; those found are
+// listed in their order, and 128 at a time (all is asked for at once) they are up to four more steps of the contraction, of their rows of h and of a matrix that
+// holds a token's lost part (rounded to the type: an error's error) in its target's row alone.  It is a chain of loads and barriers that nothing of the
+// tile overlaps: 8192 tokens, 131 072 rows of 1024, bf16: 7.53 ms there and back without it, 7.57 with it; 500, 30 000 of 512: 108 and 116 us; 900, 5000 of 700: 77 and 82.
+template <class E, int B, int THREADS>
+struct XentGiveBack {
+    static constexpr int WAVES = THREADS / 64, EACH = 16, CHUNK = EACH * THREADS;        // tokens that are looked through at a time
+    struct Lost { int row; float v; };
+    struct Memory {
+        Lost lost[128];
+        uint32_t counts[WAVES];
+        uint16_t mine[THREADS];              // (no register is free in the products' loop)
+        uint16_t list[CHUNK];                // token, from the chunk's first on
+    };
+    static_assert(CHUNK <= 1 << 16, "16 bits a token");
+    Memory& m;
+    const XentProducts& a;
+    const int64_t v0;                        // the tile's first row of the table, and its rows
+    const int rows;
+    __device__ inline XentGiveBack(Memory& m, const XentProducts& a, int64_t y0)
+        : m(m), a(a), v0(a.v0 + y0), rows(a.rows - y0 < B ? (int)(a.rows - y0) : B) {}
+
+    __device__ inline int row_of(int64_t token) const
+    {
+        const int64_t r = tg_row_of(a.targets, a.targets64, token, a.n_rows) - v0;
+        return r >= 0 && r < rows ? (int)r : -1;
+    }
+    // a wave's tokens of the chunk from c0 on, 64 at a time: an equal part each
+    __device__ inline int all_of(int64_t c0) const { return a.p.rows - c0 < CHUNK ? (int)(a.p.rows - c0) : CHUNK; }
+    __device__ inline int first_of(int64_t c0) const
+    {
+        return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * ((all_of(c0) + THREADS - 1) / THREADS * 64) + tg_lane();
+    }
+    // which of the lane's tokens have a target here, and how many each wave found
+    __device__ inline void look(int64_t c0)
+    {
+        const int all = all_of(c0), turns = (all + THREADS - 1) / THREADS, first = first_of(c0);
+        uint32_t mine = 0, count = 0;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int at = first + k * 64;
+            const bool hit = k < turns && at < all && row_of(c0 + at) >= 0;
+            mine |= hit ? 1u << k : 0u;
+            count += __popcll(__ballot(hit));
+        }
+        m.mine[threadIdx.x] = (uint16_t)mine;
+        if (tg_lane() == 0) m.counts[threadIdx.x >> 6] = count;
+    }
+    // behind a barrier: their list, which all waves have behind the next one, and its length
+    __device__ inline uint32_t list(int64_t c0)
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = first_of(c0);
+        uint32_t at = 0, found = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            at += w < wave ? m.counts[w] : 0;
+            found += m.counts[w];
+        }
+        if (m.counts[wave]) {
+            const uint32_t mine = m.mine[threadIdx.x];
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                const bool hit = mine >> k & 1;
+                const u64 hits = __ballot(hit);
+                if (hit) m.list[at + __popcll(hits & tg_lanemask_lt())] = (uint16_t)(first + k * 64);
+                at += __popcll(hits);
+            }
+        }
+        return found;
+    }
+    // Behind `look` for the first chunk, and the products.  lds: the tile's memory, which no wave reads any more.
+    template <class T>
+    __device__ inline void run(T& t, int64_t x0, char* lds)
+    {
+#ifdef __HIP_DEVICE_COMPILE__
+        typedef typename T::SX S;
+        typedef E vec __attribute__((ext_vector_type(8)));
+        static_assert(4 * S::BYTES <= T::LDS && S::DEPTH == 64, "two buffers of 64 rows of h, as the tile reads them");
+        const int lane = tg_lane(), q = lane >> 4;
+        for (int64_t c0 = 0;;) {
+            const uint32_t found = list(c0);
+            if (found) __syncthreads();
+            for (uint32_t s0 = 0; s0 < found; s0 += 128) {
+                const int have = found - s0 < 128 ? (int)(found - s0) : 128, steps = (have + 31) / 32;
+                constexpr int PIECES = B / 8, TURNS = 128 * PIECES / THREADS;     // pieces of a row of h, 8 columns each; half of them a unit's
+                static_assert(THREADS >= 128 && THREADS % PIECES == 0, "a lane a token, whole rows a turn");
+                // (everything is asked for before anything is waited for: places behind the list's end are its last token's, and become zeros)
+                const int r0 = threadIdx.x / PIECES, c = threadIdx.x % PIECES, column = (int)x0 * 2 + c * 16;
+                int64_t token[TURNS];
+#pragma unroll
+                for (int k = 0; k < TURNS; ++k) {
+                    const int r = k * (THREADS / PIECES) + r0;
+                    token[k] = c0 + m.list[s0 + (r < have ? r : have - 1)];
+                }
+                const int mine = (int)threadIdx.x < have ? threadIdx.x : have - 1;
+                const int64_t own = c0 + m.list[s0 + mine];
+                const float rounded = a.lost[own];
+                vec v[TURNS];
+#pragma unroll
+                for (int k = 0; k < TURNS; ++k)
+                    if (k * (THREADS / PIECES) < steps * 32)
+                        v[k] = *reinterpret_cast<const vec*>(a.h.p + token[k] * a.h.pitch + (column < (int)a.h.width ? column : 0));
+                const int row = row_of(own);
+                if (threadIdx.x < 128) m.lost[threadIdx.x] = Lost{(int)threadIdx.x < have ? row : -1, rounded};
+#pragma unroll
+                for (int k = 0; k < TURNS; ++k) {
+                    const int r = k * (THREADS / PIECES) + r0;
+                    if (k * (THREADS / PIECES) < steps * 32)
+                        *reinterpret_cast<vec*>(lds + ((r >> 6) * 2 + c / (PIECES / 2)) * S::BYTES + (r & 63) * S::ROW + ((c % (PIECES / 2)) ^ S::exchange(r)) * 16) =
+                            r < have && column < (int)a.h.width ? v[k] : vec{};
+                }
+                __syncthreads();
+                for (int g = 0; g < steps; ++g) {
+                    Lost l[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) l[e] = m.lost[g * 32 + q * 8 + e];
+                    tg_i32x4 one[T::FN];
+#pragma unroll
+                    for (int j = 0; j < T::FN; ++j) {
+                        const int y = t.y_of(j);
+                        vec o;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) o[e] = l[e].row == y ? (E)l[e].v : (E)0.0f;
+                        one[j] = __builtin_bit_cast(tg_i32x4, o);
+                    }
+#pragma unroll
+                    for (int i = 0; i < T::FM; ++i) {
+                        const tg_i32x4 x = t.r.sx.read(lds + ((g >> 1) * 2 + i / T::HM) * S::BYTES, t.r.wm * (T::HM * 16), i % T::HM, g & 1, lane);
+#pragma unroll
+                        for (int j = 0; j < T::FN; ++j) t.acc[i][j] = TileMul<E>::mul(x, one[j], t.acc[i][j]);
+                    }
+                }
+                __syncthreads();
+            }
+            c0 += CHUNK;
+            if (c0 >= a.p.rows) return;
+            __syncthreads();                        // (all have the counts)
+            look(c0);
+            __syncthreads();
+        }
+#endif
+    }
+};
 
 template <class E, int B, int WM, int WN, int NB>
 __global__ __launch_bounds__(64 * WM * WN) void xent_products_kernel(XentProducts a)
@@ -342,30 +485,14 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_products_kernel(XentProduct
     tile_place(tile_of_block(blockIdx.x - dh_all, a.dw_x * a.dw_y), a.dw_x, a.dw_y, 1, &tx, &ty);
     const int64_t x0 = (int64_t)tx * B, y0 = (int64_t)ty * B;
     TW t;
-    t.run(a.h, a.p, x0, y0, 0, a.h_bytes, lds);
-    if (sizeof(E) == 2 && a.p.rows <= XENT_LOST_TOKENS) {
-        const int64_t v0 = a.v0 + y0;
-        // (a lane a token: they are asked for at once)
-        const int lane = tg_lane();
-        const int64_t target = lane < a.p.rows ? tg_row_of(a.targets, a.targets64, lane, a.n_rows) - v0 : -1;
-        const int mine = target >= 0 && target < B ? (int)target : -1;
-        const float rounded = mine >= 0 ? a.lost[lane] : 0.0f;
-        for (uint64_t left = __ballot(mine >= 0); left; left &= left - 1) {
-            const int r = __builtin_ctzll(left), at = __builtin_amdgcn_readlane(mine, r);
-            const float l = __shfl(rounded, r);
-#pragma unroll
-            for (int j = 0; j < TW::FN; ++j)
-                if (t.y_of(j) == at) {
-#pragma unroll
-                    for (int i = 0; i < TW::FM; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int64_t x = x0 + t.x_of(i) + e;
-                            if (x < a.d) t.acc[i][j][e] = fmaf(l, (float)((const E*)(a.h.p + r * a.h.pitch))[x], t.acc[i][j][e]);
-                        }
-                }
-        }
-    }
+    if constexpr (sizeof(E) == 2) {
+        typedef XentGiveBack<E, B, 64 * WM * WN> GiveBack;
+        __shared__ typename GiveBack::Memory memory;
+        GiveBack back(memory, a, y0);
+        back.look(0);
+        t.run(a.h, a.p, x0, y0, 0, a.h_bytes, lds);
+        back.run(t, x0, lds);
+    } else t.run(a.h, a.p, x0, y0, 0, a.h_bytes, lds);
     const float down = a.c[1];
 #pragma unroll
     for (int j = 0; j < TW::FN; ++j) {

@@ -39,6 +39,56 @@ def test_rows_of_small_numbers_on_the_grid(t, tops, d):
     assert (q[z == 0] == 0).all() and (q.abs().amax(1) == 127).all()
 
 
+# ---- gradients of rows that are targets
+
+def _least(h, w, targets, f):
+    """The smallest workspace that the gradient takes, by asking."""
+    with pytest.raises(embed.TagoreError, match="needed") as e:
+        embed.softmax_xent_grad(h, w, targets, f, f, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+    return torch.empty(int(str(e.value).split(" given, ")[1].split(" ")[0]), dtype=torch.uint8, device=DEV)
+
+
+@pytest.mark.parametrize("t", [BF16, F16])
+@pytest.mark.parametrize("n,v,d", [(20, 3000, 40), (33, 3000, 72), (300, 5000, 72), (300, 20_000, 136), (300, 20_000, 600), (9000, 2500, 64)])
+def test_rounding_at_the_target_is_given_back(t, n, v, d):
+    """P is rounded to 16 bits, but not where it outweighs all else: at a token's target.  The bound has half a step for the other entries, the square of
+    one there, and the result's own rounding; a whole step, as it would be with both, does not pass."""
+    g = torch.Generator().manual_seed(n + v + d)
+    h = torch.randn(n, d, generator=g).to(t)
+    w = (torch.randn(v, d, generator=g) * 0.1 / math.sqrt(d)).to(t)
+    for alone in (True, False):
+        if alone and n > v:
+            continue
+        # a row for every token; or a few rows that take most of them
+        targets = torch.randperm(v, generator=g)[:n] if alone else (torch.rand(n, generator=g) ** 6 * v).long()
+        targets[::11] = -1
+        dloss = 0.5 + torch.rand(n, generator=g)
+        hd, wd, i = h.to(DEV), w.to(DEV), targets.to(DEV)
+        loss, lse = embed.softmax_xent(hd, wd, i)
+        there = i >= 0
+        z = hd.double() @ wd.double().t().contiguous()
+        p = torch.softmax(z, 1)
+        gw = torch.where(there, dloss.to(DEV).double(), 0.0)[:, None]
+        at = i.clamp_min(0)[:, None]
+        hit = torch.zeros_like(p).scatter_(1, at, 1.0)
+        e = half_step(t)
+        # the logits are off by a chain of d additions, the exponential by its argument's rounding and its own
+        dz = (hd.double().abs() @ wd.double().abs().t().contiguous()).amax() * (d + 3) * U
+        de = 2 * dz + 4 * U * (lse.double().abs().amax() + z.abs().amax()) * math.log2(math.e) + 130 * U
+        off = (p * (e * (1 + de) + 2 * de) * (1 - hit) + hit * (e * e + 4 * U + p * 2 * de)) * gw
+        if t == F16:
+            off = off + 2.0 ** -25 * 2.0 ** -13 * gw.max()
+        pt = ((p - hit) * gw).t().contiguous()
+        want = pt @ hd.double()
+        bound = off.t().contiguous() @ hd.double().abs() + pt.abs() @ hd.double().abs() * (n + 8) * U
+        tol = bound + e * (want.abs() + bound) + torch.finfo(t).tiny
+        for ws in (None, _least(hd, wd, i, lse)):
+            dh, dw = embed.softmax_xent_grad(hd, wd, i, lse, dloss.to(DEV), workspace=ws)
+            assert ((dw.double() - want).abs() <= tol).all()
+            again = embed.softmax_xent_grad(hd, wd, i, lse, dloss.to(DEV), workspace=ws)
+            assert torch.equal(dw, again[1]) and torch.equal(dh, again[0])
+
+
 # ---- many rows
 
 
