@@ -17,8 +17,8 @@
  * dtype: a tg_dtype.  Matrices are row-major; `ld` is the distance of two rows in elements, at least
  * the row length (a matrix without `ld` has its rows back to back); rows need no alignment beyond their
  * element's, 16-byte aligned ones are faster.  Sums, norms and softmax statistics are held in 32 bits or
- * more, results are rounded once (the softmax's gradient rounds an intermediate as well, see there).  Equal inputs give equal results, bit for bit: no sum depends on the
- * order in which workgroups arrive.
+ * more, results are rounded once (the softmax's gradient rounds an intermediate as well, see there).  Equal
+ * inputs give equal results, bit for bit: no sum depends on the order in which workgroups arrive.
  */
 #ifndef TAGORE_EMBED_H
 #define TAGORE_EMBED_H
@@ -55,7 +55,7 @@ int tg_embed_lookup_grad(const void* grad, int64_t ld, int32_t dtype, const void
  * r = x + residual, rounded to the type of x (residual = NULL: r = x, and out_r is not written and may be
  * NULL); rstd = 1 / sqrt(mean(r^2) + eps); out_y = r * rstd * weight.  x, residual: n x d of type dtype;
  * weight: d of the same type; out_y, out_r: n x d; out_rstd: n fp32, or NULL.  out_r may be x or residual
- * itself.  0 <= n < 2^30, 1 <= d <= 8192, eps >= 0.
+ * itself where that one's rows are back to back (refused otherwise: rows still to be read would be written over).  0 <= n < 2^30, 1 <= d <= 8192, eps >= 0.
  */
 int tg_add_rms_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, const void* weight,
                     int32_t dtype, int64_t n, int32_t d, float eps, void* out_y, void* out_r, float* out_rstd,

@@ -103,6 +103,12 @@ static int check_norm(const void* x, int64_t ld_x, const void* residual, int64_t
     if (residual) CHECK(check_ld("ld_residual", ld_residual, d));
     return n > 0 && !x ? null_argument() : TG_OK;
 }
+// out_r in place of x or the residual: its rows are d apart, so theirs have to be
+static int check_in_place(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, const void* out_r, int64_t n, int32_t d)
+{
+    if (!residual || n < 2 || !((out_r == x && ld_x != d) || (out_r == residual && ld_residual != d))) return TG_OK;
+    return tg_fail(TG_ERR_INVALID_ARG, "out_r is an input whose rows are not back to back");
+}
 static int check_eps(float eps)
 {
     return eps >= 0.0f && eps <= 3.4028234e38f ? TG_OK : tg_fail(TG_ERR_INVALID_ARG, "eps must be finite and not below 0");
@@ -115,6 +121,7 @@ extern "C" int tg_add_rms_norm(const void* x, int64_t ld_x, const void* residual
     CHECK(check_eps(eps));
     if (n == 0) return TG_OK;
     if (!weight || !out_y || (residual && !out_r)) return null_argument();
+    CHECK(check_in_place(x, ld_x, residual, ld_residual, out_r, n, d));
     tg_launch_norm(x, ld_x, residual, ld_residual, weight, dtype, n, d, eps, out_y, out_r, out_rstd, stream_of(stream));
     return launched("norm");
 }
@@ -143,6 +150,7 @@ extern "C" int tg_add_rms_norm_q8(const void* x, int64_t ld_x, const void* resid
     CHECK(check_eps(eps));
     if (n == 0) return TG_OK;
     if (!weight || !out_q || !out_scale || (residual && !out_r)) return null_argument();
+    CHECK(check_in_place(x, ld_x, residual, ld_residual, out_r, n, d));
     tg_launch_norm_q8(x, ld_x, residual, ld_residual, weight, dtype, n, d, eps, out_q, out_scale, out_r, stream_of(stream));
     return launched("norm to 8 bits");
 }

@@ -89,6 +89,29 @@ def test_rounding_at_the_target_is_given_back(t, n, v, d):
             assert torch.equal(dw, again[1]) and torch.equal(dh, again[0])
 
 
+# ---- in place
+
+@pytest.mark.parametrize("which", ["x", "residual"])
+def test_the_residual_stream_in_place(which):
+    """Through the C boundary: out_r is one of the inputs, with its rows back to back, or its only row at any distance."""
+    L = embed.lib()
+    g = torch.Generator().manual_seed(3)
+    for n, d, ld in ((40, 96, 96), (1, 96, 100), (3000, 520, 520)):
+        x, res = torch.randn(n, d, generator=g).to(DEV), torch.randn(n, d, generator=g).to(DEV)
+        w = torch.rand(d, generator=g).to(DEV)
+        want_y, want_r, want_rstd = embed.add_rms_norm(x, w, residual=res)
+        want_q, want_scale, _ = embed.add_rms_norm_q8(x, w, residual=res)
+        for form in ("norm", "q8"):
+            a, b = x.clone(), res.clone()
+            r, ld_x, ld_res = (a, ld, d) if which == "x" else (b, d, ld)
+            out, f = torch.empty_like(x) if form == "norm" else torch.empty_like(want_q), torch.empty(n, device=DEV)
+            head = [a.data_ptr(), ld_x, b.data_ptr(), ld_res, w.data_ptr(), 0, n, d, 1e-6, out.data_ptr()]
+            stream = torch.cuda.current_stream().cuda_stream
+            rc = L.tg_add_rms_norm(*head, r.data_ptr(), f.data_ptr(), stream) if form == "norm" else L.tg_add_rms_norm_q8(*head, f.data_ptr(), r.data_ptr(), stream)
+            assert rc == 0 and torch.equal(r, want_r)
+            assert torch.equal(out, want_y if form == "norm" else want_q) and torch.equal(f, want_rstd if form == "norm" else want_scale)
+
+
 # ---- many rows
 
 
