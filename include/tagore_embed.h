@@ -104,6 +104,7 @@ int tg_matmul_q8(const int8_t* a, const float* a_scale, const int8_t* b, const f
  * Softmax cross entropy of n rows against all n_rows rows of a table, without the n x n_rows logits:
  *   z[t][v] = scale * <h[t], w[v]>,  lse[t] = log sum_v exp(z[t][v]),  loss[t] = lse[t] - z[t][targets[t]].
  * A target outside [0, n_rows) is none: the token's loss is 0 and it has no part in any gradient.
+ * Infinite logits count as they are (lse is then infinite, the loss of an infinite target NaN or infinite); a NaN among a token's makes both NaN.
  * h: n x d, w: n_rows x d, both of type dtype; targets: n whole numbers of 32 bits, or of 64 where targets64 is 1;
  * out_loss, out_lse: n fp32.  0 <= n < 2^28, 1 <= n_rows < 2^30, 1 <= d <= 8192.
  * aligned: 1 where h and w start at a multiple of 16 bytes and their rows are a multiple of 16 bytes (of at most 1 MiB)

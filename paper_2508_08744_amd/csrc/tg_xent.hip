@@ -18,11 +18,26 @@
 
 __device__ inline float xent_exp(float x) { return __builtin_amdgcn_exp2f(x * XENT_LOG2E); }
 
+// Up to here exp(z - m) is 2 to the power of one multiply-add, z log2(e) - m log2(e), whose rounding is that of its terms: 2^-7 at this size, and beyond it
+// more and more, up to results that overflow.  Logits (or a scale) beyond it take the difference first: in the place of the products it makes the
+// exponents, to be taken with a factor of 1 and nothing subtracted, so that what follows is the same for both.
+#define XENT_NEAR 65536.0f
+__device__ inline bool xent_near(float m, float base) { return fabsf(m) < XENT_NEAR && fabsf(base) <= 3.4028234e38f; }
+// m: the largest logit, or lse: one that is infinite is taken in by its equals alone; a NaN stays one
+__device__ inline float xent_far(float product, float scale, float m)
+{
+    // (the logit is rounded before the difference, as m was: one multiply-add of both would leave m's rounding, which is large here)
+#pragma clang fp contract(off)
+    asm volatile("" : "+v"(product));        // (nothing of this is made out where it is not needed)
+    const float z = product * scale;
+    return z == m ? (m == -__builtin_inff() ? m : 0.0f) : (z - m) * XENT_LOG2E;
+}
+
 // (maximum, sum) pairs: one that stands for nothing is (-infinity, 0)
 __device__ inline void xent_join(float& m, float& l, float m2, float l2)
 {
     const float top = fmaxf(m, m2);
-    l = (m == -__builtin_inff() ? l : l * xent_exp(m - top)) + (m2 == -__builtin_inff() ? l2 : l2 * xent_exp(m2 - top));
+    l = (m == top ? l : l * xent_exp(m - top)) + (m2 == top ? l2 : l2 * xent_exp(m2 - top));
     m = top;
 }
 
@@ -50,6 +65,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, Til
     float2* const s_pair = reinterpret_cast<float2*>(lds) + (threadIdx.x >> 6) / WN * BN;
     static_assert(WM * BN * sizeof(float2) <= T::LDS, "the pairs' place");
     const int have = x0 + BM <= X.rows ? BM : (int)(X.rows - x0);
+    const int none = (threadIdx.x >> 6) / WN * (T::HM * 16);        // the wave's first row: where the table ends before it there are no logits
     const float base = scale * XENT_LOG2E;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
@@ -75,17 +91,24 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, Til
         }
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
-        const float b = (m == -__builtin_inff() ? 0.0f : m) * XENT_LOG2E;
+        const bool near = xent_near(m, base) || have <= none;
+        const float f = near ? base : 1.0f, b = near ? m * XENT_LOG2E : 0.0f;
+        if (__builtin_expect(!__all(near), 0)) {           // (out of the way: code that is jumped over is fetched late)
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t.acc[i][j][e] = near ? t.acc[i][j][e] : xent_far(t.acc[i][j][e], scale, m);
+        }
 #pragma unroll
         for (int i = 0; i < T::FM; ++i) {
             const int x = t.x_of(i);
             if (x + 4 <= have) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], base, -b));
+                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], f, -b));
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (x + e < have) l += __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], base, -b));
+                    if (x + e < have) l += __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], f, -b));
             }
         }
         l += __shfl_xor(l, 16);
@@ -199,7 +222,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
     __shared__ __align__(1024) char lds[T::LDS];
     // what a token's logits become P with: its target among the tile's rows, its factor and its lse.  A token without a target has no part in
     // anything, whatever its logits are.
-    struct Token { int hit, there; float g, b; };
+    struct Token { int hit, there; float g, b; };                // there: 0 without a target, 1, or 2 with an lse that is not near, which b then is as it is
     __shared__ Token s_token[BN];
     const float up = c[0], base = scale * XENT_LOG2E;
     uint32_t tx, ty;
@@ -212,7 +235,9 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
         Token k{target >= 0 && hit >= 0 && hit < BM ? (int)hit : -1, target >= 0, 0.0f, 0.0f};
         if (target >= 0) {
             k.g = dloss[y] * scale * up;
-            k.b = lse[y] * XENT_LOG2E;
+            const bool near = xent_near(lse[y], base);
+            k.there = near ? 1 : 2;
+            k.b = near ? lse[y] * XENT_LOG2E : lse[y];
         }
         s_token[threadIdx.x] = k;
     }
@@ -234,18 +259,26 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
         for (int i = 0; i < T::FM; ++i) asm volatile("" : "+v"(t.acc[i][j]));
         const int r = t.y_of(j);
         const Token k = s_token[r];
+        const bool near = k.there < 2;
+        const float f = near ? base : 1.0f, b = near ? k.b : 0.0f;
+        if (__builtin_expect(!__all(near), 0)) {           // (out of the way: code that is jumped over is fetched late)
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t.acc[i][j][e] = near ? t.acc[i][j][e] : xent_far(t.acc[i][j][e], scale, k.b);
+        }
         char* const row = lds + r * (PIECES * 16);
 #pragma unroll
         for (int i = 0; i < T::FM; ++i) {
             const int x = t.x_of(i);
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], base, -k.b)) * k.g;
+            for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], f, -b)) * k.g;
             if ((unsigned)(k.hit - x) < 4u) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (x + e == k.hit) {
-                        v[e] = (__builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], base, -k.b)) - 1.0f) * k.g;
+                        v[e] = (__builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], f, -b)) - 1.0f) * k.g;
                         if (sizeof(E) == 2) lost[y0 + r] = v[e] - (float)(E)v[e];
                     }
             }

@@ -89,6 +89,68 @@ def test_rounding_at_the_target_is_given_back(t, n, v, d):
             assert torch.equal(dw, again[1]) and torch.equal(dh, again[0])
 
 
+# ---- infinite and huge logits
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("n,v,d", [(1, 40, 8), (9, 700, 16), (40, 30_000, 8), (70, 300, 24), (300, 2100, 8), (300, 50_000, 40)])
+def test_infinite_and_huge_logits(t, n, v, d):
+    """One column of h and w makes the logits, so that they are exact products; lse and loss are the definition's, infinities and NaN among them."""
+    g = torch.Generator().manual_seed(n + v)
+    w = torch.zeros(v, d)
+    w[:, 3] = torch.rand(v, generator=g) + 0.5
+    w[::3, 3] *= -1
+    w = w.to(t)
+    targets = torch.randint(0, v, (n,), generator=g)
+    for column, scale in ((float("inf"), 1.0), (float("nan"), 1.0), (2.0, 1.0), (2.0, 1e38), (-2.0, 1.1e38), (2.0, 3e38), (1.5, 3e30), (float("inf"), -1.0)):
+        h = torch.zeros(n, d)
+        h[:, 3] = 1.0
+        h[n // 2:, 3] = column
+        only = w.clone()
+        if scale > 1e30:
+            only[1:, 3] *= 2.0 ** -10                      # one row alone is far out
+        for ww in (w, only, w.abs()):
+            z = (h.to(t)[:, 3:4] * ww[:, 3].float()).float() * torch.tensor(scale)       # (fp32: a product of two 16-bit values is exact)
+            lse = torch.logsumexp(z.double(), 1)
+            loss = (lse - z.double().gather(1, targets[:, None])[:, 0]).float().double()
+            lse = lse.float().double()                     # (what fp32 does not hold is infinite)
+            got_loss, got_lse = (x.cpu().double() for x in embed.softmax_xent(h.to(t).to(DEV), ww.to(DEV), targets.to(DEV), scale=scale))
+            for got, want, size in ((got_lse, lse, lse.abs()), (got_loss, loss, lse.abs() + loss.abs())):
+                odd = ~torch.isfinite(want)
+                assert torch.equal(torch.nan_to_num(got[odd], nan=7.0), torch.nan_to_num(want[odd], nan=7.0))
+                # the exponents' arguments and lse are rounded at the size of the logits
+                bound = 8 * U * (size + torch.where(torch.isfinite(z), z.abs(), 0.0).amax(1).double()) + 200 * U
+                assert ((got - want).abs() <= bound)[~odd].all()
+
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("n,v", [(3, 40), (40, 3000), (300, 2100), (300, 30_000)])
+def test_gradient_of_huge_logits(t, n, v):
+    """One row is far above the others: it has the whole softmax, exactly."""
+    g = torch.Generator().manual_seed(n)
+    w = torch.zeros(v, 8)
+    w[:, 3] = torch.rand(v, generator=g) * 2.0 ** -10
+    w[v // 2, 3] = 1.5
+    w = w.to(t)
+    h = torch.zeros(n, 8)
+    h[:, 3] = 1.0
+    targets = torch.randint(0, v, (n,), generator=g)
+    targets[1] = v // 2
+    for scale in (1e6, 3e9, 1e12, 1e30, 2e38):
+        hd, wd, i = h.to(t).to(DEV), w.to(DEV), targets.to(DEV)
+        loss, lse = embed.softmax_xent(hd, wd, i, scale=scale)
+        # (the power of two next to 1 / scale: the factor is a short number, and what P is rounded to of it is given back or nothing)
+        dloss = torch.full((n,), 2.0 ** -round(math.log2(scale)))
+        dh, dw = embed.softmax_xent_grad(hd, wd, i, lse, dloss.to(DEV), scale=scale)
+        f = (dloss * torch.tensor(scale)).double()
+        p = torch.zeros(n, v, dtype=torch.float64)
+        p[:, v // 2] = 1
+        p[torch.arange(n), targets] -= 1
+        p *= f[:, None]
+        e = half_step(t)
+        for got, want, size in ((dh, p @ w.double(), p.abs() @ w.double()), (dw, p.t() @ h.double(), p.abs().t() @ h.double())):
+            assert ((got.cpu().double() - want).abs() <= size * (e + (n + 8) * U) + e * want.abs() + torch.finfo(t).tiny).all()
+
+
 # ---- in place
 
 @pytest.mark.parametrize("which", ["x", "residual"])
