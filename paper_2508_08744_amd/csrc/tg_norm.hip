@@ -55,6 +55,7 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_kernel(const E* x,
 {
     typedef TgPiece<E> P;
     __shared__ float s_sum[16];
+    __shared__ double s_sum64[16];
     const int lane = threadIdx.x % T;
     const int64_t row = (int64_t)blockIdx.x * NormShare<T>::ROWS + threadIdx.x / T;
     if (row >= n) return;                                   // (whole waves: with T > 64 a workgroup has one row)
@@ -79,7 +80,20 @@ __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_kernel(const E* x,
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < P::E; ++i) sum = fmaf(p[c].v[i], p[c].v[i], sum);
-    const float rstd = 1.0f / sqrtf(row_sum<T>(sum, s_sum) / (float)d + eps);
+    const float mean = row_sum<T>(sum, s_sum) / (float)d + eps;
+    float rstd = 1.0f / sqrtf(mean);
+    // (squares that leave fp32's range, above or below: rows beyond 1.8e19, or of less than 1e-15 under no eps to speak of)
+    if (__builtin_expect(!(mean >= 0x1p-100f && mean <= 3.4028234e38f), 0)) {
+        double sum64 = 0.0;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < P::E; ++i) {
+                asm volatile("" : "+v"(p[c].v[i]));        // (nothing of this is made out where it is not needed)
+                sum64 = fma((double)p[c].v[i], (double)p[c].v[i], sum64);
+            }
+        rstd = (float)(1.0 / sqrt(row_sum<T>(sum64, s_sum64) / d + (double)eps));
+    }
     if (rstd_out && lane == 0) rstd_out[row] = rstd;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {

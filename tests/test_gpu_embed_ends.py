@@ -151,6 +151,34 @@ def test_gradient_of_huge_logits(t, n, v):
             assert ((got.cpu().double() - want).abs() <= size * (e + (n + 8) * U) + e * want.abs() + torch.finfo(t).tiny).all()
 
 
+# ---- norms of rows whose squares leave fp32's range
+
+@pytest.mark.parametrize("d", [8, 77, 960, 1024, 2056, 4100, 8192])
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_norm_of_huge_and_tiny_rows(t, d):
+    g = torch.Generator().manual_seed(d)
+    size = torch.tensor([1.0, 1e17, 3e18, 2e19, 1e25, 1.5e38, 1e-18, 1e-20, 1e-23, 1e-30, 1e-37])
+    x = ((0.5 + torch.rand(len(size), d, generator=g)) * torch.where(torch.rand(len(size), d, generator=g) < 0.5, -1.0, 1.0) * size[:, None]).to(t)
+    w = (1 + 0.2 * torch.randn(d, generator=g)).to(t)
+    z = x.double()
+    for eps in (0.0, 1e-6, 1e-38):
+        eps = torch.tensor(eps, dtype=F32).item()
+        rstd = 1.0 / torch.sqrt((z * z).mean(1, keepdim=True) + eps)
+        y = z * rstd * w.double()
+        for res in (None, torch.zeros_like(x)):
+            got_y, got_r, got_rstd = embed.add_rms_norm(x.to(DEV), w.to(DEV), residual=None if res is None else res.to(DEV), eps=eps)
+            # (64: the longest chain of a row's sum and a few roundings; a subnormal rstd has a step of 2^-149)
+            assert ((got_rstd.cpu().double() - rstd[:, 0]).abs() <= rstd[:, 0] * 64 * U + 2.0 ** -149).all()
+            assert ((got_y.cpu().double() - y).abs() <= y.abs() * (68 * U + half_step(t)) + torch.finfo(t).tiny).all()
+            assert torch.equal(got_r.cpu(), x)
+    # a row that is not finite, and one of zeros
+    x[0, 0], x[1, d - 1] = float("nan"), float("inf")
+    x[2] = 0
+    y, _, rstd = embed.add_rms_norm(x.to(DEV), w.to(DEV))
+    y, rstd = y.cpu(), rstd.cpu()
+    assert torch.isnan(y[0]).all() and torch.isnan(rstd[0]) and rstd[1] == 0 and torch.isnan(y[1, d - 1]) and (y[1, :d - 1] == 0).all() and (y[2] == 0).all()
+
+
 # ---- in place
 
 @pytest.mark.parametrize("which", ["x", "residual"])
