@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(const E* __restrict__ table
             P p;
             p.load(table + (v < 0 ? 0 : v) * ld + at, v < 0 ? 0 : d - at);
 #pragma unroll
-            for (int i = 0; i < P::E; ++i) p.v[i] *= scale;
+            for (int i = 0; i < P::E; ++i) p.v[i] *= v < 0 ? 0.0f : scale;       // (no row is zero at any scale)
             p.store(out + t * d + at, d - at);
         }
     }

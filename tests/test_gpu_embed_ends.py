@@ -179,6 +179,18 @@ def test_norm_of_huge_and_tiny_rows(t, d):
     assert torch.isnan(y[0]).all() and torch.isnan(rstd[0]) and rstd[1] == 0 and torch.isnan(y[1, d - 1]) and (y[1, :d - 1] == 0).all() and (y[2] == 0).all()
 
 
+# ---- lookup
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+def test_no_row_is_zero_at_any_scale(t):
+    table = torch.randn(20, 50, generator=torch.Generator().manual_seed(1)).to(t).to(DEV)
+    ids = torch.tensor([-1, 3, 20, 1 << 40, 7], device=DEV)
+    for scale in (float("inf"), -float("inf"), float("nan"), -2.0, 3e38):
+        out = embed.lookup(table, ids, scale=scale).float()
+        assert (out[[0, 2, 3]] == 0).all() and not torch.signbit(out[[0, 2, 3]]).any()
+        assert torch.equal(torch.nan_to_num(out[[1, 4]], nan=7.0), torch.nan_to_num((table[[3, 7]].float() * scale).to(t).float(), nan=7.0))
+
+
 # ---- in place
 
 @pytest.mark.parametrize("which", ["x", "residual"])
