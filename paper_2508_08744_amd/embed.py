@@ -137,7 +137,7 @@ def lookup_grad(grad, ids, n_rows, scale=1.0, out=None):
     """
     wide = _ids("ids", ids)
     n = ids.numel()
-    if isinstance(grad, torch.Tensor) and grad.dim() > 2 and grad.shape[:-1] == ids.shape:
+    if isinstance(grad, torch.Tensor) and 2 != grad.dim() == ids.dim() + 1 and grad.shape[:-1] == ids.shape:
         grad = grad.reshape(-1, grad.shape[-1])
     ld, rows, d = _rows("grad", grad)
     if rows != n:

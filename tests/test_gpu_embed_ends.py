@@ -191,6 +191,18 @@ def test_no_row_is_zero_at_any_scale(t):
         assert torch.equal(torch.nan_to_num(out[[1, 4]], nan=7.0), torch.nan_to_num((table[[3, 7]].float() * scale).to(t).float(), nan=7.0))
 
 
+# ---- how they are called
+
+def test_the_gradient_of_a_single_rows_lookup():
+    table = torch.randn(20, 24, generator=torch.Generator().manual_seed(2)).to(DEV)
+    one = torch.tensor(7, device=DEV)
+    x = embed.lookup(table, one, scale=2.0)
+    assert torch.equal(x, table[7] * 2)
+    want = torch.zeros_like(table)
+    want[7] = 3 * x
+    assert torch.equal(embed.lookup_grad(x, one, 20, scale=3.0), want)
+
+
 # ---- in place
 
 @pytest.mark.parametrize("which", ["x", "residual"])
