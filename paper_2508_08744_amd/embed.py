@@ -2,6 +2,7 @@
 
 Argument marshalling only, like ``knn``: torch supplies device memory and the current stream, the HIP library does the work, and there
 is no fallback.  Training calls come in pairs, an operator and its gradient; nothing is kept between them but what the caller passes on.
+torch's autograd sees none of it: tensors that require a gradient are refused while gradients are recorded.
 Matrices may have any row stride (their last dimension must be contiguous); results are new contiguous tensors.
 """
 from __future__ import annotations
@@ -61,11 +62,15 @@ _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _stream(*tensors):
-    """The current stream's handle; refuses tensors that are not on its device."""
+    """The current stream's handle; refuses tensors that are not on its device, or whose gradient would go missing."""
     device = _device()
     for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError("a tensor is not on the current device")
+        if t is not None:
+            if t.get_device() != device:
+                raise ValueError("a tensor is not on the current device")
+            if t.requires_grad and torch.is_grad_enabled():
+                raise ValueError("a tensor requires a gradient, and these calls record none: call them under torch.no_grad() or from a "
+                                 "torch.autograd.Function, with the gradient's own call in its backward")
     return _raw_stream(device)
 
 

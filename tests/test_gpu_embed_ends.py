@@ -203,6 +203,41 @@ def test_the_gradient_of_a_single_rows_lookup():
     assert torch.equal(embed.lookup_grad(x, one, 20, scale=3.0), want)
 
 
+def test_tensors_that_require_a_gradient_are_refused():
+    """The calls record nothing: a gradient that would go missing is an error, unless none is being recorded."""
+    x = torch.randn(4, 8, device=DEV)
+    w, f = torch.ones(8, device=DEV), torch.ones(4, device=DEV)
+    i = torch.zeros(4, dtype=torch.int64, device=DEV)
+    q, s = embed.quantize_rows(x)
+    p = torch.nn.Parameter
+    calls = [lambda: embed.lookup(p(x), i), lambda: embed.lookup_grad(p(x), i, 5), lambda: embed.lookup_grad(x, i, 4, out=p(x.clone())),
+             lambda: embed.add_rms_norm(p(x), w), lambda: embed.add_rms_norm(x, p(w)), lambda: embed.add_rms_norm(x, w, residual=p(x) * 1),
+             lambda: embed.add_rms_norm_grad(x, x, p(w), f), lambda: embed.add_rms_norm_q8(x, p(w)), lambda: embed.quantize_rows(p(x)),
+             lambda: embed.dequantize_rows(q, p(s)), lambda: embed.matmul_q8(q, s, q, s, bias=p(f)), lambda: embed.softmax_xent(x, p(x), i),
+             lambda: embed.softmax_xent(p(x), x, i), lambda: embed.softmax_xent_grad(x, p(x), i, f, f)]
+    for call in calls:
+        with pytest.raises(ValueError, match="no_grad"):
+            call()
+        with torch.no_grad():
+            call()
+
+    class Lookup(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, table, ids):
+            ctx.save_for_backward(ids)
+            ctx.rows = table.shape[0]
+            return embed.lookup(table, ids)
+
+        @staticmethod
+        def backward(ctx, grad):
+            return embed.lookup_grad(grad.contiguous(), *ctx.saved_tensors, ctx.rows), None
+    table = p(x.clone())
+    (Lookup.apply(table, i) * 2).sum().backward()
+    want = torch.zeros_like(x)
+    want[0] = 8
+    assert torch.equal(table.grad, want)
+
+
 # ---- in place
 
 @pytest.mark.parametrize("which", ["x", "residual"])
