@@ -56,9 +56,10 @@ def _check(rc):
         raise TagoreError("tagore_knn error %d: %s" % (rc, lib().tg_last_error().decode()))
 
 
-# the current device and stream without an object around them: 0.2 instead of 3.1 us of a call that takes 8
-_device = torch._C._cuda_getDevice
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# The current device and stream without an object around them, 0.2 instead of 3.1 us of a call that takes 8: names of torch's own, so
+# where a build of it has others, the public ones are taken.
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _stream(*tensors):

@@ -1,5 +1,8 @@
 """CPU-only: calls of include/tagore_embed.h that are refused, and what the workspaces cost."""
 import ctypes
+import importlib.util
+
+import torch
 
 P, Q, R = (ctypes.c_void_p(256 * i) for i in (1, 2, 3))          # never followed: every call below is refused
 
@@ -13,3 +16,20 @@ def test_norms_in_place_of_rows_that_are_apart():
         assert b"back to back" in L.tg_last_error()
         assert L.tg_add_rms_norm_q8(x, ld_x, res, ld_res, P, 1, 10, 64, 1e-6, P, P, R, None) == -1
         assert b"back to back" in L.tg_last_error()
+
+
+def test_binding_without_torchs_private_names(monkeypatch):
+    """A build of torch without them: the module is imported, and asks for the stream by the public names."""
+    from paper_2508_08744_amd import embed
+    for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+        if hasattr(torch._C, name):
+            monkeypatch.delattr(torch._C, name)
+    spec = importlib.util.spec_from_file_location("paper_2508_08744_amd.embed_of_another_torch", embed.__file__)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+
+    class Stream:
+        def __init__(self, device):
+            self.cuda_stream = 100 + device
+    monkeypatch.setattr(torch.cuda, "current_stream", Stream)
+    assert m._device is torch.cuda.current_device and m._raw_stream(3) == 103
