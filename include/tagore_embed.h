@@ -107,9 +107,9 @@ int tg_matmul_q8(const int8_t* a, const float* a_scale, const int8_t* b, const f
  * Infinite logits count as they are (lse is then infinite, the loss of an infinite target NaN or infinite); a NaN among a token's makes both NaN.
  * h: n x d, w: n_rows x d, both of type dtype; targets: n whole numbers of 32 bits, or of 64 where targets64 is 1;
  * out_loss, out_lse: n fp32.  0 <= n < 2^28, 1 <= n_rows < 2^30, 1 <= d <= 8192.
- * aligned: 1 where h and w start at a multiple of 16 bytes and their rows are a multiple of 16 bytes (of at most 1 MiB)
- * apart, 0 where that is not known: rows that do not, or whose length is no such multiple, are copied
- * into the workspace first.
+ * Rows are read where they are if they start at a multiple of 16 bytes, are a multiple of 16 bytes (of at most 1 MiB) apart and have
+ * such a length; h or w is copied into the workspace first if not (the gradient always copies h).  aligned: of which operand the first two are known:
+ * 1 of both, 2 of w, 3 of h, 0 of none.
  */
 size_t tg_softmax_xent_workspace(int64_t n, int64_t n_rows, int32_t d, int32_t dtype, int32_t aligned);
 int tg_softmax_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32_t dtype, int64_t n,

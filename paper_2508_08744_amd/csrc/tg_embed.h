@@ -110,10 +110,11 @@ void tg_launch_product(const int8_t* a, const float* as, const int8_t* b, const 
                        void* out, int dtype, void* space, hipStream_t s);
 
 // ---- tg_xent.hip
-size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready);
+// aligned: 0, or 1 where the rows of h and w can be read where they are but for their length, 2: those of w, 3: those of h
+size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, int aligned);
 void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const void* targets,
                     int targets64, float scale, float* loss, float* lse, void* space, hipStream_t s);
-size_t tg_xent_grad_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready, bool least);
+size_t tg_xent_grad_space(int64_t n, int64_t n_rows, int d, int dtype, int aligned, bool least);
 void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d,
                          const void* targets, int targets64, const float* lse, const float* dloss, float scale, void* dh, void* dw,
                          void* space, size_t bytes, hipStream_t s);

@@ -203,15 +203,20 @@ static int check_xent(int64_t n, int64_t n_rows, int32_t d, int32_t dtype)
     if (n >= TG_MAX_TOKENS) return tg_fail(TG_ERR_INVALID_ARG, "n = %lld must be below 2^28", (long long)n);
     return check_length("d", d, TG_MAX_D);
 }
-// the rows begin at multiples of 16 bytes (that their length is one is looked at where it is known, with the sizes)
-static bool rows_ready(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32_t d, int32_t dtype)
+static int check_aligned(int32_t aligned)
 {
-    const int64_t e = (int64_t)tg_type_bytes(dtype), lh = ld_h * e, lw = ld_w * e;
-    return (((uintptr_t)h | (uintptr_t)w) & 15) == 0 && ((lh | lw) & 15) == 0 && lh <= TG_MAX_PITCH && lw <= TG_MAX_PITCH;
+    return aligned >= 0 && aligned <= 3 ? TG_OK : tg_fail(TG_ERR_INVALID_ARG, "aligned = %d outside 0..3", aligned);
+}
+// which operand's rows begin at multiples of 16 bytes, as `aligned` says it (that their length is one is looked at where it is known, with the sizes)
+static int rows_ready(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32_t dtype)
+{
+    const int64_t e = (int64_t)tg_type_bytes(dtype);
+    const auto ready = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (ld * e & 15) == 0 && ld * e <= TG_MAX_PITCH; };
+    return ready(w, ld_w) ? (ready(h, ld_h) ? 1 : 2) : ready(h, ld_h) ? 3 : 0;
 }
 extern "C" size_t tg_softmax_xent_workspace(int64_t n, int64_t n_rows, int32_t d, int32_t dtype, int32_t aligned)
 {
-    return check_xent(n, n_rows, d, dtype) != TG_OK || check_flag("aligned", aligned) != TG_OK ? 0 : tg_xent_space(n, n_rows, d, dtype, aligned != 0);
+    return check_xent(n, n_rows, d, dtype) != TG_OK || check_aligned(aligned) != TG_OK ? 0 : tg_xent_space(n, n_rows, d, dtype, aligned);
 }
 extern "C" int tg_softmax_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32_t dtype, int64_t n, int64_t n_rows, int32_t d,
                                const void* targets, int32_t targets64, float scale, float* out_loss, float* out_lse, void* workspace,
@@ -223,13 +228,13 @@ extern "C" int tg_softmax_xent(const void* h, int64_t ld_h, const void* w, int64
     CHECK(check_flag("targets64", targets64));
     if (n == 0) return TG_OK;
     if (!h || !w || !targets || !out_loss || !out_lse) return null_argument();
-    CHECK(check_space(workspace, workspace_bytes, tg_xent_space(n, n_rows, d, dtype, rows_ready(h, ld_h, w, ld_w, d, dtype))));
+    CHECK(check_space(workspace, workspace_bytes, tg_xent_space(n, n_rows, d, dtype, rows_ready(h, ld_h, w, ld_w, dtype))));
     tg_launch_xent(h, ld_h, w, ld_w, dtype, n, n_rows, d, targets, targets64, scale, out_loss, out_lse, workspace, stream_of(stream));
     return launched("softmax cross entropy");
 }
 extern "C" size_t tg_softmax_xent_grad_workspace(int64_t n, int64_t n_rows, int32_t d, int32_t dtype, int32_t aligned)
 {
-    return check_xent(n, n_rows, d, dtype) != TG_OK || check_flag("aligned", aligned) != TG_OK ? 0 : tg_xent_grad_space(n, n_rows, d, dtype, aligned != 0, false);
+    return check_xent(n, n_rows, d, dtype) != TG_OK || check_aligned(aligned) != TG_OK ? 0 : tg_xent_grad_space(n, n_rows, d, dtype, aligned, false);
 }
 extern "C" int tg_softmax_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32_t dtype, int64_t n, int64_t n_rows, int32_t d,
                                     const void* targets, int32_t targets64, const float* lse, const float* dloss, float scale, void* out_dh,
@@ -240,7 +245,7 @@ extern "C" int tg_softmax_xent_grad(const void* h, int64_t ld_h, const void* w, 
     CHECK(check_ld("ld_w", ld_w, d));
     CHECK(check_flag("targets64", targets64));
     if (!out_dw || (n > 0 && (!h || !w || !targets || !lse || !dloss || !out_dh))) return null_argument();
-    CHECK(check_space(workspace, workspace_bytes, tg_xent_grad_space(n, n_rows, d, dtype, rows_ready(h, ld_h, w, ld_w, d, dtype), true)));
+    CHECK(check_space(workspace, workspace_bytes, tg_xent_grad_space(n, n_rows, d, dtype, rows_ready(h, ld_h, w, ld_w, dtype), true)));
     tg_launch_xent_grad(h, ld_h, w, ld_w, dtype, n, n_rows, d, targets, targets64, lse, dloss, scale, out_dh, out_dw, workspace, workspace_bytes,
                         stream_of(stream));
     return launched("gradient of the softmax cross entropy");

@@ -583,14 +583,14 @@ static void xent_rows(XentRows* r, TgCarve* c, const void* h, int64_t ld_h, cons
 // 398 us in tiles of 128 x 128, 359 in these; 2048 tokens, 8000 rows of 1500: 1502 and 1444).
 #define XENT_STRETCH 64         // rows of the table that leave one (maximum, sum) at least (BM)
 
-size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready)
+size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, int aligned)
 {
     if (n == 0) return 0;
     const int e = (int)tg_type_bytes(dtype);
     TgCarve c{nullptr, 0};
     XentRows r;
-    const bool rd = ready && (d * e & 15) == 0;
-    xent_rows(&r, &c, nullptr, d, nullptr, d, n, n_rows, d, e, rd, rd);
+    const bool whole = (d * e & 15) == 0;
+    xent_rows(&r, &c, nullptr, d, nullptr, d, n, n_rows, d, e, whole && (aligned == 1 || aligned == 3), whole && (aligned == 1 || aligned == 2));
     c.take<float2>((size_t)((n_rows + XENT_STRETCH - 1) / XENT_STRETCH + 8) * n);
     c.take<float>(n);
     return c.used;
@@ -627,12 +627,10 @@ void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, in
     const int e = (int)tg_type_bytes(dtype);
     TgCarve c{(char*)space, 0};
     XentRows r;
-    const bool rh = tile_ready(h, ld_h, d, e), rw = tile_ready(w, ld_w, d, e), both = rh && rw;
-    xent_rows(&r, &c, h, ld_h, w, ld_w, n, n_rows, d, e, both, both);
-    if (!both) {
-        tg_launch_pack(h, ld_h, n, d, e, r.ph, s);
-        tg_launch_pack(w, ld_w, n_rows, d, e, r.pw, s);
-    }
+    const bool rh = tile_ready(h, ld_h, d, e), rw = tile_ready(w, ld_w, d, e);
+    xent_rows(&r, &c, h, ld_h, w, ld_w, n, n_rows, d, e, rh, rw);
+    if (!rh) tg_launch_pack(h, ld_h, n, d, e, r.ph, s);
+    if (!rw) tg_launch_pack(w, ld_w, n_rows, d, e, r.pw, s);
     float2* parts = c.take<float2>((size_t)((n_rows + XENT_STRETCH - 1) / XENT_STRETCH + 8) * n);
     float* at = c.take<float>(n);
     int64_t count = 0;
@@ -734,9 +732,10 @@ static size_t xent_grad_bytes(int64_t n, int64_t n_rows, int d, int e, bool read
     char* p;
     return carve_xent_grad(&r, &c, nullptr, d, nullptr, d, n, n_rows, d, e, ready && (d * e & 15) == 0, xent_grad_shape(n, n_rows, d, e, p_bytes), &k, &p, &sums, &lost);
 }
-size_t tg_xent_grad_space(int64_t n, int64_t n_rows, int d, int dtype, bool ready, bool least)
+size_t tg_xent_grad_space(int64_t n, int64_t n_rows, int d, int dtype, int aligned, bool least)
 {
     if (n == 0) return 0;
+    const bool ready = aligned == 1 || aligned == 2;           // (h is always copied)
     const size_t asked = xent_grad_bytes(n, n_rows, d, (int)tg_type_bytes(dtype), ready, XENT_PIECE_BYTES);
     if (!least) return asked;
     // (one piece can do with less than many: dh then needs no sums)
@@ -824,7 +823,7 @@ void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_
         tg_launch_zero(dw, (size_t)n_rows * d * e, s);
         return;
     }
-    const bool ready = tile_ready(w, ld_w, d, e) && (((uintptr_t)h & 15) == 0 && (ld_h * e & 15) == 0);
+    const bool ready = tile_ready(w, ld_w, d, e);
     // the largest piece that the workspace holds
     int64_t p_bytes = XENT_PIECE_BYTES * 64;
     while (p_bytes > 0 && xent_grad_bytes(n, n_rows, d, e, ready, p_bytes) > bytes) p_bytes = p_bytes > (1 << 20) ? p_bytes / 2 : 0;

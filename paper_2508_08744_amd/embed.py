@@ -119,10 +119,14 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _aligned(t, ld, u, ld_u):
-    """Whether two matrices start at multiples of 16 bytes and their rows are such a multiple (of at most 1 MiB) apart."""
-    e = t.element_size()
-    return 0 if (t.data_ptr() | u.data_ptr() | ld * e | ld_u * e) % 16 or max(ld, ld_u) * e > 1 << 20 else 1
+def _aligned(h, ld_h, w, ld_w):
+    """Which of two matrices starts at a multiple of 16 bytes, with rows such a multiple (of at most 1 MiB) apart: 1 both, 2 w, 3 h, 0 none."""
+    e = h.element_size()
+    far = 1 << 20
+    h_is = not (h.data_ptr() | ld_h * e) % 16 and ld_h * e <= far
+    if not (w.data_ptr() | ld_w * e) % 16 and ld_w * e <= far:
+        return 1 if h_is else 2
+    return 3 if h_is else 0
 
 
 def lookup(table, ids, scale=1.0):

@@ -33,3 +33,15 @@ def test_binding_without_torchs_private_names(monkeypatch):
             self.cuda_stream = 100 + device
     monkeypatch.setattr(torch.cuda, "current_stream", Stream)
     assert m._device is torch.cuda.current_device and m._raw_stream(3) == 103
+
+
+def test_workspaces_copy_only_the_odd_operand():
+    from paper_2508_08744_amd import embed
+    f, g = embed.lib().tg_softmax_xent_workspace, embed.lib().tg_softmax_xent_grad_workspace
+    n, v, d = 48, 100_000, 96
+    h, w = n * d * 2, v * d * 2
+    both, table, tokens, none = (f(n, v, d, 1, a) for a in (1, 2, 3, 0))
+    assert h <= table - both <= h + 256 and w <= tokens - both <= w + 256 and h + w <= none - both <= h + w + 512
+    assert g(n, v, d, 1, 1) == g(n, v, d, 1, 2) and w <= g(n, v, d, 1, 3) - g(n, v, d, 1, 1) <= w + 256 and g(n, v, d, 1, 3) == g(n, v, d, 1, 0)
+    assert f(n, v, d, 1, 4) == 0 and f(n, v, d, 1, -1) == 0 and g(n, v, d, 1, 4) == 0
+    assert f(n, v, 97, 1, 1) == f(n, v, 97, 1, 0)                # rows of such a length are copied wherever they start

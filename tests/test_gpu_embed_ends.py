@@ -238,6 +238,37 @@ def test_tensors_that_require_a_gradient_are_refused():
     assert torch.equal(table.grad, want)
 
 
+# ---- operands of uneven alignment
+
+@pytest.mark.parametrize("n", [5, 200])
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_only_the_odd_operand_is_copied(t, n):
+    v, d = 60_000, 64
+    g = torch.Generator().manual_seed(n)
+    h, w = torch.randn(n, d, generator=g).to(t).to(DEV), torch.randn(v, d, generator=g).to(t).to(DEV)
+    targets = torch.randint(0, v, (n,), generator=g).to(DEV)
+    dloss = torch.rand(n, generator=g).to(DEV)
+    odd = torch.zeros(n, d + 3, dtype=t, device=DEV)[:, 1:d + 1]
+    odd.copy_(h)
+
+    def run(h):
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        loss, lse = embed.softmax_xent(h, w, targets)
+        first = torch.cuda.max_memory_allocated() - before
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        dh, dw = embed.softmax_xent_grad(h, w, targets, lse, dloss)
+        return (loss, lse, dh, dw), first, torch.cuda.max_memory_allocated() - before
+    want, *even = run(h)
+    got, *uneven = run(odd)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    # (h's copy, and what the allocator rounds up to)
+    for a, b in zip(uneven, even):
+        assert a - b <= h.numel() * h.element_size() + (4 << 20) < w.numel() * w.element_size()
+
+
 # ---- in place
 
 @pytest.mark.parametrize("which", ["x", "residual"])
