@@ -418,15 +418,19 @@ void tg_launch_product(const int8_t* a, const float* as, const int8_t* b, const 
                        void* out, int dtype, void* space, hipStream_t s)
 {
     TileRows Y{(const char*)a, m, (uint32_t)k, (uint32_t)k}, X{(const char*)b, n, (uint32_t)k, (uint32_t)k};
-    if (!product_as_is(m, k) && (!tile_ready(a, k, k, 1) || !tile_ready(b, k, k, 1))) {
+    if (!product_as_is(m, k)) {
+        // (a width of its own only for a length that is no multiple of 16, where both are copied)
         TgCarve c{(char*)space, 0};
-        Y.pitch = X.pitch = Y.width = X.width = tile_pitch(k, 1);
-        char* pa = c.take<char>((size_t)m * Y.pitch);
-        char* pb = c.take<char>((size_t)n * X.pitch);
-        tg_launch_pack(a, k, m, k, 1, pa, s);
-        tg_launch_pack(b, k, n, k, 1, pb, s);
-        Y.p = pa;
-        X.p = pb;
+        const auto copy = [&](TileRows& rows, const int8_t* p) {
+            const bool ready = tile_ready(p, k, k, 1);
+            rows.pitch = rows.width = tile_pitch(k, 1);
+            char* const place = c.take<char>((size_t)rows.rows * rows.pitch);
+            if (ready) return;
+            tg_launch_pack(p, k, rows.rows, k, 1, place, s);
+            rows.p = place;
+        };
+        copy(Y, a);
+        copy(X, b);
     }
     const int bytes = (int)X.width;
     if (m <= PRODUCT_FEW && bytes > PRODUCT_SHORT) {

@@ -269,6 +269,31 @@ def test_only_the_odd_operand_is_copied(t, n):
         assert a - b <= h.numel() * h.element_size() + (4 << 20) < w.numel() * w.element_size()
 
 
+@pytest.mark.parametrize("odd", ["a", "b", "both", "neither"])
+def test_the_product_copies_only_the_odd_operand(odd):
+    m, n, k = 100, 3000, 320
+    g = torch.Generator().manual_seed(4)
+    a, b = (torch.randint(-127, 128, (rows, k), generator=g, dtype=torch.int8) for rows in (m, n))
+    sa, sb = torch.rand(m, generator=g).to(DEV), torch.rand(n, generator=g).to(DEV)
+    L = embed.lib()
+
+    def there(x, move):
+        y = torch.empty(x.numel() + 16, dtype=torch.int8, device=DEV)[move:move + x.numel()].view(x.shape)
+        return y.copy_(x)
+    x, y = there(a, 5 if odd in ("a", "both") else 0), there(b, 3 if odd in ("b", "both") else 0)
+    nbytes = L.tg_matmul_q8_workspace(m, n, k, 0)
+    ws = torch.full((nbytes,), 85, dtype=torch.uint8, device=DEV)
+    out = torch.empty(m, n, device=DEV)
+    rc = L.tg_matmul_q8(x.data_ptr(), sa.data_ptr(), y.data_ptr(), sb.data_ptr(), None, m, n, k, out.data_ptr(), 0, ws.data_ptr(), nbytes,
+                        torch.cuda.current_stream().cuda_stream)
+    assert rc == 0 and torch.equal(out, embed.matmul_q8(a.to(DEV), sa, b.to(DEV), sb))
+    written = (ws != 85).view(-1, k).sum(1)
+    # rows of random bytes: of a copied one hardly any is 85
+    first, last = written[:m] > k // 2, written[m:] > k // 2
+    assert first.all() if odd in ("a", "both") else not written[:m].any()
+    assert last.sum() >= n - 1 if odd in ("b", "both") else not written[m:].any()
+
+
 # ---- in place
 
 @pytest.mark.parametrize("which", ["x", "residual"])
