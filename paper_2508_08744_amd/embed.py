@@ -298,6 +298,8 @@ def softmax_xent_grad(h, w, targets, lse, dloss, scale=1.0, workspace=None):
         keep, ws = _space(nbytes, h)
     else:
         _on_device("workspace", workspace, (torch.uint8,), 1)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
         ws, nbytes = workspace.data_ptr(), workspace.numel()
     _check(L.tg_softmax_xent_grad(h.data_ptr(), ld_h, w.data_ptr(), ld_w, t, n, v, d, targets.data_ptr(), wide, lse.data_ptr(), dloss.data_ptr(),
                                   scale, dh.data_ptr(), dw.data_ptr(), ws, nbytes, _stream(h, w, targets, lse, dloss, workspace)))

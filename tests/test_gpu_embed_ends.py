@@ -294,6 +294,15 @@ def test_the_product_copies_only_the_odd_operand(odd):
     assert last.sum() >= n - 1 if odd in ("b", "both") else not written[m:].any()
 
 
+def test_a_workspace_that_is_less_than_it_says_is_refused():
+    """A broadcast one has as many elements as wanted, and the memory of one."""
+    h, w, f = torch.zeros(4, 8, device=DEV), torch.zeros(50, 8, device=DEV), torch.zeros(4, device=DEV)
+    i = torch.zeros(4, dtype=torch.int64, device=DEV)
+    for ws in (torch.zeros(1, dtype=torch.uint8, device=DEV).expand(1 << 20), torch.zeros(1 << 21, dtype=torch.uint8, device=DEV)[::2]):
+        with pytest.raises(ValueError, match="contiguous"):
+            embed.softmax_xent_grad(h, w, i, f, f, workspace=ws)
+
+
 # ---- in place
 
 @pytest.mark.parametrize("which", ["x", "residual"])
