@@ -346,3 +346,64 @@ def test_losses_over_more_than_half_of_2_to_the_30_rows(n):
     # a tile of equal terms is exact; a lane of the join adds a 256th of the tiles one after another; the far rows' logits and exponents: 400
     tol = (v / 64 / 256 + 400) * U
     assert ((lse.double() - want).abs() <= tol).all() and ((loss.double() - (want - z_t)).abs() <= 2 * tol).all()
+
+def test_cross_entropy_of_a_table_past_32_bits_of_elements():
+    """More than 2^31 elements in w and dw, pieces of the most rows that one has (2^20)."""
+    n, v, d = 5, 17_000_003, 128
+    gd = torch.Generator(device=DEV).manual_seed(1)
+    w = torch.empty(v, d, dtype=BF16, device=DEV)
+    w.normal_(0, 0.05, generator=gd)
+    h = torch.randn(n, d, device=DEV, generator=gd).to(BF16)
+    targets = torch.tensor([0, v - 1, 16_777_216, -1, 1_048_576], device=DEV)
+    dloss = torch.rand(n, device=DEV, generator=gd)
+    loss, lse = embed.softmax_xent(h, w, targets)
+    dh, dw = embed.softmax_xent_grad(h, w, targets, lse, dloss)
+    step = 1 << 20
+    mass, want_dh, size_dh = (torch.zeros(s, dtype=torch.float64, device=DEV) for s in ((n,), (n, d), (n, d)))
+    hd = h.double()
+    for i in range(0, v, step):
+        mass += torch.exp(hd @ w[i:i + step].double().t().contiguous()).sum(1)
+    want = torch.log(mass)
+    rows = w[targets.clamp_min(0)].double()
+    z_t = (hd * rows).sum(1)
+    there = targets >= 0
+    # logits below 10: exponentials to 2^-18, sums of as many roundings as there are tiles
+    assert ((lse.double() - want).abs() <= 1e-4).all()
+    assert ((loss.double() - torch.where(there, want - z_t, 0.0)).abs() <= 2e-4).all()
+    g = torch.where(there, dloss.double(), 0.0)[:, None]
+    e = half_step(BF16) + 4e-4
+    for i in range(0, v, step):
+        ww = w[i:i + step].double()
+        p = torch.exp(hd @ ww.t().contiguous() - want[:, None]) * g
+        for t in range(n):
+            if i <= targets[t] < i + len(ww):
+                p[t, targets[t] - i] -= g[t, 0]
+        want_dh += p @ ww
+        size_dh += p.abs() @ ww.abs()
+        pt = p.t().contiguous()
+        want_dw = pt @ hd
+        tol = (pt.abs() @ hd.abs()) * e
+        assert ((dw[i:i + step].double() - want_dw).abs() <= tol + half_step(BF16) * (want_dw.abs() + tol) + torch.finfo(BF16).tiny).all()
+    # (a part of dh is a chain of at most 2^14 rows in each of 17 pieces)
+    tol = size_dh * (e + 17 * (1 << 14) * U)
+    assert ((dh.double() - want_dh).abs() <= tol + half_step(BF16) * (want_dh.abs() + tol)).all()
+
+
+def test_norms_of_more_rows_than_a_launch_has():
+    n, d = (1 << 21) + 5, 24
+    gd = torch.Generator(device=DEV).manual_seed(2)
+    x = torch.randn(n, d, device=DEV, generator=gd)
+    w = 1 + 0.1 * torch.randn(d, device=DEV, generator=gd)
+    res = torch.randn(n, d, device=DEV, generator=gd)
+    r = (x + res).double()
+    rstd = torch.rsqrt((r * r).mean(1, keepdim=True) + 1e-6)
+    y = r * rstd * w.double()
+    got, got_r, got_rstd = embed.add_rms_norm(x, w, residual=res)
+    assert torch.equal(got_r, x + res)
+    assert ((got.double() - y).abs() <= y.abs() * 69 * U).all() and ((got_rstd.double() - rstd[:, 0]).abs() <= rstd[:, 0] * 64 * U).all()
+    q, scale, got_r = embed.add_rms_norm_q8(x, w, residual=res)
+    assert torch.equal(got_r, x + res)
+    for q, scale, z in ((q, scale, y), (*embed.quantize_rows(x), x.double())):
+        top = z.abs().amax(1) / 127
+        assert ((scale.double() - top).abs() <= top * 2 * U).all()
+        assert ((z / scale.double()[:, None]) - q.double()).abs().max() <= 0.5 + 1e-9
