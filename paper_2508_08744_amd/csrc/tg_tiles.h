@@ -356,9 +356,9 @@ struct Tile {
         start(X, Y, x0, y0, k0, k1, lds);
         loop();
     }
-    // the rows of X and Y that acc[i][j][0] belongs to; acc[i][j][e] is for x + e
-    __device__ inline int x_of(int i) const { return (i / HM) * (BM / 2) + ((threadIdx.x >> 6) / WN) * (HM * 16) + (i % HM) * 16 + (tg_lane() >> 4) * 4; }
-    __device__ inline int y_of(int j) const { return (j / HN) * (BN / 2) + ((threadIdx.x >> 6) % WN) * (HN * 16) + (j % HN) * 16 + (tg_lane() & 15); }
+    // the rows of X and Y that acc[i][j][0] belongs to; acc[i][j][e] is for x + e (from the thread's number alone: the products' loop has no register for more)
+    __device__ inline int x_of(int i) const { return (i / HM) * (BM / 2) + ((threadIdx.x >> 6) / WN) * (HM * 16) + (i % HM) * 16 + (threadIdx.x >> 4 & 3) * 4; }
+    __device__ inline int y_of(int j) const { return (j / HN) * (BN / 2) + ((threadIdx.x >> 6) % WN) * (HN * 16) + (j % HN) * 16 + (threadIdx.x & 15); }
 };
 
 // four neighbours of an output row

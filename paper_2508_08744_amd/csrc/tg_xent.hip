@@ -224,7 +224,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
     // anything, whatever its logits are.
     struct Token { int hit, there; float g, b; };                // there: 0 without a target, 1, or 2 with an lse that is not near, which b then is as it is
     __shared__ Token s_token[BN];
-    const float up = c[0], base = scale * XENT_LOG2E;
+    const float up = c[0];
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
         Token k{target >= 0 && hit >= 0 && hit < BM ? (int)hit : -1, target >= 0, 0.0f, 0.0f};
         if (target >= 0) {
             k.g = dloss[y] * scale * up;
-            const bool near = xent_near(lse[y], base);
+            const bool near = xent_near(lse[y], scale * XENT_LOG2E);
             k.there = near ? 1 : 2;
             k.b = near ? lse[y] * XENT_LOG2E : lse[y];
         }
@@ -251,6 +251,9 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
     typedef E vec __attribute__((ext_vector_type(W)));
     // (r & SWAP, whatever j)
     int swap = threadIdx.x & SWAP;
+    float base = scale;
+    asm volatile("" : "+v"(base));
+    base *= XENT_LOG2E;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
         // (nothing of this is made out in front of the products, in whose loop no register is free)
@@ -373,14 +376,23 @@ struct XentGiveBack {
     __device__ inline void look(int64_t c0)
     {
         const int all = all_of(c0), turns = (all + THREADS - 1) / THREADS, first = first_of(c0);
+        // (asked for at once; a place behind the end is the first token's, and no hit)
+        int64_t target[EACH];
+        const auto ask = [&](auto* targets) {
+#pragma unroll
+            for (int k = 0; k < EACH; ++k)
+                if (k < turns) target[k] = targets[c0 + (first + k * 64 < all ? first + k * 64 : 0)];
+        };
+        if (a.targets64) ask(reinterpret_cast<const int64_t*>(a.targets));
+        else ask(reinterpret_cast<const int32_t*>(a.targets));
         uint32_t mine = 0, count = 0;
 #pragma unroll
-        for (int k = 0; k < EACH; ++k) {
-            const int at = first + k * 64;
-            const bool hit = k < turns && at < all && row_of(c0 + at) >= 0;
-            mine |= hit ? 1u << k : 0u;
-            count += __popcll(__ballot(hit));
-        }
+        for (int k = 0; k < EACH; ++k)
+            if (k < turns) {
+                const bool hit = first + k * 64 < all && target[k] >= v0 && target[k] < v0 + rows;
+                mine |= hit ? 1u << k : 0u;
+                count += __popcll(__ballot(hit));
+            }
         m.mine[threadIdx.x] = (uint16_t)mine;
         if (tg_lane() == 0) m.counts[threadIdx.x >> 6] = count;
     }
