@@ -44,7 +44,8 @@ int tg_embed_lookup(const void* table, int64_t ld, int32_t dtype, int64_t n_rows
  * over the t with ids[t] = v, in fp32 and in an order that depends on the ids alone (the tokens are sorted by
  * id first).  grad: n x d of type dtype.  out: n_rows x d of type out_dtype (TG_DTYPE_F32, or dtype).
  * accumulate = 0: rows without a token become zero; 1: the sums are added to what out holds, and rows
- * without a token are not touched (a table that is also the softmax's: its gradient first, then this).
+ * without a token are not touched (a table that is also the softmax's: its gradient first, then this; with out in fp32 only the first of
+ * the two is rounded to the table's type).
  */
 size_t tg_embed_lookup_grad_workspace(int64_t n, int64_t n_rows, int32_t d);
 int tg_embed_lookup_grad(const void* grad, int64_t ld, int32_t dtype, const void* ids, int32_t ids64, int64_t n,
@@ -53,9 +54,10 @@ int tg_embed_lookup_grad(const void* grad, int64_t ld, int32_t dtype, const void
 
 /*
  * r = x + residual, rounded to the type of x (residual = NULL: r = x, and out_r is not written and may be
- * NULL); rstd = 1 / sqrt(mean(r^2) + eps); out_y = r * rstd * weight.  x, residual: n x d of type dtype;
- * weight: d of the same type; out_y, out_r: n x d; out_rstd: n fp32, or NULL.  out_r may be x or residual
- * itself where that one's rows are back to back (refused otherwise: rows still to be read would be written over).  0 <= n < 2^30, 1 <= d <= 8192, eps >= 0.
+ * NULL); rstd = 1 / sqrt(mean(r^2) + eps), of whatever size the row is (a row of zeros with eps = 0: infinite, and
+ * out_y NaN); out_y = r * rstd * weight.  x, residual: n x d of type dtype; weight: d of the same type; out_y, out_r:
+ * n x d; out_rstd: n fp32, or NULL.  out_r may be x or residual itself where that one's rows are back to back (refused
+ * otherwise: rows still to be read would be written over).  0 <= n < 2^30, 1 <= d <= 8192, eps >= 0.
  */
 int tg_add_rms_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, const void* weight,
                     int32_t dtype, int64_t n, int32_t d, float eps, void* out_y, void* out_r, float* out_rstd,
@@ -73,8 +75,8 @@ int tg_add_rms_norm_grad(const void* dy, int64_t ld_dy, const void* dr, int64_t 
 /*
  * tg_add_rms_norm with the normed rows on an 8-bit grid: scale = max|y| / 127 (rounded to fp32) and
  * q = y / scale rounded to the nearest whole number (ties to the even one), -127..127.  out_q: n x d int8,
- * out_scale: n fp32.  A row of zeros has scale 0; a row that holds a NaN, or whose norm is not finite, has scale NaN
- * and zeros.  y is formed and divided in 64 bits: which side of a border a value falls on does not depend
+ * out_scale: n fp32.  A row of zeros has scale 0 (with eps = 0 its norm is not finite); a row that holds a NaN, or whose norm is not finite,
+ * has scale NaN and zeros.  y is formed and divided in 64 bits: which side of a border a value falls on does not depend
  * on how the row was cut up.
  */
 int tg_add_rms_norm_q8(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, const void* weight,
@@ -104,7 +106,7 @@ int tg_matmul_q8(const int8_t* a, const float* a_scale, const int8_t* b, const f
  * Softmax cross entropy of n rows against all n_rows rows of a table, without the n x n_rows logits:
  *   z[t][v] = scale * <h[t], w[v]>,  lse[t] = log sum_v exp(z[t][v]),  loss[t] = lse[t] - z[t][targets[t]].
  * A target outside [0, n_rows) is none: the token's loss is 0 and it has no part in any gradient.
- * Infinite logits count as they are (lse is then infinite, the loss of an infinite target NaN or infinite); a NaN among a token's makes both NaN.
+ * Infinite logits count as they are (lse is then infinite, the loss of an infinite target NaN or infinite); a NaN among a token's logits makes lse NaN, and the loss if it has a target.
  * h: n x d, w: n_rows x d, both of type dtype; targets: n whole numbers of 32 bits, or of 64 where targets64 is 1;
  * out_loss, out_lse: n fp32.  0 <= n < 2^28, 1 <= n_rows < 2^30, 1 <= d <= 8192.
  * Rows are read where they are if they start at a multiple of 16 bytes, are a multiple of 16 bytes (of at most 1 MiB) apart and have

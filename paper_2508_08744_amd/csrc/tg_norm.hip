@@ -1,7 +1,7 @@
 // Root-mean-square norm with the residual's addition, its gradient, and rows on an 8-bit grid with a scale each.
 //
 // All of these are bound by the bytes of their rows: a row is read once, stays in the registers of the lanes that share it (a wave where
-// it is short, a workgroup of up to 16 waves where it is long) through its sums, and is written once.  (30 011 rows of 960 bf16: 44 us there, 5.2 TB/s, 43 back; with
+// it is short, a workgroup of up to 16 waves where it is long) through its sums, and is written once.  (30 011 rows of 960 bf16: 42 us there, 5.5 TB/s, 42 back; with
 // the rows of the gradient asked for one by one 54.)
 #include "tg_embed.h"
 #include "tg_device.h"
@@ -126,7 +126,7 @@ __device__ inline double norm_rcp(double x)
 // The norm in 64 bits, the normed row on its grid.  Which whole number a value next to a border becomes must not depend on how its row
 // was summed, so sum, scale and quotient are taken in 64 bits; the bytes of the rows still bound the kernel.  A 16-bit value times its weight is exact in
 // 32 bits while it stays within their range (a row that leaves it takes its products in 64 bits), and so is its quotient's
-// rounding, except next to a border.  (16 384 rows of 4096 bf16: 101 us, 4.7 TB/s, as a copy; 109
+// rounding, except next to a border.  (16 384 rows of 4096 bf16: 100 us, 4.7 TB/s, as a copy; 109
 // with the divisions and the root spelt out and code for parts of a piece.)
 template <class E, int T, int CH, bool WHOLE, bool NORM>
 __global__ __launch_bounds__(NormShare<T>::THREADS) void norm_q8_kernel(const E* x, int64_t ld_x, const E* res, int64_t ld_res,
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__
     if (j == 0 && col < d) dw[col] = (E)s[0][c];
 }
 
-// The lanes a row of `d` elements gets and the pieces a lane holds: a wave up to four pieces a lane (2048 elements of 16 bits), four
+// The lanes a row of `d` elements gets and the pieces a lane holds: a wave up to two pieces a lane (1024 elements of 16 bits), four
 // waves up to four (8192), sixteen beyond (8192 elements of 32 bits).
 #define NORM_SHAPE(pieces, WHOLE, LAUNCH)                                            \
     do {                                                                             \

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(TileRows X, TileR
 }
 
 // Up to 16 FN tokens.  A workgroup has 16 channels, a wave a quarter of the contraction in one piece, STEPS x 64 bytes of every row in
-// flight.  (16 384 channels of 4096, 4 tokens, fp16: 16 steps 16.1 us, 4.2 TB/s; 4 steps 16.9; 4 steps with the waves' pieces in turn 19.3.)
+// flight.  (16 384 channels of 4096, 4 tokens, fp16: 16 steps 13.0 us, 5.2 TB/s; 4 steps 13.3.)
 template <class O, int FN>
 __global__ __launch_bounds__(256) void product_few_kernel(TileRows X, TileRows Y, int bytes, const float* __restrict__ as,
                                                           const float* __restrict__ bs, const float* __restrict__ bias, int64_t first,

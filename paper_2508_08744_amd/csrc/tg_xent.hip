@@ -2,13 +2,13 @@
 //
 // Forward: a tile of logits stays in the registers of the workgroup that formed it and leaves a maximum and a sum of exponentials for
 // every token; a second kernel joins them over the table.  2 n n_rows d operations on the matrix instructions bound it, or, for
-// few tokens, the bytes of the table.  (8192 tokens, 131 072 rows of 1024 bf16: 1.9 ms, 1.15 PFLOP/s; 48 tokens: 41 us, 6.5 TB/s.)
+// few tokens, the bytes of the table.  (8192 tokens, 131 072 rows of 1024 bf16: 1.9 ms, 1.14 PFLOP/s; 48 tokens: 41 us, 6.6 TB/s.)
 //
 // Gradient: the logits are formed again, a piece of the table at a time, and become P = scale dloss (softmax - [target]) in the
 // inputs' type, which goes to memory once (a piece is small enough to be read again while the last-level cache holds it) and into two products:
 // dh += P w over the piece's rows, dw = P^T h over the tokens.  The products read w, h and, for dw, P across their rows, through LDS
-// reads that turn them; no transposed copy is made.  dh is kept in fp32 over the pieces.  (The same step: 8 pieces of 285 us for P and 419 for both
-// products, 1.31 PFLOP/s.)  P in 16 bits is a choice for its bytes.  Its roundings are half a step of the type each; the one at a token's target,
+// reads that turn them; no transposed copy is made.  dh is kept in fp32 over the pieces.  (The same step: 8 pieces of 288 us for P and 435 for both
+// products, 1.26 PFLOP/s.)  P in 16 bits is a choice for its bytes.  Its roundings are half a step of the type each; the one at a token's target,
 // the entry that outweighs the others together, is given back to both gradients.  Of the other entries' roundings as much remains in a sum as the sum keeps of the
 // entries themselves: a relative error like that of rounding the result, which comes on top.
 #include "tg_embed.h"
