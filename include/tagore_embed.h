@@ -106,7 +106,8 @@ int tg_matmul_q8(const int8_t* a, const float* a_scale, const int8_t* b, const f
  * Softmax cross entropy of n rows against all n_rows rows of a table, without the n x n_rows logits:
  *   z[t][v] = scale * <h[t], w[v]>,  lse[t] = log sum_v exp(z[t][v]),  loss[t] = lse[t] - z[t][targets[t]].
  * A target outside [0, n_rows) is none: the token's loss is 0 and it has no part in any gradient.
- * Infinite logits count as they are (lse is then infinite, the loss of an infinite target NaN or infinite); a NaN among a token's logits makes lse NaN, and the loss if it has a target.
+ * Infinite logits count as the formulas have them (lse is then infinite, and undefined what takes an infinite one's difference from
+ * it); a NaN among a token's logits makes lse NaN, and the loss if it has a target.
  * h: n x d, w: n_rows x d, both of type dtype; targets: n whole numbers of 32 bits, or of 64 where targets64 is 1;
  * out_loss, out_lse: n fp32.  0 <= n < 2^28, 1 <= n_rows < 2^30, 1 <= d <= 8192.
  * Rows are read where they are if they start at a multiple of 16 bytes, are a multiple of 16 bytes (of at most 1 MiB) apart and have

@@ -23,14 +23,15 @@ __device__ inline float xent_exp(float x) { return __builtin_amdgcn_exp2f(x * XE
 // exponents, to be taken with a factor of 1 and nothing subtracted, so that what follows is the same for both.
 #define XENT_NEAR 65536.0f
 __device__ inline bool xent_near(float m, float base) { return fabsf(m) < XENT_NEAR && fabsf(base) <= 3.4028234e38f; }
-// m: the largest logit, or lse: one that is infinite is taken in by its equals alone; a NaN stays one
+// LARGEST: m is the largest logit, and one that is infinite is taken in by its equals alone.  Else it is lse, and the difference what it is.
+template <bool LARGEST>
 __device__ inline float xent_far(float product, float scale, float m)
 {
     // (the logit is rounded before the difference, as m was: one multiply-add of both would leave m's rounding, which is large here)
 #pragma clang fp contract(off)
     asm volatile("" : "+v"(product));        // (nothing of this is made out where it is not needed)
     const float z = product * scale;
-    return z == m ? (m == -__builtin_inff() ? m : 0.0f) : (z - m) * XENT_LOG2E;
+    return LARGEST && z == m ? (m == -__builtin_inff() ? m : 0.0f) : (z - m) * XENT_LOG2E;
 }
 
 // (maximum, sum) pairs: one that stands for nothing is (-infinity, 0)
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_part_kernel(TileRows X, Til
 #pragma unroll
             for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) t.acc[i][j][e] = near ? t.acc[i][j][e] : xent_far(t.acc[i][j][e], scale, m);
+                for (int e = 0; e < 4; ++e) t.acc[i][j][e] = near ? t.acc[i][j][e] : xent_far<true>(t.acc[i][j][e], scale, m);
         }
 #pragma unroll
         for (int i = 0; i < T::FM; ++i) {
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
 #pragma unroll
             for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) t.acc[i][j][e] = near ? t.acc[i][j][e] : xent_far(t.acc[i][j][e], scale, k.b);
+                for (int e = 0; e < 4; ++e) t.acc[i][j][e] = near ? t.acc[i][j][e] : xent_far<false>(t.acc[i][j][e], scale, k.b);
         }
         char* const row = lds + r * (PIECES * 16);
 #pragma unroll

@@ -151,6 +151,26 @@ def test_gradient_of_huge_logits(t, n, v):
             assert ((got.cpu().double() - want).abs() <= size * (e + (n + 8) * U) + e * want.abs() + torch.finfo(t).tiny).all()
 
 
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("n,v", [(5, 40), (300, 2100), (300, 30_000)])
+def test_gradient_of_an_infinite_logit(t, n, v):
+    """exp(z - lse) of the one that is infinite is undefined, and what it reaches; the others' is zero."""
+    w = torch.full((v, 8), 2.0 ** -10)
+    w[v // 2] = 2.0
+    h = torch.zeros(n, 8)
+    h[:, 3] = 1.0
+    targets = torch.arange(n) * 7 % v
+    hd, wd, i = h.to(t).to(DEV), w.to(t).to(DEV), targets.to(DEV)
+    loss, lse = embed.softmax_xent(hd, wd, i, scale=3e38)
+    assert (lse == float("inf")).all()
+    f = (torch.full((n,), 2.0 ** -127) * torch.tensor(3e38)).double()
+    dh, dw = embed.softmax_xent_grad(hd, wd, i, lse, torch.full((n,), 2.0 ** -127, device=DEV), scale=3e38)
+    assert torch.isnan(dh).all() and torch.isnan(dw[v // 2, 3])
+    want = torch.zeros(v, 8, dtype=torch.float64).index_add_(0, targets, -f[:, None] * h.double())
+    rest = torch.arange(v) != v // 2
+    assert ((dw.cpu().double() - want).abs() <= want.abs() * (2 * half_step(t) + (n + 8) * U))[rest].all()
+
+
 # ---- norms of rows whose squares leave fp32's range
 
 @pytest.mark.parametrize("d", [8, 77, 960, 1024, 2056, 4100, 8192])
