@@ -1,4 +1,4 @@
-// Shared by the operators behind include/tagore_embed.h: element types, 16-byte pieces of rows, and the launchers.
+// Shared by the operators behind include/tagore_embed.h and include/tagore_learn.h: element types, 16-byte pieces of rows, and the launchers.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -114,7 +114,27 @@ void tg_launch_product(const int8_t* a, const float* as, const int8_t* b, const 
 size_t tg_xent_space(int64_t n, int64_t n_rows, int d, int dtype, int aligned);
 void tg_launch_xent(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const void* targets,
                     int targets64, float scale, float* loss, float* lse, void* space, hipStream_t s);
-size_t tg_xent_grad_space(int64_t n, int64_t n_rows, int d, int dtype, int aligned, bool least);
-void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d,
-                         const void* targets, int targets64, const float* lse, const float* dloss, float scale, void* dh, void* dw,
-                         void* space, size_t bytes, hipStream_t s);
+// What a softmax's gradient starts from: the gradients of the losses (gain -1: of the log probabilities), and of the entropies, or null.
+struct XentTokens {
+    const void* targets;
+    int targets64;
+    const float *lse, *dloss;
+    float gain;
+    const float *entropy, *dentropy;
+};
+// table: whether dw is asked for
+size_t tg_xent_grad_space(int64_t n, int64_t n_rows, int d, int dtype, int aligned, bool least, bool table);
+void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const XentTokens& t,
+                         float scale, void* dh, void* dw, void* space, size_t bytes, hipStream_t s);
+
+// ---- tg_logprobs.hip
+size_t tg_log_probs_space(int64_t n, int64_t n_rows, int d, int dtype, int top, int aligned);
+void tg_launch_log_probs(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const void* targets,
+                         int targets64, float scale, int top, float* logp, float* entropy, float* lse, int32_t* rows, float* row_logp, void* space,
+                         hipStream_t s);
+
+// ---- tg_clip.hip
+size_t tg_grad_norm_space(const int64_t* counts, int tensors);
+// out null: the norm alone
+void tg_launch_clip(const void* const* grads, void* const* out, const int64_t* counts, const int32_t* dtypes, int tensors, float scale, float max_norm,
+                    float* norm, void* space, hipStream_t s);

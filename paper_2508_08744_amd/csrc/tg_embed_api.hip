@@ -1,14 +1,21 @@
-// The C boundary of include/tagore_embed.h: argument checks and workspaces.  Host code only; the device's steps are the launchers of
+// The C boundary of include/tagore_embed.h and include/tagore_learn.h: argument checks and workspaces.  Host code only; the device's steps are the launchers of
 // tg_embed.h.
 #include "../../include/tagore_embed.h"
+#include "../../include/tagore_learn.h"
 #include "tg_embed.h"
 #include "tg_error.h"
+
+#include <algorithm>
+#include <new>
 
 #define TG_MAX_COUNT (1ll << 30)
 #define TG_MAX_LOOKUP_D 65536
 #define TG_MAX_D 8192
 #define TG_MAX_TOKENS (1ll << 28)  // of a softmax: its gradient runs along them, in bytes of 32 bits
 #define TG_MAX_K 65536
+#define TG_MAX_BEST 32                // rows of a token
+#define TG_MAX_TENSORS (1 << 20)
+#define TG_MAX_VALUES (1ll << 40)
 #define TG_MAX_PITCH (1 << 20)       // bytes between rows that are read where they are
 
 static hipStream_t stream_of(void* s) { return reinterpret_cast<hipStream_t>(s); }
@@ -234,7 +241,7 @@ extern "C" int tg_softmax_xent(const void* h, int64_t ld_h, const void* w, int64
 }
 extern "C" size_t tg_softmax_xent_grad_workspace(int64_t n, int64_t n_rows, int32_t d, int32_t dtype, int32_t aligned)
 {
-    return check_xent(n, n_rows, d, dtype) != TG_OK || check_aligned(aligned) != TG_OK ? 0 : tg_xent_grad_space(n, n_rows, d, dtype, aligned, false);
+    return check_xent(n, n_rows, d, dtype) != TG_OK || check_aligned(aligned) != TG_OK ? 0 : tg_xent_grad_space(n, n_rows, d, dtype, aligned, false, true);
 }
 extern "C" int tg_softmax_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32_t dtype, int64_t n, int64_t n_rows, int32_t d,
                                     const void* targets, int32_t targets64, const float* lse, const float* dloss, float scale, void* out_dh,
@@ -245,8 +252,133 @@ extern "C" int tg_softmax_xent_grad(const void* h, int64_t ld_h, const void* w, 
     CHECK(check_ld("ld_w", ld_w, d));
     CHECK(check_flag("targets64", targets64));
     if (!out_dw || (n > 0 && (!h || !w || !targets || !lse || !dloss || !out_dh))) return null_argument();
-    CHECK(check_space(workspace, workspace_bytes, tg_xent_grad_space(n, n_rows, d, dtype, rows_ready(h, ld_h, w, ld_w, dtype), true)));
-    tg_launch_xent_grad(h, ld_h, w, ld_w, dtype, n, n_rows, d, targets, targets64, lse, dloss, scale, out_dh, out_dw, workspace, workspace_bytes,
-                        stream_of(stream));
+    CHECK(check_space(workspace, workspace_bytes, tg_xent_grad_space(n, n_rows, d, dtype, rows_ready(h, ld_h, w, ld_w, dtype), true, true)));
+    const XentTokens t{targets, targets64, lse, dloss, 1.0f, nullptr, nullptr};
+    tg_launch_xent_grad(h, ld_h, w, ld_w, dtype, n, n_rows, d, t, scale, out_dh, out_dw, workspace, workspace_bytes, stream_of(stream));
     return launched("gradient of the softmax cross entropy");
+}
+
+static int check_best(int32_t top)
+{
+    return top >= 0 && top <= TG_MAX_BEST ? TG_OK : tg_fail(TG_ERR_INVALID_ARG, "top = %d outside 0..%d", top, TG_MAX_BEST);
+}
+extern "C" size_t tg_log_probs_workspace(int64_t n, int64_t n_rows, int32_t d, int32_t dtype, int32_t top, int32_t aligned)
+{
+    return check_xent(n, n_rows, d, dtype) != TG_OK || check_best(top) != TG_OK || check_aligned(aligned) != TG_OK ? 0
+                                                                                                                  : tg_log_probs_space(n, n_rows, d, dtype, top, aligned);
+}
+extern "C" int tg_log_probs(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32_t dtype, int64_t n, int64_t n_rows, int32_t d,
+                            const void* targets, int32_t targets64, float scale, int32_t top, float* out_logp, float* out_entropy, float* out_lse,
+                            int32_t* out_rows, float* out_row_logp, void* workspace, size_t workspace_bytes, void* stream)
+{
+    CHECK(check_xent(n, n_rows, d, dtype));
+    CHECK(check_best(top));
+    CHECK(check_ld("ld_h", ld_h, d));
+    CHECK(check_ld("ld_w", ld_w, d));
+    CHECK(check_flag("targets64", targets64));
+    if (n == 0) return TG_OK;
+    if (!h || !w || (targets && !out_logp) || !out_entropy || !out_lse || (top && (!out_rows || !out_row_logp))) return null_argument();
+    CHECK(check_space(workspace, workspace_bytes, tg_log_probs_space(n, n_rows, d, dtype, top, rows_ready(h, ld_h, w, ld_w, dtype))));
+    tg_launch_log_probs(h, ld_h, w, ld_w, dtype, n, n_rows, d, targets, targets64, scale, top, out_logp, out_entropy, out_lse, out_rows, out_row_logp,
+                        workspace, stream_of(stream));
+    return launched("log probabilities");
+}
+extern "C" size_t tg_log_probs_grad_workspace(int64_t n, int64_t n_rows, int32_t d, int32_t dtype, int32_t table, int32_t aligned)
+{
+    return check_xent(n, n_rows, d, dtype) != TG_OK || check_flag("table", table) != TG_OK || check_aligned(aligned) != TG_OK
+               ? 0
+               : tg_xent_grad_space(n, n_rows, d, dtype, aligned, false, table != 0);
+}
+extern "C" int tg_log_probs_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32_t dtype, int64_t n, int64_t n_rows, int32_t d,
+                                 const void* targets, int32_t targets64, const float* lse, const float* dlogp, const float* entropy,
+                                 const float* dentropy, float scale, void* out_dh, void* out_dw, void* workspace, size_t workspace_bytes, void* stream)
+{
+    CHECK(check_xent(n, n_rows, d, dtype));
+    CHECK(check_ld("ld_h", ld_h, d));
+    CHECK(check_ld("ld_w", ld_w, d));
+    CHECK(check_flag("targets64", targets64));
+    if (n > 0 && (!h || !w || !targets || !lse || !dlogp || !out_dh || (dentropy && !entropy))) return null_argument();
+    if (n == 0 && !out_dw) return TG_OK;
+    CHECK(check_space(workspace, workspace_bytes, tg_xent_grad_space(n, n_rows, d, dtype, rows_ready(h, ld_h, w, ld_w, dtype), true, out_dw != nullptr)));
+    const XentTokens t{targets, targets64, lse, dlogp, -1.0f, entropy, dentropy};
+    tg_launch_xent_grad(h, ld_h, w, ld_w, dtype, n, n_rows, d, t, scale, out_dh, out_dw, workspace, workspace_bytes, stream_of(stream));
+    return launched("gradient of the log probabilities");
+}
+
+static int check_counts(const int64_t* counts, int32_t tensors)
+{
+    if (tensors < 0 || tensors > TG_MAX_TENSORS) return tg_fail(TG_ERR_INVALID_ARG, "tensors = %d outside 0..2^20", tensors);
+    if (tensors && !counts) return null_argument();
+    for (int32_t i = 0; i < tensors; ++i)
+        if (counts[i] < 0 || counts[i] >= TG_MAX_VALUES) return tg_fail(TG_ERR_INVALID_ARG, "counts[%d] = %lld outside 0..2^40-1", i, (long long)counts[i]);
+    return TG_OK;
+}
+static int check_grads(const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t tensors, float scale)
+{
+    CHECK(check_counts(counts, tensors));
+    if (tensors && (!grads || !dtypes)) return null_argument();
+    if (!(scale >= -3.4028234e38f && scale <= 3.4028234e38f)) return tg_fail(TG_ERR_INVALID_ARG, "scale must be finite");
+    for (int32_t i = 0; i < tensors; ++i) {
+        CHECK(check_dtype(dtypes[i]));
+        if (counts[i] > 0 && !grads[i]) return null_argument();
+        if ((uintptr_t)grads[i] % tg_type_bytes(dtypes[i])) return tg_fail(TG_ERR_INVALID_ARG, "grads[%d] is not aligned to its type", i);
+    }
+    return TG_OK;
+}
+extern "C" size_t tg_grad_norm_workspace(const int64_t* counts, int32_t tensors)
+{
+    return check_counts(counts, tensors) != TG_OK ? 0 : tg_grad_norm_space(counts, tensors);
+}
+extern "C" int tg_grad_norm(const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t tensors, float scale, float* out_norm,
+                            void* workspace, size_t workspace_bytes, void* stream)
+{
+    CHECK(check_grads(grads, counts, dtypes, tensors, scale));
+    if (!out_norm) return null_argument();
+    CHECK(check_space(workspace, workspace_bytes, tg_grad_norm_space(counts, tensors)));
+    tg_launch_clip(grads, nullptr, counts, dtypes, tensors, scale, 0.0f, out_norm, workspace, stream_of(stream));
+    return launched("norm of the gradients");
+}
+
+// No tensor is written where another is read or written.
+struct ClipRange {
+    uintptr_t from, to;
+    bool written;
+};
+static int check_ranges(const void* const* grads, void* const* out, const int64_t* counts, const int32_t* dtypes, int32_t tensors)
+{
+    ClipRange* const r = new (std::nothrow) ClipRange[2 * (size_t)tensors + 1];
+    if (!r) return tg_fail(TG_ERR_INVALID_ARG, "no memory for the ranges of %d tensors", tensors);
+    size_t n = 0;
+    for (int32_t i = 0; i < tensors; ++i) {
+        const uintptr_t bytes = (uintptr_t)counts[i] * tg_type_bytes(dtypes[i]), o = (uintptr_t)out[i], g = (uintptr_t)grads[i];
+        if (!bytes) continue;
+        r[n++] = ClipRange{o, o + bytes, true};
+        if (o != g) r[n++] = ClipRange{g, g + bytes, false};
+    }
+    const auto before = [](const ClipRange& x, const ClipRange& y) { return x.from < y.from; };
+    if (!std::is_sorted(r, r + n, before)) std::sort(r, r + n, before);
+    uintptr_t read = 0, written = 0;             // the ends of what is before
+    bool apart = true;
+    for (size_t i = 0; i < n; ++i) {
+        apart = apart && r[i].from >= written && !(r[i].written && r[i].from < read);
+        uintptr_t& end = r[i].written ? written : read;
+        if (r[i].to > end) end = r[i].to;
+    }
+    delete[] r;
+    return apart ? TG_OK : tg_fail(TG_ERR_INVALID_ARG, "a tensor would be written where another one of the call is");
+}
+extern "C" int tg_clip_grads(const void* const* grads, void* const* out, const int64_t* counts, const int32_t* dtypes, int32_t tensors, float max_norm,
+                             float scale, float* out_norm, void* workspace, size_t workspace_bytes, void* stream)
+{
+    CHECK(check_grads(grads, counts, dtypes, tensors, scale));
+    if (!(max_norm >= 0.0f)) return tg_fail(TG_ERR_INVALID_ARG, "max_norm must not be below 0");
+    if (!out_norm || (tensors && !out)) return null_argument();
+    for (int32_t i = 0; i < tensors; ++i) {
+        if (counts[i] > 0 && !out[i]) return null_argument();
+        if ((uintptr_t)out[i] % tg_type_bytes(dtypes[i])) return tg_fail(TG_ERR_INVALID_ARG, "out[%d] is not aligned to its type", i);
+    }
+    CHECK(check_ranges(grads, out, counts, dtypes, tensors));
+    CHECK(check_space(workspace, workspace_bytes, tg_grad_norm_space(counts, tensors)));
+    tg_launch_clip(grads, out, counts, dtypes, tensors, scale, max_norm, out_norm, workspace, stream_of(stream));
+    return launched("clipping of the gradients");
 }

@@ -1,0 +1,636 @@
+// Log probabilities of given rows of a table, the entropy of the softmax over all of them, and the best rows, without the logits.
+//
+// A tile of logits stays in the registers of the workgroup that formed it.  For every token it leaves the maximum m, the sum l of 2^t and the
+// sum s of t 2^t, t = (z - m) log2(e): joined over the table they give lse = m + log l and the entropy log l - log(2) s / l.  2 n n_rows d operations on the
+// matrix instructions bound it, or, for few tokens, the bytes of the table.
+//
+// The best rows are those of the largest logits in 64 bits, and the logits of the tiles are in 32.  So the tiles leave, of every 32 logits of a token (LP_GROUP), the
+// largest with its row and an upper bound of the second: a quarter of a byte a logit.  With 64 lanes over a token's groups, the k-th largest of the lanes' largest is below the k-th
+// logit; whatever is further below it than the roundings of 32 bits reach (a bound from the norms of the token's row and of the table's, see lp_margin) is none of
+// the k best.  What is left, some k rows, is scored again in 64 bits and put in order.  A group whose second is not out of reach is scored as a whole.
+#include "tg_embed.h"
+#include "tg_softmax.h"
+#include "tg_tiles.h"
+
+#define LP_GROUP 32             // logits of a token that leave their largest
+#define LP_MAX_TOP 32           // best rows; half the lanes of a wave, see lp_kth
+#define LP_BELOW (-1000.0f)     // exponents below have a power of 0: so is their part in s, at -infinity too
+
+typedef unsigned int lp_u32;
+
+// (maximum, sum, sum below it) over stretches of a table; one that stands for nothing is (-infinity, 0, 0)
+struct LpSum { float m, l, s; };
+__device__ inline void lp_join(LpSum& a, const LpSum& b)
+{
+    const float top = fmaxf(a.m, b.m);
+    const float wa = a.m == top ? 1.0f : xent_exp(a.m - top), wb = b.m == top ? 1.0f : xent_exp(b.m - top);
+    // (a weight of 0 may come from a difference that is infinite)
+    const float sa = a.m == top ? a.s : wa > 0.0f ? wa * (a.s + (a.m - top) * XENT_LOG2E * a.l) : 0.0f;
+    const float sb = b.m == top ? b.s : wb > 0.0f ? wb * (b.s + (b.m - top) * XENT_LOG2E * b.l) : 0.0f;
+    a.l = a.l * wa + b.l * wb;
+    a.s = sa + sb;
+    a.m = top;
+}
+
+// The second of a group, rounded up, with the largest one's row in the tile (below 256) in its last bits.  As a value it is no smaller than the second; beyond
+// fp32's range it is a NaN, which is below nothing.
+__device__ inline lp_u32 lp_pack(float second, int row) { return ((tg_ord(fmaxf(second, -3.38e38f)) & ~255u) + 256u) | (lp_u32)row; }
+__device__ inline float lp_second(lp_u32 key) { return tg_unord(key); }
+__device__ inline int lp_row(lp_u32 key) { return (int)(key & 255u); }
+
+// x: rows of the table from v0 on, y: tokens.  parts: for every token the tiles along x; groups: for every token, tile and group (largest, packed second).
+template <class E, int BM, int BN, int WM, int WN, int NB, bool TOP>
+__global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
+                                                               float scale, int64_t v0, int64_t n_rows, uint32_t nx, uint32_t ny, uint32_t group,
+                                                               float4* __restrict__ parts, int64_t parts_pitch, uint2* __restrict__ groups,
+                                                               float* __restrict__ at_target)
+{
+    typedef Tile<E, BM, BN, WM, WN, false, false, NB> T;
+    constexpr int Q = 8 / T::FM, GROUPS = BM / LP_GROUP;       // quarters of a wave (16 lanes each) that share a group; groups of a tile
+    static_assert(!TOP || (Q >= 1 && Q * T::FM == 8), "groups of 32 rows");
+    __shared__ __align__(1024) char lds[T::LDS];
+    // the tokens' targets among the tile's rows: asked for before the products, so that nothing waits for them behind
+    __shared__ int s_target[BN];
+    uint32_t tx, ty;
+    tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
+    const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
+    T t;
+    t.start(X, Y, x0, y0, 0, bytes, lds);
+    if (threadIdx.x < BN) {
+        const int64_t y = y0 + threadIdx.x, target = targets && y < Y.rows ? tg_row_of(targets, targets64, y, n_rows) - v0 - x0 : -1;
+        s_target[threadIdx.x] = target >= 0 && target < BM ? (int)target : -1;
+    }
+    t.loop();
+    // (the tile's memory is free: a sum for every token and wave along x)
+    LpSum* const s_sum = reinterpret_cast<LpSum*>(lds) + (threadIdx.x >> 6) / WN * BN;
+    static_assert(WM * BN * sizeof(LpSum) <= T::LDS, "the sums' place");
+    const int have = x0 + BM <= X.rows ? BM : (int)(X.rows - x0);
+    const int none = (threadIdx.x >> 6) / WN * (T::HM * 16);        // the wave's first row: where the table ends before it there are no logits
+    const float base = scale * XENT_LOG2E;
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+        const int64_t y = y0 + t.y_of(j);
+        const int target = s_target[t.y_of(j)];
+        float m = -__builtin_inff(), second = m, l = 0.0f, s = 0.0f;
+        int at = 0;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+            const int x = t.x_of(i);
+            if ((unsigned)(target - x) < 4u) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (x + e == target) at_target[y] = t.acc[i][j][e] * scale;
+            }
+            const auto take = [&](int e) {
+                const float z = t.acc[i][j][e] * scale;
+                if (TOP) {
+                    at = z > m ? i * 4 + e : at;
+                    second = __builtin_amdgcn_fmed3f(m, second, z);
+                }
+                m = fmaxf(m, z);
+            };
+            if (x + 4 <= have) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) take(e);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (x + e < have) take(e);
+            }
+        }
+        if (TOP) {
+            // (x_of for an i that is not known in advance)
+            const int i = at >> 2;
+            int x = (i / T::HM) * (BM / 2) + none + (i % T::HM) * 16 + (threadIdx.x >> 4 & 3) * 4 + (at & 3);
+            float top = m;
+#pragma unroll
+            for (int q = 1; q < Q; q <<= 1) {
+                const float top2 = __shfl_xor(top, q * 16), second2 = __shfl_xor(second, q * 16);
+                const int x2 = __shfl_xor(x, q * 16);
+                x = top2 > top ? x2 : x;
+                second = fmaxf(fminf(top, top2), fmaxf(second, second2));
+                top = fmaxf(top, top2);
+            }
+            const int quarter = threadIdx.x >> 4 & 3;
+            if (quarter % Q == 0 && y < Y.rows)
+                groups[(y * parts_pitch + tx) * GROUPS + (threadIdx.x >> 6) / WN * (4 / Q) + quarter / Q] = make_uint2(__float_as_uint(top), lp_pack(second, x));
+        }
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const bool near = xent_near(m, base) || have <= none;
+        const float f = near ? base : 1.0f, b = near ? m * XENT_LOG2E : 0.0f;
+        if (__builtin_expect(!__all(near), 0)) {           // (out of the way: code that is jumped over is fetched late)
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t.acc[i][j][e] = near ? t.acc[i][j][e] : xent_far<true>(t.acc[i][j][e], scale, m);
+        }
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+            const int x = t.x_of(i);
+            const auto take = [&](int e) {
+                const float u = fmaf(t.acc[i][j][e], f, -b), p = __builtin_amdgcn_exp2f(u);
+                l += p;
+                s = fmaf(p, fmaxf(u, LP_BELOW), s);
+            };
+            if (x + 4 <= have) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) take(e);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (x + e < have) take(e);
+            }
+        }
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if (tg_lane() < 16) s_sum[t.y_of(j)] = LpSum{m, l, s};
+    }
+    __syncthreads();
+    if (threadIdx.x < BN && y0 + threadIdx.x < Y.rows) {
+        const LpSum* sum = reinterpret_cast<const LpSum*>(lds) + threadIdx.x;
+        LpSum a = sum[0];
+#pragma unroll
+        for (int w = 1; w < WM; ++w) lp_join(a, sum[w * BN]);
+        parts[(y0 + threadIdx.x) * parts_pitch + tx] = make_float4(a.m, a.l, a.s, 0.0f);
+    }
+}
+
+// The largest sum of the squares of `each` rows at a time.  LANES lanes a row; a row is read once.
+template <class E>
+__global__ __launch_bounds__(256) void lp_norms_kernel(const E* __restrict__ w, int64_t ld, int64_t n_rows, int d, int each, int lanes, float* __restrict__ out, int64_t count)
+{
+    __shared__ float s_top[4];
+    typedef TgPiece<E> P;
+    const int of = threadIdx.x & (lanes - 1), rows = 256 / lanes, first = threadIdx.x / lanes;
+    for (int64_t b = blockIdx.x; b < count; b += gridDim.x) {
+        float top = 0.0f;
+        for (int r = first; r < each; r += rows) {
+            const int64_t v = b * each + r;
+            float sum = 0.0f;
+            if (v < n_rows)
+                for (int c = of * P::E; c < d; c += lanes * P::E) {
+                    P p;
+                    p.load(w + v * ld + c, d - c);
+#pragma unroll
+                    for (int e = 0; e < P::E; ++e) sum = fmaf(p.v[e], p.v[e], sum);
+                }
+            for (int m = 1; m < lanes; m <<= 1) sum += __shfl_xor(sum, m);
+            top = fmaxf(top, sum);
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+        if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
+        __syncthreads();
+        if (threadIdx.x == 0) out[b] = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+        __syncthreads();
+    }
+}
+
+// How far a logit of the tiles is from its exact value at most.  Every one of the d products and sums is off by less than 2^-23 of the sum of the products'
+// magnitudes (twice the step of rounding to the nearest: nothing is taken for granted of how the matrix instructions add), the factor's product by as much, and that
+// sum is at most |h| |w|.  The squares' sums are off by less than d 2^-23 themselves, and what of them is too small for the type's products is added.
+template <class E>
+__device__ inline double lp_margin(float scale, int d, double h2, double w2)
+{
+    const double lost = (__is_same(E, tg_f16) ? 0x1p-28 : 0x1p-126) * d, more = 1.0 + d * 0x1p-22;
+    return fabs((double)scale) * (d + 2) * 0x1p-23 * sqrt((h2 + lost) * more) * sqrt((w2 + lost) * more) + 0x1p-120;
+}
+
+// The k-th largest of a wave's values (k <= 64), the same in all lanes; a NaN counts as the smallest.
+__device__ inline float lp_kth(float v, int k)
+{
+    const lp_u32 mine = v != v ? 0u : tg_ord(v);
+    int rank = 0;
+#pragma unroll 8
+    for (int i = 0; i < 64; ++i) {
+        const lp_u32 other = (lp_u32)__builtin_amdgcn_readlane((int)mine, i);
+        rank += other > mine || (other == mine && i < tg_lane()) ? 1 : 0;
+    }
+    const u64 is = __ballot(rank == k - 1);
+    return __uint_as_float((lp_u32)__builtin_amdgcn_readlane((int)__float_as_uint(v), __builtin_ctzll(is)));
+}
+
+__device__ inline double lp_lane64(double x, int lane)
+{
+    const u64 b = __double_as_longlong(x);
+    const u64 lo = (u32)__builtin_amdgcn_readlane((int)(u32)b, lane), hi = (u32)__builtin_amdgcn_readlane((int)(u32)(b >> 32), lane);
+    return __longlong_as_double((long long)(hi << 32 | lo));
+}
+__device__ inline double lp_xor64(double x, int m) { return __longlong_as_double((long long)tg_shfl_xor64((u64)__double_as_longlong(x), m)); }
+
+// A wave's k best so far, the i-th in lane i: by logit, then by row.
+struct LpBest {
+    static constexpr int NONE = 0x7FFFFFFF;
+    double z;
+    int row;
+    int k;
+    double last_z;               // the k-th
+    int last_row;
+
+    __device__ inline void begin(int count)
+    {
+        z = last_z = 0.0;             // (no 64-bit infinity: hipcc 7.2 moves such a constant into scalar registers by an instruction that holds 32 bits of it)
+        row = last_row = NONE;
+        k = count;
+    }
+    // (a place without a row is behind all)
+    static __device__ inline bool before(double az, int ar, double bz, int br) { return br == NONE ? ar != NONE : ar != NONE && (az > bz || (az == bz && ar < br)); }
+    // whether a row of a logit up to `most` is worth a look
+    __device__ inline bool wants(double most, int r) const { return before(most, r, last_z, last_row); }
+    // (the same in all lanes)
+    __device__ inline void add(double cz, int cr)
+    {
+        if (!before(cz, cr, last_z, last_row)) return;
+        const u64 ahead = __ballot(before(z, row, cz, cr));
+        const int at = __popcll(ahead);             // (in order: those ahead are the first lanes)
+        const double up_z = __longlong_as_double((long long)tg_shfl64((u64)__double_as_longlong(z), (tg_lane() + 63) & 63));
+        const int up_row = __shfl(row, (tg_lane() + 63) & 63);
+        if (tg_lane() == at) {
+            z = cz;
+            row = cr;
+        } else if (tg_lane() > at) {
+            z = up_z;
+            row = up_row;
+        }
+        last_z = lp_lane64(z, k - 1);
+        last_row = __builtin_amdgcn_readlane(row, k - 1);
+    }
+};
+
+struct LpTop {
+    const void *h, *w;           // the caller's
+    int64_t ld_h, ld_w;
+    int d, tile, shared;         // tile: rows of the table; shared: the quarters of a wave that share a group
+    int top;
+    const float* norms;
+    const uint2* groups;
+    int64_t n_groups;
+    int32_t* rows;
+    float* row_logp;
+};
+
+// Eight rows' logits in 64 bits, by one wave: every lane has the same places of all rows, so a row's sum does not depend on where it was found.
+template <class E>
+__device__ inline void lp_score(const LpTop& a, const E* h, double scale, const int* pending, int count, LpBest& best)
+{
+    typedef TgPiece<E> P;
+    const int lane = tg_lane();
+    int rows[8];
+    const E* w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        rows[i] = __builtin_amdgcn_readfirstlane(pending[i < count ? i : 0]);
+        w[i] = (const E*)a.w + (int64_t)rows[i] * a.ld_w;
+    }
+    double sum[8] = {};
+    for (int c = lane * P::E; c < a.d; c += 64 * P::E) {
+        typename P::vec x[8];
+        P hp;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = P::raw(w[i] + c, a.d - c);
+        hp.load(h + c, a.d - c);
+#pragma unroll
+        for (int e = 0; e < P::E; ++e)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = fma((double)hp.v[e], (double)(float)x[i][e], sum[i]);
+    }
+    // row i's sum ends up in the lanes whose bits 5, 4, 3 are i's bits 2, 1, 0
+    double s4[4], s2[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s4[i] = (lane & 32 ? sum[i + 4] : sum[i]) + lp_xor64(lane & 32 ? sum[i] : sum[i + 4], 32);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) s2[i] = (lane & 16 ? s4[i + 2] : s4[i]) + lp_xor64(lane & 16 ? s4[i] : s4[i + 2], 16);
+    double s = (lane & 8 ? s2[1] : s2[0]) + lp_xor64(lane & 8 ? s2[0] : s2[1], 8);
+#pragma unroll
+    for (int m = 4; m >= 1; m >>= 1) s += lp_xor64(s, m);
+    s *= scale;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < count) best.add(lp_lane64(s, i * 8), rows[i]);
+}
+
+// The tiles' sums joined, and the best rows, by W waves a token.
+template <class E, int W, bool TOP>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const float4* __restrict__ parts, int64_t count, int64_t n, int64_t n_rows,
+                                                                       const void* __restrict__ targets, int targets64, const float* __restrict__ at_target,
+                                                                       float scale, LpTop a, float* __restrict__ logp, float* __restrict__ entropy,
+                                                                       float* __restrict__ lse)
+{
+    constexpr int TOKENS = W == 1 ? 4 : 1;
+    constexpr int PENDING = 7 + 64 + LP_GROUP;
+    __shared__ LpSum s_sum[W];
+    __shared__ double s_h2[W];
+    __shared__ float s_w2[W], s_top[W > 1 ? W : 1][W > 1 ? 64 : 1];
+    __shared__ int s_pending[TOP ? TOKENS * W : 1][TOP ? PENDING : 1];
+    __shared__ double s_best_z[TOP && W > 1 ? W : 1][LP_MAX_TOP];
+    __shared__ int s_best_row[TOP && W > 1 ? W : 1][LP_MAX_TOP];
+    const int lane = tg_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int of = W == 1 ? lane : threadIdx.x;                  // of the token's lanes
+    const int mine = W == 1 ? 0 : wave;                          // of its waves
+    for (int64_t y = (int64_t)blockIdx.x * TOKENS + (W == 1 ? wave : 0); y < n; y += (int64_t)gridDim.x * TOKENS) {
+        LpSum sum{-__builtin_inff(), 0.0f, 0.0f};
+        for (int64_t p0 = of; p0 < count; p0 += 4 * 64 * W) {
+            float4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = p0 + i * 64 * W < count ? parts[y * count + p0 + i * 64 * W] : make_float4(-__builtin_inff(), 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lp_join(sum, LpSum{v[i].x, v[i].y, v[i].z});
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) lp_join(sum, LpSum{__shfl_xor(sum.m, m), __shfl_xor(sum.l, m), __shfl_xor(sum.s, m)});
+        // what the margin is made of, and the largest logits of the lanes' groups
+        double h2 = 0.0;
+        float w2 = 0.0f, high = -__builtin_inff();
+        const E* const h = (const E*)a.h + y * a.ld_h;
+        const uint2* const groups = a.groups + y * a.n_groups;
+        if (TOP) {
+            typedef TgPiece<E> P;
+            for (int c = of * P::E; c < a.d; c += 64 * W * P::E) {
+                P p;
+                p.load(h + c, a.d - c);
+#pragma unroll
+                for (int e = 0; e < P::E; ++e) h2 = fma((double)p.v[e], (double)p.v[e], h2);
+            }
+            for (int64_t p = of; p < count; p += 64 * W) w2 = fmaxf(w2, a.norms[p]);
+            for (int64_t g0 = of; g0 < a.n_groups; g0 += 8 * 64 * W) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = g0 + i * 64 * W < a.n_groups ? __uint_as_float(groups[g0 + i * 64 * W].x) : -__builtin_inff();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) high = fmaxf(high, v[i]);
+            }
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) {
+                h2 += lp_xor64(h2, m);
+                w2 = fmaxf(w2, __shfl_xor(w2, m));
+            }
+        }
+        if (W > 1) {
+            __syncthreads();                                     // (the token before is done with these)
+            if (lane == 0) {
+                s_sum[wave] = sum;
+                s_h2[wave] = h2;
+                s_w2[wave] = w2;
+            }
+            if (TOP) s_top[wave][lane] = high;
+            __syncthreads();
+            sum = s_sum[0];
+#pragma unroll
+            for (int i = 1; i < W; ++i) lp_join(sum, s_sum[i]);
+            if (TOP) {
+                h2 = 0.0;
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    h2 += s_h2[i];
+                    w2 = fmaxf(w2, s_w2[i]);
+                    high = fmaxf(high, s_top[i][lane]);
+                }
+            }
+        }
+        const float all = sum.m + logf(sum.l);
+        if (of == 0) {
+            lse[y] = all;
+            const float below = logf(sum.l) - 0.6931471805599453f * (sum.s / sum.l);
+            // (probabilities of infinite logits are not defined)
+            entropy[y] = fabsf(all) <= 3.4028234e38f ? fmaxf(below, 0.0f) : __builtin_nanf("");
+            if (logp) logp[y] = tg_row_of(targets, targets64, y, n_rows) >= 0 ? at_target[y] - all : 0.0f;
+        }
+        if (!TOP) continue;
+        if (all != all) {                                        // a NaN among the logits
+            if (mine == 0 && lane < a.top) {
+                a.rows[y * a.top + lane] = -1;
+                a.row_logp[y * a.top + lane] = all;
+            }
+            continue;
+        }
+        const double margin = lp_margin<E>(scale, a.d, h2, w2);
+        const double low = (double)lp_kth(high, a.top) - 2.0 * margin;
+        LpBest best;
+        best.begin(a.top);
+        int* const pending = s_pending[TOP ? wave : 0];
+        int waiting = 0;
+        const int per = a.tile / LP_GROUP;
+        const auto drain = [&](int least) {
+            int done = 0;
+            while (waiting - done >= least && waiting > done) {
+                const int now = waiting - done < 8 ? waiting - done : 8;
+                lp_score<E>(a, h, (double)scale, pending + done, now, best);
+                done += now;
+            }
+            // the rest to the front: fewer than 8
+            const int rest = waiting - done, r = lane < rest ? pending[done + lane] : 0;
+            __builtin_amdgcn_wave_barrier();
+            if (lane < rest) pending[lane] = r;
+            __builtin_amdgcn_wave_barrier();
+            waiting = rest;
+        };
+        for (int64_t g0 = (int64_t)mine * 64; g0 < a.n_groups; g0 += 64 * W) {
+            const int64_t g = g0 + lane;
+            const uint2 v = g < a.n_groups ? groups[g] : make_uint2(0, 0);
+            const double first = (double)__uint_as_float(v.x);
+            const int64_t row0 = g / per * a.tile;
+            // (what a NaN is compared with is not out of reach)
+            const bool hit = g < a.n_groups && !(first < low) && best.wants(first + margin, (int)row0);
+            u64 many = __ballot(hit && !((double)lp_second(v.y) < low));
+            const int64_t row = row0 + lp_row(v.y);
+            const u64 one = __ballot(hit && (double)lp_second(v.y) < low && row < n_rows);
+            if (one >> lane & 1) pending[waiting + __popcll(one & tg_lanemask_lt())] = (int)row;
+            waiting += __popcll(one);
+            __builtin_amdgcn_wave_barrier();
+            if (waiting >= 8) drain(8);
+            while (many) {
+                const int from = __builtin_ctzll(many);
+                const double most = lp_lane64(first + margin, from);
+                many &= many - 1;
+                const int64_t gg = g0 + from, tile = gg / per;
+                const int in = (int)(gg - tile * per), sh = a.shared, waves = 4 / sh;
+                // row number `lane` of the group: of value e, quarter q and block i of the wave's rows (see lp_part_kernel)
+                const int e = lane & 3, q = (lane >> 2) % sh + in % waves * sh, i = (lane >> 2) / sh, half = 4 / sh;
+                const int64_t r = tile * a.tile + i / half * (a.tile / 2) + in / waves * (half * 16) + i % half * 16 + q * 4 + e;
+                const bool is = lane < LP_GROUP && r < n_rows && best.wants(most, (int)r);
+                const u64 some = __ballot(is);
+                if (is) pending[waiting + __popcll(some & tg_lanemask_lt())] = (int)r;
+                waiting += __popcll(some);
+                __builtin_amdgcn_wave_barrier();
+                drain(8);
+            }
+        }
+        drain(1);
+        if (W > 1) {
+            if (lane < a.top) {
+                s_best_z[wave][lane] = best.z;
+                s_best_row[wave][lane] = best.row;
+            }
+            __syncthreads();
+            if (wave == 0) {
+                for (int i = 1; i < W; ++i)
+                    for (int j = 0; j < a.top; ++j) {
+                        const double z = s_best_z[i][j];
+                        const int r = s_best_row[i][j];
+                        if (r == LpBest::NONE || !best.wants(z, r)) break;        // (theirs are in order too)
+                        best.add(z, r);
+                    }
+            }
+        }
+        if (mine == 0 && lane < a.top) {
+            const double p = best.z - (double)all;
+            a.rows[y * a.top + lane] = best.row == LpBest::NONE ? -1 : best.row;
+            a.row_logp[y * a.top + lane] = best.row == LpBest::NONE ? -__builtin_inff() : (float)(p > 0.0 ? 0.0 : p);
+        }
+    }
+}
+
+// ---- workspaces and launches
+struct LpShape {
+    int bm, bn, shared;          // the tile; see LpTop
+    bool few;                    // four stages in flight
+    int64_t tiles;               // along the table
+    int64_t tokens;              // at a time
+};
+// tokens at a time: as many as the groups' stretches have room for, in whole tiles
+#define LP_GROUP_BYTES (512ll << 20)
+static LpShape lp_shape(int64_t n, int64_t n_rows, int e)
+{
+    LpShape s;
+    // (the tiles of the cross entropy's logits)
+    int64_t most = LP_GROUP_BYTES / (int64_t)sizeof(uint2) / ((n_rows + LP_GROUP - 1) / LP_GROUP);
+    most = most >= 256 ? most / 256 * 256 : most >= 64 ? 64 : 32;
+    s.tokens = n < most ? n : most;
+    const auto tiles = [&](int64_t x, int64_t y) { return ((n_rows + x - 1) / x) * ((s.tokens + y - 1) / y); };
+    s.few = tiles(128, 128) <= 128;
+    if (s.tokens <= 32) s.bm = 128, s.bn = 32, s.shared = 4;
+    else if (s.few || (e == 4 && s.tokens > 64)) s.bm = 64, s.bn = 64, s.shared = 4;
+    else if (s.tokens <= 64) s.bm = 128, s.bn = 64, s.shared = 4;
+    else if (tiles(256, 256) >= 200) s.bm = 256, s.bn = 256, s.shared = 1;
+    else s.bm = 128, s.bn = 128, s.shared = 2;
+    s.tiles = (n_rows + s.bm - 1) / s.bm;
+    return s;
+}
+struct LpSpace {
+    TileRows h, w;
+    void *ph, *pw;               // copies, or null
+    float4* parts;
+    float *at_target, *norms;
+    uint2* groups;
+};
+static size_t carve_lp(LpSpace* r, TgCarve* c, const LpShape& s, const void* h, int64_t ld_h, const void* w, int64_t ld_w, int64_t n, int64_t n_rows, int d, int e,
+                       bool ready_h, bool ready_w, int top)
+{
+    const uint32_t pitch = tile_pitch(d, e);
+    r->ph = ready_h ? nullptr : c->take<char>((size_t)n * pitch);
+    r->pw = ready_w ? nullptr : c->take<char>((size_t)n_rows * pitch);
+    r->h = ready_h ? TileRows{(const char*)h, n, (uint32_t)(ld_h * e), pitch} : TileRows{(const char*)r->ph, n, pitch, pitch};
+    r->w = ready_w ? TileRows{(const char*)w, n_rows, (uint32_t)(ld_w * e), pitch} : TileRows{(const char*)r->pw, n_rows, pitch, pitch};
+    r->parts = c->take<float4>((size_t)s.tiles * s.tokens);
+    r->at_target = c->take<float>(s.tokens);
+    r->norms = c->take<float>(top ? s.tiles : 0);
+    r->groups = c->take<uint2>(top ? (size_t)s.tiles * (s.bm / LP_GROUP) * s.tokens : 0);
+    return c->used;
+}
+size_t tg_log_probs_space(int64_t n, int64_t n_rows, int d, int dtype, int top, int aligned)
+{
+    if (n == 0) return 0;
+    const int e = (int)tg_type_bytes(dtype);
+    TgCarve c{nullptr, 0};
+    LpSpace r;
+    const bool whole = (d * e & 15) == 0;
+    return carve_lp(&r, &c, lp_shape(n, n_rows, e), nullptr, d, nullptr, d, n, n_rows, d, e, whole && (aligned == 1 || aligned == 3),
+                    whole && (aligned == 1 || aligned == 2), top);
+}
+
+struct LpCall {
+    const void* targets;         // of the tokens at hand
+    int targets64;
+    float scale;
+    hipStream_t s;
+};
+template <class E, int BM, int BN, int WM, int WN, int NB, bool TOP>
+static void launch_parts(const LpShape& shape, const LpSpace& r, const TileRows& Y, const LpCall& call)
+{
+    // as many tiles along the table as a launch's work-items allow (all of them up to 2^29 rows), then as many tokens
+    constexpr int64_t TILES = TILE_LAUNCH_ITEMS / (64 * WM * WN);
+    const TileRows& X = r.w;
+    for (int64_t t0 = 0; t0 < shape.tiles; t0 += TILES) {
+        const int64_t tiles = shape.tiles - t0 < TILES ? shape.tiles - t0 : TILES, v0 = t0 * BM, most = TILES / tiles * BN;
+        const TileRows table{X.p + v0 * X.pitch, X.rows - v0 < tiles * BM ? X.rows - v0 : tiles * BM, X.pitch, X.width};
+        for (int64_t y0 = 0; y0 < Y.rows; y0 += most) {
+            const int64_t rows = Y.rows - y0 < most ? Y.rows - y0 : most;
+            const uint32_t ny = (uint32_t)((rows + BN - 1) / BN);
+            const TileRows part{Y.p + y0 * Y.pitch, rows, Y.pitch, Y.width};
+            hipLaunchKernelGGL((lp_part_kernel<E, BM, BN, WM, WN, NB, TOP>), dim3((unsigned)(tiles * ny)), dim3(64 * WM * WN), 0, call.s, table, part, (int)X.width,
+                               call.targets ? (const char*)call.targets + y0 * (call.targets64 ? 8 : 4) : nullptr, call.targets64, call.scale, v0, X.rows,
+                               (uint32_t)tiles, ny, 8u, r.parts + y0 * shape.tiles + t0, shape.tiles,
+                               TOP ? r.groups + (y0 * shape.tiles + t0) * (BM / LP_GROUP) : nullptr, r.at_target + y0);
+        }
+    }
+}
+template <class E, bool TOP>
+static void launch_all_parts(const LpShape& shape, const LpSpace& r, const TileRows& Y, const LpCall& call)
+{
+    if (shape.bn == 32) {
+        if (shape.few) launch_parts<E, 128, 32, 4, 1, 4, TOP>(shape, r, Y, call);
+        else launch_parts<E, 128, 32, 4, 1, 2, TOP>(shape, r, Y, call);
+    } else if (shape.bm == 64) {
+        if (shape.few) launch_parts<E, 64, 64, 2, 2, 4, TOP>(shape, r, Y, call);
+        else if constexpr (sizeof(E) == 4) launch_parts<E, 64, 64, 2, 2, 2, TOP>(shape, r, Y, call);
+    } else if (shape.bn == 64) launch_parts<E, 128, 64, 4, 1, 2, TOP>(shape, r, Y, call);
+    else if constexpr (sizeof(E) == 2) {
+        if (shape.bm == 256) launch_parts<E, 256, 256, 2, 4, 2, TOP>(shape, r, Y, call);
+        else launch_parts<E, 128, 128, 2, 2, 2, TOP>(shape, r, Y, call);
+    }
+}
+template <class E, bool TOP>
+static void launch_join(const LpShape& shape, const LpSpace& r, int64_t n, int64_t n_rows, const LpTop& a, const LpCall& call, float* logp, float* entropy, float* lse)
+{
+    const auto go = [&](auto kernel, int waves) {
+        const int64_t wgs = waves == 1 ? (n + 3) / 4 : n;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs < 65536 ? wgs : 65536)), dim3(waves == 1 ? 256 : 64 * waves), 0, call.s, r.parts, shape.tiles, n, n_rows,
+                           call.targets, call.targets64, r.at_target, call.scale, a, logp, entropy, lse);
+    };
+    if (n <= 256) go(lp_join_kernel<E, 16, TOP>, 16);
+    else if (n <= 2048) go(lp_join_kernel<E, 4, TOP>, 4);
+    else go(lp_join_kernel<E, 1, TOP>, 1);
+}
+
+void tg_launch_log_probs(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const void* targets,
+                         int targets64, float scale, int top, float* logp, float* entropy, float* lse, int32_t* rows, float* row_logp, void* space,
+                         hipStream_t s)
+{
+    const int e = (int)tg_type_bytes(dtype);
+    const LpShape shape = lp_shape(n, n_rows, e);
+    TgCarve c{(char*)space, 0};
+    LpSpace r;
+    const bool rh = tile_ready(h, ld_h, d, e), rw = tile_ready(w, ld_w, d, e);
+    carve_lp(&r, &c, shape, h, ld_h, w, ld_w, n, n_rows, d, e, rh, rw, top);
+    if (!rh) tg_launch_pack(h, ld_h, n, d, e, r.ph, s);
+    if (!rw) tg_launch_pack(w, ld_w, n_rows, d, e, r.pw, s);
+    LpTop a{h, w, ld_h, ld_w, d, shape.bm, shape.shared, top, r.norms, r.groups, shape.tiles * (shape.bm / LP_GROUP), rows, row_logp};
+    TG_WITH_TYPE(dtype, E, {
+        if (top) {
+            int lanes = 1;
+            while (lanes < 64 && lanes * TgPiece<E>::E < d) lanes *= 2;
+            hipLaunchKernelGGL(lp_norms_kernel<E>, dim3((unsigned)(shape.tiles < 65536 ? shape.tiles : 65536)), dim3(256), 0, s, (const E*)w, ld_w, n_rows, d, shape.bm,
+                               lanes, r.norms, shape.tiles);
+        }
+        for (int64_t y0 = 0; y0 < n; y0 += shape.tokens) {
+            const int64_t now = n - y0 < shape.tokens ? n - y0 : shape.tokens;
+            const LpCall call{targets ? (const char*)targets + y0 * (targets64 ? 8 : 4) : nullptr, targets64, scale, s};
+            const TileRows Y{r.h.p + y0 * r.h.pitch, now, r.h.pitch, r.h.width};
+            a.h = (const E*)h + y0 * ld_h;
+            a.rows = top ? rows + y0 * top : nullptr;
+            a.row_logp = top ? row_logp + y0 * top : nullptr;
+            float* const out = logp ? logp + y0 : nullptr;
+            if (top) {
+                launch_all_parts<E, true>(shape, r, Y, call);
+                launch_join<E, true>(shape, r, now, n_rows, a, call, out, entropy + y0, lse + y0);
+            } else {
+                launch_all_parts<E, false>(shape, r, Y, call);
+                launch_join<E, false>(shape, r, now, n_rows, a, call, out, entropy + y0, lse + y0);
+            }
+        }
+    });
+}

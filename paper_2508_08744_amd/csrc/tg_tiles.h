@@ -203,8 +203,25 @@ struct TileSide {
 #endif
 };
 
-// BM x BN in WM x WN waves, NB stages in LDS
-template <class E, int BM, int BN, int WM, int WN, bool XT = false, bool YT = false, int NB = 2>
+// the sum of the squares of a lane's 16 bytes, added to c
+template <class E> __device__ inline float tile_squares(tg_i32x4 x, float c)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef tg_bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef tg_f16 f16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (__is_same(E, tg_bf16)) c = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x[i]), __builtin_bit_cast(bf16x2, x[i]), c, false);
+        else if constexpr (__is_same(E, tg_f16)) c = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, x[i]), __builtin_bit_cast(f16x2, x[i]), c, false);
+        else c = fmaf(__builtin_bit_cast(float, x[i]), __builtin_bit_cast(float, x[i]), c);
+    }
+#endif
+    return c;
+}
+
+// BM x BN in WM x WN waves, NB stages in LDS.  SQUARES: the sums of the squares of X's rows as well, from the registers that feed the products (a lane's share
+// in squares[i], of row 16 (i % HM) + lane % 16 of the wave's rows in half i / HM; lanes 16, 32 and 48 on have the others).
+template <class E, int BM, int BN, int WM, int WN, bool XT = false, bool YT = false, int NB = 2, bool SQUARES = false>
 struct Tile {
     static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;       // products of 16 x 16 of a wave
@@ -217,6 +234,7 @@ struct Tile {
     static_assert(FM % 2 == 0 && FN % 2 == 0 && (NB == 2 || NB == 4), "halves");
 
     acc_t acc[FM][FN];
+    float squares[SQUARES ? FM : 1];
 
 #ifdef __HIP_DEVICE_COMPILE__
     struct Run {
@@ -254,7 +272,7 @@ struct Tile {
     }
     // The products of halves hx and hy, out of registers; between them the reads of a unit of X (XU) or Y for the next phase, and the loads
     // of one, so that the matrix instructions wait for neither's turn to be issued.
-    template <bool XU, class Fill>
+    template <bool XU, bool SQ, class Fill>
     __device__ inline void phase(const Run& r, Halves& f, int hx, int hy, int read_buffer, int read_half, Fill fill)
     {
         constexpr int PRODUCTS = 2 * HM * HN, READS = XU ? 2 * HM : 2 * HN;
@@ -262,6 +280,9 @@ struct Tile {
         for (int m = 0; m < PRODUCTS; ++m) {
             const int s = m / (HM * HN), i = m / HN % HM, j = m % HN;
             acc[hx * HM + i][hy * HN + j] = TileMul<E>::mul(f.x[hx][s][i], f.y[hy][s][j], acc[hx * HM + i][hy * HN + j]);
+            if constexpr (SQ) {
+                if (j == 0) squares[hx * HM + i] = tile_squares<E>(f.x[hx][s][i], squares[hx * HM + i]);
+            }
 #pragma unroll
             for (int n = 0; n < READS; ++n)
                 if (n * PRODUCTS / READS == m) {
@@ -279,13 +300,13 @@ struct Tile {
     {
         constexpr int P = B & 1, NEXT = (B + 1) % NB, FAR = (NB - 2) * (2 * LX + 2 * LY);
         meet<FAR + 4 * LX + 2 * LY>();
-        phase<false>(r, f, 0, P, B, 1 - P, [&] { fill_y(r, B, P, r.k + NB * TILE_BYTES); });
+        phase<false, SQUARES>(r, f, 0, P, B, 1 - P, [&] { fill_y(r, B, P, r.k + NB * TILE_BYTES); });
         meet<FAR + 3 * LX + 3 * LY>();
-        phase<true>(r, f, 0, 1 - P, B, 1, [&] { fill_y(r, B, 1 - P, r.k + NB * TILE_BYTES); });
+        phase<true, false>(r, f, 0, 1 - P, B, 1, [&] { fill_y(r, B, 1 - P, r.k + NB * TILE_BYTES); });
         meet<FAR + 2 * LX + 4 * LY>();
-        phase<true>(r, f, 1, 1 - P, NEXT, 0, [&] { fill_x(r, B, 1, r.k + NB * TILE_BYTES); });
+        phase<true, SQUARES>(r, f, 1, 1 - P, NEXT, 0, [&] { fill_x(r, B, 1, r.k + NB * TILE_BYTES); });
         meet<FAR + 3 * LX + 3 * LY>();
-        phase<false>(r, f, 1, P, NEXT, 1 - P, [&] { fill_x(r, NEXT, 0, r.k + (NB + 1) * TILE_BYTES); });
+        phase<false, false>(r, f, 1, P, NEXT, 1 - P, [&] { fill_x(r, NEXT, 0, r.k + (NB + 1) * TILE_BYTES); });
         r.k += TILE_BYTES;
     }
     Run r;
@@ -325,6 +346,10 @@ struct Tile {
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = acc_t{0, 0, 0, 0};
+        if constexpr (SQUARES) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i) squares[i] = 0.0f;
+        }
         constexpr int FAR = (NB - 2) * (2 * LX + 2 * LY);
         Halves f;
         // the reads of the two phases in front of the first

@@ -12,35 +12,12 @@
 // the entry that outweighs the others together, is given back to both gradients.  Of the other entries' roundings as much remains in a sum as the sum keeps of the
 // entries themselves: a relative error like that of rounding the result, which comes on top.
 #include "tg_embed.h"
+#include "tg_softmax.h"
 #include "tg_tiles.h"
 
-#define XENT_LOG2E 1.4426950408889634f
+#include <type_traits>
 
-__device__ inline float xent_exp(float x) { return __builtin_amdgcn_exp2f(x * XENT_LOG2E); }
-
-// Up to here exp(z - m) is 2 to the power of one multiply-add, z log2(e) - m log2(e), whose rounding is that of its terms: 2^-7 at this size, and beyond it
-// more and more, up to results that overflow.  Logits (or a scale) beyond it take the difference first: in the place of the products it makes the
-// exponents, to be taken with a factor of 1 and nothing subtracted, so that what follows is the same for both.
-#define XENT_NEAR 65536.0f
-__device__ inline bool xent_near(float m, float base) { return fabsf(m) < XENT_NEAR && fabsf(base) <= 3.4028234e38f; }
-// LARGEST: m is the largest logit, and one that is infinite is taken in by its equals alone.  Else it is lse, and the difference what it is.
-template <bool LARGEST>
-__device__ inline float xent_far(float product, float scale, float m)
-{
-    // (the logit is rounded before the difference, as m was: one multiply-add of both would leave m's rounding, which is large here)
-#pragma clang fp contract(off)
-    asm volatile("" : "+v"(product));        // (nothing of this is made out where it is not needed)
-    const float z = product * scale;
-    return LARGEST && z == m ? (m == -__builtin_inff() ? m : 0.0f) : (z - m) * XENT_LOG2E;
-}
-
-// (maximum, sum) pairs: one that stands for nothing is (-infinity, 0)
-__device__ inline void xent_join(float& m, float& l, float m2, float l2)
-{
-    const float top = fmaxf(m, m2);
-    l = (m == top ? l : l * xent_exp(m - top)) + (m2 == top ? l2 : l2 * xent_exp(m2 - top));
-    m = top;
-}
+#define XENT_BELOW (-1000.0f)
 
 // x: rows of the table from v0 on, y: tokens.  parts: for every tile along x (BM rows of the table), (maximum, sum) of every token.
 template <class E, int BM, int BN, int WM, int WN, int NB>
@@ -169,12 +146,18 @@ __global__ __launch_bounds__(1024) void xent_join_kernel(const float2* __restric
 
 // ---- gradient
 
-// h without the rows of tokens that have no target (nothing of theirs, not even a NaN, may reach dw), packed for the tiles.  The last
+// With the entropy's gradient dH, P = scale (dloss ([v = target]'s part as without) - dH p (z - lse + H)): a token whose dH is not 0 has a part in the gradients
+// without a target too.
+__device__ inline bool xent_has_part(int64_t target, const float* __restrict__ dentropy, int64_t t) { return target >= 0 || (dentropy && dentropy[t] != 0.0f); }
+
+// h without the rows of tokens that have no part (nothing of theirs, not even a NaN, may reach dw), packed for the tiles.  The last
 // workgroup finds, for fp16, the power of two that P is kept under: P is at most |scale| max |dloss|, so that times c[0] it stays below 2^14, and
-// values down to 2^-28 of the largest keep all their bits (bf16 and fp32 have the range as they are: c[0] = 1); c[1] = 1 / c[0].
+// values down to 2^-28 of the largest keep all their bits (bf16 and fp32 have the range as they are: c[0] = 1); c[1] = 1 / c[0].  The entropy's part is at most
+// |scale dH| (H + 1 / e).
 template <class E>
 __global__ __launch_bounds__(256) void xent_prepare_kernel(const E* __restrict__ h, int64_t ld, int64_t n, int64_t n_rows, int d, int per,
                                                            const void* __restrict__ targets, int targets64, const float* __restrict__ dloss,
+                                                           const float* __restrict__ entropy, const float* __restrict__ dentropy,
                                                            float scale, E* __restrict__ out, float* __restrict__ c)
 {
     constexpr bool NARROW = __is_same(E, tg_f16);
@@ -184,15 +167,18 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(const E* __restrict__
             typedef TgPiece<E> P;
             const int64_t r = i / per;
             const int at = (int)(i - r * per) * P::E;
-            *reinterpret_cast<typename P::vec*>(out + r * per * P::E + at) = P::raw(h + r * ld + at, tg_row_of(targets, targets64, r, n_rows) >= 0 ? d - at : 0);
+            *reinterpret_cast<typename P::vec*>(out + r * per * P::E + at) = P::raw(h + r * ld + at, xent_has_part(tg_row_of(targets, targets64, r, n_rows), dentropy, r) ? d - at : 0);
         }
         return;
     }
     float top = 0.0f;
     if (NARROW) {
         __shared__ float s[4];
-        for (int64_t t = threadIdx.x; t < n; t += 256)
-            if (tg_row_of(targets, targets64, t, n_rows) >= 0) top = fmaxf(top, fabsf(dloss[t] * scale));
+        for (int64_t t = threadIdx.x; t < n; t += 256) {
+            float most = tg_row_of(targets, targets64, t, n_rows) >= 0 ? fabsf(dloss[t] * scale) : 0.0f;
+            if (dentropy && dentropy[t] != 0.0f) most += fabsf(dentropy[t] * scale) * (fabsf(entropy[t]) + 0.375f);
+            top = fmaxf(top, most);
+        }
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
         if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = top;
@@ -212,10 +198,10 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(const E* __restrict__
 }
 
 // P of a piece: x: rows v0.. of the table, y: tokens; p: n rows, `pitch` elements apart, zeros behind the piece's rows up to `width`.  lost: for types
-// of 16 bits, what rounding took from P at the token's target, the entry that outweighs all others together.
-template <class E, int BM, int BN, int WM, int WN, int NB>
-__global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
-                                                              const float* __restrict__ lse, const float* __restrict__ dloss,
+// of 16 bits, what rounding took from P at the token's target, the entry that outweighs all others together.  ENTROPY: with the entropy's gradient,
+// p (g + h t) for t = (z - lse) log2(e), g = scale (dloss - dH H) and h = -scale dH log(2), and at the target g less (scale dloss) beside it.
+template <class E, int BM, int BN, int WM, int WN, int NB, bool ENTROPY>
+__global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRows Y, int bytes, XentTokens tokens,
                                                               const float* __restrict__ c, float scale, int64_t v0, int64_t n_rows, uint32_t nx,
                                                               uint32_t ny, uint32_t group, E* __restrict__ p, int64_t pitch, int width, float* __restrict__ lost)
 {
@@ -223,8 +209,10 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
     __shared__ __align__(1024) char lds[T::LDS];
     // what a token's logits become P with: its target among the tile's rows, its factor and its lse.  A token without a target has no part in
     // anything, whatever its logits are.
-    struct Token { int hit, there; float g, b; };                // there: 0 without a target, 1, or 2 with an lse that is not near, which b then is as it is
+    struct Token { int hit, there; float g, b; };                // there: 0 without a part, 1, or 2 with an lse that is not near, which b then is as it is
+    struct More { float h, less; };
     __shared__ Token s_token[BN];
+    __shared__ More s_more[ENTROPY ? BN : 1];
     const float up = c[0];
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
@@ -232,15 +220,23 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
     T t;
     t.start(X, Y, x0, y0, 0, bytes, lds);
     if (threadIdx.x < BN) {
-        const int64_t y = y0 + threadIdx.x, target = y < Y.rows ? tg_row_of(targets, targets64, y, n_rows) : -1, hit = target - v0 - x0;
-        Token k{target >= 0 && hit >= 0 && hit < BM ? (int)hit : -1, target >= 0, 0.0f, 0.0f};
-        if (target >= 0) {
-            k.g = dloss[y] * scale * up;
-            const bool near = xent_near(lse[y], scale * XENT_LOG2E);
+        const int64_t y = y0 + threadIdx.x, target = y < Y.rows ? tg_row_of(tokens.targets, tokens.targets64, y, n_rows) : -1, hit = target - v0 - x0;
+        Token k{target >= 0 && hit >= 0 && hit < BM ? (int)hit : -1, 0, 0.0f, 0.0f};
+        More more{0.0f, 0.0f};
+        if (y < Y.rows && xent_has_part(target, ENTROPY ? tokens.dentropy : nullptr, y)) {
+            if (target >= 0) k.g = more.less = tokens.dloss[y] * tokens.gain * scale * up;
+            if (ENTROPY && tokens.dentropy[y] != 0.0f) {
+                const float dh = tokens.dentropy[y] * scale * up;
+                k.g = fmaf(-dh, tokens.entropy[y], k.g);
+                more.h = dh * -0.6931471805599453f;
+            }
+            const float lse = tokens.lse[y];
+            const bool near = xent_near(lse, scale * XENT_LOG2E);
             k.there = near ? 1 : 2;
-            k.b = near ? lse[y] * XENT_LOG2E : lse[y];
+            k.b = near ? lse * XENT_LOG2E : lse;
         }
         s_token[threadIdx.x] = k;
+        if (ENTROPY) s_more[threadIdx.x] = more;
     }
     t.loop();
     const int have = x0 + BM <= X.rows ? BM : (int)(X.rows - x0), room = x0 + BM <= width ? BM : (int)(width - x0);
@@ -263,6 +259,13 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
         for (int i = 0; i < T::FM; ++i) asm volatile("" : "+v"(t.acc[i][j]));
         const int r = t.y_of(j);
         const Token k = s_token[r];
+        More more{0.0f, 0.0f};
+        if (ENTROPY) more = s_more[r];
+        // P of an exponent but for the target's part (below XENT_BELOW the power is 0, and the entropy's part with it)
+        const auto of = [&](float u, float less) {
+            if (!ENTROPY) return (__builtin_amdgcn_exp2f(u) - less) * k.g;
+            return fmaf(__builtin_amdgcn_exp2f(u), fmaf(more.h, fmaxf(u, XENT_BELOW), k.g), -(less * more.less));
+        };
         const bool near = k.there < 2;
         const float f = near ? base : 1.0f, b = near ? k.b : 0.0f;
         if (__builtin_expect(!__all(near), 0)) {           // (out of the way: code that is jumped over is fetched late)
@@ -277,12 +280,12 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
             const int x = t.x_of(i);
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], f, -b)) * k.g;
+            for (int e = 0; e < 4; ++e) v[e] = of(fmaf(t.acc[i][j][e], f, -b), 0.0f);
             if ((unsigned)(k.hit - x) < 4u) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (x + e == k.hit) {
-                        v[e] = (__builtin_amdgcn_exp2f(fmaf(t.acc[i][j][e], f, -b)) - 1.0f) * k.g;
+                        v[e] = of(fmaf(t.acc[i][j][e], f, -b), 1.0f);
                         if (sizeof(E) == 2) lost[y0 + r] = v[e] - (float)(E)v[e];
                     }
             }
@@ -319,6 +322,7 @@ struct XentProducts {
     int splits, first, direct;
     const void* targets;
     int targets64;
+    const float* dentropy;          // or null
     const void* table;              // the caller's w
     int64_t ld_table;
     const float *c, *lost;
@@ -335,7 +339,7 @@ __device__ inline void xent_put_dh(const XentProducts& a, int64_t y, int x, floa
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if (sizeof(E) == 2 && x + e < a.d) v[e] = fmaf(l, (float)row[e], v[e]);
-        v[e] = target >= 0 ? v[e] * a.c[1] : 0.0f;
+        v[e] = xent_has_part(target, a.dentropy, y) ? v[e] * a.c[1] : 0.0f;
     }
     tile_put((E*)a.dh + y * a.d + x, v, a.d - x);
 }
@@ -687,17 +691,19 @@ static int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 // bytes between the rows of P.  Its tiles are stored sixteen rows at a time: at a distance of a power of two those would meet in one channel of
 // the caches.
 static uint32_t xent_pitch(int64_t rows, int e) { return (uint32_t)round_up(rows * e, 16) + XENT_PAD; }
-static void xent_splits(XentGrad* g, int64_t n, int64_t n_rows, int d, int e)
+static void xent_splits(XentGrad* g, int64_t n, int64_t n_rows, int d, int e, bool table)
 {
     // both products take tiles of 256 x 256, of which a CU holds one, where those are enough; else of 128 x 128, of which it holds two, in fp32 of
     // 64 x 64, of which it holds four; and of 64 x 64, with four stages in flight, where each of 128 x 128 would have a CU of its own
     const auto tiles = [](int64_t x, int64_t y, int64_t side) { return ((x + side - 1) / side) * ((y + side - 1) / side); };
-    g->few = tiles(n, d, 128) + tiles(g->piece, d, 128) <= 128;
-    g->side = e == 2 && n > 128 && d > 128 && tiles(g->piece, d, 256) >= 200 ? 256 : g->few || e == 4 ? 64 : 128;
+    // (without dw, dh's parts alone are to fill the card)
+    const int64_t beside = table ? g->piece : 0;
+    g->few = tiles(n, d, 128) + tiles(beside, d, 128) <= 128;
+    g->side = e == 2 && n > 128 && d > 128 && tiles(table ? g->piece : n, d, 256) >= 200 ? 256 : g->few || e == 4 ? 64 : 128;
     // dh in as many parts as fill the card, each with sixteen stages of the contraction or more; where dw, beside it, has fewer, with as many as
     // that, but four, up to 32 parts whose bytes are half of the table's (there and back, bf16: 7 tokens, 6938 rows of 688: 39.8 us with sixteen, 37.2;
     // 900 tokens, 5000 rows of 700: 77.7 and 75.2)
-    const int64_t fill = g->side == 256 ? 256 : g->few || g->side == 128 ? 512 : 1024, dw_stages = (n * e + TILE_BYTES - 1) / TILE_BYTES;
+    const int64_t fill = g->side == 256 ? 256 : g->few || g->side == 128 ? 512 : 1024, dw_stages = table ? (n * e + TILE_BYTES - 1) / TILE_BYTES : 0;
     const int64_t least = g->few || dw_stages < 4 ? 4 : dw_stages < 16 ? dw_stages : 16, light = g->piece * e / (8 * n);
     const int64_t dh = tiles(n, d, g->side), stages = (g->piece * e + TILE_BYTES - 1) / TILE_BYTES;
     int64_t s = (fill + dh - 1) / dh;
@@ -722,7 +728,7 @@ static size_t carve_xent_grad(XentRows* r, TgCarve* c, const void* h, int64_t ld
     *p = c->take<char>((size_t)n * xent_pitch(g.piece, e));
     return c->used;
 }
-static XentGrad xent_grad_shape(int64_t n, int64_t n_rows, int d, int e, int64_t p_bytes)
+static XentGrad xent_grad_shape(int64_t n, int64_t n_rows, int d, int e, int64_t p_bytes, bool table)
 {
     XentGrad g;
     g.piece = p_bytes / ((n > 0 ? n : 1) * e) / 256 * 256;
@@ -734,37 +740,36 @@ static XentGrad xent_grad_shape(int64_t n, int64_t n_rows, int d, int e, int64_t
         const int64_t count = (n_rows + g.piece - 1) / g.piece;
         g.piece = round_up((n_rows + count - 1) / count, 256);
     }
-    xent_splits(&g, n, n_rows, d, e);
+    xent_splits(&g, n, n_rows, d, e, table);
     return g;
 }
-static size_t xent_grad_bytes(int64_t n, int64_t n_rows, int d, int e, bool ready, int64_t p_bytes)
+static size_t xent_grad_bytes(int64_t n, int64_t n_rows, int d, int e, bool ready, int64_t p_bytes, bool table)
 {
     TgCarve c{nullptr, 0};
     XentRows r;
     float *k, *sums, *lost;
     char* p;
-    return carve_xent_grad(&r, &c, nullptr, d, nullptr, d, n, n_rows, d, e, ready && (d * e & 15) == 0, xent_grad_shape(n, n_rows, d, e, p_bytes), &k, &p, &sums, &lost);
+    return carve_xent_grad(&r, &c, nullptr, d, nullptr, d, n, n_rows, d, e, ready && (d * e & 15) == 0, xent_grad_shape(n, n_rows, d, e, p_bytes, table), &k, &p, &sums, &lost);
 }
-size_t tg_xent_grad_space(int64_t n, int64_t n_rows, int d, int dtype, int aligned, bool least)
+size_t tg_xent_grad_space(int64_t n, int64_t n_rows, int d, int dtype, int aligned, bool least, bool table)
 {
     if (n == 0) return 0;
     const bool ready = aligned == 1 || aligned == 2;           // (h is always copied)
-    const size_t asked = xent_grad_bytes(n, n_rows, d, (int)tg_type_bytes(dtype), ready, XENT_PIECE_BYTES);
+    const size_t asked = xent_grad_bytes(n, n_rows, d, (int)tg_type_bytes(dtype), ready, XENT_PIECE_BYTES, table);
     if (!least) return asked;
     // (one piece can do with less than many: dh then needs no sums)
-    const size_t pieces = xent_grad_bytes(n, n_rows, d, (int)tg_type_bytes(dtype), ready, 0);
+    const size_t pieces = xent_grad_bytes(n, n_rows, d, (int)tg_type_bytes(dtype), ready, 0, table);
     return pieces < asked ? pieces : asked;
 }
 
 template <class E>
 static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h, int64_t ld_h, const void* w, int64_t ld_w, int64_t n, int64_t n_rows,
-                             int d, const void* targets, int targets64, const float* lse, const float* dloss, float scale, float* consts, char* p,
-                             float* sums, float* lost, E* dh, E* dw, hipStream_t s)
+                             int d, const XentTokens& t, float scale, float* consts, char* p, float* sums, float* lost, E* dh, E* dw, hipStream_t s)
 {
     const int e = (int)sizeof(E), per = (int)(r.h.pitch / 16);
     const int64_t wgs = (n * per + 255) / 256;
     hipLaunchKernelGGL(xent_prepare_kernel<E>, dim3((unsigned)(wgs < 16384 ? wgs : 16384) + 1), dim3(256), 0, s, (const E*)h, ld_h, n, n_rows, d, per,
-                       targets, targets64, dloss, scale, (E*)r.ph, consts);
+                       t.targets, t.targets64, t.dloss, t.entropy, t.dentropy, scale, (E*)r.ph, consts);
     XentProducts a;
     a.h = r.h;
     a.n_rows = n_rows;
@@ -772,8 +777,9 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
     a.h_bytes = (int)(n * e);
     a.splits = g.splits;
     a.direct = g.direct ? 1 : 0;
-    a.targets = targets;
-    a.targets64 = targets64;
+    a.targets = t.targets;
+    a.targets64 = t.targets64;
+    a.dentropy = t.dentropy;
     a.table = w;
     a.ld_table = ld_w;
     a.c = consts;
@@ -792,28 +798,32 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
         a.p = TileRows{p, n, pitch, width};
         const auto logits = [&](auto kernel, int bm, int bn, int threads) {
             const uint32_t nx = over(rows, bm), ny = over(n, bn);
-            hipLaunchKernelGGL(kernel, dim3(nx * ny), dim3(threads), 0, s, a.w, r.h, (int)a.w.width, targets, targets64, lse, dloss, (const float*)consts,
-                               scale, v0, n_rows, nx, ny, 8u, (E*)p, (int64_t)(pitch / e), (int)(width / e), lost);
+            hipLaunchKernelGGL(kernel, dim3(nx * ny), dim3(threads), 0, s, a.w, r.h, (int)a.w.width, t, (const float*)consts, scale, v0, n_rows, nx, ny, 8u, (E*)p, (int64_t)(pitch / e), (int)(width / e), lost);
         };
-        if (xent_small(rows, n)) logits(xent_p_kernel<E, 64, 64, 2, 2, 4>, 64, 64, 256);
-        else if (n <= 64) logits(xent_p_kernel<E, 128, 64, 4, 1, 2>, 128, 64, 256);
-        else {
-            bool wide = false;
-            if constexpr (sizeof(E) == 2) {
-                wide = (int64_t)over(rows, 256) * over(n, 256) >= 200;
-                if (wide) logits(xent_p_kernel<E, 256, 256, 2, 4, 2>, 256, 256, 512);
+        const auto all_logits = [&](auto with) {
+            constexpr bool ENTROPY = decltype(with)::value;
+            if (xent_small(rows, n)) logits(xent_p_kernel<E, 64, 64, 2, 2, 4, ENTROPY>, 64, 64, 256);
+            else if (n <= 64) logits(xent_p_kernel<E, 128, 64, 4, 1, 2, ENTROPY>, 128, 64, 256);
+            else {
+                bool wide = false;
+                if constexpr (sizeof(E) == 2) {
+                    wide = (int64_t)over(rows, 256) * over(n, 256) >= 200;
+                    if (wide) logits(xent_p_kernel<E, 256, 256, 2, 4, 2, ENTROPY>, 256, 256, 512);
+                }
+                if constexpr (sizeof(E) == 4) logits(xent_p_kernel<E, 64, 64, 2, 2, 2, ENTROPY>, 64, 64, 256);
+                else if (!wide) logits(xent_p_kernel<E, 128, 128, 2, 2, 2, ENTROPY>, 128, 128, 256);
             }
-            if constexpr (sizeof(E) == 4) logits(xent_p_kernel<E, 64, 64, 2, 2, 2>, 64, 64, 256);
-            else if (!wide) logits(xent_p_kernel<E, 128, 128, 2, 2, 2>, 128, 128, 256);
-        }
+        };
+        if (t.dentropy) all_logits(std::true_type{});
+        else all_logits(std::false_type{});
         const int stages = (int)((width + TILE_BYTES - 1) / TILE_BYTES);
         a.v0 = v0;
         a.rows = rows;
         a.p_bytes = (int)width;
         a.each = (stages + g.splits - 1) / g.splits * TILE_BYTES;
         a.first = v0 == 0 ? 1 : 0;
-        a.dw = dw + v0 * d;
-        a.dw_y = over(rows, side);
+        a.dw = dw ? dw + v0 * d : nullptr;
+        a.dw_y = dw ? over(rows, side) : 0;
         const dim3 grid(a.dh_x * a.dh_y * g.splits + a.dw_x * a.dw_y);
         const auto products = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a); };
         if constexpr (sizeof(E) == 2) {
@@ -828,25 +838,24 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
     hipLaunchKernelGGL(xent_dh_kernel<E>, dim3((unsigned)(out_wgs < 16384 ? out_wgs : 16384)), dim3(256), 0, s, a, (d + 3) / 4);
 }
 
-void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const void* targets,
-                         int targets64, const float* lse, const float* dloss, float scale, void* dh, void* dw, void* space, size_t bytes, hipStream_t s)
+void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const XentTokens& t,
+                         float scale, void* dh, void* dw, void* space, size_t bytes, hipStream_t s)
 {
     const int e = (int)tg_type_bytes(dtype);
     if (n == 0) {
-        tg_launch_zero(dw, (size_t)n_rows * d * e, s);
+        if (dw) tg_launch_zero(dw, (size_t)n_rows * d * e, s);
         return;
     }
     const bool ready = tile_ready(w, ld_w, d, e);
     // the largest piece that the workspace holds
     int64_t p_bytes = XENT_PIECE_BYTES * 64;
-    while (p_bytes > 0 && xent_grad_bytes(n, n_rows, d, e, ready, p_bytes) > bytes) p_bytes = p_bytes > (1 << 20) ? p_bytes / 2 : 0;
-    const XentGrad g = xent_grad_shape(n, n_rows, d, e, p_bytes);
+    while (p_bytes > 0 && xent_grad_bytes(n, n_rows, d, e, ready, p_bytes, dw != nullptr) > bytes) p_bytes = p_bytes > (1 << 20) ? p_bytes / 2 : 0;
+    const XentGrad g = xent_grad_shape(n, n_rows, d, e, p_bytes, dw != nullptr);
     TgCarve c{(char*)space, 0};
     XentRows r;
     float *consts, *sums, *lost;
     char* p;
     carve_xent_grad(&r, &c, h, ld_h, w, ld_w, n, n_rows, d, e, ready, g, &consts, &p, &sums, &lost);
     if (!ready) tg_launch_pack(w, ld_w, n_rows, d, e, r.pw, s);
-    TG_WITH_TYPE(dtype, E, launch_xent_grad<E>(r, g, h, ld_h, w, ld_w, n, n_rows, d, targets, targets64, lse, dloss, scale, consts, p, sums, lost,
-                                            (E*)dh, (E*)dw, s));
+    TG_WITH_TYPE(dtype, E, launch_xent_grad<E>(r, g, h, ld_h, w, ld_w, n, n_rows, d, t, scale, consts, p, sums, lost, (E*)dh, (E*)dw, s));
 }
