@@ -14,6 +14,7 @@
 
 #define LP_GROUP 32             // logits of a token that leave their largest
 #define LP_MAX_TOP 32           // best rows; half the lanes of a wave, see lp_kth
+#define LP_NORM_ROWS 64         // of the table, where the tiles leave no norms
 #define LP_BELOW (-1000.0f)     // exponents below have a power of 0: so is their part in s, at -infinity too
 
 typedef unsigned int lp_u32;
@@ -43,14 +44,17 @@ template <class E, int BM, int BN, int WM, int WN, int NB, bool TOP>
 __global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
                                                                float scale, int64_t v0, int64_t n_rows, uint32_t nx, uint32_t ny, uint32_t group,
                                                                float4* __restrict__ parts, int64_t parts_pitch, uint2* __restrict__ groups,
-                                                               float* __restrict__ at_target)
+                                                               float* __restrict__ norms, float* __restrict__ at_target)
 {
-    typedef Tile<E, BM, BN, WM, WN, false, false, NB> T;
+    // (the norms' squares ride along where registers are left for their sums: tiles of up to 128 rows)
+    constexpr bool SQUARES = TOP && BM <= 128;
+    typedef Tile<E, BM, BN, WM, WN, false, false, NB, SQUARES> T;
     constexpr int Q = 8 / T::FM, GROUPS = BM / LP_GROUP;       // quarters of a wave (16 lanes each) that share a group; groups of a tile
     static_assert(!TOP || (Q >= 1 && Q * T::FM == 8), "groups of 32 rows");
     __shared__ __align__(1024) char lds[T::LDS];
     // the tokens' targets among the tile's rows: asked for before the products, so that nothing waits for them behind
     __shared__ int s_target[BN];
+    __shared__ float s_norm[WM * WN];
     uint32_t tx, ty;
     tile_place(tile_of_block(blockIdx.x, nx * ny), nx, ny, group, &tx, &ty);
     const int64_t x0 = (int64_t)tx * BM, y0 = (int64_t)ty * BN;
@@ -61,6 +65,19 @@ __global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileR
         s_target[threadIdx.x] = target >= 0 && target < BM ? (int)target : -1;
     }
     t.loop();
+    if constexpr (SQUARES) {
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+            float q = t.squares[i];
+            q += __shfl_xor(q, 16);
+            q += __shfl_xor(q, 32);
+            top = fmaxf(top, q);
+        }
+#pragma unroll
+        for (int m = 1; m < 16; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+        if (tg_lane() == 0) s_norm[threadIdx.x >> 6] = top;
+    }
     // (the tile's memory is free: a sum for every token and wave along x)
     LpSum* const s_sum = reinterpret_cast<LpSum*>(lds) + (threadIdx.x >> 6) / WN * BN;
     static_assert(WM * BN * sizeof(LpSum) <= T::LDS, "the sums' place");
@@ -156,29 +173,42 @@ __global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileR
         for (int w = 1; w < WM; ++w) lp_join(a, sum[w * BN]);
         parts[(y0 + threadIdx.x) * parts_pitch + tx] = make_float4(a.m, a.l, a.s, 0.0f);
     }
+    // (every column of tiles has the same: the first says it)
+    if (SQUARES && norms && ty == 0 && threadIdx.x == 0) {
+        float top = s_norm[0];
+#pragma unroll
+        for (int w = 1; w < WM * WN; ++w) top = fmaxf(top, s_norm[w]);
+        norms[tx] = top;
+    }
 }
 
-// The largest sum of the squares of `each` rows at a time.  LANES lanes a row; a row is read once.
+// The largest sum of the squares of LP_NORM_ROWS rows at a time.  `lanes` lanes a row; four rows are asked for at once.
 template <class E>
-__global__ __launch_bounds__(256) void lp_norms_kernel(const E* __restrict__ w, int64_t ld, int64_t n_rows, int d, int each, int lanes, float* __restrict__ out, int64_t count)
+__global__ __launch_bounds__(256) void lp_norms_kernel(const E* __restrict__ w, int64_t ld, int64_t n_rows, int d, int lanes, float* __restrict__ out, int64_t count)
 {
     __shared__ float s_top[4];
     typedef TgPiece<E> P;
     const int of = threadIdx.x & (lanes - 1), rows = 256 / lanes, first = threadIdx.x / lanes;
     for (int64_t b = blockIdx.x; b < count; b += gridDim.x) {
         float top = 0.0f;
-        for (int r = first; r < each; r += rows) {
-            const int64_t v = b * each + r;
-            float sum = 0.0f;
-            if (v < n_rows)
-                for (int c = of * P::E; c < d; c += lanes * P::E) {
-                    P p;
-                    p.load(w + v * ld + c, d - c);
+        for (int r = first; r < LP_NORM_ROWS; r += 4 * rows) {
+            float sum[4] = {};
+            for (int c = of * P::E; c < d; c += lanes * P::E) {
+                typename P::vec v[4];
 #pragma unroll
-                    for (int e = 0; e < P::E; ++e) sum = fmaf(p.v[e], p.v[e], sum);
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t row = b * LP_NORM_ROWS + r + i * rows;
+                    v[i] = P::raw(w + (row < n_rows ? row : 0) * ld + c, r + i * rows < LP_NORM_ROWS && row < n_rows ? d - c : 0);
                 }
-            for (int m = 1; m < lanes; m <<= 1) sum += __shfl_xor(sum, m);
-            top = fmaxf(top, sum);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < P::E; ++e) sum[i] = fmaf((float)v[i][e], (float)v[i][e], sum[i]);
+            }
+            for (int m = 1; m < lanes; m <<= 1)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], m);
+            top = fmaxf(fmaxf(fmaxf(sum[0], sum[1]), fmaxf(sum[2], sum[3])), top);
         }
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
@@ -263,28 +293,26 @@ struct LpBest {
 struct LpTop {
     const void *h, *w;           // the caller's
     int64_t ld_h, ld_w;
-    int d, tile, shared;         // tile: rows of the table; shared: the quarters of a wave that share a group
+    int d, per_shift, shared_shift;     // the groups of a tile, and the quarters of a wave that share one: log2
     int top;
     const float* norms;
+    int n_norms;
     const uint2* groups;
-    int64_t n_groups;
+    int n_groups;                // below 2^26
     int32_t* rows;
     float* row_logp;
 };
 
-// Eight rows' logits in 64 bits, by one wave: every lane has the same places of all rows, so a row's sum does not depend on where it was found.
+// Up to eight rows' logits in 64 bits, by one wave: row i's in the lanes 8 i to 8 i + 7.  Every lane has the same places of all rows, so a row's sum does not depend
+// on where it was found.
 template <class E>
-__device__ inline void lp_score(const LpTop& a, const E* h, double scale, const int* pending, int count, LpBest& best)
+__device__ inline double lp_score(const LpTop& a, const E* h, double scale, const int (&rows)[8])
 {
     typedef TgPiece<E> P;
     const int lane = tg_lane();
-    int rows[8];
     const E* w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        rows[i] = __builtin_amdgcn_readfirstlane(pending[i < count ? i : 0]);
-        w[i] = (const E*)a.w + (int64_t)rows[i] * a.ld_w;
-    }
+    for (int i = 0; i < 8; ++i) w[i] = (const E*)a.w + (int64_t)__builtin_amdgcn_readfirstlane(rows[i]) * a.ld_w;
     double sum[8] = {};
     for (int c = lane * P::E; c < a.d; c += 64 * P::E) {
         typename P::vec x[8];
@@ -306,13 +334,54 @@ __device__ inline void lp_score(const LpTop& a, const E* h, double scale, const 
     double s = (lane & 8 ? s2[1] : s2[0]) + lp_xor64(lane & 8 ? s2[0] : s2[1], 8);
 #pragma unroll
     for (int m = 4; m >= 1; m >>= 1) s += lp_xor64(s, m);
-    s *= scale;
+    return s * scale;
+}
+
+// The groups of a token, as a wave goes through them: W waves in turn, LP_AHEAD times 64 groups asked for at once.
+#define LP_AHEAD 8
+template <int W, class Take>
+__device__ inline void lp_scan(const uint2* __restrict__ groups, int n_groups, int wave, Take take)
+{
+    for (int g0 = wave * 64 + tg_lane(); g0 - tg_lane() < n_groups; g0 += LP_AHEAD * 64 * W) {
+        uint2 v[LP_AHEAD];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < count) best.add(lp_lane64(s, i * 8), rows[i]);
+        for (int i = 0; i < LP_AHEAD; ++i) v[i] = g0 + i * 64 * W < n_groups ? groups[g0 + i * 64 * W] : make_uint2(0xFF800000u /* -infinity */, 0u);
+        take(g0, v);
+    }
+}
+// ... those of them that reach `low`: some lanes' at a time, take(whether the lane has one, its number, its largest, its packed second)
+template <int W, class Take>
+__device__ inline void lp_reach(const uint2* __restrict__ groups, int n_groups, int wave, double low, Take take)
+{
+    lp_scan<W>(groups, n_groups, wave, [&](int g0, const uint2 (&v)[LP_AHEAD]) {
+        unsigned hits = 0;
+#pragma unroll
+        for (int i = 0; i < LP_AHEAD; ++i)          // (what a NaN is compared with is not out of reach)
+            hits |= g0 + i * 64 * W < n_groups && !((double)__uint_as_float(v[i].x) < low) ? 1u << i : 0u;
+        while (__any(hits != 0)) {
+            const int at = hits ? __builtin_ctz(hits) : 0;
+            uint2 x = v[0];
+#pragma unroll
+            for (int i = 1; i < LP_AHEAD; ++i) x = at == i ? v[i] : x;
+            take(hits != 0, g0 + at * 64 * W, __uint_as_float(x.x), x.y);
+            hits &= hits - 1;
+        }
+    });
+}
+// row number `lane` of group g: of value e, quarter q and block i of the wave's rows, as lp_part_kernel has them (below LP_GROUP)
+__device__ inline int lp_group_row(const LpTop& a, int g, int lane)
+{
+    const int tile = g >> a.per_shift, in = g & ((1 << a.per_shift) - 1), sh = a.shared_shift, waves_shift = 2 - sh;
+    const int e = lane & 3, q = ((lane >> 2) & ((1 << sh) - 1)) + ((in & ((1 << waves_shift) - 1)) << sh), i = lane >> (2 + sh);
+    const int half = 1 << waves_shift;             // blocks of the wave in half of the tile's rows
+    return (tile << (a.per_shift + 5)) + ((i >> waves_shift) << (a.per_shift + 4)) + (in >> waves_shift) * (half * 16) + (i & (half - 1)) * 16 + q * 4 + e;
 }
 
 // The tiles' sums joined, and the best rows, by W waves a token.
+//
+// What is not below the threshold is listed and scored, eight rows at a time a wave, and a row's place is the number of those before it.  Where the list does not hold
+// them (rows that are equal, or nearly, by the hundreds) every wave goes through its groups again with its k best so far in order in its lanes, and passes over
+// what cannot be among them.
 template <class E, int W, bool TOP>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const float4* __restrict__ parts, int64_t count, int64_t n, int64_t n_rows,
                                                                        const void* __restrict__ targets, int targets64, const float* __restrict__ at_target,
@@ -320,17 +389,19 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
                                                                        float* __restrict__ lse)
 {
     constexpr int TOKENS = W == 1 ? 4 : 1;
-    constexpr int PENDING = 7 + 64 + LP_GROUP;
-    __shared__ LpSum s_sum[W];
+    constexpr int LIST = W == 1 ? 128 : 256;
+    __shared__ float s_m[W], s_l[W], s_s[W], s_w2[W];
     __shared__ double s_h2[W];
-    __shared__ float s_w2[W], s_top[W > 1 ? W : 1][W > 1 ? 64 : 1];
-    __shared__ int s_pending[TOP ? TOKENS * W : 1][TOP ? PENDING : 1];
-    __shared__ double s_best_z[TOP && W > 1 ? W : 1][LP_MAX_TOP];
-    __shared__ int s_best_row[TOP && W > 1 ? W : 1][LP_MAX_TOP];
+    __shared__ float s_top[W > 1 ? W : 1][W > 1 ? 64 : 1];
+    __shared__ int s_list[TOP ? TOKENS : 1][TOP ? LIST : 1];
+    __shared__ double s_z[TOP ? TOKENS : 1][TOP ? LIST : 1];
+    __shared__ int s_found;
     const int lane = tg_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int of = W == 1 ? lane : threadIdx.x;                  // of the token's lanes
-    const int mine = W == 1 ? 0 : wave;                          // of its waves
-    for (int64_t y = (int64_t)blockIdx.x * TOKENS + (W == 1 ? wave : 0); y < n; y += (int64_t)gridDim.x * TOKENS) {
+    const int mine = W == 1 ? 0 : wave, team = W == 1 ? wave : 0;
+    for (int64_t y = (int64_t)blockIdx.x * TOKENS + team; y < n; y += (int64_t)gridDim.x * TOKENS) {
+        const E* const h = (const E*)a.h + y * a.ld_h;
+        const uint2* const groups = a.groups + y * (int64_t)a.n_groups;
         LpSum sum{-__builtin_inff(), 0.0f, 0.0f};
         for (int64_t p0 = of; p0 < count; p0 += 4 * 64 * W) {
             float4 v[4];
@@ -340,13 +411,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
 #pragma unroll
             for (int i = 0; i < 4; ++i) lp_join(sum, LpSum{v[i].x, v[i].y, v[i].z});
         }
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) lp_join(sum, LpSum{__shfl_xor(sum.m, m), __shfl_xor(sum.l, m), __shfl_xor(sum.s, m)});
         // what the margin is made of, and the largest logits of the lanes' groups
         double h2 = 0.0;
         float w2 = 0.0f, high = -__builtin_inff();
-        const E* const h = (const E*)a.h + y * a.ld_h;
-        const uint2* const groups = a.groups + y * a.n_groups;
         if (TOP) {
             typedef TgPiece<E> P;
             for (int c = of * P::E; c < a.d; c += 64 * W * P::E) {
@@ -355,16 +422,16 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
 #pragma unroll
                 for (int e = 0; e < P::E; ++e) h2 = fma((double)p.v[e], (double)p.v[e], h2);
             }
-            for (int64_t p = of; p < count; p += 64 * W) w2 = fmaxf(w2, a.norms[p]);
-            for (int64_t g0 = of; g0 < a.n_groups; g0 += 8 * 64 * W) {
-                float v[8];
+            for (int p = of; p < a.n_norms; p += 64 * W) w2 = fmaxf(w2, a.norms[p]);
+            lp_scan<W>(groups, a.n_groups, mine, [&](int, const uint2 (&v)[LP_AHEAD]) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = g0 + i * 64 * W < a.n_groups ? __uint_as_float(groups[g0 + i * 64 * W].x) : -__builtin_inff();
+                for (int i = 0; i < LP_AHEAD; ++i) high = fmaxf(high, __uint_as_float(v[i].x));
+            });
+        }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) high = fmaxf(high, v[i]);
-            }
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
+        for (int m = 1; m < 64; m <<= 1) {
+            lp_join(sum, LpSum{__shfl_xor(sum.m, m), __shfl_xor(sum.l, m), __shfl_xor(sum.s, m)});
+            if (TOP) {
                 h2 += lp_xor64(h2, m);
                 w2 = fmaxf(w2, __shfl_xor(w2, m));
             }
@@ -372,26 +439,34 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
         if (W > 1) {
             __syncthreads();                                     // (the token before is done with these)
             if (lane == 0) {
-                s_sum[wave] = sum;
+                s_m[wave] = sum.m;
+                s_l[wave] = sum.l;
+                s_s[wave] = sum.s;
                 s_h2[wave] = h2;
                 s_w2[wave] = w2;
             }
+            if (threadIdx.x == 0) s_found = 0;
             if (TOP) s_top[wave][lane] = high;
             __syncthreads();
-            sum = s_sum[0];
+            // (every wave has all waves' W times over)
+            sum = LpSum{s_m[lane % W], s_l[lane % W], s_s[lane % W]};
+            h2 = s_h2[lane % W];
+            w2 = s_w2[lane % W];
 #pragma unroll
-            for (int i = 1; i < W; ++i) lp_join(sum, s_sum[i]);
-            if (TOP) {
-                h2 = 0.0;
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    h2 += s_h2[i];
-                    w2 = fmaxf(w2, s_w2[i]);
-                    high = fmaxf(high, s_top[i][lane]);
+            for (int m = 1; m < W; m <<= 1) {
+                lp_join(sum, LpSum{__shfl_xor(sum.m, m), __shfl_xor(sum.l, m), __shfl_xor(sum.s, m)});
+                if (TOP) {
+                    h2 += lp_xor64(h2, m);
+                    w2 = fmaxf(w2, __shfl_xor(w2, m));
                 }
             }
+            if (TOP) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) high = fmaxf(high, s_top[i][lane]);
+            }
         }
-        const float all = sum.m + logf(sum.l);
+        // (the first lane's: the others joined the same in other orders)
+        const float all = __uint_as_float((lp_u32)__builtin_amdgcn_readfirstlane((int)__float_as_uint(sum.m + logf(sum.l))));
         if (of == 0) {
             lse[y] = all;
             const float below = logf(sum.l) - 0.6931471805599453f * (sum.s / sum.l);
@@ -400,87 +475,122 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
             if (logp) logp[y] = tg_row_of(targets, targets64, y, n_rows) >= 0 ? at_target[y] - all : 0.0f;
         }
         if (!TOP) continue;
+        const auto put = [&](int place, double z, int row) {
+            const double p = z - (double)all;
+            a.rows[y * a.top + place] = row == LpBest::NONE ? -1 : row;
+            a.row_logp[y * a.top + place] = row == LpBest::NONE ? -__builtin_inff() : (float)(p > 0.0 ? 0.0 : p);
+        };
         if (all != all) {                                        // a NaN among the logits
-            if (mine == 0 && lane < a.top) {
-                a.rows[y * a.top + lane] = -1;
-                a.row_logp[y * a.top + lane] = all;
+            if (of < a.top) {
+                a.rows[y * a.top + of] = -1;
+                a.row_logp[y * a.top + of] = all;
             }
             continue;
         }
         const double margin = lp_margin<E>(scale, a.d, h2, w2);
         const double low = (double)lp_kth(high, a.top) - 2.0 * margin;
+        int* const list = s_list[TOP ? team : 0];
+        double* const score = s_z[TOP ? team : 0];
+        int found = 0;
+        // `some` rows more for the list: the place of the first, and of what is behind the last
+        const auto room = [&](int some) {
+            int at = found;
+            if (W > 1) {
+                if (lane == 0) at = atomicAdd(&s_found, some);
+                at = __builtin_amdgcn_readfirstlane(at);
+            }
+            found = at + some;
+            return at;
+        };
+        lp_reach<W>(groups, a.n_groups, mine, low, [&](bool hit, int g, float, lp_u32 second) {
+            u64 many = __ballot(hit && !((double)lp_second(second) < low));
+            const int row = (g >> a.per_shift << (a.per_shift + 5)) + lp_row(second);
+            const u64 one = __ballot(hit && (double)lp_second(second) < low && row < (int)n_rows);
+            if (one) {
+                const int at = room(__popcll(one)) + __popcll(one & tg_lanemask_lt());
+                if ((one >> lane & 1) && at < LIST) list[at] = row;
+            }
+            for (; many && found <= LIST; many &= many - 1) {
+                const int r = lp_group_row(a, __builtin_amdgcn_readlane(g, __builtin_ctzll(many)), lane);
+                const u64 some = __ballot(lane < LP_GROUP && r < (int)n_rows);
+                const int at = room(__popcll(some)) + __popcll(some & tg_lanemask_lt());
+                if ((some >> lane & 1) && at < LIST) list[at] = r;
+            }
+        });
+        if (W > 1) {
+            __syncthreads();
+            found = s_found;
+        } else __builtin_amdgcn_wave_barrier();
+        if (__builtin_expect(found <= LIST, 1)) {
+            for (int c0 = mine; c0 < found; c0 += 8 * W) {
+                int rows[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) rows[i] = list[c0 + i * W < found ? c0 + i * W : c0];
+                const double z = lp_score<E>(a, h, (double)scale, rows);
+                const int c = c0 + (lane >> 3) * W;
+                if ((lane & 7) == 0 && c < found) score[c] = z;
+            }
+            if (W > 1) __syncthreads();
+            else __builtin_amdgcn_wave_barrier();
+            for (int c = of; c < found || c < a.top; c += 64 * W) {
+                if (c >= found) {
+                    put(c, 0.0, LpBest::NONE);
+                    continue;
+                }
+                const double z = score[c];
+                const int row = list[c];
+                int place = 0;
+                for (int i = 0; i < found; ++i) place += LpBest::before(score[i], list[i], z, row) ? 1 : 0;
+                if (place < a.top) put(place, z, row);
+            }
+            continue;
+        }
         LpBest best;
         best.begin(a.top);
-        int* const pending = s_pending[TOP ? wave : 0];
-        int waiting = 0;
-        const int per = a.tile / LP_GROUP;
-        const auto drain = [&](int least) {
-            int done = 0;
-            while (waiting - done >= least && waiting > done) {
-                const int now = waiting - done < 8 ? waiting - done : 8;
-                lp_score<E>(a, h, (double)scale, pending + done, now, best);
-                done += now;
-            }
-            // the rest to the front: fewer than 8
-            const int rest = waiting - done, r = lane < rest ? pending[done + lane] : 0;
-            __builtin_amdgcn_wave_barrier();
-            if (lane < rest) pending[lane] = r;
-            __builtin_amdgcn_wave_barrier();
-            waiting = rest;
-        };
-        for (int64_t g0 = (int64_t)mine * 64; g0 < a.n_groups; g0 += 64 * W) {
-            const int64_t g = g0 + lane;
-            const uint2 v = g < a.n_groups ? groups[g] : make_uint2(0, 0);
-            const double first = (double)__uint_as_float(v.x);
-            const int64_t row0 = g / per * a.tile;
-            // (what a NaN is compared with is not out of reach)
-            const bool hit = g < a.n_groups && !(first < low) && best.wants(first + margin, (int)row0);
-            u64 many = __ballot(hit && !((double)lp_second(v.y) < low));
-            const int64_t row = row0 + lp_row(v.y);
-            const u64 one = __ballot(hit && (double)lp_second(v.y) < low && row < n_rows);
-            if (one >> lane & 1) pending[waiting + __popcll(one & tg_lanemask_lt())] = (int)row;
-            waiting += __popcll(one);
-            __builtin_amdgcn_wave_barrier();
-            if (waiting >= 8) drain(8);
-            while (many) {
-                const int from = __builtin_ctzll(many);
+        lp_reach<W>(groups, a.n_groups, mine, low, [&](bool hit, int g, float first, lp_u32 second) {
+            const int row0 = g >> a.per_shift << (a.per_shift + 5);
+            u64 hits = __ballot(hit && best.wants(first + margin, row0));
+            const u64 many = __ballot(!((double)lp_second(second) < low));
+            for (; hits; hits &= hits - 1) {
+                const int from = __builtin_ctzll(hits);
                 const double most = lp_lane64(first + margin, from);
-                many &= many - 1;
-                const int64_t gg = g0 + from, tile = gg / per;
-                const int in = (int)(gg - tile * per), sh = a.shared, waves = 4 / sh;
-                // row number `lane` of the group: of value e, quarter q and block i of the wave's rows (see lp_part_kernel)
-                const int e = lane & 3, q = (lane >> 2) % sh + in % waves * sh, i = (lane >> 2) / sh, half = 4 / sh;
-                const int64_t r = tile * a.tile + i / half * (a.tile / 2) + in / waves * (half * 16) + i % half * 16 + q * 4 + e;
-                const bool is = lane < LP_GROUP && r < n_rows && best.wants(most, (int)r);
-                const u64 some = __ballot(is);
-                if (is) pending[waiting + __popcll(some & tg_lanemask_lt())] = (int)r;
-                waiting += __popcll(some);
-                __builtin_amdgcn_wave_barrier();
-                drain(8);
+                const bool all_rows = many >> from & 1;
+                const int r = all_rows ? lp_group_row(a, __builtin_amdgcn_readlane(g, from), lane) : __builtin_amdgcn_readlane(row0 + lp_row(second), from);
+                u64 some = __ballot(lane < (all_rows ? LP_GROUP : 1) && r < (int)n_rows && best.wants(most, r));
+                while (some) {
+                    int rows[8], have = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        rows[i] = some ? __builtin_amdgcn_readlane(r, __builtin_ctzll(some)) : rows[0];
+                        have += some ? 1 : 0;
+                        some &= some - 1;
+                    }
+                    const double z = lp_score<E>(a, h, (double)scale, rows);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i < have) best.add(lp_lane64(z, i * 8), rows[i]);
+                }
             }
-        }
-        drain(1);
+        });
         if (W > 1) {
-            if (lane < a.top) {
-                s_best_z[wave][lane] = best.z;
-                s_best_row[wave][lane] = best.row;
-            }
-            __syncthreads();
-            if (wave == 0) {
-                for (int i = 1; i < W; ++i)
+            // the waves' lists, one behind the other, to the first
+            for (int i = 1; i < W; ++i) {
+                if (wave == i && lane < a.top) {
+                    score[lane] = best.z;
+                    list[lane] = best.row;
+                }
+                __syncthreads();
+                if (wave == 0)
                     for (int j = 0; j < a.top; ++j) {
-                        const double z = s_best_z[i][j];
-                        const int r = s_best_row[i][j];
+                        const double z = score[j];
+                        const int r = __builtin_amdgcn_readfirstlane(list[j]);
                         if (r == LpBest::NONE || !best.wants(z, r)) break;        // (theirs are in order too)
                         best.add(z, r);
                     }
+                __syncthreads();
             }
         }
-        if (mine == 0 && lane < a.top) {
-            const double p = best.z - (double)all;
-            a.rows[y * a.top + lane] = best.row == LpBest::NONE ? -1 : best.row;
-            a.row_logp[y * a.top + lane] = best.row == LpBest::NONE ? -__builtin_inff() : (float)(p > 0.0 ? 0.0 : p);
-        }
+        if (mine == 0 && lane < a.top) put(lane, best.z, best.row);
     }
 }
 
@@ -493,6 +603,7 @@ struct LpShape {
 };
 // tokens at a time: as many as the groups' stretches have room for, in whole tiles
 #define LP_GROUP_BYTES (512ll << 20)
+
 static LpShape lp_shape(int64_t n, int64_t n_rows, int e)
 {
     LpShape s;
@@ -515,6 +626,7 @@ struct LpSpace {
     void *ph, *pw;               // copies, or null
     float4* parts;
     float *at_target, *norms;
+    int64_t n_norms;             // stretches of the table with a largest square of a norm each
     uint2* groups;
 };
 static size_t carve_lp(LpSpace* r, TgCarve* c, const LpShape& s, const void* h, int64_t ld_h, const void* w, int64_t ld_w, int64_t n, int64_t n_rows, int d, int e,
@@ -527,7 +639,8 @@ static size_t carve_lp(LpSpace* r, TgCarve* c, const LpShape& s, const void* h, 
     r->w = ready_w ? TileRows{(const char*)w, n_rows, (uint32_t)(ld_w * e), pitch} : TileRows{(const char*)r->pw, n_rows, pitch, pitch};
     r->parts = c->take<float4>((size_t)s.tiles * s.tokens);
     r->at_target = c->take<float>(s.tokens);
-    r->norms = c->take<float>(top ? s.tiles : 0);
+    r->n_norms = s.bm == 256 ? (n_rows + LP_NORM_ROWS - 1) / LP_NORM_ROWS : s.tiles;
+    r->norms = c->take<float>(top ? r->n_norms : 0);
     r->groups = c->take<uint2>(top ? (size_t)s.tiles * (s.bm / LP_GROUP) * s.tokens : 0);
     return c->used;
 }
@@ -546,6 +659,7 @@ struct LpCall {
     const void* targets;         // of the tokens at hand
     int targets64;
     float scale;
+    bool first;                  // of the calls for a table
     hipStream_t s;
 };
 template <class E, int BM, int BN, int WM, int WN, int NB, bool TOP>
@@ -564,7 +678,8 @@ static void launch_parts(const LpShape& shape, const LpSpace& r, const TileRows&
             hipLaunchKernelGGL((lp_part_kernel<E, BM, BN, WM, WN, NB, TOP>), dim3((unsigned)(tiles * ny)), dim3(64 * WM * WN), 0, call.s, table, part, (int)X.width,
                                call.targets ? (const char*)call.targets + y0 * (call.targets64 ? 8 : 4) : nullptr, call.targets64, call.scale, v0, X.rows,
                                (uint32_t)tiles, ny, 8u, r.parts + y0 * shape.tiles + t0, shape.tiles,
-                               TOP ? r.groups + (y0 * shape.tiles + t0) * (BM / LP_GROUP) : nullptr, r.at_target + y0);
+                               TOP ? r.groups + (y0 * shape.tiles + t0) * (BM / LP_GROUP) : nullptr,
+                               y0 == 0 && call.first ? r.norms + t0 : nullptr, r.at_target + y0);
         }
     }
 }
@@ -591,7 +706,7 @@ static void launch_join(const LpShape& shape, const LpSpace& r, int64_t n, int64
         hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs < 65536 ? wgs : 65536)), dim3(waves == 1 ? 256 : 64 * waves), 0, call.s, r.parts, shape.tiles, n, n_rows,
                            call.targets, call.targets64, r.at_target, call.scale, a, logp, entropy, lse);
     };
-    if (n <= 256) go(lp_join_kernel<E, 16, TOP>, 16);
+    if (n <= 512) go(lp_join_kernel<E, 8, TOP>, 8);
     else if (n <= 2048) go(lp_join_kernel<E, 4, TOP>, 4);
     else go(lp_join_kernel<E, 1, TOP>, 1);
 }
@@ -608,17 +723,20 @@ void tg_launch_log_probs(const void* h, int64_t ld_h, const void* w, int64_t ld_
     carve_lp(&r, &c, shape, h, ld_h, w, ld_w, n, n_rows, d, e, rh, rw, top);
     if (!rh) tg_launch_pack(h, ld_h, n, d, e, r.ph, s);
     if (!rw) tg_launch_pack(w, ld_w, n_rows, d, e, r.pw, s);
-    LpTop a{h, w, ld_h, ld_w, d, shape.bm, shape.shared, top, r.norms, r.groups, shape.tiles * (shape.bm / LP_GROUP), rows, row_logp};
+    LpTop a{h, w, ld_h, ld_w, d, __builtin_ctz(shape.bm / LP_GROUP), __builtin_ctz(shape.shared), top, r.norms, (int)r.n_norms, r.groups,
+            (int)(shape.tiles * (shape.bm / LP_GROUP)), rows, row_logp};
     TG_WITH_TYPE(dtype, E, {
-        if (top) {
-            int lanes = 1;
-            while (lanes < 64 && lanes * TgPiece<E>::E < d) lanes *= 2;
-            hipLaunchKernelGGL(lp_norms_kernel<E>, dim3((unsigned)(shape.tiles < 65536 ? shape.tiles : 65536)), dim3(256), 0, s, (const E*)w, ld_w, n_rows, d, shape.bm,
-                               lanes, r.norms, shape.tiles);
+        if constexpr (sizeof(E) == 2) {
+            if (top && shape.bm == 256) {
+                int lanes = 1;
+                while (lanes < 64 && lanes * TgPiece<E>::E < d) lanes *= 2;
+                hipLaunchKernelGGL(lp_norms_kernel<E>, dim3((unsigned)(r.n_norms < 65536 ? r.n_norms : 65536)), dim3(256), 0, s, (const E*)w, ld_w, n_rows, d,
+                                   lanes, r.norms, r.n_norms);
+            }
         }
         for (int64_t y0 = 0; y0 < n; y0 += shape.tokens) {
             const int64_t now = n - y0 < shape.tokens ? n - y0 : shape.tokens;
-            const LpCall call{targets ? (const char*)targets + y0 * (targets64 ? 8 : 4) : nullptr, targets64, scale, s};
+            const LpCall call{targets ? (const char*)targets + y0 * (targets64 ? 8 : 4) : nullptr, targets64, scale, y0 == 0, s};
             const TileRows Y{r.h.p + y0 * r.h.pitch, now, r.h.pitch, r.h.width};
             a.h = (const E*)h + y0 * ld_h;
             a.rows = top ? rows + y0 * top : nullptr;
