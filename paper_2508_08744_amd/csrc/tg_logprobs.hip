@@ -15,6 +15,7 @@
 #define LP_GROUP 32             // logits of a token that leave their largest
 #define LP_MAX_TOP 32           // best rows; half the lanes of a wave, see lp_kth
 #define LP_NORM_ROWS 64         // of the table, where the tiles leave no norms
+#define LP_MANY_TILES 256       // from here on the tiles' maxima make the threshold: two of the best in one tile are rare
 #define LP_BELOW (-1000.0f)     // exponents below have a power of 0: so is their part in s, at -infinity too
 
 typedef unsigned int lp_u32;
@@ -337,36 +338,36 @@ __device__ inline double lp_score(const LpTop& a, const E* h, double scale, cons
     return s * scale;
 }
 
-// The groups of a token, as a wave goes through them: W waves in turn, LP_AHEAD times 64 groups asked for at once.
+// The groups of a token that reach `low`, as a wave goes through them: W waves in turn, LP_AHEAD times 64 tiles' maxima asked for at once, then the groups of those tiles that do.
+// Some lanes' groups at a time: take(whether the lane has one, its number, its largest, its packed second).
 #define LP_AHEAD 8
 template <int W, class Take>
-__device__ inline void lp_scan(const uint2* __restrict__ groups, int n_groups, int wave, Take take)
+__device__ inline void lp_reach(const float4* __restrict__ parts, int tiles, const uint2* __restrict__ groups, int per_shift, int wave, double low, Take take)
 {
-    for (int g0 = wave * 64 + tg_lane(); g0 - tg_lane() < n_groups; g0 += LP_AHEAD * 64 * W) {
-        uint2 v[LP_AHEAD];
+    for (int t0 = wave * 64 + tg_lane(); t0 - tg_lane() < tiles; t0 += LP_AHEAD * 64 * W) {
+        float v[LP_AHEAD];
 #pragma unroll
-        for (int i = 0; i < LP_AHEAD; ++i) v[i] = g0 + i * 64 * W < n_groups ? groups[g0 + i * 64 * W] : make_uint2(0xFF800000u /* -infinity */, 0u);
-        take(g0, v);
-    }
-}
-// ... those of them that reach `low`: some lanes' at a time, take(whether the lane has one, its number, its largest, its packed second)
-template <int W, class Take>
-__device__ inline void lp_reach(const uint2* __restrict__ groups, int n_groups, int wave, double low, Take take)
-{
-    lp_scan<W>(groups, n_groups, wave, [&](int g0, const uint2 (&v)[LP_AHEAD]) {
+        for (int i = 0; i < LP_AHEAD; ++i) v[i] = t0 + i * 64 * W < tiles ? parts[t0 + i * 64 * W].x : 0.0f;
         unsigned hits = 0;
 #pragma unroll
-        for (int i = 0; i < LP_AHEAD; ++i)          // (what a NaN is compared with is not out of reach)
-            hits |= g0 + i * 64 * W < n_groups && !((double)__uint_as_float(v[i].x) < low) ? 1u << i : 0u;
-        while (__any(hits != 0)) {
-            const int at = hits ? __builtin_ctz(hits) : 0;
-            uint2 x = v[0];
+        for (int i = 0; i < LP_AHEAD; ++i) hits |= t0 + i * 64 * W < tiles && !((double)v[i] < low) ? 1u << i : 0u;      // (what a NaN is compared with is not out of reach)
+        for (; __any(hits != 0); hits &= hits - 1) {
+            const int t = t0 + (hits ? __builtin_ctz(hits) : 0) * 64 * W;
+            uint2 q[8];
 #pragma unroll
-            for (int i = 1; i < LP_AHEAD; ++i) x = at == i ? v[i] : x;
-            take(hits != 0, g0 + at * 64 * W, __uint_as_float(x.x), x.y);
-            hits &= hits - 1;
+            for (int j = 0; j < 8; ++j) q[j] = hits && j < 1 << per_shift ? groups[(t << per_shift) + j] : make_uint2(0u, 0u);
+            unsigned deep = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) deep |= hits && j < 1 << per_shift && !((double)__uint_as_float(q[j].x) < low) ? 1u << j : 0u;
+            for (; __any(deep != 0); deep &= deep - 1) {
+                const int at = deep ? __builtin_ctz(deep) : 0;
+                uint2 x = q[0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) x = at == j ? q[j] : x;
+                take(deep != 0, (t << per_shift) + at, __uint_as_float(x.x), x.y);
+            }
         }
-    });
+    }
 }
 // row number `lane` of group g: of value e, quarter q and block i of the wave's rows, as lp_part_kernel has them (below LP_GROUP)
 __device__ inline int lp_group_row(const LpTop& a, int g, int lane)
@@ -401,13 +402,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
     const int mine = W == 1 ? 0 : wave, team = W == 1 ? wave : 0;
     for (int64_t y = (int64_t)blockIdx.x * TOKENS + team; y < n; y += (int64_t)gridDim.x * TOKENS) {
         const E* const h = (const E*)a.h + y * a.ld_h;
+        const float4* const own = parts + y * count;
         const uint2* const groups = a.groups + y * (int64_t)a.n_groups;
         LpSum sum{-__builtin_inff(), 0.0f, 0.0f};
         for (int64_t p0 = of; p0 < count; p0 += 4 * 64 * W) {
             float4 v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                v[i] = p0 + i * 64 * W < count ? parts[y * count + p0 + i * 64 * W] : make_float4(-__builtin_inff(), 0.0f, 0.0f, 0.0f);
+                v[i] = p0 + i * 64 * W < count ? own[p0 + i * 64 * W] : make_float4(-__builtin_inff(), 0.0f, 0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < 4; ++i) lp_join(sum, LpSum{v[i].x, v[i].y, v[i].z});
         }
@@ -423,10 +425,10 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
                 for (int e = 0; e < P::E; ++e) h2 = fma((double)p.v[e], (double)p.v[e], h2);
             }
             for (int p = of; p < a.n_norms; p += 64 * W) w2 = fmaxf(w2, a.norms[p]);
-            lp_scan<W>(groups, a.n_groups, mine, [&](int, const uint2 (&v)[LP_AHEAD]) {
-#pragma unroll
-                for (int i = 0; i < LP_AHEAD; ++i) high = fmaxf(high, __uint_as_float(v[i].x));
-            });
+            // (the maxima of many tiles are as good)
+            if (count >= LP_MANY_TILES) high = sum.m;
+            else
+                for (int g = of; g < a.n_groups; g += 64 * W) high = fmaxf(high, __uint_as_float(groups[g].x));
         }
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
@@ -502,7 +504,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
             found = at + some;
             return at;
         };
-        lp_reach<W>(groups, a.n_groups, mine, low, [&](bool hit, int g, float, lp_u32 second) {
+        lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, [&](bool hit, int g, float, lp_u32 second) {
             u64 many = __ballot(hit && !((double)lp_second(second) < low));
             const int row = (g >> a.per_shift << (a.per_shift + 5)) + lp_row(second);
             const u64 one = __ballot(hit && (double)lp_second(second) < low && row < (int)n_rows);
@@ -547,7 +549,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
         }
         LpBest best;
         best.begin(a.top);
-        lp_reach<W>(groups, a.n_groups, mine, low, [&](bool hit, int g, float first, lp_u32 second) {
+        lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, [&](bool hit, int g, float first, lp_u32 second) {
             const int row0 = g >> a.per_shift << (a.per_shift + 5);
             u64 hits = __ballot(hit && best.wants(first + margin, row0));
             const u64 many = __ballot(!((double)lp_second(second) < low));
