@@ -109,7 +109,7 @@ __device__ inline void clip_scale(const E* p, E* q, uint64_t left, float factor)
         for (int i = 0; i < TURNS; ++i) {
 #pragma unroll
             for (int e = 0; e < P::E; ++e) v[i][e] = (E)((float)v[i][e] * factor);
-            *reinterpret_cast<typename P::vec*>(q + (i * 256 + threadIdx.x) * P::E) = v[i];
+            __builtin_nontemporal_store(v[i], reinterpret_cast<typename P::vec*>(q + (i * 256 + threadIdx.x) * P::E));    // (in the place of what is still to be read they would take room)
         }
     } else {
 #pragma unroll

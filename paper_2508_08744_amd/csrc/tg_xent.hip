@@ -696,10 +696,11 @@ static void xent_splits(XentGrad* g, int64_t n, int64_t n_rows, int d, int e, bo
     // both products take tiles of 256 x 256, of which a CU holds one, where those are enough; else of 128 x 128, of which it holds two, in fp32 of
     // 64 x 64, of which it holds four; and of 64 x 64, with four stages in flight, where each of 128 x 128 would have a CU of its own
     const auto tiles = [](int64_t x, int64_t y, int64_t side) { return ((x + side - 1) / side) * ((y + side - 1) / side); };
-    // (without dw, dh's parts alone are to fill the card)
-    const int64_t beside = table ? g->piece : 0;
-    g->few = tiles(n, d, 128) + tiles(beside, d, 128) <= 128;
-    g->side = e == 2 && n > 128 && d > 128 && tiles(table ? g->piece : n, d, 256) >= 200 ? 256 : g->few || e == 4 ? 64 : 128;
+    // Without dw, dh's parts alone are to fill the card: the tiles are those that as many parts as the contraction is long enough for would make.
+    const int64_t all_stages = (g->piece * e + TILE_BYTES - 1) / TILE_BYTES;
+    const auto parts = [&](int64_t side) { return tiles(n, d, side) * (all_stages >= 64 * 16 ? 64 : all_stages >= 16 ? all_stages / 16 : 1); };
+    g->few = table ? tiles(n, d, 128) + tiles(g->piece, d, 128) <= 128 : n <= 64 || parts(128) <= 128;
+    g->side = e == 2 && n > 128 && d > 128 && (table ? tiles(g->piece, d, 256) : parts(256)) >= 200 ? 256 : g->few || e == 4 ? 64 : 128;
     // dh in as many parts as fill the card, each with sixteen stages of the contraction or more; where dw, beside it, has fewer, with as many as
     // that, but four, up to 32 parts whose bytes are half of the table's (there and back, bf16: 7 tokens, 6938 rows of 688: 39.8 us with sixteen, 37.2;
     // 900 tokens, 5000 rows of 700: 77.7 and 75.2)
