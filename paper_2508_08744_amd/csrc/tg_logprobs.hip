@@ -40,6 +40,13 @@ __device__ inline lp_u32 lp_pack(float second, int row) { return ((tg_ord(fmaxf(
 __device__ inline float lp_second(lp_u32 key) { return tg_unord(key); }
 __device__ inline int lp_row(lp_u32 key) { return (int)(key & 255u); }
 
+// a product that is no smaller than the exact one
+__device__ inline float lp_times_up(float x, float by)
+{
+    const float z = x * by;
+    return fmaf(fabsf(z), 0x1p-23f, z);
+}
+
 // x: rows of the table from v0 on, y: tokens.  parts: for every token the tiles along x; groups: for every token, tile and group (largest, packed second).
 template <class E, int BM, int BN, int WM, int WN, int NB, bool TOP>
 __global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileRows Y, int bytes, const void* __restrict__ targets, int targets64,
@@ -82,61 +89,99 @@ __global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileR
     // (the tile's memory is free: a sum for every token and wave along x)
     LpSum* const s_sum = reinterpret_cast<LpSum*>(lds) + (threadIdx.x >> 6) / WN * BN;
     static_assert(WM * BN * sizeof(LpSum) <= T::LDS, "the sums' place");
+    // From here on the factor is above 0, so that the largest logit is the largest product times it (rounding keeps the order), and there is no row behind the table's end
+    // that anything is taken of.
+    if (__builtin_expect(!(scale > 0.0f), 0)) {
+        const float by = scale < 0.0f ? -1.0f : scale;             // (0, or a NaN)
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::FN; ++j) t.acc[i][j] *= by;
+        scale = scale < 0.0f ? -scale : 1.0f;
+    }
     const int have = x0 + BM <= X.rows ? BM : (int)(X.rows - x0);
+    if (__builtin_expect(have < BM, 0)) {
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (t.x_of(i) + e >= have)
+#pragma unroll
+                    for (int j = 0; j < T::FN; ++j) t.acc[i][j][e] = -__builtin_inff();
+    }
     const int none = (threadIdx.x >> 6) / WN * (T::HM * 16);        // the wave's first row: where the table ends before it there are no logits
     const float base = scale * XENT_LOG2E;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
         const int64_t y = y0 + t.y_of(j);
         const int target = s_target[t.y_of(j)];
-        float m = -__builtin_inff(), second = m, l = 0.0f, s = 0.0f;
-        int at = 0;
+        if (__any(target >= 0)) {
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (t.x_of(i) + e == target) at_target[y] = t.acc[i][j][e] * scale;
+        }
+        float m = -__builtin_inff(), least = -m, l = 0.0f, s = 0.0f;
 #pragma unroll
         for (int i = 0; i < T::FM; ++i) {
-            const int x = t.x_of(i);
-            if ((unsigned)(target - x) < 4u) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (x + e == target) at_target[y] = t.acc[i][j][e] * scale;
-            }
-            const auto take = [&](int e) {
-                const float z = t.acc[i][j][e] * scale;
-                if (TOP) {
-                    at = z > m ? i * 4 + e : at;
-                    second = __builtin_amdgcn_fmed3f(m, second, z);
-                }
-                m = fmaxf(m, z);
-            };
-            if (x + 4 <= have) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) take(e);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (x + e < have) take(e);
+            m = fmaxf(fmaxf(m, t.acc[i][j][0]), t.acc[i][j][1]);
+            m = fmaxf(fmaxf(m, t.acc[i][j][2]), t.acc[i][j][3]);
+            if (TOP) {
+                least = fminf(fminf(least, t.acc[i][j][0]), t.acc[i][j][1]);
+                least = fminf(fminf(least, t.acc[i][j][2]), t.acc[i][j][3]);
             }
         }
+        const float largest = m;
+        m *= scale;
         if (TOP) {
-            // (x_of for an i that is not known in advance)
+            // The largest and the second with their place in the last five bits, as numbers: off by less than 2^-18 of them.  Where that makes another one the largest, the
+            // second, rounded up, is no smaller than the largest.  (Infinite ones have no such bits: they are compared as they are.)
+            float first = -__builtin_inff(), second = first;
+            int at = 0;
+            if (__builtin_expect(__all(largest < __builtin_inff() && least > -__builtin_inff()), 1)) {
+#pragma unroll
+                for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float z = __uint_as_float((__float_as_uint(t.acc[i][j][e]) & ~31u) | (unsigned)(i * 4 + e));
+                        second = __builtin_amdgcn_fmed3f(first, second, z);
+                        first = fmaxf(first, z);
+                    }
+                at = (int)(__float_as_uint(first) & 31u);
+                const lp_u32 bits = __float_as_uint(second);
+                second = __uint_as_float(bits >> 31 ? bits & ~31u : bits | 31u);
+            } else {
+#pragma unroll
+                for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float z = t.acc[i][j][e];
+                        at = z > first ? i * 4 + e : at;
+                        second = fmaxf(second, fminf(first, z));
+                        first = fmaxf(first, z);
+                    }
+            }
             const int i = at >> 2;
+            // (x_of for an i that is not known in advance)
             int x = (i / T::HM) * (BM / 2) + none + (i % T::HM) * 16 + (threadIdx.x >> 4 & 3) * 4 + (at & 3);
-            float top = m;
+            float top = m, most = lp_times_up(second, scale);
 #pragma unroll
             for (int q = 1; q < Q; q <<= 1) {
-                const float top2 = __shfl_xor(top, q * 16), second2 = __shfl_xor(second, q * 16);
+                const float top2 = __shfl_xor(top, q * 16), most2 = __shfl_xor(most, q * 16);
                 const int x2 = __shfl_xor(x, q * 16);
                 x = top2 > top ? x2 : x;
-                second = fmaxf(fminf(top, top2), fmaxf(second, second2));
+                most = fmaxf(fminf(top, top2), fmaxf(most, most2));
                 top = fmaxf(top, top2);
             }
             const int quarter = threadIdx.x >> 4 & 3;
             if (quarter % Q == 0 && y < Y.rows)
-                groups[(y * parts_pitch + tx) * GROUPS + (threadIdx.x >> 6) / WN * (4 / Q) + quarter / Q] = make_uint2(__float_as_uint(top), lp_pack(second, x));
+                groups[(y * parts_pitch + tx) * GROUPS + (threadIdx.x >> 6) / WN * (4 / Q) + quarter / Q] = make_uint2(__float_as_uint(top), lp_pack(most, x));
         }
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
         const bool near = xent_near(m, base) || have <= none;
-        const float f = near ? base : 1.0f, b = near ? m * XENT_LOG2E : 0.0f;
+        const float f = near ? base : 1.0f, b = near && have > none ? m * XENT_LOG2E : 0.0f;
         if (__builtin_expect(!__all(near), 0)) {           // (out of the way: code that is jumped over is fetched late)
 #pragma unroll
             for (int i = 0; i < T::FM; ++i)
@@ -144,21 +189,22 @@ __global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileR
                 for (int e = 0; e < 4; ++e) t.acc[i][j][e] = near ? t.acc[i][j][e] : xent_far<true>(t.acc[i][j][e], scale, m);
         }
 #pragma unroll
-        for (int i = 0; i < T::FM; ++i) {
-            const int x = t.x_of(i);
-            const auto take = [&](int e) {
+        for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
                 const float u = fmaf(t.acc[i][j][e], f, -b), p = __builtin_amdgcn_exp2f(u);
                 l += p;
-                s = fmaf(p, fmaxf(u, LP_BELOW), s);
-            };
-            if (x + 4 <= have) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) take(e);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (x + e < have) take(e);
+                s = fmaf(p, u, s);
             }
+        if (__builtin_expect(__any(s != s), 0)) {          // (a power of 0 times the -infinity that it is of)
+            s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float u = fmaf(t.acc[i][j][e], f, -b);
+                    s = fmaf(__builtin_amdgcn_exp2f(u), fmaxf(u, LP_BELOW), s);
+                }
         }
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
@@ -227,21 +273,22 @@ template <class E>
 __device__ inline double lp_margin(float scale, int d, double h2, double w2)
 {
     const double lost = (__is_same(E, tg_f16) ? 0x1p-28 : 0x1p-126) * d, more = 1.0 + d * 0x1p-22;
-    return fabs((double)scale) * (d + 2) * 0x1p-23 * sqrt((h2 + lost) * more) * sqrt((w2 + lost) * more) + 0x1p-120;
+    // (roots in 32 bits, rounded up)
+    const float h = sqrtf((float)((h2 + lost) * more)), w = sqrtf((float)((w2 + lost) * more));
+    return fabs((double)scale) * (d + 2) * 0x1.00001p-23 * (double)h * (double)w + 0x1p-120;
 }
 
-// The k-th largest of a wave's values (k <= 64), the same in all lanes; a NaN counts as the smallest.
+// What the k-th largest of a wave's values is not below, in all lanes: its first 20 bits (a NaN counts as the smallest; less than everything is a NaN itself).
 __device__ inline float lp_kth(float v, int k)
 {
     const lp_u32 mine = v != v ? 0u : tg_ord(v);
-    int rank = 0;
-#pragma unroll 8
-    for (int i = 0; i < 64; ++i) {
-        const lp_u32 other = (lp_u32)__builtin_amdgcn_readlane((int)mine, i);
-        rank += other > mine || (other == mine && i < tg_lane()) ? 1 : 0;
+    lp_u32 least = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 12; --bit) {
+        const lp_u32 more = least | 1u << bit;
+        least = __popcll(__ballot(mine >= more)) >= k ? more : least;
     }
-    const u64 is = __ballot(rank == k - 1);
-    return __uint_as_float((lp_u32)__builtin_amdgcn_readlane((int)__float_as_uint(v), __builtin_ctzll(is)));
+    return tg_unord(least);
 }
 
 __device__ inline double lp_lane64(double x, int lane)
@@ -304,38 +351,38 @@ struct LpTop {
     float* row_logp;
 };
 
-// Up to eight rows' logits in 64 bits, by one wave: row i's in the lanes 8 i to 8 i + 7.  Every lane has the same places of all rows, so a row's sum does not depend
+// R rows' logits in 64 bits, by one wave: row i's in the lanes 64 / R i and on.  Every lane has the same places of all rows, so a row's sum does not depend
 // on where it was found.
-template <class E>
-__device__ inline double lp_score(const LpTop& a, const E* h, double scale, const int (&rows)[8])
+template <int R, class E>
+__device__ inline double lp_score(const LpTop& a, const E* h, double scale, const int (&rows)[R])
 {
     typedef TgPiece<E> P;
     const int lane = tg_lane();
-    const E* w[8];
+    const E* w[R];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = (const E*)a.w + (int64_t)__builtin_amdgcn_readfirstlane(rows[i]) * a.ld_w;
-    double sum[8] = {};
+    for (int i = 0; i < R; ++i) w[i] = (const E*)a.w + (int64_t)__builtin_amdgcn_readfirstlane(rows[i]) * a.ld_w;
+    double sum[R] = {};
     for (int c = lane * P::E; c < a.d; c += 64 * P::E) {
-        typename P::vec x[8];
+        typename P::vec x[R];
         P hp;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = P::raw(w[i] + c, a.d - c);
+        for (int i = 0; i < R; ++i) x[i] = P::raw(w[i] + c, a.d - c);
         hp.load(h + c, a.d - c);
 #pragma unroll
         for (int e = 0; e < P::E; ++e)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] = fma((double)hp.v[e], (double)(float)x[i][e], sum[i]);
+            for (int i = 0; i < R; ++i) sum[i] = fma((double)hp.v[e], (double)(float)x[i][e], sum[i]);
     }
-    // row i's sum ends up in the lanes whose bits 5, 4, 3 are i's bits 2, 1, 0
-    double s4[4], s2[2];
+    // half of the rows goes to either half of the lanes, as long as there are two
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s4[i] = (lane & 32 ? sum[i + 4] : sum[i]) + lp_xor64(lane & 32 ? sum[i] : sum[i + 4], 32);
+    for (int left = R, m = 32; m >= 1; m >>= 1) {
+        if (left > 1) {
+            left /= 2;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) s2[i] = (lane & 16 ? s4[i + 2] : s4[i]) + lp_xor64(lane & 16 ? s4[i] : s4[i + 2], 16);
-    double s = (lane & 8 ? s2[1] : s2[0]) + lp_xor64(lane & 8 ? s2[0] : s2[1], 8);
-#pragma unroll
-    for (int m = 4; m >= 1; m >>= 1) s += lp_xor64(s, m);
-    return s * scale;
+            for (int i = 0; i < left; ++i) sum[i] = (lane & m ? sum[i + left] : sum[i]) + lp_xor64(lane & m ? sum[i] : sum[i + left], m);
+        } else sum[0] += lp_xor64(sum[0], m);
+    }
+    return sum[0] * scale;
 }
 
 // The groups of a token that reach `low`, as a wave goes through them: W waves in turn, LP_AHEAD times 64 tiles' maxima asked for at once, then the groups of those tiles that do.
@@ -384,7 +431,7 @@ __device__ inline int lp_group_row(const LpTop& a, int g, int lane)
 // them (rows that are equal, or nearly, by the hundreds) every wave goes through its groups again with its k best so far in order in its lanes, and passes over
 // what cannot be among them.
 template <class E, int W, bool TOP>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const float4* __restrict__ parts, int64_t count, int64_t n, int64_t n_rows,
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join_kernel(const float4* __restrict__ parts, int64_t count, int64_t n, int64_t n_rows,
                                                                        const void* __restrict__ targets, int targets64, const float* __restrict__ at_target,
                                                                        float scale, LpTop a, float* __restrict__ logp, float* __restrict__ entropy,
                                                                        float* __restrict__ lse)
@@ -404,27 +451,34 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
         const E* const h = (const E*)a.h + y * a.ld_h;
         const float4* const own = parts + y * count;
         const uint2* const groups = a.groups + y * (int64_t)a.n_groups;
+        // what the margin is made of, its first pieces asked for in front of everything
+        double h2 = 0.0;
+        float w2 = 0.0f;
+        typedef TgPiece<E> P;
+        typename P::vec h_first;
+        if (TOP) {
+            h_first = P::raw(h + (of * P::E < a.d ? of * P::E : 0), a.d - of * P::E);
+            w2 = of < a.n_norms ? a.norms[of] : 0.0f;
+        }
         LpSum sum{-__builtin_inff(), 0.0f, 0.0f};
         for (int64_t p0 = of; p0 < count; p0 += 4 * 64 * W) {
             float4 v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                v[i] = p0 + i * 64 * W < count ? own[p0 + i * 64 * W] : make_float4(-__builtin_inff(), 0.0f, 0.0f, 0.0f);
+            for (int i = 0; i < 4; ++i) v[i] = p0 + i * 64 * W < count ? own[p0 + i * 64 * W] : make_float4(-__builtin_inff(), 0.0f, 0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < 4; ++i) lp_join(sum, LpSum{v[i].x, v[i].y, v[i].z});
         }
-        // what the margin is made of, and the largest logits of the lanes' groups
-        double h2 = 0.0;
-        float w2 = 0.0f, high = -__builtin_inff();
+        float high = -__builtin_inff();          // of the lane's groups
         if (TOP) {
-            typedef TgPiece<E> P;
-            for (int c = of * P::E; c < a.d; c += 64 * W * P::E) {
+#pragma unroll
+            for (int e = 0; e < P::E; ++e) h2 = fma((double)(float)h_first[e], (double)(float)h_first[e], h2);
+            for (int c = (of + 64 * W) * P::E; c < a.d; c += 64 * W * P::E) {
                 P p;
                 p.load(h + c, a.d - c);
 #pragma unroll
                 for (int e = 0; e < P::E; ++e) h2 = fma((double)p.v[e], (double)p.v[e], h2);
             }
-            for (int p = of; p < a.n_norms; p += 64 * W) w2 = fmaxf(w2, a.norms[p]);
+            for (int p = of + 64 * W; p < a.n_norms; p += 64 * W) w2 = fmaxf(w2, a.norms[p]);
             // (the maxima of many tiles are as good)
             if (count >= LP_MANY_TILES) high = sum.m;
             else
@@ -524,14 +578,20 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
             found = s_found;
         } else __builtin_amdgcn_wave_barrier();
         if (__builtin_expect(found <= LIST, 1)) {
-            for (int c0 = mine; c0 < found; c0 += 8 * W) {
-                int rows[8];
+            const auto some = [&](auto rows) {
+                constexpr int R = sizeof(rows) / sizeof(int);
+                for (int c0 = mine; c0 < found; c0 += R * W) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) rows[i] = list[c0 + i * W < found ? c0 + i * W : c0];
-                const double z = lp_score<E>(a, h, (double)scale, rows);
-                const int c = c0 + (lane >> 3) * W;
-                if ((lane & 7) == 0 && c < found) score[c] = z;
-            }
+                    for (int i = 0; i < R; ++i) rows.v[i] = list[c0 + i * W < found ? c0 + i * W : c0];
+                    const double z = lp_score<R, E>(a, h, (double)scale, rows.v);
+                    const int c = c0 + lane / (64 / R) * W;
+                    if (lane % (64 / R) == 0 && c < found) score[c] = z;
+                }
+            };
+            struct Two { int v[2]; };
+            struct Eight { int v[8]; };
+            if (W > 1 && found <= 2 * W) some(Two{});
+            else some(Eight{});
             if (W > 1) __syncthreads();
             else __builtin_amdgcn_wave_barrier();
             for (int c = of; c < found || c < a.top; c += 64 * W) {
@@ -542,7 +602,17 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
                 const double z = score[c];
                 const int row = list[c];
                 int place = 0;
-                for (int i = 0; i < found; ++i) place += LpBest::before(score[i], list[i], z, row) ? 1 : 0;
+                for (int i0 = 0; i0 < found; i0 += 8) {
+                    double zs[8];
+                    int rows[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        zs[i] = score[i0 + i];
+                        rows[i] = list[i0 + i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) place += i0 + i < found && (zs[i] > z || (zs[i] == z && rows[i] < row)) ? 1 : 0;
+                }
                 if (place < a.top) put(place, z, row);
             }
             continue;
@@ -567,7 +637,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void lp_join_kernel(const fl
                         have += some ? 1 : 0;
                         some &= some - 1;
                     }
-                    const double z = lp_score<E>(a, h, (double)scale, rows);
+                    const double z = lp_score<8, E>(a, h, (double)scale, rows);
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         if (i < have) best.add(lp_lane64(z, i * 8), rows[i]);
@@ -606,10 +676,11 @@ struct LpShape {
 // tokens at a time: as many as the groups' stretches have room for, in whole tiles
 #define LP_GROUP_BYTES (512ll << 20)
 
-static LpShape lp_shape(int64_t n, int64_t n_rows, int e)
+static LpShape lp_shape(int64_t n, int64_t n_rows, int e, int top)
 {
     LpShape s;
-    // (the tiles of the cross entropy's logits)
+    // The tiles of the cross entropy's logits; but where the best rows are asked for those of 128 rows, which have the norms' squares beside their products, up to 384 tokens
+    // (131 072 rows of 1024 bf16, 8 best: 100 tokens 122 us in tiles of 256 rows behind a pass for the norms, 77 in these; 300: 202 and 178; 512: the other way round).
     int64_t most = LP_GROUP_BYTES / (int64_t)sizeof(uint2) / ((n_rows + LP_GROUP - 1) / LP_GROUP);
     most = most >= 256 ? most / 256 * 256 : most >= 64 ? 64 : 32;
     s.tokens = n < most ? n : most;
@@ -618,7 +689,7 @@ static LpShape lp_shape(int64_t n, int64_t n_rows, int e)
     if (s.tokens <= 32) s.bm = 128, s.bn = 32, s.shared = 4;
     else if (s.few || (e == 4 && s.tokens > 64)) s.bm = 64, s.bn = 64, s.shared = 4;
     else if (s.tokens <= 64) s.bm = 128, s.bn = 64, s.shared = 4;
-    else if (tiles(256, 256) >= 200) s.bm = 256, s.bn = 256, s.shared = 1;
+    else if ((!top || s.tokens > 384) && tiles(256, 256) >= 200) s.bm = 256, s.bn = 256, s.shared = 1;
     else s.bm = 128, s.bn = 128, s.shared = 2;
     s.tiles = (n_rows + s.bm - 1) / s.bm;
     return s;
@@ -653,7 +724,7 @@ size_t tg_log_probs_space(int64_t n, int64_t n_rows, int d, int dtype, int top, 
     TgCarve c{nullptr, 0};
     LpSpace r;
     const bool whole = (d * e & 15) == 0;
-    return carve_lp(&r, &c, lp_shape(n, n_rows, e), nullptr, d, nullptr, d, n, n_rows, d, e, whole && (aligned == 1 || aligned == 3),
+    return carve_lp(&r, &c, lp_shape(n, n_rows, e, top), nullptr, d, nullptr, d, n, n_rows, d, e, whole && (aligned == 1 || aligned == 3),
                     whole && (aligned == 1 || aligned == 2), top);
 }
 
@@ -708,8 +779,7 @@ static void launch_join(const LpShape& shape, const LpSpace& r, int64_t n, int64
         hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs < 65536 ? wgs : 65536)), dim3(waves == 1 ? 256 : 64 * waves), 0, call.s, r.parts, shape.tiles, n, n_rows,
                            call.targets, call.targets64, r.at_target, call.scale, a, logp, entropy, lse);
     };
-    if (n <= 512) go(lp_join_kernel<E, 8, TOP>, 8);
-    else if (n <= 2048) go(lp_join_kernel<E, 4, TOP>, 4);
+    if (n <= 256) go(lp_join_kernel<E, 8, TOP>, 8);
     else go(lp_join_kernel<E, 1, TOP>, 1);
 }
 
@@ -718,7 +788,7 @@ void tg_launch_log_probs(const void* h, int64_t ld_h, const void* w, int64_t ld_
                          hipStream_t s)
 {
     const int e = (int)tg_type_bytes(dtype);
-    const LpShape shape = lp_shape(n, n_rows, e);
+    const LpShape shape = lp_shape(n, n_rows, e, top);
     TgCarve c{(char*)space, 0};
     LpSpace r;
     const bool rh = tile_ready(h, ld_h, d, e), rw = tile_ready(w, ld_w, d, e);
