@@ -15,7 +15,6 @@
 #define LP_GROUP 32             // logits of a token that leave their largest
 #define LP_MAX_TOP 32           // best rows; half the lanes of a wave, see lp_kth
 #define LP_NORM_ROWS 64         // of the table, where the tiles leave no norms
-#define LP_MANY_TILES 256       // from here on the tiles' maxima make the threshold: two of the best in one tile are rare
 #define LP_BELOW (-1000.0f)     // exponents below have a power of 0: so is their part in s, at -infinity too
 
 typedef unsigned int lp_u32;
@@ -479,8 +478,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
                 for (int e = 0; e < P::E; ++e) h2 = fma((double)p.v[e], (double)p.v[e], h2);
             }
             for (int p = of + 64 * W; p < a.n_norms; p += 64 * W) w2 = fmaxf(w2, a.norms[p]);
-            // (the maxima of many tiles are as good)
-            if (count >= LP_MANY_TILES) high = sum.m;
+            // (the tiles' maxima are as good, where there are so many that few tiles have two of the best)
+            if (count >= 4 * a.top) high = sum.m;
             else
                 for (int g = of; g < a.n_groups; g += 64 * W) high = fmaxf(high, __uint_as_float(groups[g].x));
         }
