@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void clip_norm_kernel(const double* __restrict
 }
 
 template <class E>
-__device__ inline void clip_scale(const E* p, E* q, uint64_t left, float factor)
+__device__ inline void clip_scale(const E* p, E* q, uint64_t left, float factor, float then)
 {
     typedef TgPiece<E> P;
     constexpr int TURNS = CLIP_PIECE / (256 * P::E);
@@ -108,7 +108,7 @@ __device__ inline void clip_scale(const E* p, E* q, uint64_t left, float factor)
 #pragma unroll
         for (int i = 0; i < TURNS; ++i) {
 #pragma unroll
-            for (int e = 0; e < P::E; ++e) v[i][e] = (E)((float)v[i][e] * factor);
+            for (int e = 0; e < P::E; ++e) v[i][e] = (E)((float)v[i][e] * factor * then);
             __builtin_nontemporal_store(v[i], reinterpret_cast<typename P::vec*>(q + (i * 256 + threadIdx.x) * P::E));    // (in the place of what is still to be read they would take room)
         }
     } else {
@@ -122,7 +122,7 @@ __device__ inline void clip_scale(const E* p, E* q, uint64_t left, float factor)
             const int at = (i * 256 + threadIdx.x) * P::E;
             P o;
 #pragma unroll
-            for (int e = 0; e < P::E; ++e) o.v[e] = (float)v[i][e] * factor;
+            for (int e = 0; e < P::E; ++e) o.v[e] = (float)v[i][e] * factor * then;
             o.store(q + at, (int)left - at);
         }
     }
@@ -134,17 +134,20 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(ClipList a, const doubl
     __shared__ double s[4];
     const double norm = fabs((double)scale) * sqrt(clip_total(sums, count, s));
     // (a norm that is no number, or infinite, brings nothing under anything)
-    const float factor = (float)(norm > (double)max_norm && norm <= 1.7e308 ? (double)scale * ((double)max_norm / norm) : (double)scale);
+    const double by = norm > (double)max_norm && norm <= 1.7e308 ? (double)scale * ((double)max_norm / norm) : (double)scale;
+    // (in two steps where 32 bits have few bits left for it: norms beyond them)
+    const bool tiny = fabs(by) < 0x1p-64;
+    const float factor = (float)(tiny ? by * 0x1p64 : by), then = tiny ? 0x1p-64f : 1.0f;
     if (out_norm && blockIdx.x == 0 && threadIdx.x == 0) *out_norm = (float)norm;
     const uint32_t p0 = blockIdx.x * a.each, all = a.first[a.tensors], p1 = p0 + a.each < all ? p0 + a.each : all;
     if (p0 >= p1) return;
     int t = clip_tensor(a, p1 - 1);
     for (uint32_t p = p1; p-- > p0;) {
         while (a.first[t] > p) --t;
-        if (factor == 1.0f && a.in[t] == a.out[t]) continue;        // they are what they would become
+        if (factor == 1.0f && then == 1.0f && a.in[t] == a.out[t]) continue;        // they are what they would become
         const uint64_t values = a.count[t] << 2 >> 2, at = (uint64_t)(p - a.first[t]) * CLIP_PIECE;
         const int type = (int)(a.count[t] >> 62);
-        TG_WITH_TYPE(type, E, clip_scale((const E*)a.in[t] + at, (E*)a.out[t] + at, values - at, factor));
+        TG_WITH_TYPE(type, E, clip_scale((const E*)a.in[t] + at, (E*)a.out[t] + at, values - at, factor, then));
     }
 }
 

@@ -385,10 +385,11 @@ __device__ inline double lp_score(const LpTop& a, const E* h, double scale, cons
 }
 
 // The groups of a token that reach `low`, as a wave goes through them: W waves in turn, LP_AHEAD times 64 tiles' maxima asked for at once, then the groups of those tiles that do.
-// Some lanes' groups at a time: take(whether the lane has one, its number, its largest, its packed second).
+// Some lanes' groups at a time: take(whether the lane has one, its number, its largest, its packed second).  look(a tile's maximum, its number): whether its groups are still of
+// interest.
 #define LP_AHEAD 8
-template <int W, class Take>
-__device__ inline void lp_reach(const float4* __restrict__ parts, int tiles, const uint2* __restrict__ groups, int per_shift, int wave, double low, Take take)
+template <int W, class Look, class Take>
+__device__ inline void lp_reach(const float4* __restrict__ parts, int tiles, const uint2* __restrict__ groups, int per_shift, int wave, double low, Look look, Take take)
 {
     for (int t0 = wave * 64 + tg_lane(); t0 - tg_lane() < tiles; t0 += LP_AHEAD * 64 * W) {
         float v[LP_AHEAD];
@@ -398,13 +399,18 @@ __device__ inline void lp_reach(const float4* __restrict__ parts, int tiles, con
 #pragma unroll
         for (int i = 0; i < LP_AHEAD; ++i) hits |= t0 + i * 64 * W < tiles && !((double)v[i] < low) ? 1u << i : 0u;      // (what a NaN is compared with is not out of reach)
         for (; __any(hits != 0); hits &= hits - 1) {
-            const int t = t0 + (hits ? __builtin_ctz(hits) : 0) * 64 * W;
+            const int i = hits ? __builtin_ctz(hits) : 0, t = t0 + i * 64 * W;
+            float max = v[0];
+#pragma unroll
+            for (int j = 1; j < LP_AHEAD; ++j) max = i == j ? v[j] : max;
+            const bool in = hits && look(max, t);
+            if (!__any(in)) continue;
             uint2 q[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] = hits && j < 1 << per_shift ? groups[(t << per_shift) + j] : make_uint2(0u, 0u);
+            for (int j = 0; j < 8; ++j) q[j] = in && j < 1 << per_shift ? groups[(t << per_shift) + j] : make_uint2(0u, 0u);
             unsigned deep = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) deep |= hits && j < 1 << per_shift && !((double)__uint_as_float(q[j].x) < low) ? 1u << j : 0u;
+            for (int j = 0; j < 8; ++j) deep |= in && j < 1 << per_shift && !((double)__uint_as_float(q[j].x) < low) ? 1u << j : 0u;
             for (; __any(deep != 0); deep &= deep - 1) {
                 const int at = deep ? __builtin_ctz(deep) : 0;
                 uint2 x = q[0];
@@ -442,7 +448,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
     __shared__ float s_top[W > 1 ? W : 1][W > 1 ? 64 : 1];
     __shared__ int s_list[TOP ? TOKENS : 1][TOP ? LIST : 1];
     __shared__ double s_z[TOP ? TOKENS : 1][TOP ? LIST : 1];
-    __shared__ int s_found;
+    __shared__ int s_found, s_zero[W];
     const int lane = tg_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int of = W == 1 ? lane : threadIdx.x;                  // of the token's lanes
     const int mine = W == 1 ? 0 : wave, team = W == 1 ? wave : 0;
@@ -453,6 +459,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
         // what the margin is made of, its first pieces asked for in front of everything
         double h2 = 0.0;
         float w2 = 0.0f;
+        bool zero = true;                        // a row of zeros (padding): its logits are exact, and all equal
         typedef TgPiece<E> P;
         typename P::vec h_first;
         if (TOP) {
@@ -470,13 +477,20 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
         float high = -__builtin_inff();          // of the lane's groups
         if (TOP) {
 #pragma unroll
-            for (int e = 0; e < P::E; ++e) h2 = fma((double)(float)h_first[e], (double)(float)h_first[e], h2);
+            for (int e = 0; e < P::E; ++e) {
+                h2 = fma((double)(float)h_first[e], (double)(float)h_first[e], h2);
+                zero = zero && h_first[e] == (E)0.0f;
+            }
             for (int c = (of + 64 * W) * P::E; c < a.d; c += 64 * W * P::E) {
                 P p;
                 p.load(h + c, a.d - c);
 #pragma unroll
-                for (int e = 0; e < P::E; ++e) h2 = fma((double)p.v[e], (double)p.v[e], h2);
+                for (int e = 0; e < P::E; ++e) {
+                    h2 = fma((double)p.v[e], (double)p.v[e], h2);
+                    zero = zero && p.v[e] == 0.0f;
+                }
             }
+            zero = __all(zero);
             for (int p = of + 64 * W; p < a.n_norms; p += 64 * W) w2 = fmaxf(w2, a.norms[p]);
             // (the tiles' maxima are as good, where there are so many that few tiles have two of the best)
             if (count >= 4 * a.top) high = sum.m;
@@ -498,6 +512,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
                 s_l[wave] = sum.l;
                 s_s[wave] = sum.s;
                 s_h2[wave] = h2;
+                s_zero[wave] = zero;
                 s_w2[wave] = w2;
             }
             if (threadIdx.x == 0) s_found = 0;
@@ -507,6 +522,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
             sum = LpSum{s_m[lane % W], s_l[lane % W], s_s[lane % W]};
             h2 = s_h2[lane % W];
             w2 = s_w2[lane % W];
+            zero = __all(s_zero[lane % W] != 0);
 #pragma unroll
             for (int m = 1; m < W; m <<= 1) {
                 lp_join(sum, LpSum{__shfl_xor(sum.m, m), __shfl_xor(sum.l, m), __shfl_xor(sum.s, m)});
@@ -542,7 +558,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
             }
             continue;
         }
-        const double margin = lp_margin<E>(scale, a.d, h2, w2);
+        const double margin = zero ? 0.0 : lp_margin<E>(scale, a.d, h2, w2);
         const double low = (double)lp_kth(high, a.top) - 2.0 * margin;
         int* const list = s_list[TOP ? team : 0];
         double* const score = s_z[TOP ? team : 0];
@@ -557,7 +573,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
             found = at + some;
             return at;
         };
-        lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, [&](bool hit, int g, float, lp_u32 second) {
+        lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, [&](float, int) { return found <= LIST; }, [&](bool hit, int g, float, lp_u32 second) {
             u64 many = __ballot(hit && !((double)lp_second(second) < low));
             const int row = (g >> a.per_shift << (a.per_shift + 5)) + lp_row(second);
             const u64 one = __ballot(hit && (double)lp_second(second) < low && row < (int)n_rows);
@@ -618,7 +634,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
         }
         LpBest best;
         best.begin(a.top);
-        lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, [&](bool hit, int g, float first, lp_u32 second) {
+        const auto look = [&](float max, int t) { return best.wants((double)max + margin, t << (a.per_shift + 5)); };
+        lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, look, [&](bool hit, int g, float first, lp_u32 second) {
             const int row0 = g >> a.per_shift << (a.per_shift + 5);
             u64 hits = __ballot(hit && best.wants(first + margin, row0));
             const u64 many = __ballot(!((double)lp_second(second) < low));
