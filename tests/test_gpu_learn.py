@@ -109,7 +109,7 @@ def test_log_probs(t, n, v, d, top):
         assert torch.equal(a, b)
     for a, b in zip(first, learn.log_probs(strided(hd, 8, 8), strided(wd, 5, 3), i, scale=scale, top=top)):
         assert torch.equal(a, b)
-    # nothing depends on what else is asked for
+    # of one kind of tiles nothing depends on what else is asked for
     logp, entropy, lse, rows, row_logp = learn.log_probs(hd, wd, scale=scale, top=top)
     assert logp is None and all(torch.equal(a, b) for a, b in zip((entropy, lse, rows, row_logp), first[1:]))
     none = learn.log_probs(hd, wd, i, scale=scale)
@@ -165,7 +165,7 @@ def test_log_probs_of_many_tiles(t, n, v, d, top):
 # ---- order of the best rows
 
 @pytest.mark.parametrize("t", TYPES)
-@pytest.mark.parametrize("n,v", [(1, 700), (9, 5000), (40, 5000), (100, 3000), (300, 2000), (300, 20_000), (3000, 4000)])
+@pytest.mark.parametrize("n,v", [(1, 700), (9, 5000), (40, 5000), (100, 3000), (300, 2000), (300, 20_000), (3000, 4000), (700, 20_000)])
 def test_equal_logits_go_to_the_lower_row(t, n, v):
     # small whole numbers: logits are exact, and most of them equal to others; some tokens' are all 0, the table's rows come several times
     g = gen(n + v)
@@ -187,7 +187,7 @@ def test_equal_logits_go_to_the_lower_row(t, n, v):
 
 
 @pytest.mark.parametrize("t", TYPES)
-@pytest.mark.parametrize("n,v,d", [(1, 3000, 64), (20, 5000, 256), (100, 3000, 96), (300, 3000, 512), (300, 30_000, 128)])
+@pytest.mark.parametrize("n,v,d", [(1, 3000, 64), (20, 5000, 256), (100, 3000, 96), (300, 3000, 512), (300, 30_000, 128), (450, 30_000, 96)])
 def test_order_below_the_roundings_of_the_logits(t, n, v, d):
     """Large terms that cancel leave logits which 32 bits have no place of: their order is that of the exact sums."""
     g = gen(d)
@@ -212,7 +212,7 @@ def test_order_below_the_roundings_of_the_logits(t, n, v, d):
 # ---- infinite and undefined logits
 
 @pytest.mark.parametrize("t", TYPES)
-@pytest.mark.parametrize("n,v", [(3, 40), (40, 3000), (100, 2100), (300, 2100), (300, 30_000)])
+@pytest.mark.parametrize("n,v", [(3, 40), (40, 3000), (100, 2100), (300, 2100), (300, 30_000), (450, 30_000)])
 def test_infinite_logits(t, n, v):
     w = torch.full((v, 8), 2.0 ** -10)
     w[v // 2, 3] = -2.0
@@ -259,7 +259,7 @@ def test_infinite_logits(t, n, v):
 
 
 @pytest.mark.parametrize("t", TYPES)
-@pytest.mark.parametrize("n,v", [(3, 40), (40, 3000), (100, 2100), (300, 2100), (300, 30_000), (2500, 2000)])
+@pytest.mark.parametrize("n,v", [(3, 40), (40, 3000), (100, 2100), (300, 2100), (300, 30_000), (2500, 2000), (450, 30_000)])
 def test_a_nan_stays_with_its_token(t, n, v):
     h, w, targets = inputs(t, n, v, 24, 5)
     want = learn.log_probs(h.to(DEV), w.to(DEV), targets.to(DEV), top=5)
@@ -277,6 +277,40 @@ def test_a_nan_stays_with_its_token(t, n, v):
     odd[v - 1, 7] = math.nan
     logp, entropy, lse, rows, row_logp = learn.log_probs(h.to(DEV), odd.to(DEV), targets.to(DEV), top=5)
     assert entropy.isnan().all() and lse.isnan().all() and (rows == -1).all() and row_logp.isnan().all()
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,v", [(3, 40), (40, 3000), (100, 2100), (300, 30_000), (450, 30_000)])
+def test_huge_logits(t, n, v):
+    """One column of h and w makes the logits, exact products of a size whose exponents leave fp32 by far: one row has the whole softmax, or logits are infinite."""
+    g = gen(n)
+    w = torch.zeros(v, 8)
+    w[:, 3] = torch.rand(v, generator=g) * 2.0 ** -10
+    w[v // 2, 3] = 1.5
+    w = w.to(t)
+    h = torch.zeros(n, 8)
+    h[:, 3] = 1.0
+    h[n // 2:, 3] = -1.0
+    targets = torch.randint(0, v, (n,), generator=g)
+    targets[1] = v // 2
+    for scale in (1e6, 3e9, 1e12, 1e30, 2e38, -1e30, 3e38):
+        z = (h[:, 3:4].double() @ w[:, 3:4].double().t()) * torch.tensor(scale).double()
+        logp, entropy, lse, rows, row_logp = [x.cpu() for x in learn.log_probs(h.to(t).to(DEV), w.to(DEV), targets.to(DEV), scale=scale, top=5)]
+        best, at = torch.sort(z, dim=1, descending=True, stable=True)
+        assert torch.equal(rows.long(), at[:, :5])
+        finite = z.amax(1) < 3.4e38
+        assert (lse[~finite] == math.inf).all() and entropy[~finite].isnan().all()
+        lse64 = torch.logsumexp(z, 1)
+        assert ((lse.double() - lse64).abs() <= 4 * U * lse64.abs() + 200 * U * math.log(v))[finite].all()
+        p = torch.softmax(z, 1)
+        h64 = -torch.where(p > 0, p * torch.log_softmax(z, 1), 0.0).sum(1)
+        # an exponent's difference is rounded at the size of the logits, and log p and p with it where others count at all
+        size = torch.where(h64 > 1e-30, z.abs().amax(1), 0.0)
+        assert ((entropy.double() - h64).abs() <= (2 * h64 + 1) * 8 * U * size + 300 * U * (1 + math.log(v)))[finite].all()
+        want = (z.gather(1, targets[:, None])[:, 0] - lse64).float().double()           # (what fp32 does not hold is infinite)
+        fine = finite & torch.isfinite(want)
+        assert ((logp.double() - want).abs() <= 8 * U * (lse64.abs() + want.abs()) + 200 * U * math.log(v))[fine].all()
+        assert (row_logp <= 0).logical_or(row_logp.isnan())[finite].all()
 
 
 @pytest.mark.parametrize("t", [F32, BF16])
