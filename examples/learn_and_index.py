@@ -2,10 +2,11 @@
 
 Synthetic sessions: items belong to topics, a session's next item is mostly one of the same topic.  A row is learnt for every item by
 predicting the next one: the item's row is looked up, normed and scored against all rows of the table by a softmax cross entropy, whose
-gradients go back through the norm and the lookup to the one table.  Then the normed rows are put on an 8-bit grid, a few of them are scored against all by the
+gradients go back through the norm and the lookup to the one table.  Some steps of tuning by rewards follow: answers are drawn from the best rows by their
+probabilities, and those of the item's topic are made likelier.  Then the normed rows are put on an 8-bit grid, a few of them are scored against all by the
 integer product, and the k-NN graph of the rows is built and pruned.
 
-    python examples/learn_and_index.py [--items 20000] [--dim 128] [--tokens 8192] [--steps 60]
+    python examples/learn_and_index.py [--items 20000] [--dim 128] [--tokens 8192] [--steps 60] [--tune 20]
 """
 import argparse
 import math
@@ -16,6 +17,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2508_08744_amd import embed, knn  # noqa: E402
+from paper_2508_08744_amd import learn as ops  # noqa: E402
 
 
 def sessions(gen, tokens, items, topics):
@@ -50,12 +52,50 @@ def learn(items, dim, tokens, steps, topics=50, rate=0.02, seed=0, device="cuda"
         item, target = sessions(gen, tokens, items, topics)
         loss, *grads = step(master[0].bfloat16(), master[1].bfloat16(), item, target, 1.0)
         losses.append(loss)
+        ops.clip_grads(grads, 1.0)
         for p, m, v, g in zip(master, first, second, grads):
             g = g.float()
             m.lerp_(g, 0.1)
             v.lerp_(g * g, 0.01)
             p.sub_(rate * (m / (1 - 0.9 ** i)) / ((v / (1 - 0.99 ** i)).sqrt() + 1e-8))
     return master[0].bfloat16(), master[1].bfloat16(), torch.stack(losses)
+
+
+def answers(table, weight, item, top=16):
+    """The best rows for each item, and their log probabilities."""
+    y, _, _ = embed.add_rms_norm(embed.lookup(table, item, scale=math.sqrt(table.shape[1])), weight)
+    return ops.log_probs(y, table, top=top)[3:]
+
+
+def tune_step(table, weight, item, answer, gain, bonus, max_norm=1.0):
+    """The gradients, under a norm of max_norm, of minus the sum of gain times an answer's log probability and bonus times the entropy; and their norm before."""
+    root = math.sqrt(table.shape[1])
+    x = embed.lookup(table, item, scale=root)
+    y, r, rstd = embed.add_rms_norm(x, weight)
+    _, entropy, lse, _, _ = ops.log_probs(y, table, answer)
+    dy, dtable = ops.log_probs_grad(y, table, answer, lse, -gain, entropy, -bonus)
+    dx, dweight = embed.add_rms_norm_grad(dy, r, weight, rstd)
+    embed.lookup_grad(dx, item, table.shape[0], scale=root, out=dtable)
+    norm = ops.clip_grads([dtable, dweight], max_norm)
+    return dtable, dweight, norm
+
+
+def tune(table, weight, topics, tokens, steps, rate=0.5, seed=1):
+    """The tuned table and weight, and every step's share of answers of the item's topic (plain steps on fp32 copies)."""
+    gen = torch.Generator(device=table.device).manual_seed(seed)
+    table, weight, shares = table.float(), weight.float(), []
+    for _ in range(steps):
+        item = torch.randint(0, table.shape[0], (tokens,), generator=gen, device=table.device)
+        rows, logp = answers(table.bfloat16(), weight.bfloat16(), item)
+        drawn = torch.multinomial(logp.exp(), 1, generator=gen)
+        answer = rows.gather(1, drawn)[:, 0].long()
+        reward = ((answer % topics == item % topics) & (answer != item)).float()
+        shares.append(reward.mean())
+        gain = (reward - reward.mean()) / tokens
+        dtable, dweight, _ = tune_step(table.bfloat16(), weight.bfloat16(), item, answer, gain, torch.full_like(gain, 0.01 / tokens))
+        table.sub_(rate * dtable.float())
+        weight.sub_(rate * dweight.float())
+    return table.bfloat16(), weight.bfloat16(), torch.stack(shares) if shares else None
 
 
 def serve(table, weight, queries, k=32):
@@ -69,12 +109,15 @@ def serve(table, weight, queries, k=32):
 
 def main():
     a = argparse.ArgumentParser(description=__doc__.split("\n")[0])
-    for name, value in (("items", 20_000), ("dim", 128), ("tokens", 8192), ("steps", 60)):
+    for name, value in (("items", 20_000), ("dim", 128), ("tokens", 8192), ("steps", 60), ("tune", 20)):
         a.add_argument("--" + name, type=int, default=value)
     a = a.parse_args()
     topics = 50
     table, weight, losses = learn(a.items, a.dim, a.tokens, a.steps, topics)
     print("loss %.3f -> %.3f (the topics alone: %.3f)" % (losses[0], losses[-1], math.log(a.items / topics)))
+    table, weight, shares = tune(table, weight, topics, a.tokens, a.tune)
+    if shares is not None:
+        print("answers of the item's topic: %.3f -> %.3f" % (shares[0], shares[-1]))
     queries = torch.arange(0, a.items, max(1, a.items // 200), device=table.device)
     scores, ids, graph = serve(table, weight, queries)
     best = scores.scatter(1, queries[:, None], -math.inf).topk(10, dim=1).indices
