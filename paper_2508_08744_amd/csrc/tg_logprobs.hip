@@ -701,11 +701,15 @@ static LpShape lp_shape(int64_t n, int64_t n_rows, int e, int top)
     most = most >= 256 ? most / 256 * 256 : most >= 64 ? 64 : 32;
     s.tokens = n < most ? n : most;
     const auto tiles = [&](int64_t x, int64_t y) { return ((n_rows + x - 1) / x) * ((s.tokens + y - 1) / y); };
+    // A CU holds one tile of 256 x 256, or two of 128 x 128, which take 1.28 times as long for as many logits: the smaller ones where the larger leave more of their last round, or of
+    // their last tokens, unused (bf16: 300 tokens, 40 000 rows of 512: 38.0 us in the larger, 30.2 in the smaller; 8192, 3000 of 1000, 3 best: 154 and 143; 2003, 50 257 of 500: 158 and 176).
+    const auto rounds = [](int64_t count, int64_t at_once) { return (count + at_once - 1) / at_once; };
+    const bool larger = (double)rounds(tiles(256, 256), 256) * 256 * 65536 <= 1.28 * (double)rounds(tiles(128, 128), 512) * 512 * 16384;
     s.few = tiles(128, 128) <= 128;
     if (s.tokens <= 32) s.bm = 128, s.bn = 32, s.shared = 4;
     else if (s.few || (e == 4 && s.tokens > 64)) s.bm = 64, s.bn = 64, s.shared = 4;
     else if (s.tokens <= 64) s.bm = 128, s.bn = 64, s.shared = 4;
-    else if ((!top || s.tokens > 384) && tiles(256, 256) >= 200) s.bm = 256, s.bn = 256, s.shared = 1;
+    else if ((!top || s.tokens > 384) && tiles(256, 256) >= 200 && larger) s.bm = 256, s.bn = 256, s.shared = 1;
     else s.bm = 128, s.bn = 128, s.shared = 2;
     s.tiles = (n_rows + s.bm - 1) / s.bm;
     return s;
