@@ -14,7 +14,7 @@
 
 #define LP_GROUP 32             // logits of a token that leave their largest
 #define LP_MAX_TOP 32           // best rows; half the lanes of a wave, see lp_kth
-#define LP_NORM_ROWS 64         // of the table, where the tiles leave no norms
+#define LP_NORM_ROWS 256        // of the table, where the tiles leave no norms
 #define LP_BELOW (-1000.0f)     // exponents below have a power of 0: so is their part in s, at -infinity too
 
 typedef unsigned int lp_u32;
@@ -230,11 +230,11 @@ __global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileR
 
 // The largest sum of the squares of LP_NORM_ROWS rows at a time.  `lanes` lanes a row; four rows are asked for at once.
 template <class E>
-__global__ __launch_bounds__(256) void lp_norms_kernel(const E* __restrict__ w, int64_t ld, int64_t n_rows, int d, int lanes, float* __restrict__ out, int64_t count)
+__global__ __launch_bounds__(1024) void lp_norms_kernel(const E* __restrict__ w, int64_t ld, int64_t n_rows, int d, int lanes, float* __restrict__ out, int64_t count)
 {
-    __shared__ float s_top[4];
+    __shared__ float s_top[16];
     typedef TgPiece<E> P;
-    const int of = threadIdx.x & (lanes - 1), rows = 256 / lanes, first = threadIdx.x / lanes;
+    const int of = threadIdx.x & (lanes - 1), rows = 1024 / lanes, first = threadIdx.x / lanes;
     for (int64_t b = blockIdx.x; b < count; b += gridDim.x) {
         float top = 0.0f;
         for (int r = first; r < LP_NORM_ROWS; r += 4 * rows) {
@@ -260,7 +260,10 @@ __global__ __launch_bounds__(256) void lp_norms_kernel(const E* __restrict__ w, 
         for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
         if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
         __syncthreads();
-        if (threadIdx.x == 0) out[b] = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+        top = s_top[threadIdx.x & 15];
+#pragma unroll
+        for (int m = 1; m < 16; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+        if (threadIdx.x == 0) out[b] = top;
         __syncthreads();
     }
 }
@@ -491,7 +494,13 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
                 }
             }
             zero = __all(zero);
-            for (int p = of + 64 * W; p < a.n_norms; p += 64 * W) w2 = fmaxf(w2, a.norms[p]);
+            for (int p0 = of + 64 * W; p0 < a.n_norms; p0 += 8 * 64 * W) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = a.norms[p0 + i * 64 * W < a.n_norms ? p0 + i * 64 * W : 0];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w2 = fmaxf(w2, v[i]);
+            }
             // (the tiles' maxima are as good, where there are so many that few tiles have two of the best)
             if (count >= 4 * a.top) high = sum.m;
             else
@@ -822,7 +831,7 @@ void tg_launch_log_probs(const void* h, int64_t ld_h, const void* w, int64_t ld_
             if (top && shape.bm == 256) {
                 int lanes = 1;
                 while (lanes < 64 && lanes * TgPiece<E>::E < d) lanes *= 2;
-                hipLaunchKernelGGL(lp_norms_kernel<E>, dim3((unsigned)(r.n_norms < 65536 ? r.n_norms : 65536)), dim3(256), 0, s, (const E*)w, ld_w, n_rows, d,
+                hipLaunchKernelGGL(lp_norms_kernel<E>, dim3((unsigned)(r.n_norms < 65536 ? r.n_norms : 65536)), dim3(1024), 0, s, (const E*)w, ld_w, n_rows, d,
                                    lanes, r.norms, r.n_norms);
             }
         }
