@@ -220,17 +220,19 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
     T t;
     t.start(X, Y, x0, y0, 0, bytes, lds);
     if (threadIdx.x < BN) {
-        const int64_t y = y0 + threadIdx.x, target = y < Y.rows ? tg_row_of(tokens.targets, tokens.targets64, y, n_rows) : -1, hit = target - v0 - x0;
+        // (all of it is asked for at once: one way to memory, not four)
+        const int64_t y = y0 + threadIdx.x, at = y < Y.rows ? y : 0;
+        const float lse = tokens.lse[at], dloss = tokens.dloss[at], dentropy = ENTROPY ? tokens.dentropy[at] : 0.0f, entropy = ENTROPY ? tokens.entropy[at] : 0.0f;
+        const int64_t target = y < Y.rows ? tg_row_of(tokens.targets, tokens.targets64, at, n_rows) : -1, hit = target - v0 - x0;
         Token k{target >= 0 && hit >= 0 && hit < BM ? (int)hit : -1, 0, 0.0f, 0.0f};
         More more{0.0f, 0.0f};
-        if (y < Y.rows && xent_has_part(target, ENTROPY ? tokens.dentropy : nullptr, y)) {
-            if (target >= 0) k.g = more.less = tokens.dloss[y] * tokens.gain * scale * up;
-            if (ENTROPY && tokens.dentropy[y] != 0.0f) {
-                const float dh = tokens.dentropy[y] * scale * up;
-                k.g = fmaf(-dh, tokens.entropy[y], k.g);
+        if (y < Y.rows && (target >= 0 || dentropy != 0.0f)) {
+            if (target >= 0) k.g = more.less = dloss * tokens.gain * scale * up;
+            if (ENTROPY && dentropy != 0.0f) {
+                const float dh = dentropy * scale * up;
+                k.g = fmaf(-dh, entropy, k.g);
                 more.h = dh * -0.6931471805599453f;
             }
-            const float lse = tokens.lse[y];
             const bool near = xent_near(lse, scale * XENT_LOG2E);
             k.there = near ? 1 : 2;
             k.b = near ? lse * XENT_LOG2E : lse;
@@ -564,7 +566,7 @@ template <class E>
 __global__ __launch_bounds__(256) void xent_dh_kernel(XentProducts a, int pieces)
 {
     const int64_t n = a.p.rows, all = n * pieces;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < all; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t y = i / pieces;
         const int at = (int)(i - y * pieces) * 4;
         TgPiece<float> sum;
@@ -835,8 +837,9 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
         else if (g.side == 128) products(xent_products_kernel<E, 128, 2, 2, 2>, 256);
     }
     if (g.direct) return;
-    const int64_t out_wgs = (n * ((d + 3) / 4) + 255) / 256;
-    hipLaunchKernelGGL(xent_dh_kernel<E>, dim3((unsigned)(out_wgs < 16384 ? out_wgs : 16384)), dim3(256), 0, s, a, (d + 3) / 4);
+    // (few outputs: a wave a workgroup, so that more CUs ask for their parts)
+    const int64_t outs = n * ((d + 3) / 4), threads = outs < 64 * 1024 ? 64 : 256, out_wgs = (outs + threads - 1) / threads;
+    hipLaunchKernelGGL(xent_dh_kernel<E>, dim3((unsigned)(out_wgs < 16384 ? out_wgs : 16384)), dim3((unsigned)threads), 0, s, a, (d + 3) / 4);
 }
 
 void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const XentTokens& t,
