@@ -462,7 +462,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
         // what the margin is made of, its first pieces asked for in front of everything
         double h2 = 0.0;
         float w2 = 0.0f;
-        bool zero = true;                        // a row of zeros (padding): its logits are exact, and all equal
+        bool zero = true;                        // a row of zeros (padding): its logits are exact, and all equal (as with a factor of 0)
         typedef TgPiece<E> P;
         typename P::vec h_first;
         if (TOP) {
@@ -567,7 +567,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
             }
             continue;
         }
-        const double margin = zero ? 0.0 : lp_margin<E>(scale, a.d, h2, w2);
+        const double margin = zero || scale == 0.0f ? 0.0 : lp_margin<E>(scale, a.d, h2, w2);
         const double low = (double)lp_kth(high, a.top) - 2.0 * margin;
         int* const list = s_list[TOP ? team : 0];
         double* const score = s_z[TOP ? team : 0];

@@ -209,6 +209,20 @@ def test_order_below_the_roundings_of_the_logits(t, n, v, d):
     assert torch.equal(rows.cpu().long(), at[:, :10])
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,v", [(1, 3000), (50, 3000), (100, 3000), (450, 30_000)])
+def test_order_of_rows_of_the_smallest_numbers(t, n, v):
+    """Values below the type's normal ones: whatever the tiles make of them, the best rows are those of the exact sums."""
+    g = gen(n)
+    tiny = torch.finfo(t).tiny
+    w = (torch.randint(-100, 101, (v, 24), generator=g).double() * tiny / 128).to(t)
+    h = torch.randn(n, 24, generator=g).to(t)
+    scale = float(torch.tensor(0.03 / tiny).float()) if t == F16 else 2.0 ** 124
+    z = (h.double() @ w.double().t()) * scale
+    _, _, _, rows, _ = learn.log_probs(h.to(DEV), w.to(DEV), scale=scale, top=12)
+    assert torch.equal(rows.cpu().long(), torch.sort(z, dim=1, descending=True, stable=True)[1][:, :12])
+
+
 # ---- infinite and undefined logits
 
 @pytest.mark.parametrize("t", TYPES)
