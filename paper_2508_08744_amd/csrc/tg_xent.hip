@@ -11,6 +11,9 @@
 // products, 1.26 PFLOP/s.)  P in 16 bits is a choice for its bytes.  Its roundings are half a step of the type each; the one at a token's target,
 // the entry that outweighs the others together, is given back to both gradients.  Of the other entries' roundings as much remains in a sum as the sum keeps of the
 // entries themselves: a relative error like that of rounding the result, which comes on top.
+//
+// The gradient of log probabilities and entropy (include/tagore_learn.h) is the same with another P; without dw, where the table stays as it is, dh's parts alone fill the card.
+// (4096 tokens, 131 072 rows of 1024 bf16: 4 pieces of 280 us for P and 416 for both products.)
 #include "tg_embed.h"
 #include "tg_softmax.h"
 #include "tg_tiles.h"
