@@ -334,19 +334,20 @@ struct XentProducts {
     float* sums;
     void *dh, *dw;
 };
-// four neighbours of row y of dh, with what rounding took from P at the target
-template <class E>
+// four neighbours (or one) of row y of dh, with what rounding took from P at the target
+template <class E, int W = 4>
 __device__ inline void xent_put_dh(const XentProducts& a, int64_t y, int x, float* v)
 {
     const int64_t target = tg_row_of(a.targets, a.targets64, y, a.n_rows);
     const float l = sizeof(E) == 2 && target >= 0 ? a.lost[y] : 0.0f;
     const E* row = (const E*)a.table + (target < 0 ? 0 : target) * a.ld_table + x;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < W; ++e) {
         if (sizeof(E) == 2 && x + e < a.d) v[e] = fmaf(l, (float)row[e], v[e]);
         v[e] = xent_has_part(target, a.dentropy, y) ? v[e] * a.c[1] : 0.0f;
     }
-    tile_put((E*)a.dh + y * a.d + x, v, a.d - x);
+    if (W == 1) ((E*)a.dh)[y * a.d + x] = (E)v[0];
+    else tile_put((E*)a.dh + y * a.d + x, v, a.d - x);
 }
 // What rounding took from P at the targets among a tile's rows, given back to dw's tile of 16-bit values: a row that is the target of few tokens is mostly
 // theirs, and their roundings are whole in it, whatever the number of tokens.  The tokens are looked through for targets among the rows; those found are
@@ -564,24 +565,35 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_products_kernel(XentProduct
         }
     }
 }
-// dh out of its parts
-template <class E>
+// dh out of its parts: four neighbours a lane, WHOLE where rows are whole fours; or one (W = 1) where there are few outputs and rows are not: a question for what is left of a
+// row would stand between the loads (301 tokens of 50 fp32 values, 64 parts: 11.5 us with it, 6.2; 2000 of 701, 2 us more in ones).
+template <class E, int W, bool WHOLE>
 __global__ __launch_bounds__(256) void xent_dh_kernel(XentProducts a, int pieces)
 {
-    const int64_t n = a.p.rows, all = n * pieces;
+    typedef float vec __attribute__((ext_vector_type(W)));
+    const int64_t n = a.p.rows, all = n * pieces, each = n * a.d;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < all; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t y = i / pieces;
-        const int at = (int)(i - y * pieces) * 4;
+        const int at = (int)(i - y * pieces) * W;
+        const float* p = a.sums + y * a.d + at;
         TgPiece<float> sum;
-        sum.load(a.sums + y * a.d + at, a.d - at);
+        if constexpr (WHOLE) {
+            vec x = *reinterpret_cast<const vec*>(p);
 #pragma unroll 8
-        for (int s = 1; s < a.splits; ++s) {
-            TgPiece<float> q;
-            q.load(a.sums + (s * n + y) * a.d + at, a.d - at);
+            for (int s = 1; s < a.splits; ++s) x += *reinterpret_cast<const vec*>(p + s * each);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum.v[e] += q.v[e];
+            for (int e = 0; e < W; ++e) sum.v[e] = x[e];
+        } else {
+            sum.load(p, a.d - at);
+#pragma unroll 8
+            for (int s = 1; s < a.splits; ++s) {
+                TgPiece<float> q;
+                q.load(p + s * each, a.d - at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum.v[e] += q.v[e];
+            }
         }
-        xent_put_dh<E>(a, y, at, sum.v);
+        xent_put_dh<E, W>(a, y, at, sum.v);
     }
 }
 
@@ -841,8 +853,12 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
     }
     if (g.direct) return;
     // (few outputs: a wave a workgroup, so that more CUs ask for their parts)
-    const int64_t outs = n * ((d + 3) / 4), threads = outs < 64 * 1024 ? 64 : 256, out_wgs = (outs + threads - 1) / threads;
-    hipLaunchKernelGGL(xent_dh_kernel<E>, dim3((unsigned)(out_wgs < 16384 ? out_wgs : 16384)), dim3((unsigned)threads), 0, s, a, (d + 3) / 4);
+    const int by = d % 4 == 0 || n * d >= 256 * 1024 ? 4 : 1;
+    const int64_t outs = n * ((d + by - 1) / by), threads = outs < 64 * 1024 ? 64 : 256, out_wgs = (outs + threads - 1) / threads;
+    const dim3 out_grid((unsigned)(out_wgs < 16384 ? out_wgs : 16384)), out_block((unsigned)threads);
+    if (d % 4 == 0) hipLaunchKernelGGL((xent_dh_kernel<E, 4, true>), out_grid, out_block, 0, s, a, d / 4);
+    else if (by == 1) hipLaunchKernelGGL((xent_dh_kernel<E, 1, true>), out_grid, out_block, 0, s, a, d);
+    else hipLaunchKernelGGL((xent_dh_kernel<E, 4, false>), out_grid, out_block, 0, s, a, (d + 3) / 4);
 }
 
 void tg_launch_xent_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int dtype, int64_t n, int64_t n_rows, int d, const XentTokens& t,
