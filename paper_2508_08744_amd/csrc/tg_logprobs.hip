@@ -5,15 +5,15 @@
 // matrix instructions bound it, or, for few tokens, the bytes of the table.  (131 072 rows of 1024 bf16: 4096 tokens 902 us, 1.22 PFLOP/s, with 8 best rows 1054, 44 for the
 // norms and 54 for the join; one token 40 us, 6.7 TB/s, and 12 for the join.)
 //
-// The best rows are those of the largest logits in 64 bits, and the logits of the tiles are in 32.  So the tiles leave, of every 32 logits of a token (LP_GROUP), the
-// largest with its row and an upper bound of the second: a quarter of a byte a logit.  With 64 lanes over a token's groups, the k-th largest of the lanes' largest is below the k-th
+// The best rows are those of the largest logits in 64 bits, and the logits of the tiles are in 32.  So every lane of a tile leaves, of its 8, 16 or 32
+// logits of a token (a group), the largest with its row and an upper bound of the second: at most a byte a logit.  With 64 lanes over a token's groups, the k-th largest of the lanes' largest is below the k-th
 // logit; whatever is further below it than the roundings of 32 bits reach (a bound from the norms of the token's row and of the table's, see lp_margin) is none of
 // the k best.  What is left, some k rows, is scored again in 64 bits and put in order.  A group whose second is not out of reach is scored as a whole.
 #include "tg_embed.h"
 #include "tg_softmax.h"
 #include "tg_tiles.h"
 
-#define LP_GROUP 32             // logits of a token that leave their largest
+#define LP_GROUP_LEAST 8        // logits of a token that leave their largest, in the smallest tiles
 #define LP_MAX_TOP 32           // best rows; half the lanes of a wave, see lp_kth
 #define LP_NORM_ROWS 256        // of the table, where the tiles leave no norms
 #define LP_BELOW (-1000.0f)     // exponents below have a power of 0: so is their part in s, at -infinity too
@@ -58,8 +58,8 @@ __global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileR
     // (the norms' squares ride along where registers are left for their sums: tiles of up to 128 rows)
     constexpr bool SQUARES = TOP && BM <= 128;
     typedef Tile<E, BM, BN, WM, WN, false, false, NB, SQUARES> T;
-    constexpr int Q = 8 / T::FM, GROUPS = BM / LP_GROUP;       // quarters of a wave (16 lanes each) that share a group; groups of a tile
-    static_assert(!TOP || (Q >= 1 && Q * T::FM == 8), "groups of 32 rows");
+    constexpr int GROUPS = 4 * WM;                 // of a tile: one for each quarter of a wave (16 lanes), which has 4 FM of its rows
+    static_assert(4 * T::FM <= 32, "five bits for a place");
     __shared__ __align__(1024) char lds[T::LDS];
     // the tokens' targets among the tile's rows: asked for before the products, so that nothing waits for them behind
     __shared__ int s_target[BN];
@@ -165,19 +165,9 @@ __global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileR
             }
             const int i = at >> 2;
             // (x_of for an i that is not known in advance)
-            int x = (i / T::HM) * (BM / 2) + none + (i % T::HM) * 16 + (threadIdx.x >> 4 & 3) * 4 + (at & 3);
-            float top = m, most = lp_times_up(second, scale);
-#pragma unroll
-            for (int q = 1; q < Q; q <<= 1) {
-                const float top2 = __shfl_xor(top, q * 16), most2 = __shfl_xor(most, q * 16);
-                const int x2 = __shfl_xor(x, q * 16);
-                x = top2 > top ? x2 : x;
-                most = fmaxf(fminf(top, top2), fmaxf(most, most2));
-                top = fmaxf(top, top2);
-            }
-            const int quarter = threadIdx.x >> 4 & 3;
-            if (quarter % Q == 0 && y < Y.rows)
-                groups[(y * parts_pitch + tx) * GROUPS + (threadIdx.x >> 6) / WN * (4 / Q) + quarter / Q] = make_uint2(__float_as_uint(top), lp_pack(most, x));
+            const int quarter = threadIdx.x >> 4 & 3, x = (i / T::HM) * (BM / 2) + none + (i % T::HM) * 16 + quarter * 4 + (at & 3);
+            if (y < Y.rows)
+                groups[(y * parts_pitch + tx) * GROUPS + (threadIdx.x >> 6) / WN * 4 + quarter] = make_uint2(__float_as_uint(m), lp_pack(lp_times_up(second, scale), x));
         }
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
@@ -345,12 +335,12 @@ struct LpBest {
 struct LpTop {
     const void *h, *w;           // the caller's
     int64_t ld_h, ld_w;
-    int d, per_shift, shared_shift;     // the groups of a tile, and the quarters of a wave that share one: log2
+    int d, tile_shift, per_shift, half_shift;     // log2 of a tile's rows, of its groups, and of the blocks of 16 rows that a wave has in half of a tile
     int top;
     const float* norms;
     int n_norms;
     const uint2* groups;
-    int n_groups;                // below 2^26
+    int n_groups;                // below 2^28
     int32_t* rows;
     float* row_logp;
 };
@@ -410,29 +400,30 @@ __device__ inline void lp_reach(const float4* __restrict__ parts, int tiles, con
             for (int j = 1; j < LP_AHEAD; ++j) max = i == j ? v[j] : max;
             const bool in = hits && look(max, t);
             if (!__any(in)) continue;
-            uint2 q[8];
+            for (int g0 = t << per_shift, end = 0; end < 1 << per_shift; g0 += 8, end += 8) {        // (8 or 16 a tile)
+                uint2 q[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] = in && j < 1 << per_shift ? groups[(t << per_shift) + j] : make_uint2(0u, 0u);
-            unsigned deep = 0;
+                for (int j = 0; j < 8; ++j) q[j] = in ? groups[g0 + j] : make_uint2(0u, 0u);
+                unsigned deep = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) deep |= in && j < 1 << per_shift && !((double)__uint_as_float(q[j].x) < low) ? 1u << j : 0u;
-            for (; __any(deep != 0); deep &= deep - 1) {
-                const int at = deep ? __builtin_ctz(deep) : 0;
-                uint2 x = q[0];
+                for (int j = 0; j < 8; ++j) deep |= in && !((double)__uint_as_float(q[j].x) < low) ? 1u << j : 0u;
+                for (; __any(deep != 0); deep &= deep - 1) {
+                    const int at = deep ? __builtin_ctz(deep) : 0;
+                    uint2 x = q[0];
 #pragma unroll
-                for (int j = 1; j < 8; ++j) x = at == j ? q[j] : x;
-                take(deep != 0, (t << per_shift) + at, __uint_as_float(x.x), x.y);
+                    for (int j = 1; j < 8; ++j) x = at == j ? q[j] : x;
+                    take(deep != 0, g0 + at, __uint_as_float(x.x), x.y);
+                }
             }
         }
     }
 }
-// row number `lane` of group g: of value e, quarter q and block i of the wave's rows, as lp_part_kernel has them (below LP_GROUP)
+// a group's rows, and its row number `lane` below that: value lane % 4 of the lane's block lane / 4, as lp_part_kernel has them
+__device__ inline int lp_group_rows(const LpTop& a) { return 8 << a.half_shift; }
 __device__ inline int lp_group_row(const LpTop& a, int g, int lane)
 {
-    const int tile = g >> a.per_shift, in = g & ((1 << a.per_shift) - 1), sh = a.shared_shift, waves_shift = 2 - sh;
-    const int e = lane & 3, q = ((lane >> 2) & ((1 << sh) - 1)) + ((in & ((1 << waves_shift) - 1)) << sh), i = lane >> (2 + sh);
-    const int half = 1 << waves_shift;             // blocks of the wave in half of the tile's rows
-    return (tile << (a.per_shift + 5)) + ((i >> waves_shift) << (a.per_shift + 4)) + (in >> waves_shift) * (half * 16) + (i & (half - 1)) * 16 + q * 4 + e;
+    const int tile = g >> a.per_shift, in = g & ((1 << a.per_shift) - 1), i = lane >> 2;
+    return (tile << a.tile_shift) + ((i >> a.half_shift) << (a.tile_shift - 1)) + ((in >> 2) << (a.half_shift + 4)) + (i & ((1 << a.half_shift) - 1)) * 16 + (in & 3) * 4 + (lane & 3);
 }
 
 // The tiles' sums joined, and the best rows, by W waves a token: eight where there are few tokens (one token, 1024 tiles: 12 us, of which ways to memory, one behind the other, are most), one where
@@ -448,7 +439,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
                                                                        float* __restrict__ lse)
 {
     constexpr int TOKENS = W == 1 ? 4 : 1;
-    constexpr int LIST = W == 1 ? 128 : 256;
+    constexpr int LIST = W == 1 ? 512 : 1024;
     __shared__ float s_m[W], s_l[W], s_s[W], s_w2[W];
     __shared__ double s_h2[W];
     __shared__ float s_top[W > 1 ? W : 1][W > 1 ? 64 : 1];
@@ -587,7 +578,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
         };
         lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, [&](float, int) { return found <= LIST; }, [&](bool hit, int g, float, lp_u32 second) {
             u64 many = __ballot(hit && !((double)lp_second(second) < low));
-            const int row = (g >> a.per_shift << (a.per_shift + 5)) + lp_row(second);
+            const int row = (g >> a.per_shift << a.tile_shift) + lp_row(second);
             const u64 one = __ballot(hit && (double)lp_second(second) < low && row < (int)n_rows);
             if (one) {
                 const int at = room(__popcll(one)) + __popcll(one & tg_lanemask_lt());
@@ -595,7 +586,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
             }
             for (; many && found <= LIST; many &= many - 1) {
                 const int r = lp_group_row(a, __builtin_amdgcn_readlane(g, __builtin_ctzll(many)), lane);
-                const u64 some = __ballot(lane < LP_GROUP && r < (int)n_rows);
+                const u64 some = __ballot(lane < lp_group_rows(a) && r < (int)n_rows);
                 const int at = room(__popcll(some)) + __popcll(some & tg_lanemask_lt());
                 if ((some >> lane & 1) && at < LIST) list[at] = r;
             }
@@ -621,7 +612,30 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
             else some(Eight{});
             if (W > 1) __syncthreads();
             else __builtin_amdgcn_wave_barrier();
-            for (int c = of; c < found || c < a.top; c += 64 * W) {
+            if (mine != 0) continue;
+            if (found > 64) {
+                // those that the k-th of the lanes' largest does not rule out, to the front (32 bits of them: a step down)
+                float largest = -__builtin_inff();
+                for (int c = lane; c < found; c += 64) largest = fmaxf(largest, (float)score[c]);
+                const float kth = lp_kth(largest, a.top);
+                const double least = (double)kth - fabs((double)kth) * 0x1p-22 - 0x1p-140;
+                int kept = 0;
+                for (int c0 = 0; c0 < found; c0 += 64) {
+                    const int c = c0 + lane < found ? c0 + lane : 0;
+                    const double z = score[c];
+                    const int row = list[c];
+                    const u64 in = __ballot(c0 + lane < found && !(z < least));
+                    __builtin_amdgcn_wave_barrier();
+                    if (in >> lane & 1) {
+                        score[kept + __popcll(in & tg_lanemask_lt())] = z;
+                        list[kept + __popcll(in & tg_lanemask_lt())] = row;
+                    }
+                    __builtin_amdgcn_wave_barrier();
+                    kept += __popcll(in);
+                }
+                found = kept;
+            }
+            for (int c = lane; c < found || c < a.top; c += 64) {
                 if (c >= found) {
                     put(c, 0.0, LpBest::NONE);
                     continue;
@@ -646,9 +660,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
         }
         LpBest best;
         best.begin(a.top);
-        const auto look = [&](float max, int t) { return best.wants((double)max + margin, t << (a.per_shift + 5)); };
+        const auto look = [&](float max, int t) { return best.wants((double)max + margin, t << a.tile_shift); };
         lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, look, [&](bool hit, int g, float first, lp_u32 second) {
-            const int row0 = g >> a.per_shift << (a.per_shift + 5);
+            const int row0 = g >> a.per_shift << a.tile_shift;
             u64 hits = __ballot(hit && best.wants(first + margin, row0));
             const u64 many = __ballot(!((double)lp_second(second) < low));
             for (; hits; hits &= hits - 1) {
@@ -656,7 +670,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
                 const double most = lp_lane64(first + margin, from);
                 const bool all_rows = many >> from & 1;
                 const int r = all_rows ? lp_group_row(a, __builtin_amdgcn_readlane(g, from), lane) : __builtin_amdgcn_readlane(row0 + lp_row(second), from);
-                u64 some = __ballot(lane < (all_rows ? LP_GROUP : 1) && r < (int)n_rows && best.wants(most, r));
+                u64 some = __ballot(lane < (all_rows ? lp_group_rows(a) : 1) && r < (int)n_rows && best.wants(most, r));
                 while (some) {
                     int rows[8], have = 0;
 #pragma unroll
@@ -696,20 +710,20 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
 
 // ---- workspaces and launches
 struct LpShape {
-    int bm, bn, shared;          // the tile; see LpTop
+    int bm, bn, groups;          // the tile, and its groups
     bool few;                    // four stages in flight
     int64_t tiles;               // along the table
     int64_t tokens;              // at a time
 };
 // tokens at a time: as many as the groups' stretches have room for, in whole tiles
-#define LP_GROUP_BYTES (512ll << 20)
+#define LP_GROUP_BYTES (1ll << 30)
 
 static LpShape lp_shape(int64_t n, int64_t n_rows, int e, int top)
 {
     LpShape s;
     // The tiles of the cross entropy's logits; but where the best rows are asked for those of 128 rows, which have the norms' squares beside their products, up to 384 tokens
     // (131 072 rows of 1024 bf16, 8 best: 100 tokens 122 us in tiles of 256 rows behind a pass for the norms, 77 in these; 300: 202 and 178; 512: the other way round).
-    int64_t most = LP_GROUP_BYTES / (int64_t)sizeof(uint2) / ((n_rows + LP_GROUP - 1) / LP_GROUP);
+    int64_t most = LP_GROUP_BYTES / (int64_t)sizeof(uint2) / ((n_rows + LP_GROUP_LEAST - 1) / LP_GROUP_LEAST);
     most = most >= 256 ? most / 256 * 256 : most >= 64 ? 64 : 32;
     s.tokens = n < most ? n : most;
     const auto tiles = [&](int64_t x, int64_t y) { return ((n_rows + x - 1) / x) * ((s.tokens + y - 1) / y); };
@@ -718,11 +732,11 @@ static LpShape lp_shape(int64_t n, int64_t n_rows, int e, int top)
     const auto rounds = [](int64_t count, int64_t at_once) { return (count + at_once - 1) / at_once; };
     const bool larger = (double)rounds(tiles(256, 256), 256) * 256 * 65536 <= 1.28 * (double)rounds(tiles(128, 128), 512) * 512 * 16384;
     s.few = tiles(128, 128) <= 128;
-    if (s.tokens <= 32) s.bm = 128, s.bn = 32, s.shared = 4;
-    else if (s.few || (e == 4 && s.tokens > 64)) s.bm = 64, s.bn = 64, s.shared = 4;
-    else if (s.tokens <= 64) s.bm = 128, s.bn = 64, s.shared = 4;
-    else if ((!top || s.tokens > 384) && tiles(256, 256) >= 200 && larger) s.bm = 256, s.bn = 256, s.shared = 1;
-    else s.bm = 128, s.bn = 128, s.shared = 2;
+    if (s.tokens <= 32) s.bm = 128, s.bn = 32, s.groups = 16;
+    else if (s.few || (e == 4 && s.tokens > 64)) s.bm = 64, s.bn = 64, s.groups = 8;
+    else if (s.tokens <= 64) s.bm = 128, s.bn = 64, s.groups = 16;
+    else if ((!top || (s.tokens > 384 && n_rows >= 256 * (int64_t)top)) && tiles(256, 256) >= 200 && larger) s.bm = 256, s.bn = 256, s.groups = 8;
+    else s.bm = 128, s.bn = 128, s.groups = 8;
     s.tiles = (n_rows + s.bm - 1) / s.bm;
     return s;
 }
@@ -746,7 +760,7 @@ static size_t carve_lp(LpSpace* r, TgCarve* c, const LpShape& s, const void* h, 
     r->at_target = c->take<float>(s.tokens);
     r->n_norms = s.bm == 256 ? (n_rows + LP_NORM_ROWS - 1) / LP_NORM_ROWS : s.tiles;
     r->norms = c->take<float>(top ? r->n_norms : 0);
-    r->groups = c->take<uint2>(top ? (size_t)s.tiles * (s.bm / LP_GROUP) * s.tokens : 0);
+    r->groups = c->take<uint2>(top ? (size_t)s.tiles * s.groups * s.tokens : 0);
     return c->used;
 }
 size_t tg_log_probs_space(int64_t n, int64_t n_rows, int d, int dtype, int top, int aligned)
@@ -783,7 +797,7 @@ static void launch_parts(const LpShape& shape, const LpSpace& r, const TileRows&
             hipLaunchKernelGGL((lp_part_kernel<E, BM, BN, WM, WN, NB, TOP>), dim3((unsigned)(tiles * ny)), dim3(64 * WM * WN), 0, call.s, table, part, (int)X.width,
                                call.targets ? (const char*)call.targets + y0 * (call.targets64 ? 8 : 4) : nullptr, call.targets64, call.scale, v0, X.rows,
                                (uint32_t)tiles, ny, 8u, r.parts + y0 * shape.tiles + t0, shape.tiles,
-                               TOP ? r.groups + (y0 * shape.tiles + t0) * (BM / LP_GROUP) : nullptr,
+                               TOP ? r.groups + (y0 * shape.tiles + t0) * shape.groups : nullptr,
                                y0 == 0 && call.first ? r.norms + t0 : nullptr, r.at_target + y0);
         }
     }
@@ -827,8 +841,9 @@ void tg_launch_log_probs(const void* h, int64_t ld_h, const void* w, int64_t ld_
     carve_lp(&r, &c, shape, h, ld_h, w, ld_w, n, n_rows, d, e, rh, rw, top);
     if (!rh) tg_launch_pack(h, ld_h, n, d, e, r.ph, s);
     if (!rw) tg_launch_pack(w, ld_w, n_rows, d, e, r.pw, s);
-    LpTop a{h, w, ld_h, ld_w, d, __builtin_ctz(shape.bm / LP_GROUP), __builtin_ctz(shape.shared), top, r.norms, (int)r.n_norms, r.groups,
-            (int)(shape.tiles * (shape.bm / LP_GROUP)), rows, row_logp};
+    // (a group has bm / groups rows, in blocks of 4: half of them in either half of the tile)
+    LpTop a{h, w, ld_h, ld_w, d, __builtin_ctz(shape.bm), __builtin_ctz(shape.groups), __builtin_ctz(shape.bm / shape.groups / 8), top, r.norms, (int)r.n_norms, r.groups,
+            (int)(shape.tiles * shape.groups), rows, row_logp};
     TG_WITH_TYPE(dtype, E, {
         if constexpr (sizeof(E) == 2) {
             if (top && shape.bm == 256) {

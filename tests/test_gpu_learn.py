@@ -91,7 +91,8 @@ class Ref:
 
 
 SHAPES = [(1, 1, 1, 1), (2, 3, 8, 5), (1, 700, 64, 8), (30, 129, 96, 32), (33, 1000, 50, 20), (64, 257, 128, 1), (65, 300, 40, 7), (130, 515, 33, 32), (300, 2100, 72, 3),
-          (257, 8000, 130, 8), (1, 20_001, 16, 32), (31, 9000, 24, 5), (50, 20_000, 40, 9)]
+          (257, 8000, 130, 8), (1, 20_001, 16, 32), (31, 9000, 24, 5), (50, 20_000, 40, 9),
+          (23, 553, 91, 20), (14, 1116, 56, 28), (3000, 300, 24, 32), (3000, 1000, 16, 32), (7, 33, 8, 32)]
 
 
 @pytest.mark.parametrize("t", TYPES)
@@ -141,7 +142,8 @@ def _device_ref(hd, wd, scale, top, step=4096):
 
 
 @pytest.mark.parametrize("t,n,v,d,top", [(BF16, 2100, 30_011, 136, 8), (F16, 2100, 30_011, 136, 32), (F32, 900, 30_011, 40, 20), (BF16, 400, 6000, 64, 5),
-                                         (BF16, 70_000, 40_000, 8, 2), (BF16, 2, 1_000_003, 64, 10), (F16, 60, 300_000, 64, 31), (F32, 17, 100_000, 200, 16)])
+                                         (BF16, 70_000, 40_000, 8, 2), (BF16, 2, 1_000_003, 64, 10), (F16, 60, 300_000, 64, 31), (F32, 17, 100_000, 200, 16),
+                                         (BF16, 8192, 2000, 64, 32), (BF16, 8192, 9000, 64, 32), (F16, 3000, 1100, 64, 32), (BF16, 100, 1_000_003, 24, 32)])
 def test_log_probs_of_many_tiles(t, n, v, d, top):
     g = gen(n)
     w = (torch.randn(v, d, generator=g) / math.sqrt(d)).to(t).to(DEV)

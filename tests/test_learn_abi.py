@@ -60,8 +60,8 @@ def test_log_probs_workspaces():
     both, table, tokens, none = (f(n, v, d, 1, 8, a) for a in (1, 2, 3, 0))
     assert h <= table - both <= h + 256 and w <= tokens - both <= w + 256 and h + w <= none - both <= h + w + 512
     assert f(n, v, 97, 1, 8, 1) == f(n, v, 97, 1, 8, 0)              # rows of such a length are copied wherever they start
-    # the best rows cost a quarter of a byte a logit, and no more than half a GiB at a time
-    assert f(n, v, d, 1, 8, 1) - f(n, v, d, 1, 0, 1) <= n * v // 4 + 64 * 1024
+    # the best rows cost a byte a logit at most, and no more than a GiB at a time
+    assert f(n, v, d, 1, 8, 1) - f(n, v, d, 1, 0, 1) <= n * v + 64 * 1024
     assert f(1 << 20, 100_000, 64, 1, 8, 1) < (1 << 30) + (1 << 28)
     # without the table's gradient, no more than with it
     for n in (1, 40, 999, 8192):
