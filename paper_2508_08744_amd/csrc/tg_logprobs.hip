@@ -2,8 +2,8 @@
 //
 // A tile of logits stays in the registers of the workgroup that formed it.  For every token it leaves the maximum m, the sum l of 2^t and the
 // sum s of t 2^t, t = (z - m) log2(e): joined over the table they give lse = m + log l and the entropy log l - log(2) s / l.  2 n n_rows d operations on the
-// matrix instructions bound it, or, for few tokens, the bytes of the table.  (131 072 rows of 1024 bf16: 4096 tokens 902 us, 1.22 PFLOP/s, with 8 best rows 1054, 44 for the
-// norms and 54 for the join; one token 40 us, 6.7 TB/s, and 12 for the join.)
+// matrix instructions bound it, or, for few tokens, the bytes of the table.  (131 072 rows of 1024 bf16: 4096 tokens 944 us, 1.16 PFLOP/s, with 8 best rows 1061, 42 for the
+// norms and 41 to 54 for the join; one token 40 us, 6.7 TB/s, and 12 for the join.)
 //
 // The best rows are those of the largest logits in 64 bits, and the logits of the tiles are in 32.  So every lane of a tile leaves, of its 8, 16 or 32
 // logits of a token (a group), the largest with its row and an upper bound of the second: at most a byte a logit.  With 64 lanes over a token's groups, the k-th largest of the lanes' largest is below the k-th
@@ -427,9 +427,10 @@ __device__ inline int lp_group_row(const LpTop& a, int g, int lane)
 }
 
 // The tiles' sums joined, and the best rows, by W waves a token: eight where there are few tokens (one token, 1024 tiles: 12 us, of which ways to memory, one behind the other, are most), one where
-// there are many (4096, 512 tiles: 54 us; with four 121; four waves a SIMD at 48 spilt registers in the rare paths: with three 63).
+// there are many (4096, 512 tiles: 41 to 54 us; 121 with four at the time it was 62 with one; four waves a SIMD, at 48 registers spilt in the rare paths, 51, three 64).
 //
-// What is not below the threshold is listed and scored, eight rows at a time a wave, and a row's place is the number of those before it.  Where the list does not hold
+// What is not below the threshold is listed and scored, eight rows at a time a wave; a long list is thinned by the k-th of its lanes' largest, and a row's place is the number of those
+// before it (23 tokens, 553 rows, 20 best: 32 us with the call, 283 through sorted lists of a wave).  Where the list does not hold
 // them (rows that are equal, or nearly, by the hundreds) every wave goes through its groups again with its k best so far in order in its lanes, and passes over
 // what cannot be among them.
 template <class E, int W, bool TOP>
