@@ -15,8 +15,12 @@
 
 #define LP_GROUP_LEAST 8        // logits of a token that leave their largest, in the smallest tiles
 #define LP_MAX_TOP 32           // best rows; half the lanes of a wave, see lp_kth
-#define LP_NORM_ROWS 256        // of the table, where the tiles leave no norms
+#define LP_NORM_ROWS 256        // of the table, where the tiles, which have as many, leave no norms
 #define LP_BELOW (-1000.0f)     // exponents below have a power of 0: so is their part in s, at -infinity too
+
+// A stretch of the table whose largest square is 0 has rows of zeros alone: squares too small for their type are taken for the least above it.
+#define LP_LEAST 1.17549435e-38f
+#define LP_BITS(E) (sizeof(E) == 4 ? 0x7FFFFFFF : 0x7FFF7FFF)     // but the signs
 
 typedef unsigned int lp_u32;
 
@@ -85,7 +89,8 @@ __global__ __launch_bounds__(64 * WM * WN) void lp_part_kernel(TileRows X, TileR
         }
 #pragma unroll
         for (int m = 1; m < 16; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-        if (tg_lane() == 0) s_norm[threadIdx.x >> 6] = top;
+        const bool some = __any((t.bits & LP_BITS(E)) != 0);
+        if (tg_lane() == 0) s_norm[threadIdx.x >> 6] = some ? fmaxf(top, LP_LEAST) : 0.0f;
     }
     // (the tile's memory is free: a sum for every token and wave along x)
     LpSum* const s_sum = reinterpret_cast<LpSum*>(lds) + (threadIdx.x >> 6) / WN * BN;
@@ -231,6 +236,7 @@ __global__ __launch_bounds__(1024) void lp_norms_kernel(const E* __restrict__ w,
         float top = 0.0f;
         for (int r = first; r < LP_NORM_ROWS; r += 4 * rows) {
             float sum[4] = {};
+            bool some = false;
             for (int c = of * P::E; c < d; c += lanes * P::E) {
                 typename P::vec v[4];
 #pragma unroll
@@ -242,7 +248,13 @@ __global__ __launch_bounds__(1024) void lp_norms_kernel(const E* __restrict__ w,
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int e = 0; e < P::E; ++e) sum[i] = fmaf((float)v[i][e], (float)v[i][e], sum[i]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const tg_i32x4 x = __builtin_bit_cast(tg_i32x4, v[i]);
+                    some |= (((x[0] | x[1]) | (x[2] | x[3])) & LP_BITS(E)) != 0;
+                }
             }
+            if (some) top = fmaxf(top, LP_LEAST);
             for (int m = 1; m < lanes; m <<= 1)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], m);
@@ -338,7 +350,7 @@ struct LpTop {
     int d, tile_shift, per_shift, half_shift;     // log2 of a tile's rows, of its groups, and of the blocks of 16 rows that a wave has in half of a tile
     int top;
     const float* norms;
-    int n_norms;
+    int n_norms;                 // one a tile
     const uint2* groups;
     int n_groups;                // below 2^28
     int32_t* rows;
@@ -562,7 +574,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
             }
             continue;
         }
-        const double margin = zero || scale == 0.0f ? 0.0 : lp_margin<E>(scale, a.d, h2, w2);
+        const double margin = zero || scale == 0.0f || w2 == 0.0f ? 0.0 : lp_margin<E>(scale, a.d, h2, w2);
         const double low = (double)lp_kth(high, a.top) - 2.0 * margin;
         int* const list = s_list[TOP ? team : 0];
         double* const score = s_z[TOP ? team : 0];
@@ -661,7 +673,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
         }
         LpBest best;
         best.begin(a.top);
-        const auto look = [&](float max, int t) { return best.wants((double)max + margin, t << a.tile_shift); };
+        // (tiles of zeros are exact too)
+        const auto look = [&](float max, int t) { return best.wants((double)max + (a.norms[t] == 0.0f ? 0.0 : margin), t << a.tile_shift); };
         lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, look, [&](bool hit, int g, float first, lp_u32 second) {
             const int row0 = g >> a.per_shift << a.tile_shift;
             u64 hits = __ballot(hit && best.wants(first + margin, row0));
@@ -725,7 +738,7 @@ static LpShape lp_shape(int64_t n, int64_t n_rows, int e, int top)
     // The tiles of the cross entropy's logits; but where the best rows are asked for those of 128 rows, which have the norms' squares beside their products, up to 384 tokens
     // (131 072 rows of 1024 bf16, 8 best: 100 tokens 122 us in tiles of 256 rows behind a pass for the norms, 77 in these; 300: 202 and 178; 512: the other way round).
     int64_t most = LP_GROUP_BYTES / (int64_t)sizeof(uint2) / ((n_rows + LP_GROUP_LEAST - 1) / LP_GROUP_LEAST);
-    most = most >= 256 ? most / 256 * 256 : most >= 64 ? 64 : 32;
+    most = most >= 256 ? most / 256 * 256 : most >= 64 ? 64 : n_rows <= 1ll << 28 ? 32 : 8;        // (2^28 rows: 8 GiB for 32 tokens)
     s.tokens = n < most ? n : most;
     const auto tiles = [&](int64_t x, int64_t y) { return ((n_rows + x - 1) / x) * ((s.tokens + y - 1) / y); };
     // A CU holds one tile of 256 x 256, or two of 128 x 128, which take 1.28 times as long for as many logits: the smaller ones where the larger leave more of their last round, or of
@@ -759,7 +772,7 @@ static size_t carve_lp(LpSpace* r, TgCarve* c, const LpShape& s, const void* h, 
     r->w = ready_w ? TileRows{(const char*)w, n_rows, (uint32_t)(ld_w * e), pitch} : TileRows{(const char*)r->pw, n_rows, pitch, pitch};
     r->parts = c->take<float4>((size_t)s.tiles * s.tokens);
     r->at_target = c->take<float>(s.tokens);
-    r->n_norms = s.bm == 256 ? (n_rows + LP_NORM_ROWS - 1) / LP_NORM_ROWS : s.tiles;
+    r->n_norms = s.tiles;
     r->norms = c->take<float>(top ? r->n_norms : 0);
     r->groups = c->take<uint2>(top ? (size_t)s.tiles * s.groups * s.tokens : 0);
     return c->used;

@@ -220,7 +220,7 @@ template <class E> __device__ inline float tile_squares(tg_i32x4 x, float c)
 }
 
 // BM x BN in WM x WN waves, NB stages in LDS.  SQUARES: the sums of the squares of X's rows as well, from the registers that feed the products (a lane's share
-// in squares[i], of row 16 (i % HM) + lane % 16 of the wave's rows in half i / HM; lanes 16, 32 and 48 on have the others).
+// in squares[i], of row 16 (i % HM) + lane % 16 of the wave's rows in half i / HM; lanes 16, 32 and 48 on have the others), and all bits of them together in bits.
 template <class E, int BM, int BN, int WM, int WN, bool XT = false, bool YT = false, int NB = 2, bool SQUARES = false>
 struct Tile {
     static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
@@ -235,6 +235,7 @@ struct Tile {
 
     acc_t acc[FM][FN];
     float squares[SQUARES ? FM : 1];
+    int bits;
 
 #ifdef __HIP_DEVICE_COMPILE__
     struct Run {
@@ -281,7 +282,11 @@ struct Tile {
             const int s = m / (HM * HN), i = m / HN % HM, j = m % HN;
             acc[hx * HM + i][hy * HN + j] = TileMul<E>::mul(f.x[hx][s][i], f.y[hy][s][j], acc[hx * HM + i][hy * HN + j]);
             if constexpr (SQ) {
-                if (j == 0) squares[hx * HM + i] = tile_squares<E>(f.x[hx][s][i], squares[hx * HM + i]);
+                if (j == 0) {
+                    const tg_i32x4 x = f.x[hx][s][i];
+                    squares[hx * HM + i] = tile_squares<E>(x, squares[hx * HM + i]);
+                    bits |= (x[0] | x[1]) | (x[2] | x[3]);
+                }
             }
 #pragma unroll
             for (int n = 0; n < READS; ++n)
@@ -349,6 +354,7 @@ struct Tile {
         if constexpr (SQUARES) {
 #pragma unroll
             for (int i = 0; i < FM; ++i) squares[i] = 0.0f;
+            bits = 0;
         }
         constexpr int FAR = (NB - 2) * (2 * LX + 2 * LY);
         Halves f;

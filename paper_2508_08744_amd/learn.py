@@ -111,7 +111,7 @@ _DATA_PTR, _NUMEL, _DEVICE, _CONTIGUOUS = torch.Tensor.data_ptr, torch.Tensor.nu
 
 
 def _tensors(name, grads):
-    """The tensors' addresses, counts and types as the library takes them (whole lists at a time: 0.2 instead of 0.45 us a tensor)."""
+    """The tensors' addresses, counts and types as the library takes them (whole lists at a time: 0.27 instead of 0.45 us a tensor)."""
     try:
         types = [DTYPES[g.dtype] for g in grads]
         devices = set(map(_DEVICE, grads))

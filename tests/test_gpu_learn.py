@@ -164,6 +164,31 @@ def test_log_probs_of_many_tiles(t, n, v, d, top):
     assert (logp[~there] == 0).all()
 
 
+@pytest.mark.parametrize("n", [2, 11])
+def test_a_table_past_32_bits_of_elements(n):
+    """2^29 rows and some, of zeros but for a few far apart."""
+    v, d = (1 << 29) + 1001, 8
+    w = torch.zeros(v, d, dtype=BF16, device=DEV)
+    at = torch.tensor([3, (1 << 28) + 5, (1 << 29) - 1, (1 << 29) + 7, v - 1], device=DEV)
+    w[at] = torch.tensor([[12.0], [14.0], [11.0], [13.0], [10.0]], device=DEV).to(BF16).expand(5, d)
+    h = torch.full((n, d), 0.25, dtype=BF16, device=DEV)
+    h[1] = -0.25
+    targets = torch.full((n,), v - 1, device=DEV)
+    logp, entropy, lse, rows, row_logp = [x.cpu() for x in learn.log_probs(h, w, targets, top=4)]
+    for y, sign in ((0, 1.0), (1, -1.0), (n - 1, 1.0 if n > 2 else -1.0)):
+        z = sign * torch.tensor([24.0, 28.0, 22.0, 26.0, 20.0], dtype=torch.float64)
+        total = math.log(v - 5 + z.exp().sum().item())
+        p = (z - total).exp()
+        h64 = -(p * (z - total)).sum().item() + (v - 5) * math.exp(-total) * total
+        # every part of the table is joined once: a chain of 64 within a tile and some 100 over the parts
+        bound = 400 * U * (1 + total)
+        assert abs(lse[y].item() - total) <= bound and abs(entropy[y].item() - h64) <= 30 * bound
+        assert abs(logp[y].item() - (z[4].item() - total)) <= bound + 40 * U
+        if sign > 0:
+            assert rows[y].tolist() == [(1 << 28) + 5, (1 << 29) + 7, 3, (1 << 29) - 1]
+            assert ((row_logp[y].double() - (torch.tensor([28.0, 26.0, 24.0, 22.0]) - total)).abs() <= bound + 40 * U).all()
+
+
 # ---- order of the best rows
 
 @pytest.mark.parametrize("t", TYPES)
