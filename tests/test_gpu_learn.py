@@ -143,7 +143,7 @@ def _device_ref(hd, wd, scale, top, step=4096):
 
 @pytest.mark.parametrize("t,n,v,d,top", [(BF16, 2100, 30_011, 136, 8), (F16, 2100, 30_011, 136, 32), (F32, 900, 30_011, 40, 20), (BF16, 400, 6000, 64, 5),
                                          (BF16, 70_000, 40_000, 8, 2), (BF16, 2, 1_000_003, 64, 10), (F16, 60, 300_000, 64, 31), (F32, 17, 100_000, 200, 16),
-                                         (BF16, 8192, 2000, 64, 32), (BF16, 8192, 9000, 64, 32), (F16, 3000, 1100, 64, 32), (BF16, 100, 1_000_003, 24, 32)])
+                                         (BF16, 8192, 2000, 64, 32), (BF16, 8192, 9000, 64, 32), (F16, 3000, 1100, 64, 32), (BF16, 100, 1_000_003, 24, 32), (F16, 600, 3_000_001, 16, 6), (F32, 70, 20_000_003, 12, 4)])
 def test_log_probs_of_many_tiles(t, n, v, d, top):
     g = gen(n)
     w = (torch.randn(v, d, generator=g) / math.sqrt(d)).to(t).to(DEV)
