@@ -129,6 +129,34 @@ def test_of_negative_and_no_scale(t, n):
         ref.check_best(*got[3:], 6)
 
 
+def _log_probs_at_the_boundary(h, w, top, targets=None, targets64=1, logp=None):
+    """tg_log_probs itself: (rc, logp, entropy, lse, rows, row_logp)."""
+    L, t = learn.lib(), embed.DTYPES[h.dtype]
+    (n, d), v = h.shape, w.shape[0]
+    entropy, lse = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    rows, row_logp = torch.empty(n, top, dtype=torch.int32, device=DEV), torch.empty(n, top, device=DEV)
+    nbytes = L.tg_log_probs_workspace(n, v, d, t, top, 0)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
+    rc = L.tg_log_probs(h.data_ptr(), d, w.data_ptr(), d, t, n, v, d, embed._ptr(targets), targets64, 1.0, top, embed._ptr(logp), entropy.data_ptr(), lse.data_ptr(),
+                        rows.data_ptr(), row_logp.data_ptr(), ws.data_ptr(), nbytes, embed._stream())
+    return rc, logp, entropy, lse, rows, row_logp
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,v", [(1, 700), (40, 3000), (256, 900), (257, 900), (3000, 900), (450, 30_000)])
+def test_without_targets_every_log_probability_is_0(t, n, v):
+    """At the C boundary the targets may be missing where their log probabilities are asked for: no token has one."""
+    h, w, _ = inputs(t, n, v, 24, n)
+    hd, wd = h.to(DEV), w.to(DEV)
+    for top in (0, 5):
+        want = learn.log_probs(hd, wd, top=top)
+        for targets64 in (0, 1):
+            got = _log_probs_at_the_boundary(hd, wd, top, targets64=targets64, logp=torch.full((n,), 7.0, device=DEV))
+            assert got[0] == 0 and (got[1] == 0).all()
+            for a, b in zip(got[2:], want[1:]):
+                assert torch.equal(a, b)
+
+
 def _device_ref(hd, wd, scale, top, step=4096):
     """lse, entropy and the best rows in 64 bits, on the device, some tokens at a time."""
     out = []
