@@ -27,7 +27,7 @@ extern "C" {
  * row -1 of log probability -infinity.  (All rows whose logits fp32 cannot tell from the last best one's are scored in 64 bits: where these are thousands,
  * as in a table of equal rows, that is what a call takes.)  0 <= top <= 32; with 0, out_rows and out_row_logp may be NULL.
  * A target outside [0, n_rows) is none: the token's logp is 0, its other results are as for any other.  targets = NULL: no token has one; out_logp
- * may then be NULL too.
+ * may then be NULL too.  Log probabilities are at most 0: where lse's rounding leaves more, 0 is given.
  * A NaN among a token's logits makes all its results NaN, and its best rows -1.  Infinite logits count as the formulas have them: lse is then infinite, the
  * entropy undefined (NaN), and undefined what takes an infinite logit's difference from it; the best rows are those of the largest logits still.
  * h: n x d, w: n_rows x d, both of type dtype; targets: n whole numbers of 32 bits, or of 64 where targets64 is 1; out_logp,

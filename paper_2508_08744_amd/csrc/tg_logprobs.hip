@@ -559,8 +559,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
             const float below = logf(sum.l) - 0.6931471805599453f * (sum.s / sum.l);
             // (probabilities of infinite logits are not defined)
             entropy[y] = fabsf(all) <= 3.4028234e38f ? fmaxf(below, 0.0f) : __builtin_nanf("");
-            // (without a list of targets nobody has one)
-            if (logp) logp[y] = targets && tg_row_of(targets, targets64, y, n_rows) >= 0 ? at_target[y] - all : 0.0f;
+            // (without a list of targets nobody has one; lse, rounded, can be below the largest logit)
+            if (logp) {
+                const float p = targets && tg_row_of(targets, targets64, y, n_rows) >= 0 ? at_target[y] - all : 0.0f;
+                logp[y] = p > 0.0f ? 0.0f : p;
+            }
         }
         if (!TOP) continue;
         const auto put = [&](int place, double z, int row) {

@@ -382,6 +382,28 @@ def test_huge_logits(t, n, v):
         assert (row_logp <= 0).logical_or(row_logp.isnan())[finite].all()
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,v", [(4, 40), (256, 700), (300, 3000), (450, 30_000)])
+def test_no_log_probability_is_above_0(t, n, v):
+    """The target has all of the mass that fp32 sees: exponents of the largest logit are rounded at its size, some of them down."""
+    g = gen(v)
+    w = torch.zeros(v, 8)
+    w[v // 2, 3] = 1.0
+    h = torch.zeros(n, 8)
+    h[:, 3] = torch.exp(math.log(50) + torch.rand(n, generator=g) * math.log(1000))
+    h = h.to(t)
+    targets = torch.full((n,), v // 2)
+    targets[::9] = 0
+    for scale in (1.0, 1.1):
+        logp, _, lse, rows, row_logp = [x.cpu() for x in learn.log_probs(h.to(DEV), w.to(t).to(DEV), targets.to(DEV), scale=scale, top=3)]
+        assert (logp <= 0).all() and (row_logp <= 0).all() and (rows[:, 0] == v // 2).all()
+        # z = scale h (one product), the others are 0: lse is z and less than v e^-50
+        z = h[:, 3].double() * torch.tensor(scale, dtype=F32).double()
+        assert ((lse.double() - z).abs() <= (4 * z + 200 * math.log(v)) * U).all()
+        want = torch.where(targets == 0, -z, 0.0)
+        assert ((logp.double() - want).abs() <= (8 * z + 200 * math.log(v)) * U).all()
+
+
 @pytest.mark.parametrize("t", [F32, BF16])
 def test_logits_beyond_fp32(t):
     """Sums that fp32 does not hold: lse is infinite, and the best rows are those of the exact sums."""
