@@ -63,7 +63,8 @@ int tg_grad_norm(const void* const* grads, const int64_t* counts, const int32_t*
                  void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * out = grads * scale * min(1, max_norm / norm), norm as tg_grad_norm gives it (out_norm); where that is infinite or NaN, or not above max_norm,
+ * out = grads * scale * min(1, max_norm / norm).  The norm of the factor is the one in 64 bits: where finite values have a norm beyond fp32, out_norm, which is rounded as
+ * tg_grad_norm's is, holds infinity, and they are brought under max_norm all the same.  Where a value is infinite or NaN (out_norm then is, too), or the norm is not above max_norm,
  * out = grads * scale.  out: host array of as many device pointers, of tensors of the gradients' counts and types, each its own gradient or memory that no other
  * tensor of the call has a part in (refused otherwise).  max_norm >= 0; infinity: the scale alone.
  * Results are rounded once to their type, behind the product in 32 bits; a gradient in its own place is not written where its factor is 1.

@@ -134,7 +134,7 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(ClipList a, const doubl
 {
     __shared__ double s[4];
     const double norm = fabs((double)scale) * sqrt(clip_total(sums, count, s));
-    // (a norm that is no number, or infinite, brings nothing under anything)
+    // (a norm that is no number, or infinite, brings nothing under anything; in 64 bits it is so only where a value is: one beyond fp32 counts as it is)
     const double by = norm > (double)max_norm && norm <= 1.7e308 ? (double)scale * ((double)max_norm / norm) : (double)scale;
     // (in two steps where 32 bits have few bits left for it: norms beyond them)
     const bool tiny = fabs(by) < 0x1p-64;

@@ -160,7 +160,8 @@ def grad_norm(grads, scale=1.0):
 def clip_grads(grads, max_norm, scale=1.0, out=None):
     """tg_clip_grads: the tensors times scale, and brought under max_norm together; in their own place, or into those of ``out``.
 
-    The norm of grads * scale before that is returned, a tensor of one fp32 value.  Where it is infinite or NaN nothing is brought under max_norm.
+    The norm of grads * scale before that is returned, a tensor of one fp32 value.  Where a value is infinite or NaN (the norm then is, too) the tensors
+    are but multiplied with scale; finite values are brought under max_norm whatever their norm, also where it is beyond fp32 and returned as infinity.
     """
     if math.isnan(max_norm) or max_norm < 0:
         raise ValueError("max_norm must not be below 0")

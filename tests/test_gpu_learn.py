@@ -661,6 +661,31 @@ def test_norm_of_huge_and_tiny_values(t):
         near(g[0], torch.full((1000,), 1000 ** -0.5, dtype=torch.float64), torch.full((1000,), 8 * U), t)
 
 
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_norms_around_the_end_of_fp32(t, in_place):
+    """Finite values are brought under max_norm whether or not fp32 holds their norm; an infinite value beside them leaves all as they are."""
+    top = torch.finfo(F32).max
+    for by, scale in ((0.9, 1.0), (1.0 + 2.0 ** -7, 1.0), (10.0, 1.0), (10.0, -2.0 ** -3), (0.9, 16.0)):
+        # 100 values and 44: the norm is 12 times one of them
+        grads = [torch.full((n,), by * top / 12, dtype=t, device=DEV) for n in (100, 44)]
+        value = grads[0][0].double().item()
+        want = 12 * value * abs(scale)
+        out = [g.clone() for g in grads] if in_place else [torch.empty_like(g) for g in grads]
+        norm = learn.clip_grads(out if in_place else grads, 6.0, scale=scale, out=None if in_place else out).item()
+        assert norm == math.inf if want > top * (1 + U) else abs(norm - want) <= want * (half_step(F32) + 1e-12)
+        for o in out:
+            # (the factor's rounding, in two steps below 2^-64, and the product's)
+            near(o, torch.full(o.shape, 0.5 if scale > 0 else -0.5, dtype=torch.float64), torch.full(o.shape, 4 * U), t)
+        for bad in (math.inf, math.nan):
+            grads[1][3] = bad
+            out = [g.clone() for g in grads] if in_place else [torch.empty_like(g) for g in grads]
+            norm = learn.clip_grads(out if in_place else grads, 6.0, scale=scale, out=None if in_place else out).item()
+            assert norm == math.inf if bad == math.inf else math.isnan(norm)
+            for o, g in zip(out, grads):
+                assert torch.equal((g * scale).nan_to_num(nan=5.0), o.nan_to_num(nan=5.0))
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 def test_norms_that_are_none(bad):
     grads = _many(4, [100, 20_000, 7])
