@@ -273,7 +273,8 @@ __global__ __launch_bounds__(1024) void lp_norms_kernel(const E* __restrict__ w,
 }
 
 // How far a logit of the tiles is from its exact value at most.  Every one of the d products and sums is off by less than 2^-23 of the sum of the products'
-// magnitudes (twice the step of rounding to the nearest: nothing is taken for granted of how the matrix instructions add), the factor's product by as much, and that
+// magnitudes (twice the step of rounding to the nearest: nothing is taken for granted of how the matrix instructions add), or by 2^-126 where it is below the normal numbers (which
+// may be taken for 0), the factor's product by as much, and that
 // sum is at most |h| |w|.  The squares' sums are off by less than d 2^-23 themselves, and what of them is too small for the type's products is added.
 template <class E>
 __device__ inline double lp_margin(float scale, int d, double h2, double w2)
@@ -281,7 +282,7 @@ __device__ inline double lp_margin(float scale, int d, double h2, double w2)
     const double lost = (__is_same(E, tg_f16) ? 0x1p-28 : 0x1p-126) * d, more = 1.0 + d * 0x1p-22;
     // (roots in 32 bits, rounded up)
     const float h = sqrtf((float)((h2 + lost) * more)), w = sqrtf((float)((w2 + lost) * more));
-    return fabs((double)scale) * (d + 2) * 0x1.00001p-23 * (double)h * (double)w + 0x1p-120;
+    return fabs((double)scale) * ((d + 2) * 0x1.00001p-23 * (double)h * (double)w + d * 0x1p-125) + 0x1p-120;
 }
 
 // What the k-th largest of a wave's values is not below, in all lanes: its first 20 bits (a NaN counts as the smallest; less than everything is a NaN itself).

@@ -278,6 +278,20 @@ def test_order_of_rows_of_the_smallest_numbers(t, n, v):
     assert torch.equal(rows.cpu().long(), torch.sort(z, dim=1, descending=True, stable=True)[1][:, :12])
 
 
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("n,v", [(1, 3000), (50, 3000), (100, 3000), (300, 2100), (450, 30_000)])
+@pytest.mark.parametrize("size", [-58, -63, -65, -68])
+def test_order_of_products_of_the_smallest_size(t, n, v, size):
+    """Values that are normal numbers, whose products are not, brought up by the factor: whatever is left of the sums, the best rows are those of the exact ones."""
+    g = gen(n)
+    w = (torch.randn(v, 24, generator=g) * 2.0 ** size).to(t)
+    h = (torch.randn(n, 24, generator=g) * 2.0 ** size).to(t)
+    scale = 2.0 ** 126
+    z = (h.double() @ w.double().t()) * scale
+    _, _, _, rows, _ = learn.log_probs(h.to(DEV), w.to(DEV), scale=scale, top=12)
+    assert torch.equal(rows.cpu().long(), torch.sort(z, dim=1, descending=True, stable=True)[1][:, :12])
+
+
 # ---- infinite and undefined logits
 
 @pytest.mark.parametrize("t", TYPES)
