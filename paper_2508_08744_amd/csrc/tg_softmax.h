@@ -7,7 +7,7 @@
 __device__ inline float xent_exp(float x) { return __builtin_amdgcn_exp2f(x * XENT_LOG2E); }
 
 // Up to here exp(z - m) is 2 to the power of one multiply-add, z log2(e) - m log2(e), whose rounding is that of its terms: 2^-7 at this size, and beyond it
-// more and more, up to results that overflow.  Logits (or a scale) beyond it take the difference first: in the place of the products it makes the
+// more and more, up to results that overflow.  (For the sums it is no larger than that of the logits and of lse themselves; the gradients, which have lse as a number, give it back: xent_p_kernel.)  Logits (or a scale) beyond it take the difference first: in the place of the products it makes the
 // exponents, to be taken with a factor of 1 and nothing subtracted, so that what follows is the same for both.
 #define XENT_NEAR 65536.0f
 __device__ inline bool xent_near(float m, float base) { return fabsf(m) < XENT_NEAR && fabsf(base) <= 3.4028234e38f; }

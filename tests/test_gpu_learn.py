@@ -534,6 +534,37 @@ def test_gradients_of_large_tiles(t):
             assert more.get("table") is False
 
 
+@pytest.mark.parametrize("v", [64, 300])
+@pytest.mark.parametrize("size,shift", [(2, 0), (2, 12), (5, 40), (5, 100), (8, 1000), (8, 30_000)])
+@pytest.mark.parametrize("scale", [1.0, 1.25, -0.7])
+def test_probabilities_keep_their_bits_at_any_lse(v, size, shift, scale):
+    """With the unit matrix for a table dh is P itself, and the logits are h: whatever the size of lse, p is exp(z - lse) but for the roundings of that difference."""
+    n, g = 500, gen(v)
+    h = (size * torch.randn(n, v, generator=g) + shift) / scale
+    i = torch.randint(0, v, (n,), generator=g)
+    i[::7] = -1
+    a, b = torch.randn(n, generator=g), 0.3 * torch.randn(n, generator=g)
+    hd, wd, id_ = h.to(DEV), torch.eye(v, device=DEV), i.to(DEV)
+    _, entropy, lse, _, _ = learn.log_probs(hd, wd, id_, scale=scale)
+    s = torch.tensor(scale, dtype=F32).double()
+    u = h.double() * s - lse.cpu().double()[:, None]           # (lse and the entropy are given numbers here)
+    p = u.exp()
+    there = i >= 0
+    hit = torch.zeros(n, v, dtype=torch.float64).scatter_(1, i.clamp_min(0)[:, None], 1.0) * there[:, None]
+    aa = torch.where(there, a.double(), 0.0)[:, None]
+    for bb in (None, b):
+        bx = torch.zeros(n, 1, dtype=torch.float64) if bb is None else bb.double()[:, None]
+        e = entropy.cpu().double()[:, None]
+        dh, _ = learn.log_probs_grad(hd, wd, id_, lse, a.to(DEV), None if bb is None else entropy, None if bb is None else bb.to(DEV), scale=scale)
+        want = s * (aa * hit - p * (aa + bx * (u + e)))
+        # The exponent, log2(e) u: a factor of two roundings, its own, and 2^x by the hardware (a step); the factor of the token's: lost part (a step and a rounding), gradient, scale and
+        # 1 more; the product's.  Beside p: log p and H come in two products and sums.  Products with 0 and 1 are exact.
+        parts = p * (aa.abs() + bx.abs() * (u.abs() + e))
+        tol = abs(s) * (parts * (3 * u.abs() + 16) * U + aa.abs() * hit * 4 * U) + 2.0 ** -126
+        off = ((dh.cpu().double() - want).abs() - tol).max().item()
+        assert off <= 0, "beyond the bound by %g" % off
+
+
 def test_gradients_are_the_differences():
     g = gen(11)
     h, w, targets = inputs(F32, 50, 90, 20, 11)
