@@ -2,7 +2,7 @@
 
 Argument marshalling only, like ``knn``: torch supplies device memory and the current stream, the HIP library does the work, and there
 is no fallback.  Training calls come in pairs, an operator and its gradient; nothing is kept between them but what the caller passes on.
-torch's autograd sees none of it: tensors that require a gradient are refused while gradients are recorded.
+torch's autograd sees none of it: tensors that require a gradient are refused while gradients are recorded, and those with a tangent of its forward mode.
 Matrices may have any row stride (their last dimension must be contiguous); results are new contiguous tensors.
 """
 from __future__ import annotations
@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+import torch.autograd.forward_ad as _forward_ad
 
 from . import knn
 from .knn import TagoreError  # noqa: F401  (what a refused call raises)
@@ -72,7 +73,16 @@ def _stream(*tensors):
             if t.requires_grad and torch.is_grad_enabled():
                 raise ValueError("a tensor requires a gradient, and these calls record none: call them under torch.no_grad() or from a "
                                  "torch.autograd.Function, with the gradient's own call in its backward")
+    if _forward_mode():
+        for t in tensors:
+            if t is not None and _forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("a tensor has a tangent, which these calls do not carry on: call them with the primal, or from a torch.autograd.Function with a jvp")
     return _raw_stream(device)
+
+
+def _forward_mode():
+    """Whether tensors may have tangents: inside a dual level (a name of torch's own tells; without it they are always looked at)."""
+    return getattr(_forward_ad, "_current_level", 0) >= 0
 
 
 def _on_device(name, t, dtypes, dim):

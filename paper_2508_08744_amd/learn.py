@@ -1,7 +1,8 @@
 """Python binding of include/tagore_learn.h: the operators that tune a learnt table by what it answers with.
 
 Argument marshalling only, in the manner of ``embed``: torch supplies device memory and the current stream, the HIP library does the work,
-and there is no fallback.  torch's autograd sees none of it: tensors that require a gradient are refused while gradients are recorded.
+and there is no fallback.  torch's autograd sees none of it: tensors that require a gradient are refused while gradients are recorded, and those with a tangent
+of its forward mode.
 Matrices may have any row stride (their last dimension must be contiguous); results are new contiguous tensors.
 """
 from __future__ import annotations
@@ -14,7 +15,7 @@ import operator
 import torch
 
 from . import embed
-from .embed import DTYPES, TagoreError, _aligned, _check, _ids, _on_device, _ptr, _rows, _space, _stream, _vector  # noqa: F401
+from .embed import DTYPES, TagoreError, _aligned, _check, _forward_mode, _ids, _on_device, _ptr, _rows, _space, _stream, _vector  # noqa: F401
 
 EXPORTS = ["tg_log_probs_workspace", "tg_log_probs", "tg_log_probs_grad_workspace", "tg_log_probs_grad", "tg_grad_norm_workspace", "tg_grad_norm",
            "tg_clip_grads"]
@@ -121,12 +122,14 @@ def _tensors(name, grads):
         raise TypeError("%s must be CUDA tensors of %s" % (name, " or ".join(str(d) for d in DTYPES))) from None
     if not all(map(_CONTIGUOUS, grads)):
         raise ValueError("%s must be contiguous" % name)
-    # the checks of _stream, which looks at a tensor at a time: one of every device, and one that requires a gradient
+    # the checks of _stream, which looks at a tensor at a time: one of every device, one that requires a gradient, and those with tangents
     for g in grads if len(devices) > 1 else grads[:1]:
         _stream(g)
     if torch.is_grad_enabled():
         for g in filter(_REQUIRES_GRAD, grads):
             _stream(g)
+    if _forward_mode():
+        _stream(*grads)
     return array.array("Q", map(_DATA_PTR, grads)), array.array("q", map(_NUMEL, grads)), array.array("i", types)
 
 

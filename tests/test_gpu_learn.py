@@ -864,3 +864,29 @@ def test_tensors_that_require_a_gradient_are_refused():
             call()
         with torch.no_grad():
             call()
+
+
+def test_tangents_are_refused():
+    import torch.autograd.forward_ad as forward_ad
+    x, f = torch.randn(4, 8, device=DEV), torch.ones(4, device=DEV)
+    i = torch.zeros(4, dtype=torch.int64, device=DEV)
+    with forward_ad.dual_level():
+        dual, line = forward_ad.make_dual(x, torch.ones_like(x)), forward_ad.make_dual(f, f.clone())
+        for call in (lambda: learn.log_probs(dual, x, i), lambda: learn.log_probs(x, dual, i), lambda: learn.log_probs_grad(x, x, i, f, line), lambda: learn.grad_norm([x, dual]),
+                     lambda: learn.clip_grads([f, dual], 1.0), lambda: learn.clip_grads([x], 1.0, out=[dual]), lambda: embed.softmax_xent(dual, x, i), lambda: embed.lookup(dual, i)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        # tensors without one are taken, and a Function has them so
+        want = learn.log_probs(x, x, i)[2]
+        assert torch.equal(learn.log_probs(forward_ad.unpack_dual(dual).primal, x, i)[2], want)
+
+        class Lse(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, h):
+                return learn.log_probs(h, x, i)[2]
+
+            @staticmethod
+            def jvp(ctx, t):
+                return t.sum(1)
+        out = forward_ad.unpack_dual(Lse.apply(dual))
+        assert torch.equal(out.primal, want) and torch.equal(out.tangent, torch.full((4,), 8.0, device=DEV))
