@@ -2,7 +2,7 @@
 
 Argument marshalling only, in the manner of ``embed``: torch supplies device memory and the current stream, the HIP library does the work,
 and there is no fallback.  torch's autograd sees none of it: tensors that require a gradient are refused while gradients are recorded, and those with a tangent
-of its forward mode.
+of its forward mode; of the tensors that ``clip_grads`` writes it is told that they have changed.
 Matrices may have any row stride (their last dimension must be contiguous); results are new contiguous tensors.
 """
 from __future__ import annotations
@@ -180,4 +180,5 @@ def clip_grads(grads, max_norm, scale=1.0, out=None):
             raise ValueError("out must have the gradients' sizes and types")
     L, keep, ws, nbytes, norm = _norm_space(grads, counts)
     _check(L.tg_clip_grads(_at(at), _at(to), _at(counts), _at(types), len(grads), max_norm, scale, norm.data_ptr(), ws, nbytes, _stream()))
+    torch.autograd.graph.increment_version(grads if out is None else out)
     return norm

@@ -866,6 +866,37 @@ def test_tensors_that_require_a_gradient_are_refused():
             call()
 
 
+def test_autograd_is_told_what_is_written():
+    """A tensor that a graph has kept for its backward pass: written in place, that pass refuses as it does behind torch's own operators."""
+    def kept():
+        x = torch.randn(1000, device=DEV, requires_grad=True)
+        return x, x.exp()
+    for into in (False, True):
+        x, y = kept()
+        other = torch.ones(30, device=DEV)
+        version, beside = y._version, other._version
+        with torch.no_grad():
+            if into:
+                learn.clip_grads([other, torch.ones(1000, device=DEV)], 0.5, out=[torch.empty(30, device=DEV), y])
+            else:
+                learn.clip_grads([other, y], 0.5)
+        assert y._version > version and (other._version == beside) == into
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+    # what is only read has not changed
+    x, y = kept()
+    version = y._version
+    with torch.no_grad():
+        learn.grad_norm([y])
+        learn.clip_grads([y], 0.5, out=[torch.empty(1000, device=DEV)])
+    assert y._version == version
+    y.sum().backward()
+    with torch.inference_mode():
+        z = torch.ones(100, device=DEV)
+        learn.clip_grads([z], 1.0)
+    assert abs(z.norm().item() - 1) < 1e-6
+
+
 def test_tangents_are_refused():
     import torch.autograd.forward_ad as forward_ad
     x, f = torch.randn(4, 8, device=DEV), torch.ones(4, device=DEV)
