@@ -44,7 +44,8 @@ int tg_log_probs(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32
  * out_dh = P w (n x d) and out_dw = P^T h (n_rows x d), both of type dtype; out_dw = NULL: the table is not learnt, and its gradient not formed.
  * lse, entropy: what tg_log_probs gave; dlogp, dentropy: n fp32; dentropy = NULL: the entropy has no part (then entropy may be NULL).
  * A token without a target has no part through logp, and one without a target whose dentropy is 0 none at all, whatever its logits are.
- * How P is formed, rounded and held is as for tg_softmax_xent_grad.  table: 1 where out_dw is given, 0 where it is NULL.
+ * How P is formed, rounded and held is as for tg_softmax_xent_grad.  table: 1 where out_dw is given, 0 where it is NULL: either has a workspace of its own size, and the one
+ * without the table's gradient can be the larger (dh comes in up to 64 parts of n x d fp32, which alone are to fill the device).
  */
 size_t tg_log_probs_grad_workspace(int64_t n, int64_t n_rows, int32_t d, int32_t dtype, int32_t table, int32_t aligned);
 int tg_log_probs_grad(const void* h, int64_t ld_h, const void* w, int64_t ld_w, int32_t dtype, int64_t n, int64_t n_rows, int32_t d,

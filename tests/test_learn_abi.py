@@ -68,6 +68,20 @@ def test_log_probs_workspaces():
         assert 0 < g(n, 37_511, 512, 2, 0, 1)
 
 
+def test_the_gradients_workspace_without_the_tables():
+    """Neither with nor without the table's gradient is the other's bound; they differ by dh's parts, 64 of n x d fp32 at most, and the pieces' alignment."""
+    from paper_2508_08744_amd import learn
+    g = learn.lib().tg_log_probs_grad_workspace
+    more = 0
+    for n in (1, 7, 40, 64, 65, 300, 999, 8192):
+        for v, d in ((1, 8), (5000, 50), (37_511, 512), (131_072, 1024), (1_000_003, 96)):
+            for dtype in (0, 1, 2):
+                without, with_it = g(n, v, d, dtype, 0, 1), g(n, v, d, dtype, 1, 1)
+                assert without > 0 and with_it > 0 and abs(without - with_it) <= 64 * n * d * 4 + 512
+                more += without > with_it
+    assert more > 0
+
+
 def _lists(pointers, counts, types):
     n = len(counts)
     return (ctypes.c_void_p * n)(*pointers), (ctypes.c_int64 * n)(*counts), (ctypes.c_int32 * n)(*types)
