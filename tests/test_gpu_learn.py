@@ -265,6 +265,31 @@ def test_order_below_the_roundings_of_the_logits(t, n, v, d):
 
 
 @pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,v,d,longer", [(1, 3000, 1024, 1000), (20, 5000, 2048, 400), (40, 9000, 512, 4000), (100, 3000, 1024, 1000), (300, 3000, 2048, 400), (450, 30_000, 512, 3000)])
+def test_order_beside_a_row_far_longer_than_the_others(t, n, v, d, longer):
+    """What a logit may be off by goes by the longest row of the table: thousands of rows are then not out of reach of the best ones, and are scored in 64 bits."""
+    g = gen(n + d)
+    w = torch.randn(v, d, generator=g) / math.sqrt(d)
+    long = v // 3
+    w[long] *= longer
+    w = w.to(t)
+    h = (2 * torch.randn(n, d, generator=g)).to(t)
+    h[-1] = -h[0]                                              # (the long row is first for one of them, or last)
+    z = h.double() @ w.double().t()
+    best, at = torch.sort(z, dim=1, descending=True, stable=True)
+    # the bound of d products and sums at a step each, twice: more rows than a list of 1024 holds
+    reach = 2 * (d + 2) * 2.0 ** -23 * h.double().norm(dim=1) * w.double().norm(dim=1).max()
+    assert (z >= (best[:, 7] - reach)[:, None]).sum(1).min() > 1024
+    _, _, _, rows, row_logp = learn.log_probs(h.to(DEV), w.to(DEV), top=8)
+    assert torch.equal(rows.cpu().long(), at[:, :8])
+    lse = torch.logsumexp(z, 1)
+    # logits that count are the long row's, up to its own bound, or below 16, and the exponents' part
+    size = z.abs().amax(1)
+    dz = (h.double().abs() @ w.double().abs().t()).amax(1) * (d + 3) * U
+    near(row_logp, best[:, :8] - lse[:, None], (3 * dz + 8 * U * (lse.abs() + size) + 130 * U)[:, None] + 2 * U * (best[:, :8] - lse[:, None]).abs(), F32)
+
+
+@pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("n,v", [(1, 3000), (50, 3000), (100, 3000), (450, 30_000)])
 def test_order_of_rows_of_the_smallest_numbers(t, n, v):
     """Values below the type's normal ones: whatever the tiles make of them, the best rows are those of the exact sums."""
