@@ -25,7 +25,8 @@ extern "C" {
  * and the `top` best rows: out_rows (n x top) those of the largest z, in that order, and out_row_logp (n x top) their z - lse.  Which rows these
  * are and their order is decided by z in 64 bits, equal ones by the lower row; where the table has fewer rows than top, the rest is
  * row -1 of log probability -infinity.  (All rows whose logits fp32 cannot tell from the last best one's are scored in 64 bits: where these are thousands,
- * as in a table of equal rows, that is what a call takes.)  0 <= top <= 32; with 0, out_rows and out_row_logp may be NULL.
+ * as in a table of equal rows, that is what a call takes.  What it can tell goes by |scale| |h| d 2^-22 and the length of the longest of some 64 to 256 neighbours in the table: rows far longer
+ * than the others, a thousand times and more, take their neighbours with them, but no others.)  0 <= top <= 32; with 0, out_rows and out_row_logp may be NULL.
  * A target outside [0, n_rows) is none: the token's logp is 0, its other results are as for any other.  targets = NULL: no token has one; out_logp
  * may then be NULL too.  Log probabilities are at most 0: where lse's rounding leaves more, 0 is given.
  * A NaN among a token's logits makes all its results NaN, and its best rows -1.  Infinite logits count as the formulas have them: lse is then infinite, the

@@ -7,8 +7,9 @@
 //
 // The best rows are those of the largest logits in 64 bits, and the logits of the tiles are in 32.  So every lane of a tile leaves, of its 8, 16 or 32
 // logits of a token (a group), the largest with its row and an upper bound of the second: at most a byte a logit.  With 64 lanes over a token's groups, the k-th largest of the lanes' largest is below the k-th
-// logit; whatever is further below it than the roundings of 32 bits reach (a bound from the norms of the token's row and of the table's, see lp_margin) is none of
+// logit but for what the roundings of 32 bits reach (a bound from the norms of the token's row and of the longest row of the logit's tile, see LpMargin); whatever does not come up to it with its own bound is none of
 // the k best.  What is left, some k rows, is scored again in 64 bits and put in order.  A group whose second is not out of reach is scored as a whole.
+// (Bounds by tile: 4096 tokens, 32 768 rows of 4096 bf16, one of them 30 or 1000 times as long as the others: 1.06 and 1.6 ms; 46 and 105 with the table's longest row in all bounds; without such a row 0.99.)
 #include "tg_embed.h"
 #include "tg_softmax.h"
 #include "tg_tiles.h"
@@ -272,18 +273,24 @@ __global__ __launch_bounds__(1024) void lp_norms_kernel(const E* __restrict__ w,
     }
 }
 
-// How far a logit of the tiles is from its exact value at most.  Every one of the d products and sums is off by less than 2^-23 of the sum of the products'
+// How far a logit of a tile is from its exact value at most.  Every one of the d products and sums is off by less than 2^-23 of the sum of the products'
 // magnitudes (twice the step of rounding to the nearest: nothing is taken for granted of how the matrix instructions add), or by 2^-126 where it is below the normal numbers (which
 // may be taken for 0), the factor's product by as much, and that
 // sum is at most |h| |w|.  The squares' sums are off by less than d 2^-23 themselves, and what of them is too small for the type's products is added.
 template <class E>
-__device__ inline double lp_margin(float scale, int d, double h2, double w2)
-{
-    const double lost = (__is_same(E, tg_f16) ? 0x1p-28 : 0x1p-126) * d, more = 1.0 + d * 0x1p-22;
-    // (roots in 32 bits, rounded up)
-    const float h = sqrtf((float)((h2 + lost) * more)), w = sqrtf((float)((w2 + lost) * more));
-    return fabs((double)scale) * ((d + 2) * 0x1.00001p-23 * (double)h * (double)w + d * 0x1p-125) + 0x1p-120;
-}
+struct LpMargin {
+    double by, least;
+    float lost, more;
+    // h2: the token's square; exact: its logits are (a row of zeros, a factor of 0)
+    __device__ inline LpMargin(float scale, int d, double h2, bool exact) : lost((__is_same(E, tg_f16) ? 0x1p-28f : 0x1p-126f) * (float)d), more(1.0f + (float)d * 0x1p-22f)
+    {
+        // (roots in 32 bits, of normal numbers and a step off at most: 2^-20 more makes up for that)
+        by = exact ? 0.0 : fabs((double)scale) * (d + 2) * 0x1.00001p-23 * (double)__builtin_amdgcn_sqrtf((float)((h2 + lost) * more));
+        least = exact ? 0.0 : fabs((double)scale) * d * 0x1p-125 + 0x1p-120;
+    }
+    // of the logits of a tile with rows of squares up to w2
+    __device__ inline double of(float w2) const { return w2 == 0.0f || by == 0.0 ? 0.0 : fma(by, (double)__builtin_amdgcn_sqrtf((w2 + lost) * more), least); }
+};
 
 // What the k-th largest of a wave's values is not below, in all lanes: its first 20 bits (a NaN counts as the smallest; less than everything is a NaN itself).
 __device__ inline float lp_kth(float v, int k)
@@ -323,8 +330,8 @@ struct LpBest {
     }
     // (a place without a row is behind all)
     static __device__ inline bool before(double az, int ar, double bz, int br) { return br == NONE ? ar != NONE : ar != NONE && (az > bz || (az == bz && ar < br)); }
-    // whether a row of a logit up to `most` is worth a look
-    __device__ inline bool wants(double most, int r) const { return before(most, r, last_z, last_row); }
+    // whether a row of a logit up to `most` is worth a look (what a NaN says nothing of is)
+    __device__ inline bool wants(double most, int r) const { return last_row == NONE || !(most < last_z || (most == last_z && r > last_row)); }
     // (the same in all lanes)
     __device__ inline void add(double cz, int cr)
     {
@@ -350,8 +357,7 @@ struct LpTop {
     int64_t ld_h, ld_w;
     int d, tile_shift, per_shift, half_shift;     // log2 of a tile's rows, of its groups, and of the blocks of 16 rows that a wave has in half of a tile
     int top;
-    const float* norms;
-    int n_norms;                 // one a tile
+    const float* norms;          // one a tile
     const uint2* groups;
     int n_groups;                // below 2^28
     int32_t* rows;
@@ -392,26 +398,34 @@ __device__ inline double lp_score(const LpTop& a, const E* h, double scale, cons
     return sum[0] * scale;
 }
 
-// The groups of a token that reach `low`, as a wave goes through them: W waves in turn, LP_AHEAD times 64 tiles' maxima asked for at once, then the groups of those tiles that do.
-// Some lanes' groups at a time: take(whether the lane has one, its number, its largest, its packed second).  look(a tile's maximum, its number): whether its groups are still of
-// interest.
+// The groups of a token that reach `least` with their tile's margin, as a wave goes through them: W waves in turn, LP_AHEAD times 64 tiles' maxima asked for at once, then the groups of those
+// tiles that do.  Some lanes' groups at a time: take(whether the lane has one, its number, its largest, its packed second, its margin).  look(a tile's maximum and its margin, its number): whether its
+// groups are still of interest.
 #define LP_AHEAD 8
-template <int W, class Look, class Take>
-__device__ inline void lp_reach(const float4* __restrict__ parts, int tiles, const uint2* __restrict__ groups, int per_shift, int wave, double low, Look look, Take take)
+template <int W, class Margin, class Look, class Take>
+__device__ inline void lp_reach(const float4* __restrict__ parts, const float* __restrict__ norms, int tiles, const uint2* __restrict__ groups, int per_shift, int wave, double least,
+                                const Margin& margin, Look look, Take take)
 {
     for (int t0 = wave * 64 + tg_lane(); t0 - tg_lane() < tiles; t0 += LP_AHEAD * 64 * W) {
-        float v[LP_AHEAD];
+        float v[LP_AHEAD], w2[LP_AHEAD];
 #pragma unroll
-        for (int i = 0; i < LP_AHEAD; ++i) v[i] = t0 + i * 64 * W < tiles ? parts[t0 + i * 64 * W].x : 0.0f;
+        for (int i = 0; i < LP_AHEAD; ++i) {
+            v[i] = t0 + i * 64 * W < tiles ? parts[t0 + i * 64 * W].x : 0.0f;
+            w2[i] = t0 + i * 64 * W < tiles ? norms[t0 + i * 64 * W] : 0.0f;
+        }
         unsigned hits = 0;
 #pragma unroll
-        for (int i = 0; i < LP_AHEAD; ++i) hits |= t0 + i * 64 * W < tiles && !((double)v[i] < low) ? 1u << i : 0u;      // (what a NaN is compared with is not out of reach)
+        for (int i = 0; i < LP_AHEAD; ++i) hits |= t0 + i * 64 * W < tiles && !((double)v[i] + margin.of(w2[i]) < least) ? 1u << i : 0u;      // (what a NaN is compared with is not out of reach)
         for (; __any(hits != 0); hits &= hits - 1) {
             const int i = hits ? __builtin_ctz(hits) : 0, t = t0 + i * 64 * W;
-            float max = v[0];
+            float max = v[0], square = w2[0];
 #pragma unroll
-            for (int j = 1; j < LP_AHEAD; ++j) max = i == j ? v[j] : max;
-            const bool in = hits && look(max, t);
+            for (int j = 1; j < LP_AHEAD; ++j) {
+                max = i == j ? v[j] : max;
+                square = i == j ? w2[j] : square;
+            }
+            const double off = margin.of(square);
+            const bool in = hits && look((double)max + off, t);
             if (!__any(in)) continue;
             for (int g0 = t << per_shift, end = 0; end < 1 << per_shift; g0 += 8, end += 8) {        // (8 or 16 a tile)
                 uint2 q[8];
@@ -419,13 +433,13 @@ __device__ inline void lp_reach(const float4* __restrict__ parts, int tiles, con
                 for (int j = 0; j < 8; ++j) q[j] = in ? groups[g0 + j] : make_uint2(0u, 0u);
                 unsigned deep = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) deep |= in && !((double)__uint_as_float(q[j].x) < low) ? 1u << j : 0u;
+                for (int j = 0; j < 8; ++j) deep |= in && !((double)__uint_as_float(q[j].x) + off < least) ? 1u << j : 0u;
                 for (; __any(deep != 0); deep &= deep - 1) {
                     const int at = deep ? __builtin_ctz(deep) : 0;
                     uint2 x = q[0];
 #pragma unroll
                     for (int j = 1; j < 8; ++j) x = at == j ? q[j] : x;
-                    take(deep != 0, g0 + at, __uint_as_float(x.x), x.y);
+                    take(deep != 0, g0 + at, __uint_as_float(x.x), x.y, off);
                 }
             }
         }
@@ -454,9 +468,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
 {
     constexpr int TOKENS = W == 1 ? 4 : 1;
     constexpr int LIST = W == 1 ? 512 : 1024;
-    __shared__ float s_m[W], s_l[W], s_s[W], s_w2[W];
+    __shared__ float s_m[W], s_l[W], s_s[W];
     __shared__ double s_h2[W];
-    __shared__ float s_top[W > 1 ? W : 1][W > 1 ? 64 : 1];
+    __shared__ float2 s_top[W > 1 ? W : 1][W > 1 ? 64 : 1];
     __shared__ int s_list[TOP ? TOKENS : 1][TOP ? LIST : 1];
     __shared__ double s_z[TOP ? TOKENS : 1][TOP ? LIST : 1];
     __shared__ int s_found, s_zero[W];
@@ -467,25 +481,33 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
         const E* const h = (const E*)a.h + y * a.ld_h;
         const float4* const own = parts + y * count;
         const uint2* const groups = a.groups + y * (int64_t)a.n_groups;
-        // what the margin is made of, its first pieces asked for in front of everything
+        // the token's square, its first pieces asked for in front of everything
         double h2 = 0.0;
-        float w2 = 0.0f;
         bool zero = true;                        // a row of zeros (padding): its logits are exact, and all equal (as with a factor of 0)
         typedef TgPiece<E> P;
         typename P::vec h_first;
-        if (TOP) {
-            h_first = P::raw(h + (of * P::E < a.d ? of * P::E : 0), a.d - of * P::E);
-            w2 = of < a.n_norms ? a.norms[of] : 0.0f;
-        }
+        if (TOP) h_first = P::raw(h + (of * P::E < a.d ? of * P::E : 0), a.d - of * P::E);
         LpSum sum{-__builtin_inff(), 0.0f, 0.0f};
+        // The largest of the lane's, and the square of its tile: the tiles' maxima, or, where they are so few that many tiles have two of the best, the groups'.
+        const bool by_tile = count >= 4 * a.top;
+        float high = -__builtin_inff(), high_w2 = 0.0f;
         for (int64_t p0 = of; p0 < count; p0 += 4 * 64 * W) {
             float4 v[4];
+            float w2[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = p0 + i * 64 * W < count ? own[p0 + i * 64 * W] : make_float4(-__builtin_inff(), 0.0f, 0.0f, 0.0f);
+            for (int i = 0; i < 4; ++i) {
+                v[i] = p0 + i * 64 * W < count ? own[p0 + i * 64 * W] : make_float4(-__builtin_inff(), 0.0f, 0.0f, 0.0f);
+                if (TOP) w2[i] = a.norms[p0 + i * 64 * W < count ? p0 + i * 64 * W : 0];
+            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) lp_join(sum, LpSum{v[i].x, v[i].y, v[i].z});
+            for (int i = 0; i < 4; ++i) {
+                lp_join(sum, LpSum{v[i].x, v[i].y, v[i].z});
+                if (TOP && by_tile && v[i].x > high) {
+                    high = v[i].x;
+                    high_w2 = w2[i];
+                }
+            }
         }
-        float high = -__builtin_inff();          // of the lane's groups
         if (TOP) {
 #pragma unroll
             for (int e = 0; e < P::E; ++e) {
@@ -502,25 +524,19 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
                 }
             }
             zero = __all(zero);
-            for (int p0 = of + 64 * W; p0 < a.n_norms; p0 += 8 * 64 * W) {
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = a.norms[p0 + i * 64 * W < a.n_norms ? p0 + i * 64 * W : 0];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w2 = fmaxf(w2, v[i]);
-            }
-            // (the tiles' maxima are as good, where there are so many that few tiles have two of the best)
-            if (count >= 4 * a.top) high = sum.m;
-            else
-                for (int g = of; g < a.n_groups; g += 64 * W) high = fmaxf(high, __uint_as_float(groups[g].x));
+            if (!by_tile)
+                for (int g = of; g < a.n_groups; g += 64 * W) {
+                    const float m = __uint_as_float(groups[g].x), w2 = a.norms[g >> a.per_shift];
+                    if (m > high) {
+                        high = m;
+                        high_w2 = w2;
+                    }
+                }
         }
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
             lp_join(sum, LpSum{__shfl_xor(sum.m, m), __shfl_xor(sum.l, m), __shfl_xor(sum.s, m)});
-            if (TOP) {
-                h2 += lp_xor64(h2, m);
-                w2 = fmaxf(w2, __shfl_xor(w2, m));
-            }
+            if (TOP) h2 += lp_xor64(h2, m);
         }
         if (W > 1) {
             __syncthreads();                                     // (the token before is done with these)
@@ -530,27 +546,26 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
                 s_s[wave] = sum.s;
                 s_h2[wave] = h2;
                 s_zero[wave] = zero;
-                s_w2[wave] = w2;
             }
             if (threadIdx.x == 0) s_found = 0;
-            if (TOP) s_top[wave][lane] = high;
+            if (TOP) s_top[wave][lane] = make_float2(high, high_w2);
             __syncthreads();
             // (every wave has all waves' W times over)
             sum = LpSum{s_m[lane % W], s_l[lane % W], s_s[lane % W]};
             h2 = s_h2[lane % W];
-            w2 = s_w2[lane % W];
             zero = __all(s_zero[lane % W] != 0);
 #pragma unroll
             for (int m = 1; m < W; m <<= 1) {
                 lp_join(sum, LpSum{__shfl_xor(sum.m, m), __shfl_xor(sum.l, m), __shfl_xor(sum.s, m)});
-                if (TOP) {
-                    h2 += lp_xor64(h2, m);
-                    w2 = fmaxf(w2, __shfl_xor(w2, m));
-                }
+                if (TOP) h2 += lp_xor64(h2, m);
             }
             if (TOP) {
 #pragma unroll
-                for (int i = 0; i < W; ++i) high = fmaxf(high, s_top[i][lane]);
+                for (int i = 0; i < W; ++i) {
+                    const float2 x = s_top[i][lane];
+                    high_w2 = x.x > high ? x.y : high_w2;
+                    high = fmaxf(high, x.x);
+                }
             }
         }
         // (the first lane's: the others joined the same in other orders)
@@ -579,8 +594,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
             }
             continue;
         }
-        const double margin = zero || scale == 0.0f || w2 == 0.0f ? 0.0 : lp_margin<E>(scale, a.d, h2, w2);
-        const double low = (double)lp_kth(high, a.top) - 2.0 * margin;
+        // What the k-th best logit is not below: the lanes' largest, a margin down (one that is infinite may have been made so by the last step).  A row is out of reach where a margin more does not
+        // bring it there; margins are those of its tile, so that a few rows far longer than the others make nothing of theirs hard to tell apart.
+        const LpMargin<E> margin(scale, a.d, h2, zero || scale == 0.0f);
+        const float kth = lp_kth((float)((double)fminf(high, 3.4028234e38f) - margin.of(high_w2)), a.top);
+        const double low = (double)kth - (fabs((double)kth) * 0x1p-22 + 0x1p-140);       // (32 bits of it: a step down)
         int* const list = s_list[TOP ? team : 0];
         double* const score = s_z[TOP ? team : 0];
         int found = 0;
@@ -594,10 +612,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
             found = at + some;
             return at;
         };
-        lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, [&](float, int) { return found <= LIST; }, [&](bool hit, int g, float, lp_u32 second) {
-            u64 many = __ballot(hit && !((double)lp_second(second) < low));
+        lp_reach<W>(own, a.norms, (int)count, groups, a.per_shift, mine, low, margin, [&](double, int) { return found <= LIST; }, [&](bool hit, int g, float, lp_u32 second, double off) {
+            const bool alone = (double)lp_second(second) + off < low;
+            u64 many = __ballot(hit && !alone);
             const int row = (g >> a.per_shift << a.tile_shift) + lp_row(second);
-            const u64 one = __ballot(hit && (double)lp_second(second) < low && row < (int)n_rows);
+            const u64 one = __ballot(hit && alone && row < (int)n_rows);
             if (one) {
                 const int at = room(__popcll(one)) + __popcll(one & tg_lanemask_lt());
                 if ((one >> lane & 1) && at < LIST) list[at] = row;
@@ -635,8 +654,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
                 // those that the k-th of the lanes' largest does not rule out, to the front (32 bits of them: a step down)
                 float largest = -__builtin_inff();
                 for (int c = lane; c < found; c += 64) largest = fmaxf(largest, (float)score[c]);
-                const float kth = lp_kth(largest, a.top);
-                const double least = (double)kth - fabs((double)kth) * 0x1p-22 - 0x1p-140;
+                const float last = lp_kth(largest, a.top);
+                const double least = (double)last - fabs((double)last) * 0x1p-22 - 0x1p-140;
                 int kept = 0;
                 for (int c0 = 0; c0 < found; c0 += 64) {
                     const int c = c0 + lane < found ? c0 + lane : 0;
@@ -678,15 +697,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 1 ? 4 : 1) void lp_join
         }
         LpBest best;
         best.begin(a.top);
-        // (tiles of zeros are exact too)
-        const auto look = [&](float max, int t) { return best.wants((double)max + (a.norms[t] == 0.0f ? 0.0 : margin), t << a.tile_shift); };
-        lp_reach<W>(own, (int)count, groups, a.per_shift, mine, low, look, [&](bool hit, int g, float first, lp_u32 second) {
+        const auto look = [&](double most, int t) { return best.wants(most, t << a.tile_shift); };
+        lp_reach<W>(own, a.norms, (int)count, groups, a.per_shift, mine, low, margin, look, [&](bool hit, int g, float first, lp_u32 second, double off) {
             const int row0 = g >> a.per_shift << a.tile_shift;
-            u64 hits = __ballot(hit && best.wants(first + margin, row0));
-            const u64 many = __ballot(!((double)lp_second(second) < low));
+            u64 hits = __ballot(hit && best.wants((double)first + off, row0));
+            const u64 many = __ballot(!((double)lp_second(second) + off < low));
             for (; hits; hits &= hits - 1) {
                 const int from = __builtin_ctzll(hits);
-                const double most = lp_lane64(first + margin, from);
+                const double most = lp_lane64((double)first + off, from);
                 const bool all_rows = many >> from & 1;
                 const int r = all_rows ? lp_group_row(a, __builtin_amdgcn_readlane(g, from), lane) : __builtin_amdgcn_readlane(row0 + lp_row(second), from);
                 u64 some = __ballot(lane < (all_rows ? lp_group_rows(a) : 1) && r < (int)n_rows && best.wants(most, r));
@@ -861,7 +879,7 @@ void tg_launch_log_probs(const void* h, int64_t ld_h, const void* w, int64_t ld_
     if (!rh) tg_launch_pack(h, ld_h, n, d, e, r.ph, s);
     if (!rw) tg_launch_pack(w, ld_w, n_rows, d, e, r.pw, s);
     // (a group has bm / groups rows, in blocks of 4: half of them in either half of the tile)
-    LpTop a{h, w, ld_h, ld_w, d, __builtin_ctz(shape.bm), __builtin_ctz(shape.groups), __builtin_ctz(shape.bm / shape.groups / 8), top, r.norms, (int)r.n_norms, r.groups,
+    LpTop a{h, w, ld_h, ld_w, d, __builtin_ctz(shape.bm), __builtin_ctz(shape.groups), __builtin_ctz(shape.bm / shape.groups / 8), top, r.norms, r.groups,
             (int)(shape.tiles * shape.groups), rows, row_logp};
     TG_WITH_TYPE(dtype, E, {
         if constexpr (sizeof(E) == 2) {

@@ -290,6 +290,30 @@ def test_order_beside_a_row_far_longer_than_the_others(t, n, v, d, longer):
 
 
 @pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,v,d", [(1, 700, 64), (1, 30_000, 64), (20, 5000, 256), (40, 9000, 128), (100, 3000, 96), (300, 3000, 512), (300, 30_000, 128), (450, 30_000, 96), (3000, 1000, 64)])
+@pytest.mark.parametrize("where", ["together", "apart"])
+def test_order_where_some_rows_logits_are_what_large_terms_leave(t, n, v, d, where):
+    """Some rows' logits are off by more than the others are apart, those in tiles of ordinary rows beside them are not: each is looked at as its own tile asks for."""
+    g = gen(n + v + d)
+    w = 4 * torch.randn(v, d, generator=g) / math.sqrt(d)
+    at = torch.arange(v // 3, v // 3 + 50) if where == "together" else torch.randperm(v, generator=g)[:12]
+    big = 2.0 ** 12 * torch.randn(len(at), d // 4, generator=g)
+    w[at, : d // 4] = big
+    w[at, d // 2: d // 2 + d // 4] = -big.to(t).float()
+    w = w.to(t)
+    h = torch.randn(n, d, generator=g)
+    h[:, : d // 4] = 1.0
+    h[:, d // 2: d // 2 + d // 4] = 1.0
+    h = h.to(t)
+    z = h.double() @ w.double().t()
+    assert z.abs().max() < 60
+    best, order = torch.sort(z, dim=1, descending=True, stable=True)
+    for top in (1, 10, 32):
+        _, _, _, rows, _ = learn.log_probs(h.to(DEV), w.to(DEV), top=top)
+        assert torch.equal(rows.cpu().long(), order[:, :top])
+
+
+@pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("n,v", [(1, 3000), (50, 3000), (100, 3000), (450, 30_000)])
 def test_order_of_rows_of_the_smallest_numbers(t, n, v):
     """Values below the type's normal ones: whatever the tiles make of them, the best rows are those of the exact sums."""
