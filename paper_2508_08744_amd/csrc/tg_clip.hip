@@ -3,7 +3,7 @@
 // The tensors come as lists in the kernels' arguments (nothing is copied to the device for them, so the calls can be captured), each in pieces of CLIP_PIECE
 // values.  A workgroup has a stretch of pieces and leaves one sum of squares, in 64 bits (the squares of fp32 and bf16 leave 32 bits' range); every workgroup of the second pass adds all
 // of those up in the same order and has the factor.  It takes its stretch from the end: what was read last is still in the caches.
-// (197 M values of 16 bits: 61 us for the norm, 6.5 TB/s, and 134 to scale, 5.9 TB/s; the stretches taken forwards and results through the caches: 253 us for 200 M in the place of 203.)
+// (197 M values of 16 bits: 61 us for the norm, 6.5 TB/s, and 135 to scale, 5.8 TB/s; with the call 204 into other tensors, 209 in place, 84 in place where the factor is 1; the stretches taken forwards and results through the caches: 253 us for 200 M in the place of 203.)
 #include "tg_embed.h"
 #include "tg_device.h"
 

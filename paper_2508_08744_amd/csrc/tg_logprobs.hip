@@ -2,11 +2,11 @@
 //
 // A tile of logits stays in the registers of the workgroup that formed it.  For every token it leaves the maximum m, the sum l of 2^t and the
 // sum s of t 2^t, t = (z - m) log2(e): joined over the table they give lse = m + log l and the entropy log l - log(2) s / l.  2 n n_rows d operations on the
-// matrix instructions bound it, or, for few tokens, the bytes of the table.  (131 072 rows of 1024 bf16: 4096 tokens 944 us, 1.16 PFLOP/s, with 8 best rows 1061, 42 for the
-// norms and 41 to 54 for the join; one token 40 us, 6.7 TB/s, and 12 for the join.)
+// matrix instructions bound it, or, for few tokens, the bytes of the table.  (131 072 rows of 1024 bf16: 4096 tokens 921 us, 1.19 PFLOP/s, with 8 best rows 1047, 44 for the
+// norms and 39 to 54 for the join; one token 39 us, 6.8 TB/s, and 13 for the join.)
 //
 // The best rows are those of the largest logits in 64 bits, and the logits of the tiles are in 32.  So every lane of a tile leaves, of its 8, 16 or 32
-// logits of a token (a group), the largest with its row and an upper bound of the second: at most a byte a logit.  With 64 lanes over a token's groups, the k-th largest of the lanes' largest is below the k-th
+// logits of a token (a group), the largest with its row and an upper bound of the second: at most a byte a logit (which two waves of a tile of 256 x 256 store half a line each: 1.7 times as much is written).  With 64 lanes over a token's groups, the k-th largest of the lanes' largest is below the k-th
 // logit but for what the roundings of 32 bits reach (a bound from the norms of the token's row and of the longest row of the logit's tile, see LpMargin); whatever does not come up to it with its own bound is none of
 // the k best.  What is left, some k rows, is scored again in 64 bits and put in order.  A group whose second is not out of reach is scored as a whole.
 // (Bounds by tile: 4096 tokens, 32 768 rows of 4096 bf16, one of them 30 or 1000 times as long as the others: 1.06 and 1.6 ms; 46 and 105 with the table's longest row in all bounds; without such a row 0.99.)
@@ -453,8 +453,9 @@ __device__ inline int lp_group_row(const LpTop& a, int g, int lane)
     return (tile << a.tile_shift) + ((i >> a.half_shift) << (a.tile_shift - 1)) + ((in >> 2) << (a.half_shift + 4)) + (i & ((1 << a.half_shift) - 1)) * 16 + (in & 3) * 4 + (lane & 3);
 }
 
-// The tiles' sums joined, and the best rows, by W waves a token: eight where there are few tokens (one token, 1024 tiles: 12 us, of which ways to memory, one behind the other, are most), one where
-// there are many (4096, 512 tiles: 41 to 54 us; 121 with four at the time it was 62 with one; four waves a SIMD, at 48 registers spilt in the rare paths, 51, three 64).
+// The tiles' sums joined, and the best rows, by W waves a token: eight where there are few tokens (one token, 1024 tiles: 13 us, of which ways to memory, one behind the other, are most), one where
+// there are many (4096, 512 tiles: 39 to 54 us by what the caches still hold, 191 to 202 with eight; 1003, 587 smaller tiles: 16 and 38).  Four waves a SIMD, at some 50 registers spilt in the rare paths:
+// three take 49 to 60.
 //
 // What is not below the threshold is listed and scored, eight rows at a time a wave; a long list is thinned by the k-th of its lanes' largest, and a row's place is the number of those
 // before it (23 tokens, 553 rows, 20 best: 32 us with the call, 283 through sorted lists of a wave).  Where the list does not hold
