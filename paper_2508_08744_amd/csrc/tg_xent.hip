@@ -797,8 +797,8 @@ static void launch_xent_grad(const XentRows& r, const XentGrad& g, const void* h
                              int d, const XentTokens& t, float scale, float* consts, char* p, float* sums, float* lost, E* dh, E* dw, hipStream_t s)
 {
     const int e = (int)sizeof(E), per = (int)(r.h.pitch / 16);
-    // (base as the kernels make it)
-    const double unit = scale != 0.0f ? (double)(scale * XENT_LOG2E) / (double)scale : 1.4426950408889634;
+    // (base as the kernels make it; one below the normal numbers is off by more than a step or two, of logits that are all next to 0)
+    const double unit = fabsf(scale) >= 0x1p-126f ? (double)(scale * XENT_LOG2E) / (double)scale : 1.4426950408889634;
     const int64_t wgs = (n * per + 255) / 256;
     hipLaunchKernelGGL(xent_prepare_kernel<E>, dim3((unsigned)(wgs < 16384 ? wgs : 16384) + 1), dim3(256), 0, s, (const E*)h, ld_h, n, n_rows, d, per,
                        t.targets, t.targets64, t.dloss, t.entropy, t.dentropy, scale, (E*)r.ph, consts);

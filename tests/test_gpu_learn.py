@@ -614,6 +614,19 @@ def test_probabilities_keep_their_bits_at_any_lse(v, size, shift, scale):
         assert off <= 0, "beyond the bound by %g" % off
 
 
+@pytest.mark.parametrize("scale", [1e-37, 1.2e-38, 1e-40, -3e-43, 2.0 ** -149])
+def test_gradients_at_the_smallest_scales(scale):
+    """Factors that are no normal numbers: every row is as likely as any other, and P what a large gradient leaves of the factor."""
+    n, v, d = 70, 300, 24
+    h, w, targets = inputs(F32, n, v, d, 5)
+    a = 1e36 * torch.randn(n, generator=gen(1))
+    hd, wd, i = h.to(DEV), w.to(DEV), targets.to(DEV)
+    _, _, lse, _, _ = learn.log_probs(hd, wd, i, scale=scale)
+    ref = Ref(h, w, targets, torch.tensor(scale, dtype=F32).double().item())
+    dh, dw = learn.log_probs_grad(hd, wd, i, lse, a.to(DEV), scale=scale)
+    _grad_check(ref, a, None, F32, dh, dw)
+
+
 def test_gradients_are_the_differences():
     g = gen(11)
     h, w, targets = inputs(F32, 50, 90, 20, 11)
