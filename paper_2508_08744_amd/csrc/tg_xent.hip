@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
     // what a token's logits become P with: its target among the tile's rows, its factor and its lse.  A token without a target has no part in
     // anything, whatever its logits are.
     struct Token { int hit, there; float g, b; };                // there: 0 without a part, 1, or 2 with an lse that is not near, which b then is as it is
-    struct More { float h, less; };
+    struct More { float h, less; };                              // without the entropy's gradient: h: what the rest makes of a power
     __shared__ Token s_token[BN];
     __shared__ More s_more[BN];
     const float up = c[0];
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
         const float lse = tokens.lse[at], dloss = tokens.dloss[at], dentropy = ENTROPY ? tokens.dentropy[at] : 0.0f, entropy = ENTROPY ? tokens.entropy[at] : 0.0f;
         const int64_t target = y < Y.rows ? tg_row_of(tokens.targets, tokens.targets64, at, n_rows) : -1, hit = target - v0 - x0;
         Token k{target >= 0 && hit >= 0 && hit < BM ? (int)hit : -1, 0, 0.0f, 0.0f};
-        More more{0.0f, 0.0f};
+        More more{ENTROPY ? 0.0f : 1.0f, 0.0f};
         if (y < Y.rows && (target >= 0 || dentropy != 0.0f)) {
             if (target >= 0) k.g = more.less = dloss * tokens.gain * scale * up;
             if (ENTROPY && dentropy != 0.0f) {
@@ -247,8 +247,8 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
                 const double b = (double)lse * unit;
                 k.b = (float)b;
                 const float rest = (float)(b - (double)k.b), by = __builtin_amdgcn_exp2f(-rest);
-                k.g = fmaf(-more.h, rest, k.g) * by;
-                more.h *= by;
+                k.g = (ENTROPY ? fmaf(-more.h, rest, k.g) : k.g) * by;
+                more.h = ENTROPY ? more.h * by : by;
             }
         }
         s_token[threadIdx.x] = k;
@@ -302,7 +302,8 @@ __global__ __launch_bounds__(64 * WM * WN) void xent_p_kernel(TileRows X, TileRo
                 for (int e = 0; e < 4; ++e)
                     if (x + e == k.hit) {
                         const float u = fmaf(t.acc[i][j][e], f, -b);
-                        v[e] = fmaf(__builtin_amdgcn_exp2f(u), by(u), -s_more[r].less);
+                        const More at = s_more[r];
+                        v[e] = ENTROPY ? fmaf(__builtin_amdgcn_exp2f(u), by(u), -at.less) : fmaf(__builtin_amdgcn_exp2f(u), at.h, -1.0f) * at.less;
                         if (sizeof(E) == 2) lost[y0 + r] = v[e] - (float)(E)v[e];
                     }
             }

@@ -627,6 +627,20 @@ def test_gradients_at_the_smallest_scales(scale):
     _grad_check(ref, a, None, F32, dh, dw)
 
 
+def test_an_infinite_gradient_keeps_its_sign():
+    """fp32: the row a token's infinite gradient asks for goes one way, all others the other."""
+    h, w, targets = inputs(F32, 5, 40, 8, 6, ignored=False)
+    h = h.abs() + 0.1
+    a = torch.zeros(5)
+    a[2] = math.inf
+    hd, wd, i = h.to(DEV), w.to(DEV), targets.to(DEV)
+    _, _, lse, _, _ = learn.log_probs(hd, wd, i)
+    _, dw = learn.log_probs_grad(hd, wd, i, lse, a.to(DEV))
+    others = torch.ones(40, dtype=torch.bool)
+    others[targets[2]] = False
+    assert (dw.cpu()[targets[2]] == math.inf).all() and (dw.cpu()[others] == -math.inf).all()
+
+
 def test_gradients_are_the_differences():
     g = gen(11)
     h, w, targets = inputs(F32, 50, 90, 20, 11)
