@@ -174,6 +174,8 @@ def lookup_grad(grad, ids, n_rows, scale=1.0, out=None):
     keep, ws = _space(nbytes, grad)
     _check(L.tg_embed_lookup_grad(grad.data_ptr(), ld, DTYPES[grad.dtype], ids.data_ptr(), wide, n, n_rows, d, scale, int(add), out.data_ptr(),
                                   DTYPES[out.dtype], ws, nbytes, _stream(grad, ids, out)))
+    if add:
+        torch.autograd.graph.increment_version(out)
     return out
 
 

@@ -523,3 +523,17 @@ def test_on_another_stream():
     side.synchronize()
     for a, b in zip(want, got):
         assert torch.equal(a, b)
+
+
+def test_autograd_is_told_what_a_gradient_is_added_to():
+    """A tensor that a graph has kept for its backward pass: added to in place, that pass refuses as it does behind torch's own operators."""
+    x = torch.randn(50, 8, device=DEV, requires_grad=True)
+    y = x.exp()
+    i = torch.arange(6, device=DEV)
+    grad = torch.randn(6, 8, device=DEV)
+    version, read = y._version, grad._version
+    with torch.no_grad():
+        embed.lookup_grad(grad, i, 50, out=y)
+    assert y._version > version and grad._version == read
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
