@@ -290,6 +290,27 @@ def test_order_beside_a_row_far_longer_than_the_others(t, n, v, d, longer):
 
 
 @pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,v,d", [(1, 3000, 1024), (20, 5000, 1024), (40, 9000, 512), (100, 3000, 1024), (300, 3000, 512), (450, 30_000, 512), (3000, 2000, 256)])
+@pytest.mark.parametrize("each", [50, 1000])
+def test_order_where_many_tiles_have_a_long_row(t, n, v, d, each):
+    """Rows far longer than the others along what no token has: ordinary logits, and nothing of their tiles' out of reach of the best ones, more than a list holds."""
+    g = gen(n + v)
+    w = torch.randn(v, d, generator=g) / math.sqrt(d)
+    w[::each, 0] = 20_000.0
+    w = w.to(t)
+    h = 2 * torch.randn(n, d, generator=g)
+    h[:, 0] = 0
+    h = h.to(t)
+    z = h.double() @ w.double().t()
+    best, at = torch.sort(z, dim=1, descending=True, stable=True)
+    # a long row's part in its tile's bound, of d products and sums at a step each, on either side
+    reach = 2 * (d + 2) * 2.0 ** -23 * h.double().norm(dim=1) * 20_000
+    assert each > 50 or (z >= (best[:, 7] - reach)[:, None]).sum(1).min() > 1024
+    _, _, _, rows, _ = learn.log_probs(h.to(DEV), w.to(DEV), top=8)
+    assert torch.equal(rows.cpu().long(), at[:, :8])
+
+
+@pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("n,v,d", [(1, 700, 64), (1, 30_000, 64), (20, 5000, 256), (40, 9000, 128), (100, 3000, 96), (300, 3000, 512), (300, 30_000, 128), (450, 30_000, 96), (3000, 1000, 64)])
 @pytest.mark.parametrize("where", ["together", "apart"])
 def test_order_where_some_rows_logits_are_what_large_terms_leave(t, n, v, d, where):
